@@ -1,0 +1,98 @@
+// What the operators' translation units share (declared and documented in cada_ops.h): element types, unaligned vectors, argument checks.
+#pragma once
+
+#include "cada_internal.h"
+#include "cada_ops.h"
+
+namespace cada {
+
+struct bf16 { uint16_t bits; };      // storage type
+template <typename T> struct Elem;
+template <> struct Elem<bf16> { static constexpr int kPer16 = 8; };
+template <> struct Elem<float> { static constexpr int kPer16 = 4; };
+
+__device__ __forceinline__ float to_f32(bf16 x) { return bf2f(x.bits); }
+__device__ __forceinline__ float to_f32(float x) { return x; }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ bf16 from_f32<bf16>(float x) { return bf16{f2bf(x)}; }
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+
+// 16 bytes at an address that is a multiple of the element's size only (one access: the target runs in its unaligned mode).
+typedef uint32_t u32x4a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+template <typename T> struct Vec16;
+template <> struct Vec16<bf16> { typedef u32x4a2 type; };
+template <> struct Vec16<float> { typedef u32x4a4 type; };
+template <typename T> __device__ __forceinline__ u32x4v load16(const T *p) { return *reinterpret_cast<const typename Vec16<T>::type *>(p); }
+template <typename T> __device__ __forceinline__ void store16(T *p, u32x4v x) { *reinterpret_cast<typename Vec16<T>::type *>(p) = x; }
+
+// The first `n` elements at p (n may be anything; none if n <= 0), the others zero.
+template <typename T> __device__ __forceinline__ u32x4v load16_n(const T *p, int64_t n) {
+  constexpr int E = Elem<T>::kPer16;
+  if (n >= E) return load16(p);
+  u32x4v x = {0, 0, 0, 0};
+  if constexpr (E == 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < n) x[i >> 1] |= (uint32_t)p[i].bits << (16 * (i & 1));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (i < n) x[i] = __float_as_uint(p[i]);
+  }
+  return x;
+}
+
+// Eight consecutive values as float32, from and to memory; only the first n exist.
+template <typename T> __device__ __forceinline__ void load8_n(const T *p, int64_t n, float (&f)[8]) {
+  if constexpr (Elem<T>::kPer16 == 8) {
+    const u32x4v x = load16_n(p, n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(x[i] << 16); f[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u); }
+  } else {
+    const u32x4v x = load16_n(p, n), y = load16_n(p + 4, n - 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[i] = __uint_as_float(x[i]); f[4 + i] = __uint_as_float(y[i]); }
+  }
+}
+template <typename T> __device__ __forceinline__ void store8_n(T *p, int64_t n, const float (&f)[8]) {
+  if (n >= 8) {
+    if constexpr (Elem<T>::kPer16 == 8) {
+      store16(p, u32x4v{f2bf_pk(f[0], f[1]), f2bf_pk(f[2], f[3]), f2bf_pk(f[4], f[5]), f2bf_pk(f[6], f[7])});
+    } else {
+      store16(p, u32x4v{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
+      store16(p + 4, u32x4v{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])});
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) if (i < n) p[i] = from_f32<T>(f[i]);
+}
+
+// Activations and their derivatives, in float32 (the derivative as written in terms of z; ReLU's is 0 at 0).
+__device__ __forceinline__ float activation(float z, int act) {
+  switch (act) {
+    case CADA_ACT_RELU: return z < 0.f ? 0.f : z;          // (NaN stays NaN)
+    case CADA_ACT_GELU: return z * (0.5f * (1.f + erff(z * 0.70710678118654752f)));
+    case CADA_ACT_SILU: return z / (1.f + expf(-z));
+    default: return z;
+  }
+}
+__device__ __forceinline__ float activation_slope(float z, int act) {
+  switch (act) {
+    case CADA_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+    case CADA_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * (expf(-0.5f * z * z) * 0.39894228040143268f);
+    case CADA_ACT_SILU: { const float s = 1.f / (1.f + expf(-z)); return s * (1.f + z * (1.f - s)); }
+    default: return 1.f;
+  }
+}
+
+// ---- host ----
+constexpr size_t kOpsAlign = 256;
+inline size_t ops_align(size_t x) { return (x + kOpsAlign - 1) / kOpsAlign * kOpsAlign; }
+inline size_t type_bytes(int type) { return type == CADA_BF16 ? 2 : 4; }
+inline bool aligned16(const void *p, int64_t ld, size_t elem) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * (int64_t)elem) % 16 == 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int ops_check_workspace(const void *ws, size_t given, size_t need);      // cada_linear.hip
+int ops_launched(const char *what);
+
+}  // namespace cada

@@ -1,0 +1,308 @@
+"""The operators of include/cada_ops.h on torch tensors: argument marshalling only.
+
+``linear_forward`` / ``linear_backward``: a layer's product with bias, activation and residual, and its gradients.
+``cross_entropy``: the softmax cross-entropy over any number of classes with its gradient.
+``AdamW``: the step over many tensors at once, moments in 32 or in 8 bits.
+
+Tensors are float32 or bfloat16 on one GPU.  Work goes to ``stream``, by default the device's current stream, and nothing
+synchronises the host.  Outputs that are not handed in are allocated.  A call's workspace comes from torch's caching allocator, unless one is
+handed in; like outputs allocated here it belongs to the current stream, so with a ``stream`` of one's own hand both in, or make it current
+(``with torch.cuda.stream(s)``).
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import List, Optional, Sequence, Tuple, Union
+
+import torch
+
+from .binding import CadaError, _check, _lib, cada_last_error
+
+F32, BF16 = 0, 1
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+MOMENT_BLOCK = 256
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class cada_linear(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("type", C.c_int32), ("act", C.c_int32),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64), ("pre", C.c_void_p), ("ldpre", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+class cada_linear_grad(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("type", C.c_int32), ("act", C.c_int32),
+                ("dy", C.c_void_p), ("lddy", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64),
+                ("pre", C.c_void_p), ("ldpre", C.c_int64), ("dx", C.c_void_p), ("lddx", C.c_int64), ("dw", C.c_void_p), ("lddw", C.c_int64),
+                ("db", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+class cada_xent(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("classes", C.c_int64), ("type", C.c_int32), ("label_bytes", C.c_int32), ("logits", C.c_void_p), ("ldz", C.c_int64),
+                ("labels", C.c_void_p), ("ignore_index", C.c_int64), ("smoothing", C.c_double), ("scale", C.c_double), ("mean", C.c_void_p),
+                ("loss", C.c_void_p), ("grad", C.c_void_p), ("ldg", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("stream", C.c_void_p)]
+
+
+class cada_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32),
+                ("weight_decay", C.c_double)]
+
+
+class cada_adamw_config(C.Structure):
+    _fields_ = [("tensors", C.POINTER(cada_adamw_tensor)), ("n_tensors", C.c_int32), ("moment_bits", C.c_int32), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("norm", C.c_void_p), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("max_norm", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+for _name, _res, _args in (("cada_linear_forward_workspace", C.c_size_t, [C.POINTER(cada_linear)]), ("cada_linear_forward", C.c_int, [C.POINTER(cada_linear)]),
+                           ("cada_linear_backward_workspace", C.c_size_t, [C.POINTER(cada_linear_grad)]), ("cada_linear_backward", C.c_int, [C.POINTER(cada_linear_grad)]),
+                           ("cada_xent_workspace", C.c_size_t, [C.POINTER(cada_xent)]), ("cada_cross_entropy", C.c_int, [C.POINTER(cada_xent)]),
+                           ("cada_adamw_moment_elements", C.c_int64, [C.POINTER(cada_adamw_config)]), ("cada_adamw_workspace", C.c_size_t, [C.POINTER(cada_adamw_config)]),
+                           ("cada_adamw_init", C.c_int, [C.POINTER(cada_adamw_config), C.POINTER(C.c_void_p)]),
+                           ("cada_adamw_step", C.c_int, [C.c_void_p, C.c_int64, C.c_double, C.c_void_p]),
+                           ("cada_adamw_moments", C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]), ("cada_adamw_destroy", None, [C.c_void_p])):
+    _f = getattr(_lib, _name)
+    _f.restype, _f.argtypes = _res, _args
+
+
+def _need(ok: bool, text: str):
+    if not ok:
+        raise ValueError(text)
+
+
+def _table(name: str, t: torch.Tensor, rows: int, cols: int, like: torch.Tensor) -> Tuple[int, int]:
+    """(address, elements from one row to the next) of a [rows, cols] tensor."""
+    if t.shape != (rows, cols):
+        raise ValueError("%s must be [%d, %d], it is %s" % (name, rows, cols, list(t.shape)))
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError("%s must be %s on %s like the other operands, it is %s on %s" % (name, like.dtype, like.device, t.dtype, t.device))
+    s0, s1 = t.stride()
+    if cols > 1 and s1 != 1 or rows > 1 and s0 < cols:
+        raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, t.stride()))
+    return t.data_ptr(), s0 if rows > 1 else max(s0, cols)
+
+
+def _first(x: torch.Tensor, name: str):
+    if not x.is_cuda or x.dtype not in _TYPES or x.dim() != 2:
+        raise ValueError("%s must be a two-dimensional float32 or bfloat16 tensor on a GPU, it is %s %s on %s" % (name, list(x.shape), x.dtype, x.device))
+
+
+def _vector(name: str, t: torch.Tensor, n: int, like: torch.Tensor) -> int:
+    if t.shape != (n,) or t.dtype != like.dtype or t.device != like.device or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s must be a contiguous %s [%d] on %s" % (name, like.dtype, n, like.device))
+    return t.data_ptr()
+
+
+def _activation(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
+    return ACTIVATIONS[act]
+
+
+def _finish(a, size_of, call, device, workspace, stream):
+    """Workspace and stream of a call, and the call."""
+    need = size_of(C.byref(a))
+    if need == 0:
+        raise CadaError("libcada: %s" % cada_last_error())
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)      # (the allocator's blocks start on 512 bytes)
+    elif workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on %s" % device)
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    a.stream = (stream or torch.cuda.current_stream(device)).cuda_stream
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _check(call(C.byref(a)))
+    else:
+        _check(call(C.byref(a)))
+
+
+def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None, act: str = "none",
+                   keep_pre: bool = False, out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(y, pre) with y = act(x w + bias) + residual and pre = x w + bias; pre is None unless ``keep_pre`` or a ``pre`` to write is given.
+
+    x [rows, in], w [in, out] (the layout of the engine's parameters), bias [out], residual [rows, out], all of one type; rows contiguous, any
+    distance apart.  ``out`` may be ``residual``."""
+    _first(x, "x")
+    a = cada_linear()
+    rows, k = x.shape
+    _need(w.dim() == 2, "w must be [in, out]")
+    n = w.shape[1]
+    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[x.dtype], _activation(act)
+    a.x, a.ldx = _table("x", x, rows, k, x)
+    a.w, a.ldw = _table("w", w, k, n, x)
+    if bias is not None:
+        a.bias = _vector("bias", bias, n, x)
+    if residual is not None:
+        a.residual, a.ldr = _table("residual", residual, rows, n, x)
+    if out is None:
+        out = torch.empty(rows, n, dtype=x.dtype, device=x.device)
+    a.y, a.ldy = _table("out", out, rows, n, x)
+    if pre is None and keep_pre:
+        pre = torch.empty(rows, n, dtype=x.dtype, device=x.device)
+    if pre is not None:
+        a.pre, a.ldpre = _table("pre", pre, rows, n, x)
+    _finish(a, _lib.cada_linear_forward_workspace, _lib.cada_linear_forward, x.device, workspace, stream)
+    return out, pre
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, pre: Optional[torch.Tensor] = None, act: str = "none", need_dx: bool = True,
+                    need_dw: bool = True, need_db: bool = True, dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
+                    db: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                    ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dx, dw, db) of a layer from the gradient of its output; the residual's gradient is dy itself.  ``pre`` is what
+    linear_forward kept (not needed for act="none").  Outputs handed in are written, not added to."""
+    _first(dy, "dy")
+    a = cada_linear_grad()
+    rows, n = dy.shape
+    _need(x.dim() == 2 and w.dim() == 2, "x must be [rows, in] and w [in, out]")
+    k = x.shape[1]
+    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[dy.dtype], _activation(act)
+    a.dy, a.lddy = _table("dy", dy, rows, n, dy)
+    a.x, a.ldx = _table("x", x, rows, k, dy)
+    a.w, a.ldw = _table("w", w, k, n, dy)
+    if act != "none":
+        _need(pre is not None, "act=%r needs pre" % act)
+        a.pre, a.ldpre = _table("pre", pre, rows, n, dy)
+    if need_dx:
+        dx = torch.empty(rows, k, dtype=dy.dtype, device=dy.device) if dx is None else dx
+        a.dx, a.lddx = _table("dx", dx, rows, k, dy)
+    if need_dw:
+        dw = torch.empty(k, n, dtype=dy.dtype, device=dy.device) if dw is None else dw
+        a.dw, a.lddw = _table("dw", dw, k, n, dy)
+    if need_db:
+        db = torch.empty(n, dtype=dy.dtype, device=dy.device) if db is None else db
+        a.db = _vector("db", db, n, dy)
+    _finish(a, _lib.cada_linear_backward_workspace, _lib.cada_linear_backward, dy.device, workspace, stream)
+    return dx if need_dx else None, dw if need_dw else None, db if need_db else None
+
+
+def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, *, smoothing: float = 0.0, ignore_index: int = -100, scale: float = 1.0, need_grad: bool = True,
+                  grad: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                  ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """(mean loss, loss of each row, gradient of scale * mean loss with respect to the logits).
+
+    logits [rows, classes]; labels int32 or int64 [rows].  Rows labelled ``ignore_index`` count nowhere; classes at -inf are ruled out.  ``grad`` may be
+    the logits themselves.  Losses are float32, the gradient has the logits' type."""
+    _first(logits, "logits")
+    a = cada_xent()
+    rows, n = logits.shape
+    a.rows, a.classes, a.type = rows, n, _TYPES[logits.dtype]
+    a.logits, a.ldz = _table("logits", logits, rows, n, logits)
+    if labels.dtype not in (torch.int32, torch.int64) or labels.shape != (rows,) or labels.device != logits.device or (rows > 1 and labels.stride(0) != 1):
+        raise ValueError("labels must be a contiguous int32 or int64 [%d] on %s" % (rows, logits.device))
+    a.labels, a.label_bytes = labels.data_ptr(), labels.element_size()
+    a.ignore_index, a.smoothing, a.scale = ignore_index, smoothing, scale
+    stats = torch.empty(rows + 1, dtype=torch.float32, device=logits.device)
+    loss, mean = stats[:rows], stats[rows]
+    a.loss, a.mean = stats.data_ptr(), stats.data_ptr() + 4 * rows
+    if grad is None and need_grad:
+        grad = torch.empty(rows, n, dtype=logits.dtype, device=logits.device)
+    if grad is not None:
+        a.grad, a.ldg = _table("grad", grad, rows, n, logits)
+    _finish(a, _lib.cada_xent_workspace, _lib.cada_cross_entropy, logits.device, workspace, stream)
+    return mean, loss, grad
+
+
+class AdamW:
+    """The AdamW step over ``params`` with ``grads`` (the same tensors every step: write gradients into them).
+
+    params, grads: contiguous float32 or bfloat16 tensors, each param's type its own.  ``weight_decay``: one value or one per tensor.  ``max_norm`` > 0 clips
+    the gradients to that norm over all of them (``norm`` holds the norm of the last step).  ``state_bits``: 32, or 8 for moments in
+    8-bit codes.  ``copies``: bfloat16 tensors that receive the rounded parameters, or None each.  ``moments``: (m, v) to go on from, as ``m`` and ``v`` of another
+    AdamW, updated in place; zeros otherwise.
+
+    ``m`` and ``v`` hold the moments of all tensors one after the other, each tensor's filled up to whole blocks of 256 (``offsets`` says where each
+    starts): float32 tensors, or pairs of codes and scales.  ``moments()`` gives their values."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+                 eps: float = 1e-8, weight_decay: Union[float, Sequence[float]] = 0.0, max_norm: float = 0.0, state_bits: int = 32,
+                 copies: Optional[Sequence[Optional[torch.Tensor]]] = None, moments=None, stream: Optional[torch.cuda.Stream] = None):
+        self.plan = None
+        n = len(params)
+        _need(n >= 1 and len(grads) == n and (copies is None or len(copies) == n), "params, grads and copies must be lists of one length")
+        _need(state_bits in (32, 8), "state_bits must be 32 or 8")
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+        _need(len(decay) == n, "weight_decay must be one value or one per tensor")
+        self.device = dev = params[0].device
+        _need(dev.type == "cuda", "params must be on a GPU")
+        self.params, self.grads, self.copies = list(params), list(grads), list(copies) if copies is not None else [None] * n
+        self.lr, self.t, self.state_bits = lr, 0, state_bits
+        tensors = (cada_adamw_tensor * n)()
+        self.offsets, total = [], 0
+        for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
+            for name, t in (("param", p), ("grad", g)):
+                _need(t.device == dev and t.dtype in _TYPES and t.is_contiguous(), "%s %d must be a contiguous float32 or bfloat16 tensor on %s" % (name, i, dev))
+            _need(g.shape == p.shape, "grad %d must have its param's shape" % i)
+            _need(c is None or (c.device == dev and c.dtype == torch.bfloat16 and c.is_contiguous() and c.shape == p.shape),
+                  "copy %d must be a contiguous bfloat16 tensor of its param's shape" % i)
+            t = tensors[i]
+            t.param, t.grad, t.copy, t.n = p.data_ptr(), g.data_ptr(), c.data_ptr() if c is not None else None, p.numel()
+            t.param_type, t.grad_type, t.weight_decay = _TYPES[p.dtype], _TYPES[g.dtype], decay[i]
+            self.offsets.append(total)
+            total += -(-p.numel() // MOMENT_BLOCK) * MOMENT_BLOCK
+        if moments is None:
+            moments = tuple((torch.zeros(total, dtype=dt, device=dev), torch.zeros(total // MOMENT_BLOCK, device=dev)) for dt in (torch.int8, torch.uint8)) \
+                if state_bits == 8 else (torch.zeros(total, device=dev), torch.zeros(total, device=dev))
+        self.m, self.v = moments
+        for name, t, dt in (("m", self.m, torch.int8), ("v", self.v, torch.uint8)):
+            parts = (t[0], t[1]) if state_bits == 8 else (t,)
+            want = ((dt, total), (torch.float32, total // MOMENT_BLOCK)) if state_bits == 8 else ((torch.float32, total),)
+            for part, (dtype, size) in zip(parts, want):
+                _need(part.device == dev and part.dtype == dtype and part.is_contiguous() and part.numel() == size,
+                      "%s must hold contiguous %s of %d elements on %s" % (name, dtype, size, dev))
+        self.norm = torch.zeros((), device=dev)
+        cfg = cada_adamw_config()
+        cfg.tensors, cfg.n_tensors, cfg.moment_bits = tensors, n, state_bits
+        if state_bits == 8:
+            cfg.m, cfg.m_scale, cfg.v, cfg.v_scale = (t.data_ptr() for t in (*self.m, *self.v))
+        else:
+            cfg.m, cfg.v = self.m.data_ptr(), self.v.data_ptr()
+        cfg.norm = self.norm.data_ptr()
+        cfg.beta1, cfg.beta2, cfg.eps, cfg.max_norm = beta1, beta2, eps, max_norm
+        need = _lib.cada_adamw_workspace(C.byref(cfg))
+        if need == 0:
+            raise CadaError("libcada: %s" % cada_last_error())
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        self.stream = stream or torch.cuda.current_stream(dev)
+        cfg.workspace, cfg.workspace_bytes, cfg.stream = self.workspace.data_ptr(), need, self.stream.cuda_stream
+        plan = C.c_void_p()
+        with torch.cuda.device(dev):
+            _check(_lib.cada_adamw_init(C.byref(cfg), C.byref(plan)))
+        self.plan = plan.value
+
+    def step(self, t: Optional[int] = None, *, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None):
+        """One step on the plan's stream; ``t`` (1, 2, ...) goes up by one if it is not given.  ``grad_scale``: float32 [1] on the GPU, read when the step
+        runs (1 / loss scale)."""
+        if grad_scale is not None:
+            _need(grad_scale.device == self.device and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1, "grad_scale must be a float32 scalar on %s" % self.device)
+        t = self.t + 1 if t is None else t
+        if self.device.index != torch.cuda.current_device():
+            with torch.cuda.device(self.device):
+                _check(_lib.cada_adamw_step(self.plan, t, self.lr if lr is None else lr, None if grad_scale is None else grad_scale.data_ptr()))
+        else:
+            _check(_lib.cada_adamw_step(self.plan, t, self.lr if lr is None else lr, None if grad_scale is None else grad_scale.data_ptr()))
+        self.t = t
+
+    def moments(self) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(m, v) as float32 values, laid out as ``offsets`` says: the moments themselves with 32 bits, decoded copies with 8."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        m, v = (torch.empty(self.m[0].numel(), dtype=torch.float32, device=self.device) for _ in range(2))
+        with torch.cuda.device(self.device):
+            _check(_lib.cada_adamw_moments(self.plan, m.data_ptr(), v.data_ptr()))
+        return m, v
+
+    def close(self):
+        if self.plan:
+            _lib.cada_adamw_destroy(self.plan)
+            self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
