@@ -9,9 +9,10 @@
  *
  * Conventions, as in cada.h
  *   - Pointers are DEVICE memory owned by the caller unless marked HOST.  The library allocates no
- *     device memory; what a call needs beyond its operands is a workspace (256-byte aligned) of the
- *     size that the operator's ..._workspace() function gives.  It holds nothing between calls, and
- *     calls that may overlap (different streams) need one each.
+ *     device memory; what a call needs beyond its operands is a workspace (256-byte aligned).  The
+ *     operator's ..._workspace() function checks the arguments that it names and writes the size
+ *     into workspace_bytes; 0 means that none is needed (workspace may be NULL).  A workspace holds
+ *     nothing between calls, and calls that may overlap (different streams) need one each.
  *   - Calls enqueue work on the given stream and never synchronise the host; operands and
  *     workspace must stay valid until that work has completed.  They record no memset or copy node
  *     and may be captured into a HIP graph (cada_adamw_init copies a table from the host and may
@@ -66,8 +67,7 @@ typedef struct cada_linear {
 } cada_linear;
 #define CADA_MAX_WIDTH (1 << 24)
 
-/* Bytes of workspace (only rows, in, out and type are read); 0 and an error text if they are invalid. */
-size_t cada_linear_forward_workspace(const cada_linear *a);
+int cada_linear_forward_workspace(cada_linear *a); /* all but the pointers' contents, y, pre and stream is read */
 int cada_linear_forward(const cada_linear *a);
 
 /* Gradients of a layer: with dz = dy * act'(pre), dx = dz w^T, dw = x^T dz, db = column sums of
@@ -94,7 +94,7 @@ typedef struct cada_linear_grad {
   void *stream;
 } cada_linear_grad;
 
-size_t cada_linear_backward_workspace(const cada_linear_grad *a); /* rows, in, out, type, act are read */
+int cada_linear_backward_workspace(cada_linear_grad *a); /* all but the pointers' contents and stream is read */
 int cada_linear_backward(const cada_linear_grad *a);
 
 /* Softmax cross-entropy of rows of logits with integer labels, and its gradient, in one pass.
@@ -126,7 +126,7 @@ typedef struct cada_xent {
   void *stream;
 } cada_xent;
 
-size_t cada_xent_workspace(const cada_xent *a); /* rows is read */
+int cada_xent_workspace(cada_xent *a); /* rows, mean and loss are read */
 int cada_cross_entropy(const cada_xent *a);
 
 /* AdamW over many tensors in one launch (two with clipping).  Step t = 1, 2, ... of tensor p with gradient g:
@@ -169,7 +169,7 @@ typedef struct cada_adamw_config {
 typedef struct cada_adamw cada_adamw; /* opaque, host memory owned by the library */
 
 int64_t cada_adamw_moment_elements(const cada_adamw_config *cfg); /* the tensors' n are read; -1 and an error text if invalid */
-size_t cada_adamw_workspace(const cada_adamw_config *cfg);
+int cada_adamw_workspace(cada_adamw_config *cfg); /* the tensors' n are read */
 /* Lays the plan out in the workspace.  Does not touch the moments: a new run starts from zeros (zero bytes: also
  * CADA_MOMENTS_8), a resumed one from what was saved. */
 int cada_adamw_init(const cada_adamw_config *cfg, cada_adamw **out);

@@ -261,9 +261,11 @@ int64_t cada_adamw_moment_elements(const cada_adamw_config *cfg) {
   return sizes(cfg, &e, &c) ? e : -1;
 }
 
-size_t cada_adamw_workspace(const cada_adamw_config *cfg) {
+int cada_adamw_workspace(cada_adamw_config *cfg) {
   int64_t e, c;
-  return sizes(cfg, &e, &c) ? layout(cfg->n_tensors, c).bytes : 0;
+  if (!sizes(cfg, &e, &c)) return CADA_EINVAL;
+  cfg->workspace_bytes = layout(cfg->n_tensors, c).bytes;
+  return CADA_OK;
 }
 
 int cada_adamw_init(const cada_adamw_config *cfg, cada_adamw **out) {

@@ -482,7 +482,7 @@ BackwardPlan plan_backward(int64_t rows, int64_t in, int64_t out, int type) {
   b.off_db = off; off += ops_align((size_t)b.row_blocks * out * 4);
   b.off_dx = off; off += partial_bytes(b.dx, rows, in);
   b.off_dw = off; off += partial_bytes(b.dw, in, out);
-  b.bytes = off + kOpsAlign;
+  b.bytes = off;
   return b;
 }
 
@@ -550,10 +550,16 @@ int forward(const cada_linear *a) {
   return launch_join<T>(j, st);
 }
 
+size_t forward_workspace(const cada_linear *a) {
+  if (a->rows == 0) return 0;
+  return partial_bytes(cut(a->rows, a->out, a->in, kStepBytes / (int)type_bytes(a->type)), a->rows, a->out);
+}
+size_t backward_workspace(const cada_linear_grad *a) { return a->rows == 0 ? 0 : plan_backward(a->rows, a->in, a->out, a->type).bytes; }
+
 }  // namespace
 
 int ops_check_workspace(const void *ws, size_t given, size_t need) {
-  if (need == 0) return CADA_EINVAL;      // (the text is set)
+  if (need == 0) return CADA_OK;
   if (!ws) { set_error("workspace is NULL"); return CADA_EWORKSPACE; }
   if (reinterpret_cast<uintptr_t>(ws) % kOpsAlign != 0) { set_error("workspace must be %zu-byte aligned", kOpsAlign); return CADA_EWORKSPACE; }
   if (given < need) { set_error("workspace too small: %zu bytes given, %zu needed", given, need); return CADA_EWORKSPACE; }
@@ -572,11 +578,11 @@ using namespace cada;
 
 extern "C" {
 
-size_t cada_linear_forward_workspace(const cada_linear *a) {
-  if (!a) { set_error("the arguments are NULL"); return 0; }
-  if (!check_shape(a->rows, a->in, a->out, a->type, CADA_ACT_NONE)) return 0;
-  if (a->rows == 0) return kOpsAlign;
-  return partial_bytes(cut(a->rows, a->out, a->in, kStepBytes / (int)type_bytes(a->type)), a->rows, a->out) + kOpsAlign;
+int cada_linear_forward_workspace(cada_linear *a) {
+  if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
+  if (!check_shape(a->rows, a->in, a->out, a->type, a->act)) return CADA_EINVAL;
+  a->workspace_bytes = forward_workspace(a);
+  return CADA_OK;
 }
 
 int cada_linear_forward(const cada_linear *a) {
@@ -587,15 +593,15 @@ int cada_linear_forward(const cada_linear *a) {
   if (a->bias && !check_table("bias", a->bias, a->out, a->out, a->type)) return CADA_EINVAL;
   if (a->residual && !check_table("residual", a->residual, a->ldr, a->out, a->type)) return CADA_EINVAL;
   if (a->pre && !check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
-  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, cada_linear_forward_workspace(a))) return rc;
+  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, forward_workspace(a))) return rc;
   return a->type == CADA_BF16 ? forward<bf16>(a) : forward<float>(a);
 }
 
-size_t cada_linear_backward_workspace(const cada_linear_grad *a) {
-  if (!a) { set_error("the arguments are NULL"); return 0; }
-  if (!check_shape(a->rows, a->in, a->out, a->type, a->act)) return 0;
-  if (a->rows == 0) return kOpsAlign;
-  return plan_backward(a->rows, a->in, a->out, a->type).bytes;
+int cada_linear_backward_workspace(cada_linear_grad *a) {
+  if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
+  if (!check_shape(a->rows, a->in, a->out, a->type, a->act)) return CADA_EINVAL;
+  a->workspace_bytes = backward_workspace(a);
+  return CADA_OK;
 }
 
 int cada_linear_backward(const cada_linear_grad *a) {
@@ -606,7 +612,7 @@ int cada_linear_backward(const cada_linear_grad *a) {
     if ((a->dx || a->dw || a->db) && a->act != CADA_ACT_NONE && !check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
     if (a->dx && (!check_table("w", a->w, a->ldw, a->out, a->type) || !check_table("dx", a->dx, a->lddx, a->in, a->type))) return CADA_EINVAL;
     if (a->dw && !check_table("x", a->x, a->ldx, a->in, a->type)) return CADA_EINVAL;
-    if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, cada_linear_backward_workspace(a))) return rc;
+    if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, backward_workspace(a))) return rc;
   }
   if (a->dw && !check_table("dw", a->dw, a->lddw, a->out, a->type)) return CADA_EINVAL;
   if (a->db && !check_table("db", a->db, a->out, a->out, a->type)) return CADA_EINVAL;

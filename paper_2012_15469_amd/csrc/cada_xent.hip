@@ -192,6 +192,8 @@ bool check(const cada_xent *a) {
   return true;
 }
 
+size_t workspace(const cada_xent *a) { return kOpsAlign + (a->mean && !a->loss ? ops_align((size_t)a->rows * 4) : 0); }
+
 }  // namespace
 }  // namespace cada
 
@@ -199,9 +201,10 @@ using namespace cada;
 
 extern "C" {
 
-size_t cada_xent_workspace(const cada_xent *a) {
-  if (!check(a)) return 0;
-  return kOpsAlign + ops_align((size_t)a->rows * 4);
+int cada_xent_workspace(cada_xent *a) {
+  if (!check(a)) return CADA_EINVAL;
+  a->workspace_bytes = workspace(a);
+  return CADA_OK;
 }
 
 int cada_cross_entropy(const cada_xent *a) {
@@ -217,7 +220,7 @@ int cada_cross_entropy(const cada_xent *a) {
     if (reinterpret_cast<uintptr_t>(a->logits) % type_bytes(a->type) != 0 || reinterpret_cast<uintptr_t>(a->grad) % type_bytes(a->type) != 0 ||
         reinterpret_cast<uintptr_t>(a->labels) % a->label_bytes != 0) { set_error("logits, grad or labels are not aligned to their elements"); return CADA_EINVAL; }
   }
-  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, cada_xent_workspace(a))) return rc;
+  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, workspace(a))) return rc;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   int64_t *count = static_cast<int64_t *>(a->workspace);
   Xent x{};

@@ -16,7 +16,7 @@ from typing import List, Optional, Sequence, Tuple, Union
 
 import torch
 
-from .binding import CadaError, _check, _lib, cada_last_error
+from .binding import _check, _lib
 
 F32, BF16 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -56,10 +56,10 @@ class cada_adamw_config(C.Structure):
                 ("max_norm", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
 
 
-for _name, _res, _args in (("cada_linear_forward_workspace", C.c_size_t, [C.POINTER(cada_linear)]), ("cada_linear_forward", C.c_int, [C.POINTER(cada_linear)]),
-                           ("cada_linear_backward_workspace", C.c_size_t, [C.POINTER(cada_linear_grad)]), ("cada_linear_backward", C.c_int, [C.POINTER(cada_linear_grad)]),
-                           ("cada_xent_workspace", C.c_size_t, [C.POINTER(cada_xent)]), ("cada_cross_entropy", C.c_int, [C.POINTER(cada_xent)]),
-                           ("cada_adamw_moment_elements", C.c_int64, [C.POINTER(cada_adamw_config)]), ("cada_adamw_workspace", C.c_size_t, [C.POINTER(cada_adamw_config)]),
+for _name, _res, _args in (("cada_linear_forward_workspace", C.c_int, [C.POINTER(cada_linear)]), ("cada_linear_forward", C.c_int, [C.POINTER(cada_linear)]),
+                           ("cada_linear_backward_workspace", C.c_int, [C.POINTER(cada_linear_grad)]), ("cada_linear_backward", C.c_int, [C.POINTER(cada_linear_grad)]),
+                           ("cada_xent_workspace", C.c_int, [C.POINTER(cada_xent)]), ("cada_cross_entropy", C.c_int, [C.POINTER(cada_xent)]),
+                           ("cada_adamw_moment_elements", C.c_int64, [C.POINTER(cada_adamw_config)]), ("cada_adamw_workspace", C.c_int, [C.POINTER(cada_adamw_config)]),
                            ("cada_adamw_init", C.c_int, [C.POINTER(cada_adamw_config), C.POINTER(C.c_void_p)]),
                            ("cada_adamw_step", C.c_int, [C.c_void_p, C.c_int64, C.c_double, C.c_void_p]),
                            ("cada_adamw_moments", C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]), ("cada_adamw_destroy", None, [C.c_void_p])):
@@ -72,12 +72,12 @@ def _need(ok: bool, text: str):
         raise ValueError(text)
 
 
-def _table(name: str, t: torch.Tensor, rows: int, cols: int, like: torch.Tensor) -> Tuple[int, int]:
+def _table(name: str, t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, device: torch.device) -> Tuple[int, int]:
     """(address, elements from one row to the next) of a [rows, cols] tensor."""
-    if t.shape != (rows, cols):
+    if t.dim() != 2 or t.shape != (rows, cols):
         raise ValueError("%s must be [%d, %d], it is %s" % (name, rows, cols, list(t.shape)))
-    if t.dtype != like.dtype or t.device != like.device:
-        raise ValueError("%s must be %s on %s like the other operands, it is %s on %s" % (name, like.dtype, like.device, t.dtype, t.device))
+    if t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be %s on %s like the other operands, it is %s on %s" % (name, dtype, device, t.dtype, t.device))
     s0, s1 = t.stride()
     if cols > 1 and s1 != 1 or rows > 1 and s0 < cols:
         raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, t.stride()))
@@ -101,22 +101,27 @@ def _activation(act: str) -> int:
     return ACTIVATIONS[act]
 
 
-def _finish(a, size_of, call, device, workspace, stream):
+def _enqueue(a, size_of, call, device, workspace, stream):
     """Workspace and stream of a call, and the call."""
-    need = size_of(C.byref(a))
-    if need == 0:
-        raise CadaError("libcada: %s" % cada_last_error())
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)      # (the allocator's blocks start on 512 bytes)
+        r = C.byref(a)
+        _check(size_of(r))
+        if a.workspace_bytes:
+            workspace = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=device)      # (the allocator's blocks start on 512 bytes)
+            a.workspace = workspace.data_ptr()
     elif workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on %s" % device)
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    a.stream = (stream or torch.cuda.current_stream(device)).cuda_stream
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            _check(call(C.byref(a)))
     else:
-        _check(call(C.byref(a)))
+        r = C.byref(a)
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    index = device.index
+    # (the raw handle: torch.cuda.current_stream() makes an object, 2 us of a call that takes 8)
+    a.stream = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
+    if index == torch._C._cuda_getDevice():
+        _check(call(r))
+    else:
+        with torch.cuda.device(device):
+            _check(call(r))
 
 
 def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None, act: str = "none",
@@ -129,23 +134,24 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
     _first(x, "x")
     a = cada_linear()
     rows, k = x.shape
+    dt, dev = x.dtype, x.device
     _need(w.dim() == 2, "w must be [in, out]")
     n = w.shape[1]
-    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[x.dtype], _activation(act)
-    a.x, a.ldx = _table("x", x, rows, k, x)
-    a.w, a.ldw = _table("w", w, k, n, x)
+    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[dt], _activation(act)
+    a.x, a.ldx = _table("x", x, rows, k, dt, dev)
+    a.w, a.ldw = _table("w", w, k, n, dt, dev)
     if bias is not None:
         a.bias = _vector("bias", bias, n, x)
     if residual is not None:
-        a.residual, a.ldr = _table("residual", residual, rows, n, x)
+        a.residual, a.ldr = _table("residual", residual, rows, n, dt, dev)
     if out is None:
-        out = torch.empty(rows, n, dtype=x.dtype, device=x.device)
-    a.y, a.ldy = _table("out", out, rows, n, x)
+        out = torch.empty(rows, n, dtype=dt, device=dev)
+    a.y, a.ldy = _table("out", out, rows, n, dt, dev)
     if pre is None and keep_pre:
-        pre = torch.empty(rows, n, dtype=x.dtype, device=x.device)
+        pre = torch.empty(rows, n, dtype=dt, device=dev)
     if pre is not None:
-        a.pre, a.ldpre = _table("pre", pre, rows, n, x)
-    _finish(a, _lib.cada_linear_forward_workspace, _lib.cada_linear_forward, x.device, workspace, stream)
+        a.pre, a.ldpre = _table("pre", pre, rows, n, dt, dev)
+    _enqueue(a, _lib.cada_linear_forward_workspace, _lib.cada_linear_forward, dev, workspace, stream)
     return out, pre
 
 
@@ -158,25 +164,26 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, pre: 
     _first(dy, "dy")
     a = cada_linear_grad()
     rows, n = dy.shape
+    dt, dev = dy.dtype, dy.device
     _need(x.dim() == 2 and w.dim() == 2, "x must be [rows, in] and w [in, out]")
     k = x.shape[1]
-    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[dy.dtype], _activation(act)
-    a.dy, a.lddy = _table("dy", dy, rows, n, dy)
-    a.x, a.ldx = _table("x", x, rows, k, dy)
-    a.w, a.ldw = _table("w", w, k, n, dy)
+    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[dt], _activation(act)
+    a.dy, a.lddy = _table("dy", dy, rows, n, dt, dev)
+    a.x, a.ldx = _table("x", x, rows, k, dt, dev)
+    a.w, a.ldw = _table("w", w, k, n, dt, dev)
     if act != "none":
         _need(pre is not None, "act=%r needs pre" % act)
-        a.pre, a.ldpre = _table("pre", pre, rows, n, dy)
+        a.pre, a.ldpre = _table("pre", pre, rows, n, dt, dev)
     if need_dx:
-        dx = torch.empty(rows, k, dtype=dy.dtype, device=dy.device) if dx is None else dx
-        a.dx, a.lddx = _table("dx", dx, rows, k, dy)
+        dx = torch.empty(rows, k, dtype=dt, device=dev) if dx is None else dx
+        a.dx, a.lddx = _table("dx", dx, rows, k, dt, dev)
     if need_dw:
-        dw = torch.empty(k, n, dtype=dy.dtype, device=dy.device) if dw is None else dw
-        a.dw, a.lddw = _table("dw", dw, k, n, dy)
+        dw = torch.empty(k, n, dtype=dt, device=dev) if dw is None else dw
+        a.dw, a.lddw = _table("dw", dw, k, n, dt, dev)
     if need_db:
-        db = torch.empty(n, dtype=dy.dtype, device=dy.device) if db is None else db
+        db = torch.empty(n, dtype=dt, device=dev) if db is None else db
         a.db = _vector("db", db, n, dy)
-    _finish(a, _lib.cada_linear_backward_workspace, _lib.cada_linear_backward, dy.device, workspace, stream)
+    _enqueue(a, _lib.cada_linear_backward_workspace, _lib.cada_linear_backward, dev, workspace, stream)
     return dx if need_dx else None, dw if need_dw else None, db if need_db else None
 
 
@@ -190,8 +197,9 @@ def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, *, smoothing: floa
     _first(logits, "logits")
     a = cada_xent()
     rows, n = logits.shape
-    a.rows, a.classes, a.type = rows, n, _TYPES[logits.dtype]
-    a.logits, a.ldz = _table("logits", logits, rows, n, logits)
+    dt, dev = logits.dtype, logits.device
+    a.rows, a.classes, a.type = rows, n, _TYPES[dt]
+    a.logits, a.ldz = _table("logits", logits, rows, n, dt, dev)
     if labels.dtype not in (torch.int32, torch.int64) or labels.shape != (rows,) or labels.device != logits.device or (rows > 1 and labels.stride(0) != 1):
         raise ValueError("labels must be a contiguous int32 or int64 [%d] on %s" % (rows, logits.device))
     a.labels, a.label_bytes = labels.data_ptr(), labels.element_size()
@@ -200,10 +208,10 @@ def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, *, smoothing: floa
     loss, mean = stats[:rows], stats[rows]
     a.loss, a.mean = stats.data_ptr(), stats.data_ptr() + 4 * rows
     if grad is None and need_grad:
-        grad = torch.empty(rows, n, dtype=logits.dtype, device=logits.device)
+        grad = torch.empty(rows, n, dtype=dt, device=dev)
     if grad is not None:
-        a.grad, a.ldg = _table("grad", grad, rows, n, logits)
-    _finish(a, _lib.cada_xent_workspace, _lib.cada_cross_entropy, logits.device, workspace, stream)
+        a.grad, a.ldg = _table("grad", grad, rows, n, dt, dev)
+    _enqueue(a, _lib.cada_xent_workspace, _lib.cada_cross_entropy, dev, workspace, stream)
     return mean, loss, grad
 
 
@@ -263,12 +271,10 @@ class AdamW:
             cfg.m, cfg.v = self.m.data_ptr(), self.v.data_ptr()
         cfg.norm = self.norm.data_ptr()
         cfg.beta1, cfg.beta2, cfg.eps, cfg.max_norm = beta1, beta2, eps, max_norm
-        need = _lib.cada_adamw_workspace(C.byref(cfg))
-        if need == 0:
-            raise CadaError("libcada: %s" % cada_last_error())
-        self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check(_lib.cada_adamw_workspace(C.byref(cfg)))
+        self.workspace = torch.empty(cfg.workspace_bytes, dtype=torch.uint8, device=dev)
         self.stream = stream or torch.cuda.current_stream(dev)
-        cfg.workspace, cfg.workspace_bytes, cfg.stream = self.workspace.data_ptr(), need, self.stream.cuda_stream
+        cfg.workspace, cfg.stream = self.workspace.data_ptr(), self.stream.cuda_stream
         plan = C.c_void_p()
         with torch.cuda.device(dev):
             _check(_lib.cada_adamw_init(C.byref(cfg), C.byref(plan)))
@@ -280,11 +286,12 @@ class AdamW:
         if grad_scale is not None:
             _need(grad_scale.device == self.device and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1, "grad_scale must be a float32 scalar on %s" % self.device)
         t = self.t + 1 if t is None else t
-        if self.device.index != torch.cuda.current_device():
-            with torch.cuda.device(self.device):
-                _check(_lib.cada_adamw_step(self.plan, t, self.lr if lr is None else lr, None if grad_scale is None else grad_scale.data_ptr()))
+        args = self.plan, t, self.lr if lr is None else lr, None if grad_scale is None else grad_scale.data_ptr()
+        if self.device.index == torch._C._cuda_getDevice():
+            _check(_lib.cada_adamw_step(*args))
         else:
-            _check(_lib.cada_adamw_step(self.plan, t, self.lr if lr is None else lr, None if grad_scale is None else grad_scale.data_ptr()))
+            with torch.cuda.device(self.device):
+                _check(_lib.cada_adamw_step(*args))
         self.t = t
 
     def moments(self) -> Tuple[torch.Tensor, torch.Tensor]:

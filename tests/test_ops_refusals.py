@@ -10,6 +10,9 @@ from paper_2012_15469_amd.binding import _lib, cada_last_error
 FAKE = 1 << 20          # an aligned address that nobody reads
 
 
+LONG = dict(in_=100000, ldx=100000)          # few tiles of a long contraction: split, with its parts in a workspace
+
+
 def linear(**kw):
     a = ops.cada_linear()
     a.rows, a.in_, a.out, a.type, a.act = 4, 8, 16, 1, 0
@@ -23,7 +26,7 @@ def linear(**kw):
     (dict(rows=-1), -1, "rows"), (dict(in_=0), -1, "in and out"), (dict(out=1 << 25), -1, "in and out"), (dict(type=2), -1, "type"), (dict(act=4), -1, "act"),
     (dict(x=None), -1, "x is NULL"), (dict(ldx=7), -1, "row length of x"), (dict(ldw=15), -1, "row length of w"), (dict(y=None), -1, "y is NULL"), (dict(ldy=3), -1, "row length of y"),
     (dict(x=FAKE + 1), -1, "not aligned"), (dict(residual=FAKE, ldr=2), -1, "row length of residual"), (dict(pre=FAKE, ldpre=2), -1, "row length of pre"), (dict(bias=FAKE + 1), -1, "bias"),
-    (dict(workspace=None), -2, "workspace is NULL"), (dict(workspace=FAKE + 16), -2, "256-byte"), (dict(workspace_bytes=1), -2, "too small"), (dict(rows=1 << 40, in_=1 << 20, out=1 << 24), -1, "tiles")])
+    (dict(workspace=None, **LONG), -2, "workspace is NULL"), (dict(workspace=FAKE + 16, **LONG), -2, "256-byte"), (dict(workspace_bytes=1, **LONG), -2, "too small"), (dict(rows=1 << 40, in_=1 << 20, out=1 << 24), -1, "tiles")])
 def test_linear_forward(kw, code, text):
     assert _lib.cada_linear_forward(C.byref(linear(**kw))) == code and text in cada_last_error()
 
@@ -76,9 +79,9 @@ def test_adamw(kw, tensor, code, text):
 
 def test_null_arguments():
     assert _lib.cada_linear_forward(None) == -1 and _lib.cada_linear_backward(None) == -1 and _lib.cada_cross_entropy(None) == -1
-    assert _lib.cada_linear_forward_workspace(None) == 0 and _lib.cada_linear_backward_workspace(None) == 0 and _lib.cada_xent_workspace(None) == 0
+    assert _lib.cada_linear_forward_workspace(None) == -1 and _lib.cada_linear_backward_workspace(None) == -1 and _lib.cada_xent_workspace(None) == -1
     assert _lib.cada_adamw_init(None, None) == -1 and _lib.cada_adamw_step(None, 1, 1e-3, None) == -1 and _lib.cada_adamw_moments(None, None, None) == -1
-    assert _lib.cada_adamw_moment_elements(None) == -1 and _lib.cada_adamw_workspace(None) == 0
+    assert _lib.cada_adamw_moment_elements(None) == -1 and _lib.cada_adamw_workspace(None) == -1
     _lib.cada_adamw_destroy(None)
 
 
@@ -89,8 +92,9 @@ def test_sizes_without_gpu():
     cfg = ops.cada_adamw_config()
     cfg.tensors, cfg.n_tensors = t, 3
     assert _lib.cada_adamw_moment_elements(C.byref(cfg)) == 256 + 256 + 512
-    assert _lib.cada_adamw_workspace(C.byref(cfg)) >= 3 * 40
-    a = linear(rows=0)
+    assert _lib.cada_adamw_workspace(C.byref(cfg)) == 0 and cfg.workspace_bytes >= 3 * 40
+    a = linear(rows=0, workspace=None)
+    assert _lib.cada_linear_forward_workspace(C.byref(a)) == 0 and a.workspace_bytes == 0
     assert _lib.cada_linear_forward(C.byref(a)) == 0          # nothing to do
 
 
