@@ -37,36 +37,42 @@ struct Product {
   int32_t N, tiles_m, tiles_n, splits;
   float *partial;            // [splits][M][N] where splits > 1: the sums are joined by k_join
   Epilogue epi;
+  // small gradients: the operand that is the signal is read as dy, and dz = dy * act'(pre) is formed on its way into LDS
+  const void *pre;
+  int64_t ldpre;
+  int32_t act;
+  void *db;                  // column sums of dz (or null), by the tiles of the first rows; their parts where the contraction is split
+  float *db_part;            // [splits][N]
 };
 
 // ---- operands in LDS ----
 //
 // A tile step of an operand is kStepBytes x (BM or BN) bytes, moved in pieces of 16 bytes; piece q lies at byte 16 q, and thread t
 // of 256 moves the pieces 256 i + t, so that a wavefront fills consecutive kilobytes (what the LDS-direct load asks for).
-//   kc: [outer][8 pieces]; row r keeps its pieces in the order p ^ (r % 8): a fragment read takes the same piece of 32 consecutive
-//       rows, and 8 of them in this order cover the banks once.
+//   kc: [outer][8 pieces]; row r keeps its pieces in the order p ^ (r / 2 % 8): a fragment read takes the same piece of 32 consecutive
+//       rows, two of which lie 256 bytes apart as the 64 banks do, and in this order 16 consecutive rows cover the banks once.
 //   oc: [k][outer]; bf16 rows keep their 32-byte chunks in the order c ^ swizzle(r): a transposing read takes 32 bytes of each of four
 //       consecutive rows, which without it lie in the same banks.
-template <typename T, bool KC, int BO> struct Side {
+template <typename T, bool KC, int BO, int TH> struct Side {
   static constexpr int E = Elem<T>::kPer16;
-  static constexpr int kPieces = BO / 32;                       // per thread
+  static constexpr int kPieces = BO * 8 / TH;                   // per thread
   static constexpr int kRow16 = KC ? 8 : BO / E;                // pieces per row in LDS
   static constexpr int kBytes = kStepBytes * BO;
   __device__ static __forceinline__ int swizzle(int krow) { return sizeof(T) == 4 ? 0 : BO >= 128 ? (krow & 3) << 1 : krow & 2; }
   // row of LDS and source piece in it of thread t's i-th piece
   __device__ static __forceinline__ void place(int i, int t, int &row, int &piece) {
-    const int q = i * 256 + t;
+    const int q = i * TH + t;
     row = q / kRow16;
     const int pos = q % kRow16;
-    if constexpr (KC) piece = pos ^ (row & 7);
+    if constexpr (KC) piece = pos ^ ((row >> 1) & 7);
     else piece = pos ^ (swizzle(row) << 1);
   }
 };
 
 // The general way: through registers, any alignment, whatever lies outside [0, left) x [.., k_end) zero.
-template <typename T, bool KC, int BO>
-__device__ __forceinline__ void fetch(u32x4v (&reg)[BO / 32], const T *src, int64_t ld, int64_t left, int64_t k_left, int t) {
-  typedef Side<T, KC, BO> S;
+template <typename T, bool KC, int BO, int TH>
+__device__ __forceinline__ void fetch(u32x4v (&reg)[BO * 8 / TH], const T *src, int64_t ld, int64_t left, int64_t k_left, int t) {
+  typedef Side<T, KC, BO, TH> S;
 #pragma unroll
   for (int i = 0; i < S::kPieces; ++i) {
     int row, piece;
@@ -76,17 +82,34 @@ __device__ __forceinline__ void fetch(u32x4v (&reg)[BO / 32], const T *src, int6
     reg[i] = load16_n(src + (int64_t)row * ld + piece * S::E, row_in ? along : 0);
   }
 }
-template <typename T, bool KC, int BO>
-__device__ __forceinline__ void put(unsigned char *lds, const u32x4v (&reg)[BO / 32], int t) {
+// dz = dy * act'(pre) in place of dy, and its sums per element of a piece (the pieces of a thread of an oc table are the same columns of different rows).
+template <typename T, int N>
+__device__ __forceinline__ void signal(u32x4v (&dy)[N], const u32x4v (&pre)[N], int act, float (&sum)[Elem<T>::kPer16]) {
 #pragma unroll
-  for (int i = 0; i < BO / 32; ++i) *reinterpret_cast<u32x4v *>(lds + (i * 256 + t) * 16) = reg[i];
+  for (int i = 0; i < N; ++i) {
+    float f[Elem<T>::kPer16], z[Elem<T>::kPer16];
+    unpack<T>(dy[i], f);
+    if (act != CADA_ACT_NONE) {
+      unpack<T>(pre[i], z);
+#pragma unroll
+      for (int e = 0; e < Elem<T>::kPer16; ++e) f[e] *= activation_slope<T>(z[e], act);
+      dy[i] = pack<T>(f);
+    }
+#pragma unroll
+    for (int e = 0; e < Elem<T>::kPer16; ++e) sum[e] += f[e];
+  }
+}
+template <int N, int TH>
+__device__ __forceinline__ void put(unsigned char *lds, const u32x4v (&reg)[N], int t) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4v *>(lds + (i * TH + t) * 16) = reg[i];
 }
 
 // The direct way: LDS-direct loads of a whole step.  Every row starts on a 16-byte boundary, and pieces lie in memory whole or not at
 // all (kc: a step's are all there); one that does not is read from the last row or piece that does and enters outputs that nobody stores.
-template <typename T, bool KC, int BO>
-__device__ __forceinline__ void direct_offsets(uint32_t (&off)[BO / 32], int64_t ld, int64_t left, int t) {
-  typedef Side<T, KC, BO> S;
+template <typename T, bool KC, int BO, int TH>
+__device__ __forceinline__ void direct_offsets(uint32_t (&off)[BO * 8 / TH], int64_t ld, int64_t left, int t) {
+  typedef Side<T, KC, BO, TH> S;
 #pragma unroll
   for (int i = 0; i < S::kPieces; ++i) {
     int row, piece;
@@ -95,15 +118,25 @@ __device__ __forceinline__ void direct_offsets(uint32_t (&off)[BO / 32], int64_t
     off[i] = (uint32_t)(at * (int64_t)sizeof(T));
   }
 }
-// (one kilobyte per wavefront: 16 bytes per lane to consecutive places)
-__device__ __forceinline__ void direct_kilobyte(unsigned char *lds, const unsigned char *src) {
-  __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+// One kilobyte per wavefront: 16 bytes per lane to consecutive places.  (In assembly: for the builtin the compiler waits for the loads before
+// the next read of LDS, whatever it reads, and the loop is as slow as their latency; here the wait is the one at the step's end.)
+__device__ __forceinline__ void direct_kilobyte(uint32_t lds, const void *base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
-template <int N>
-__device__ __forceinline__ void direct(unsigned char *lds, const void *src, const uint32_t (&off)[N], int wave) {
+// The same pointer in scalar registers (it is the same in every lane, which the compiler cannot always see).
+template <typename P> __device__ __forceinline__ const P *uniform(const P *p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const P *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32);
+}
+template <int N, int TH>
+__device__ __forceinline__ void direct(const unsigned char *lds, const void *src, const uint32_t (&off)[N], int wave) {
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)lds + wave * 1024;
+  const void *base = uniform(static_cast<const unsigned char *>(src));
 #pragma unroll
-  for (int i = 0; i < N; ++i) direct_kilobyte(lds + (i * 4 + wave) * 1024, static_cast<const unsigned char *>(src) + off[i]);
+  for (int i = 0; i < N; ++i) direct_kilobyte(at + i * (TH * 16), base, off[i]);
 }
+// Everything that this wavefront has asked for has arrived, in registers and in LDS; then so for the others.
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // ---- fragments ----
 // Sub-step ks of four: lane l holds outer index l % 32; bf16: 8 contraction indices from 16 ks + 8 (l / 32) on; float32: 4 from 8 ks + 4 (l / 32) on, one
@@ -112,12 +145,12 @@ template <bool KC, int BO>
 __device__ __forceinline__ bf16x8 fragment(const unsigned char *lds, int outer, int ks, int lane, bf16) {
   if constexpr (KC) {
     const int row = outer + (lane & 31), piece = ks * 2 + (lane >> 5);
-    return *reinterpret_cast<const bf16x8 *>(lds + row * kStepBytes + ((piece ^ (row & 7)) << 4));
+    return *reinterpret_cast<const bf16x8 *>(lds + row * kStepBytes + ((piece ^ ((row >> 1) & 7)) << 4));
   } else {
     // ds_read_b64_tr_b16 works on groups of 16 lanes: source lane s of a group passes the address of four consecutive units of row s / 4, and lane
     // l receives unit l of rows 0..3.  The groups are (units 0-15 | 16-31) x (rows 0-7 | 8-15 of the sub-step), two reads of four rows each.
     const int krow = ks * 16 + ((lane >> 5) << 3) + ((lane & 15) >> 2), chunk = (outer >> 4) + ((lane >> 4) & 1);
-    const unsigned char *at = lds + krow * (BO * 2) + ((chunk ^ Side<bf16, false, BO>::swizzle(krow)) << 5) + ((lane & 3) << 3);
+    const unsigned char *at = lds + krow * (BO * 2) + ((chunk ^ Side<bf16, false, BO, 256>::swizzle(krow)) << 5) + ((lane & 3) << 3);
     typedef __attribute__((address_space(3))) i16x4 *lds_p;
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(at + 4 * BO * 2));
     return __builtin_bit_cast(bf16x8, (i16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -127,7 +160,7 @@ template <bool KC, int BO>
 __device__ __forceinline__ v4s fragment(const unsigned char *lds, int outer, int ks, int lane, float) {
   if constexpr (KC) {
     const int row = outer + (lane & 31), piece = ks * 2 + (lane >> 5);
-    return *reinterpret_cast<const v4s *>(lds + row * kStepBytes + ((piece ^ (row & 7)) << 4));
+    return *reinterpret_cast<const v4s *>(lds + row * kStepBytes + ((piece ^ ((row >> 1) & 7)) << 4));
   } else {
     const float *at = reinterpret_cast<const float *>(lds) + (ks * 8 + ((lane >> 5) << 2)) * BO + outer + (lane & 31);
     return v4s{at[0], at[BO], at[2 * BO], at[3 * BO]};
@@ -153,7 +186,7 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int
   if (e.pre) store8_n(static_cast<T *>(e.pre) + m * e.ldpre + n, left, f);
   if (e.act != CADA_ACT_NONE) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = activation(f[i], e.act);
+    for (int i = 0; i < 8; ++i) f[i] = activation<T>(f[i], e.act);
   }
   if (e.residual) {
     load8_n(static_cast<const T *>(e.residual) + m * e.ldr + n, left, o);
@@ -163,46 +196,53 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int
   store8_n(static_cast<T *>(e.out) + m * e.ldo + n, left, f);
 }
 
-template <typename T, int BM, int BN, bool AKC, bool BKC, bool DIRECT>
-__device__ __forceinline__ void tile_product(const Product &p, int64_t tile, unsigned char *lds) {
-  typedef Side<T, AKC, BM> SA;
-  typedef Side<T, BKC, BN> SB;
-  constexpr int WM = BM / 2, WN = BN / 2, FM = WM / 32, FN = WN / 32, kHalf = SA::kBytes + SB::kBytes, BK = kStep<T>;
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = (wave >> 1) * WM, wn = (wave & 1) * WN;
+enum { NO_SIGNAL = 0, A_SIGNAL = 1, B_SIGNAL = 2 };
+template <typename T, int BM, int BN, int WY, int WX, bool AKC, bool BKC, bool DIRECT, int SIGNAL = NO_SIGNAL>
+__device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, unsigned char *lds) {
+  constexpr int TH = 64 * WY * WX;
+  typedef Side<T, AKC, BM, TH> SA;
+  typedef Side<T, BKC, BN, TH> SB;
+  constexpr int WM = BM / WY, WN = BN / WX, FM = WM / 32, FN = WN / 32, kHalf = SA::kBytes + SB::kBytes, BK = kStep<T>;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WX * WM, wn = wave % WX * WN;
   // Tiles in bands of eight rows of tiles, columns slowest in a band: the tiles that run together share operands.
-  const int64_t per_split = (int64_t)p.tiles_m * p.tiles_n;
-  const int split = (int)(tile / per_split);
-  const int64_t r = tile - split * per_split, band = r / (8 * (int64_t)p.tiles_n);
-  const int in_band = (int)(r - band * 8 * p.tiles_n), rows_here = (int)min((int64_t)8, p.tiles_m - band * 8);
-  const int64_t m0 = (band * 8 + in_band % rows_here) * BM, m_left = p.M - m0;
-  const int n0 = in_band / rows_here * BN;
+  const uint32_t per_split = (uint32_t)p.tiles_m * p.tiles_n, band_tiles = 8u * p.tiles_n;
+  const uint32_t split = tile / per_split, r = tile - split * per_split, band = r / band_tiles, in_band = r - band * band_tiles;
+  const uint32_t rows_here = min(8u, (uint32_t)p.tiles_m - band * 8), col = in_band / rows_here;
+  const int64_t m0 = (int64_t)(band * 8 + in_band - col * rows_here) * BM, m_left = p.M - m0;
+  const int n0 = (int)col * BN;
   const int64_t n_left = p.N - n0, k0 = split * p.k_per_split, k1 = min(p.K, k0 + p.k_per_split);
   const T *a = static_cast<const T *>(p.a) + (AKC ? m0 * p.lda + k0 : k0 * p.lda + m0);
   const T *b = static_cast<const T *>(p.b) + (BKC ? n0 * p.ldb + k0 : k0 * p.ldb + n0);
   const int64_t a_step = AKC ? BK : BK * p.lda, b_step = BKC ? BK : BK * p.ldb;
   const int steps = (int)((k1 - k0 + BK - 1) / BK), whole = (int)((k1 - k0) / BK);
 
-  uint32_t oa[DIRECT ? SA::kPieces : 1], ob[DIRECT ? SB::kPieces : 1];
+  uint32_t oa[SA::kPieces], ob[SB::kPieces];
   if constexpr (DIRECT) {
-    direct_offsets<T, AKC, BM>(oa, p.lda, AKC ? m_left : p.a_cols - m0, t);
-    direct_offsets<T, BKC, BN>(ob, p.ldb, BKC ? n_left : p.b_cols - n0, t);
+    direct_offsets<T, AKC, BM, TH>(oa, p.lda, AKC ? m_left : p.a_cols - m0, t);
+    direct_offsets<T, BKC, BN, TH>(ob, p.ldb, BKC ? n_left : p.b_cols - n0, t);
   }
-  auto through_registers = [&](int s, unsigned char *dst) __attribute__((always_inline)) {
-    u32x4v ra[SA::kPieces], rb[SB::kPieces];
-    fetch<T, AKC, BM>(ra, a + s * a_step, p.lda, m_left, k1 - k0 - (int64_t)s * BK, t);
-    fetch<T, BKC, BN>(rb, b + s * b_step, p.ldb, n_left, k1 - k0 - (int64_t)s * BK, t);
-    put<T, AKC, BM>(dst, ra, t);
-    put<T, BKC, BN>(dst + SA::kBytes, rb, t);
+  // The way through registers: asked for early, put into LDS where the step before has been read.
+  u32x4v ra[SA::kPieces], rb[SB::kPieces], rp[SIGNAL == A_SIGNAL ? SA::kPieces : SIGNAL == B_SIGNAL ? SB::kPieces : 1];
+  float column_sum[Elem<T>::kPer16] = {};
+  auto ask = [&](int s) __attribute__((always_inline)) {
+    const int64_t k_left = k1 - k0 - (int64_t)s * BK;
+    fetch<T, AKC, BM, TH>(ra, a + s * a_step, p.lda, m_left, k_left, t);
+    fetch<T, BKC, BN, TH>(rb, b + s * b_step, p.ldb, n_left, k_left, t);
+    if constexpr (SIGNAL == A_SIGNAL) {
+      if (p.act != CADA_ACT_NONE) fetch<T, AKC, BM, TH>(rp, static_cast<const T *>(p.pre) + m0 * p.ldpre + k0 + (int64_t)s * BK, p.ldpre, m_left, k_left, t);
+    } else if constexpr (SIGNAL == B_SIGNAL) {
+      if (p.act != CADA_ACT_NONE) fetch<T, BKC, BN, TH>(rp, static_cast<const T *>(p.pre) + (k0 + (int64_t)s * BK) * p.ldpre + n0, p.ldpre, n_left, k_left, t);
+    }
+  };
+  auto put_step = [&](unsigned char *dst) __attribute__((always_inline)) {
+    if constexpr (SIGNAL == A_SIGNAL) signal<T>(ra, rp, p.act, column_sum);
+    if constexpr (SIGNAL == B_SIGNAL) signal<T>(rb, rp, p.act, column_sum);
+    put<SA::kPieces, TH>(dst, ra, t);
+    put<SB::kPieces, TH>(dst + SA::kBytes, rb, t);
   };
   auto load_step = [&](int s, unsigned char *dst) __attribute__((always_inline)) {
-    if constexpr (DIRECT) {
-      if (s < whole) {
-        direct(dst, a + s * a_step, oa, wave);
-        direct(dst + SA::kBytes, b + s * b_step, ob, wave);
-        return;
-      }
-    }
-    through_registers(s, dst);
+    direct<SA::kPieces, TH>(dst, a + s * a_step, oa, wave);
+    direct<SB::kPieces, TH>(dst + SA::kBytes, b + s * b_step, ob, wave);
   };
 
   f32x16 acc[FM][FN];
@@ -213,49 +253,123 @@ __device__ __forceinline__ void tile_product(const Product &p, int64_t tile, uns
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 
-  load_step(0, lds);
-  __syncthreads();
-  for (int s = 0; s < steps; ++s) {
-    unsigned char *here = lds + (s & 1) * kHalf;
-    if (s + 1 < steps) load_step(s + 1, lds + ((s + 1) & 1) * kHalf);
+  typedef decltype(fragment<AKC, BM>(lds, 0, 0, 0, T())) Frag;
+  auto read_fragments = [&](Frag (&fa)[FM], Frag (&fb)[FN], const unsigned char *src, int ks) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) fa[i] = fragment<AKC, BM>(src, wm + 32 * i, ks, lane, T());
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[j] = fragment<BKC, BN>(src + SA::kBytes, wn + 32 * j, ks, lane, T());
+  };
+  // (lane: row l % 32 of the tile, four consecutive columns at a time)
+  auto multiply_all = [&](const Frag (&fa)[FM], const Frag (&fb)[FN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);
+  };
+  Frag fa[2][FM], fb[2][FN];
+  auto whole_step = [&](const unsigned char *src) __attribute__((always_inline)) {
+    read_fragments(fa[0], fb[0], src, 0);
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      decltype(fragment<AKC, BM>(here, 0, 0, 0, T())) fa[FM], fb[FN];
-#pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = fragment<AKC, BM>(here, wm + 32 * i, ks, lane, T());
-#pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = fragment<BKC, BN>(here + SA::kBytes, wn + 32 * j, ks, lane, T());
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);        // lane: row l % 32 of the tile, four consecutive columns at a time
+      if (ks < 3) read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], src, ks + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply_all(fa[ks & 1], fb[ks & 1]);
     }
+  };
+  if constexpr (DIRECT) {
+    // Whole steps; what is left of the contraction comes through registers behind them.
+    if (whole > 0) {
+      load_step(0, lds);
+      landed();
+      if (whole > 1) load_step(1, lds + kHalf);
+      read_fragments(fa[0], fb[0], lds, 0);
+      for (int s = 0; s < whole; ++s) {
+        unsigned char *here = lds + (s & 1) * kHalf, *there = lds + ((s + 1) & 1) * kHalf;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          if (ks < 3) {
+            read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
+          } else {
+            landed();               // the next step is there, and everybody has read this one
+            if (s + 2 < whole) load_step(s + 2, here);
+            read_fragments(fa[0], fb[0], there, 0);        // (past the last step: what nobody uses)
+          }
+          __builtin_amdgcn_sched_barrier(0);        // (the reads of the next sub-step go out before this one's products, not between them)
+          multiply_all(fa[ks & 1], fb[ks & 1]);
+        }
+      }
+    }
+    if (whole < steps) {
+      ask(whole);
+      __syncthreads();
+      put_step(lds);
+      __syncthreads();
+      whole_step(lds);
+    }
+  } else {
+    ask(0);
+    put_step(lds);
     __syncthreads();
+    for (int s = 0; s < steps; ++s) {
+      if (s + 1 < steps) ask(s + 1);
+      whole_step(lds + (s & 1) * kHalf);
+      if (s + 1 < steps) put_step(lds + ((s + 1) & 1) * kHalf);
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+
+  if constexpr (SIGNAL == B_SIGNAL) {
+    if (p.db && m0 == 0) {
+      // threads t % (pieces of a row) hold the same columns (a thread's piece is that of its first row: rows of its others differ by multiples of four)
+      constexpr int E = Elem<T>::kPer16, kRow16 = SB::kRow16, kLanes = TH / kRow16;
+      static_assert(TH / kRow16 % 4 == 0 && kLanes * BN * 4 <= 2 * kHalf, "");
+      float *part = reinterpret_cast<float *>(lds);
+      int row, piece;
+      SB::place(0, t, row, piece);
+#pragma unroll
+      for (int e = 0; e < E; ++e) part[t / kRow16 * BN + piece * E + e] = column_sum[e];
+      __syncthreads();
+      if (t < BN && n0 + t < p.N) {
+        float x = 0.f;
+        for (int i = 0; i < kLanes; ++i) x += part[i * BN + t];
+        if (p.splits > 1) p.db_part[(int64_t)split * p.N + n0 + t] = x;
+        else static_cast<T *>(p.db)[n0 + t] = from_f32<T>(x);
+      }
+      __syncthreads();
+    }
   }
 
-  // Out through LDS, 32 rows of the wavefront's tile at a time, so that memory is met in eight consecutive columns per lane.
+  // Out through LDS, 32 rows of the wavefront's tile at a time, so that memory is met in eight consecutive columns per lane.  (One copy of the code
+  // behind it: with one for every group of rows a 256 x 256 tile spent 8 us fetching instructions.)
   constexpr int kLd = WN + 4, kLanes = WN / 8, kRows = 64 / kLanes;
-  static_assert(4 * 32 * kLd * 4 <= 2 * kHalf, "the wavefronts' strips fit the operands' LDS");
+  static_assert(WY * WX * 32 * kLd * 4 <= 2 * kHalf, "the wavefronts' strips fit the operands' LDS");
   float *strip = reinterpret_cast<float *>(lds) + wave * 32 * kLd;
-#pragma unroll
+  const int n = n0 + wn + lane % kLanes * 8;
+  const int64_t left = (int64_t)p.N - n;
+#pragma unroll 1
   for (int i = 0; i < FM; ++i) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
+    for (int ii = 0; ii < FM; ++ii) {
+      if (ii == i) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<v4s *>(strip + (lane & 31) * kLd + 32 * j + 8 * q + 4 * (lane >> 5)) = v4s{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<v4s *>(strip + (lane & 31) * kLd + 32 * j + 8 * q + 4 * (lane >> 5)) = v4s{acc[ii][j][4 * q], acc[ii][j][4 * q + 1], acc[ii][j][4 * q + 2], acc[ii][j][4 * q + 3]};
+      }
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int rr = 0; rr < 32; rr += kRows) {
-      const int row = rr + lane / kLanes, col = lane % kLanes * 8;
+#pragma unroll 2
+    for (int row = lane / kLanes; row < 32; row += kRows) {
       const int64_t m = m0 + wm + 32 * i + row;
-      const int n = n0 + wn + col;
-      const float *src = strip + row * kLd + col;
+      const float *src = strip + row * kLd + lane % kLanes * 8;
       const v4s x = *reinterpret_cast<const v4s *>(src), y = *reinterpret_cast<const v4s *>(src + 4);
       float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
       if (m < p.M) {
-        if (p.splits > 1) store8_n(p.partial + ((int64_t)split * p.M + m) * p.N + n, (int64_t)p.N - n, f);
-        else finish8<T>(p.epi, m, n, (int64_t)p.N - n, f);
+        if (p.splits > 1) store8_n(p.partial + ((int64_t)split * p.M + m) * p.N + n, left, f);
+        else finish8<T>(p.epi, m, n, left, f);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -263,27 +377,105 @@ __device__ __forceinline__ void tile_product(const Product &p, int64_t tile, uns
 }
 
 // Tiles of a launch, dealt to the eight XCDs in consecutive eighths (each has an L2 of its own).
-__device__ __forceinline__ int64_t tile_of_block(int64_t total) {
-  const int64_t per = (total + 7) / 8, t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  return (blockIdx.x >> 3) < per && t < total ? t : -1;
+__device__ __forceinline__ uint32_t tile_of_block(uint32_t total) {
+  const uint32_t per = (total + 7) / 8, t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  return (blockIdx.x >> 3) < per && t < total ? t : ~0u;
 }
 
-template <typename T, int BM, int BN, bool DIRECT>
-__global__ __launch_bounds__(256) void k_forward(const Product p) {
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT>
+__global__ __launch_bounds__(64 * WY * WX) void k_forward(const Product p) {
   __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (BM + BN)];
-  const int64_t tile = tile_of_block((int64_t)p.tiles_m * p.tiles_n * p.splits);
-  if (tile >= 0) tile_product<T, BM, BN, true, false, DIRECT>(p, tile, lds);
+  const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n * p.splits);
+  if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT>(p, tile, lds);
+}
+
+// A few rows (a single sample answered): a read of the weights.  A workgroup takes 64 columns, a lane eight of them (one line of memory per eight lanes and weight row), and
+// 128 weight rows at a time; the rows of x wait in LDS; the sums over the 128 lanes of a column are joined at the end.  One launch, no workspace.
+constexpr int kFewRows = 4, kFewThreads = 1024, kFewChunk = 2048;
+template <typename T, int R>
+__global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
+  __shared__ float xs[R][kFewChunk];
+  __shared__ float part[16][R][64];
+  constexpr int kVecs = 8 / Elem<T>::kPer16;        // of 16 bytes in eight columns
+  const int t = threadIdx.x, cg = t & 7, kl = t >> 3, n0 = blockIdx.x * 64, n = n0 + cg * 8;
+  const int64_t left = (int64_t)p.N - n;
+  const T *w = static_cast<const T *>(p.b) + n, *x = static_cast<const T *>(p.a);
+  float acc[R][8] = {};
+  for (int64_t k0 = 0; k0 < p.K; k0 += kFewChunk) {
+    const int here = (int)min((int64_t)kFewChunk, p.K - k0);
+    if (k0 > 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      for (int i = t; i < here; i += kFewThreads) xs[r][i] = r < p.M ? to_f32(x[r * p.lda + k0 + i]) : 0.f;
+    __syncthreads();
+    if (left > 0) {
+      const T *wk = w + k0 * p.ldb;
+      constexpr int U = 32 / kVecs / 4;        // weight rows on their way at once
+      for (int k = kl; k < here; k += U * 128) {
+        u32x4v raw[U][kVecs];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int v = 0; v < kVecs; ++v) raw[u][v] = load16_n(wk + (int64_t)(k + u * 128) * p.ldb + v * Elem<T>::kPer16, k + u * 128 < here ? left - v * Elem<T>::kPer16 : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (k + u * 128 >= here) break;
+          float xv[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) xv[r] = xs[r][k + u * 128];
+#pragma unroll
+          for (int v = 0; v < kVecs; ++v) {
+            float f[Elem<T>::kPer16];
+            unpack<T>(raw[u][v], f);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int e = 0; e < Elem<T>::kPer16; ++e) acc[r][v * Elem<T>::kPer16 + e] = fmaf(xv[r], f[e], acc[r][v * Elem<T>::kPer16 + e]);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float v = acc[r][e];
+      v += __shfl_xor(v, 8, 64);
+      v += __shfl_xor(v, 16, 64);
+      v += __shfl_xor(v, 32, 64);
+      if ((t & 56) == 0) part[t >> 6][r][cg * 8 + e] = v;
+    }
+  __syncthreads();
+  if (t < R * 8 && (t >> 3) < p.M) {
+    float f[8] = {};
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] += part[i][t >> 3][cg * 8 + e];
+    finish8<T>(p.epi, t >> 3, n, left, f);
+  }
 }
 
 // dx and dw in one launch (either may have no tiles).
-template <typename T, int BM, int BN, bool DIRECT>
-__global__ __launch_bounds__(256) void k_backward(const Product dx, const Product dw) {
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT>
+__global__ __launch_bounds__(64 * WY * WX) void k_backward(const Product dx, const Product dw) {
   __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (BM + BN)];
-  const int64_t n_dw = (int64_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (int64_t)dx.tiles_m * dx.tiles_n * dx.splits;
-  const int64_t tile = tile_of_block(n_dw + n_dx);
-  if (tile < 0) return;
-  if (tile < n_dw) tile_product<T, BM, BN, false, false, DIRECT>(dw, tile, lds);
-  else tile_product<T, BM, BN, true, true, DIRECT>(dx, tile - n_dw, lds);
+  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits;
+  const uint32_t tile = tile_of_block(n_dw + n_dx);
+  if (tile == ~0u) return;
+  if (tile < n_dw) tile_product<T, BM, BN, WY, WX, false, false, DIRECT>(dw, tile, lds);
+  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT>(dx, tile - n_dw, lds);
+}
+
+// The same for small gradients: any alignment, and dz formed on the way (dy's and pre's rows in the place of dz's).
+template <typename T>
+__global__ __launch_bounds__(256) void k_backward_small(const Product dx, const Product dw) {
+  __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (64 + 64)];
+  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits;
+  const uint32_t tile = tile_of_block(n_dw + n_dx);
+  if (tile == ~0u) return;
+  if (tile < n_dw) tile_product<T, 64, 64, 2, 2, false, false, false, B_SIGNAL>(dw, tile, lds);
+  else tile_product<T, 64, 64, 2, 2, true, true, false, A_SIGNAL>(dx, tile - n_dw, lds);
 }
 
 // Joins the sums of a split contraction, in the order of the splits, and finishes them; eight columns per thread.
@@ -349,7 +541,7 @@ __global__ __launch_bounds__(256) void k_signal(const Signal a) {
       if (a.act != CADA_ACT_NONE) {
         load8_n(static_cast<const T *>(a.pre) + r * a.ldpre + n, left, z);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= activation_slope(z[i], a.act);
+        for (int i = 0; i < 8; ++i) f[i] *= activation_slope<T>(z[i], a.act);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[i] += f[i];
@@ -383,17 +575,55 @@ constexpr int kCUs = 256;
 
 // How a product is cut: the tile's edge, and into how many parts its contraction.
 struct Cut { int tile, splits; int64_t k_per_split; };
-Cut cut(int64_t M, int64_t N, int64_t K, int step) {
-  Cut c;
-  const int64_t big = ceil_div(M, 128) * ceil_div(N, 128);
-  c.tile = big >= kCUs ? 128 : 64;
-  const int64_t tiles = ceil_div(M, c.tile) * ceil_div(N, c.tile), steps = ceil_div(K, step);
-  int64_t splits = 1;
-  if (tiles < kCUs) splits = std::max<int64_t>(1, std::min({2 * kCUs / tiles, steps / 4, (int64_t)32}));
-  const int64_t per = ceil_div(steps, splits);
-  c.k_per_split = per * step;
-  c.splits = (int)std::max<int64_t>(1, ceil_div(steps, per));
-  return c;
+
+// What a tile costs, in microseconds, measured (one product of random values, whole tiles, operands in the caches): a step alone on its CU and with all CUs at work, a
+// step's share of a full CU, and the tile's way in and out.  At 8192 x 4096 x 4096 bf16: 256 x 256 tiles 1220 TFLOP/s, 128 x 128 1060, 64 x 64 640.  Float32 is
+// bound by the matrix instructions at any of them (146 TFLOP/s, 64 x 64 as 128 x 128), so it takes the smallest.
+struct TileCost { int tile, slots; double alone, crowd, share, ends; };
+constexpr TileCost kCostBf16[] = {{64, 5, 0.22, 0.25, 0.235, 1.7}, {128, 2, 0.45, 0.37, 0.49, 3.8}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
+constexpr TileCost kCostF32[] = {{64, 5, 0.5, 0.1, 0.46, 1.7}};
+constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
+
+struct Shape { int64_t M, N, K; };
+// Estimated time of one or two products in one launch with this tile and these splits.
+double estimate(const TileCost &c, const Shape *s, const int *splits, int n, int step) {
+  int64_t tiles = 0, most = 0;
+  double work = 0, join = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t t = ceil_div(s[i].M, c.tile) * ceil_div(s[i].N, c.tile) * splits[i], k = ceil_div(ceil_div(s[i].K, step), splits[i]);
+    tiles += t;
+    work += (double)t * k;
+    most = std::max(most, k);
+    if (splits[i] > 1) join += (splits[i] * 4.0 + 2.0) * (double)s[i].M * s[i].N / kJoinBytesPerUs;
+  }
+  if (join > 0) join += kJoinLaunch;
+  const double per_cu = (double)ceil_div(tiles, kCUs);
+  return std::max(most * (c.alone + c.crowd * std::min(1.0, (double)tiles / kCUs)), per_cu * (work / tiles) * c.share) + c.ends * std::ceil(per_cu / c.slots) + join;
+}
+constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+// The cheapest cut of one or two products (one tile for both), by that estimate; with `largest` = 64 only the smallest tile.
+void cut(const Shape *s, int n, int type, int largest, Cut *out) {
+  const int step = kStepBytes / (int)type_bytes(type);
+  const TileCost *costs = type == CADA_BF16 ? kCostBf16 : kCostF32;
+  const int n_costs = type == CADA_BF16 ? 3 : 1;
+  double best = 1e300;
+  for (int c = 0; c < n_costs && costs[c].tile <= largest; ++c) {
+    for (int s0 : kSplits) {
+      if (s0 > 1 && ceil_div(s[0].K, step) < 2 * s0) break;
+      for (int s1 : kSplits) {
+        if (s1 > 1 && (n < 2 || ceil_div(s[1].K, step) < 2 * s1)) break;
+        const int splits[2] = {s0, s1};
+        const double e = estimate(costs[c], s, splits, n, step);
+        if (e < best) {
+          best = e;
+          for (int i = 0; i < n; ++i) {
+            const int64_t steps = ceil_div(s[i].K, step), per = ceil_div(steps, splits[i]);
+            out[i] = Cut{costs[c].tile, (int)ceil_div(steps, per), per * step};
+          }
+        }
+      }
+    }
+  }
 }
 size_t partial_bytes(const Cut &c, int64_t M, int64_t N) { return c.splits > 1 ? ops_align((size_t)c.splits * M * N * 4) : 0; }
 
@@ -425,30 +655,30 @@ bool check_table(const char *name, const void *p, int64_t ld, int64_t cols, int 
   return true;
 }
 
-template <typename T>
-int launch_forward(const Product &p, int tile, bool dir, hipStream_t st) {
+// ---- forward ----
+
+struct ForwardPlan { bool few, direct; Cut cut; size_t bytes; };
+ForwardPlan plan_forward(const cada_linear *a) {
+  ForwardPlan f{};
+  if (a->rows == 0) return f;
+  f.few = a->rows <= kFewRows;
+  f.cut = Cut{64, 1, a->in};
+  if (f.few) return f;
+  const size_t elem = type_bytes(a->type);
+  f.direct = direct_kc(a->x, a->ldx, elem) && direct_oc(a->w, a->ldw, a->out, elem);
+  const Shape s = {a->rows, a->out, a->in};
+  cut(&s, 1, a->type, f.direct ? 256 : 64, &f.cut);
+  f.bytes = partial_bytes(f.cut, a->rows, a->out);
+  return f;
+}
+
+template <typename T, int E, int W>
+void forward_tiles(const Product &p, bool dir, hipStream_t st) {
   const unsigned grid = (unsigned)(ceil_div(tiles_of(p), 8) * 8);
-  if (tile == 128) {
-    if (dir) k_forward<T, 128, 128, true><<<grid, 256, 0, st>>>(p);
-    else k_forward<T, 128, 128, false><<<grid, 256, 0, st>>>(p);
-  } else {
-    if (dir) k_forward<T, 64, 64, true><<<grid, 256, 0, st>>>(p);
-    else k_forward<T, 64, 64, false><<<grid, 256, 0, st>>>(p);
-  }
-  return ops_launched("linear");
+  if (dir) k_forward<T, E, E, 2, W, true><<<grid, 128 * W, 0, st>>>(p);
+  else if constexpr (E == 64) k_forward<T, E, E, 2, W, false><<<grid, 128 * W, 0, st>>>(p);
 }
-template <typename T>
-int launch_backward(const Product &dx, const Product &dw, int tile, bool dir, hipStream_t st) {
-  const unsigned grid = (unsigned)(ceil_div(tiles_of(dx) + tiles_of(dw), 8) * 8);
-  if (tile == 128) {
-    if (dir) k_backward<T, 128, 128, true><<<grid, 256, 0, st>>>(dx, dw);
-    else k_backward<T, 128, 128, false><<<grid, 256, 0, st>>>(dx, dw);
-  } else {
-    if (dir) k_backward<T, 64, 64, true><<<grid, 256, 0, st>>>(dx, dw);
-    else k_backward<T, 64, 64, false><<<grid, 256, 0, st>>>(dx, dw);
-  }
-  return ops_launched("linear gradients");
-}
+
 template <typename T>
 int launch_join(Join &j, hipStream_t st) {
   int64_t total = j.db_part ? j.db_n : 0;
@@ -461,27 +691,69 @@ int launch_join(Join &j, hipStream_t st) {
   return ops_launched("linear join");
 }
 
+template <typename T>
+int forward(const cada_linear *a, const ForwardPlan &f) {
+  hipStream_t st = static_cast<hipStream_t>(a->stream);
+  Product p{};
+  lay(&p, f.cut, a->x, a->ldx, a->w, a->ldw, a->rows, a->out, a->in, static_cast<float *>(a->workspace));
+  p.epi = Epilogue{a->bias, a->residual, a->pre, a->y, a->ldr, a->ldpre, a->ldy, a->act};
+  if (f.few) {
+    const unsigned grid = (unsigned)ceil_div(a->out, 64);
+    if (a->rows == 1) k_few_rows<T, 1><<<grid, kFewThreads, 0, st>>>(p);
+    else if (a->rows == 2) k_few_rows<T, 2><<<grid, kFewThreads, 0, st>>>(p);
+    else k_few_rows<T, 4><<<grid, kFewThreads, 0, st>>>(p);
+    return ops_launched("linear");
+  }
+  if (f.cut.tile == 64) forward_tiles<T, 64, 2>(p, f.direct, st);
+  if constexpr (sizeof(T) == 2) {
+    if (f.cut.tile == 128) forward_tiles<T, 128, 2>(p, f.direct, st);
+    if (f.cut.tile == 256) forward_tiles<T, 256, 4>(p, f.direct, st);
+  }
+  if (int rc = ops_launched("linear")) return rc;
+  if (p.splits == 1) return CADA_OK;
+  Join j{};
+  j.p[0] = p;
+  return launch_join<T>(j, st);
+}
+
+// ---- backward ----
+
+// Below this many products of numbers (both gradients), dz is formed on its way into the products' tiles: one launch less, for tiles that read their operands
+// through registers and each form the part of dz that they need.
+constexpr double kSmallGradients = 4e9;
+
 struct BackwardPlan {
+  bool small, own_dz, direct;
   Cut dx, dw;
   int64_t lddz, rows_per_block, row_blocks;
   size_t off_db, off_dx, off_dw, bytes;
 };
-BackwardPlan plan_backward(int64_t rows, int64_t in, int64_t out, int type) {
-  BackwardPlan b;
-  const size_t elem = type_bytes(type);
-  const int step = kStepBytes / (int)elem;
-  b.dx = cut(rows, in, out, step);
-  b.dw = cut(in, out, rows, step);
-  if (b.dx.tile != b.dw.tile) {      // one launch, one tile
-    b.dx.tile = b.dw.tile = 64;
-  }
+BackwardPlan plan_backward(const cada_linear_grad *a) {
+  BackwardPlan b{};
+  if (a->rows == 0) return b;
+  const int64_t rows = a->rows, in = a->in, out = a->out;
+  const size_t elem = type_bytes(a->type);
+  const bool products = a->dx || a->dw;
+  b.small = products && (a->dw || !a->db) && 4.0 * rows * in * out < kSmallGradients;
+  // dz in the workspace, unless dy itself will do
+  b.own_dz = products && !b.small && (a->act != CADA_ACT_NONE || !direct_oc(a->dy, a->lddy, out, elem));
+  b.direct = !b.small && (!a->dx || direct_kc(a->w, a->ldw, elem)) && (!a->dw || direct_oc(a->x, a->ldx, in, elem));
+  const Shape s[2] = {{rows, in, out}, {in, out, rows}};
+  Cut c[2];
+  const int largest = b.direct ? 256 : 64;
+  if (a->dx && a->dw) { cut(s, 2, a->type, largest, c); b.dx = c[0]; b.dw = c[1]; }
+  else if (a->dx) { cut(s, 1, a->type, largest, c); b.dx = c[0]; }
+  else if (a->dw) { cut(s + 1, 1, a->type, largest, c); b.dw = c[0]; }
   b.lddz = ceil_div(out, 8) * 8;
   b.rows_per_block = std::max<int64_t>(32, ceil_div(ceil_div(rows, 64), 8) * 8);
-  b.row_blocks = ceil_div(rows, b.rows_per_block);
-  size_t off = ops_align((size_t)rows * b.lddz * elem);
-  b.off_db = off; off += ops_align((size_t)b.row_blocks * out * 4);
-  b.off_dx = off; off += partial_bytes(b.dx, rows, in);
-  b.off_dw = off; off += partial_bytes(b.dw, in, out);
+  b.row_blocks = b.small ? b.dw.splits : ceil_div(rows, b.rows_per_block);
+  size_t off = b.own_dz ? ops_align((size_t)rows * b.lddz * elem) : 0;
+  b.off_db = off;
+  if (a->db && (!b.small || b.dw.splits > 1)) off += ops_align((size_t)b.row_blocks * out * 4);
+  b.off_dx = off;
+  if (a->dx) off += partial_bytes(b.dx, rows, in);
+  b.off_dw = off;
+  if (a->dw) off += partial_bytes(b.dw, in, out);
   b.bytes = off;
   return b;
 }
@@ -492,69 +764,61 @@ int zero_table(void *p, int64_t ld, int64_t rows, int64_t n, hipStream_t st) {
   return ops_launched("linear clear");
 }
 
+template <typename T, int E, int W>
+void backward_tiles(const Product &dx, const Product &dw, bool dir, hipStream_t st) {
+  const unsigned grid = (unsigned)(ceil_div(tiles_of(dx) + tiles_of(dw), 8) * 8);
+  if (dir) k_backward<T, E, E, 2, W, true><<<grid, 128 * W, 0, st>>>(dx, dw);
+  else if constexpr (E == 64) k_backward<T, E, E, 2, W, false><<<grid, 128 * W, 0, st>>>(dx, dw);
+}
+
 template <typename T>
-int backward(const cada_linear_grad *a) {
+int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   if (a->rows == 0) {
     if (a->dw) if (int rc = zero_table<T>(a->dw, a->lddw, a->in, a->out, st)) return rc;
     if (a->db) return zero_table<T>(a->db, a->out, 1, a->out, st);
     return CADA_OK;
   }
-  const BackwardPlan b = plan_backward(a->rows, a->in, a->out, a->type);
   char *ws = static_cast<char *>(a->workspace);
-  // dz in the workspace, unless dy itself will do
-  const bool products = a->dx || a->dw;
-  const bool own_dz = products && (a->act != CADA_ACT_NONE || !direct_oc(a->dy, a->lddy, a->out, sizeof(T)));
-  if (own_dz || a->db) {
+  float *db_part = reinterpret_cast<float *>(ws + b.off_db);
+  if (b.own_dz || (a->db && !b.small)) {
     Signal s{};
     s.dy = a->dy; s.lddy = a->lddy; s.pre = a->pre; s.ldpre = a->ldpre; s.rows = a->rows; s.rows_per_block = b.rows_per_block; s.n = (int32_t)a->out; s.act = a->act;
-    s.dz = own_dz ? ws : nullptr; s.lddz = b.lddz;
-    s.db_part = a->db ? reinterpret_cast<float *>(ws + b.off_db) : nullptr;
+    s.dz = b.own_dz ? ws : nullptr; s.lddz = b.lddz;
+    s.db_part = a->db ? db_part : nullptr;
     k_signal<T><<<dim3((unsigned)ceil_div(a->out, 256), (unsigned)b.row_blocks), 256, 0, st>>>(s);
     if (int rc = ops_launched("linear signal")) return rc;
   }
-  const void *dz = own_dz ? ws : a->dy;
-  // (dz's rows in the workspace are filled with zeros up to whole pieces)
-  const int64_t lddz = own_dz ? b.lddz : a->lddy;
+  const void *dz = b.own_dz ? ws : a->dy;
+  const int64_t lddz = b.own_dz ? b.lddz : a->lddy;
   Product dx{}, dw{};
-  bool dir = true;
   if (a->dx) {
     lay(&dx, b.dx, dz, lddz, a->w, a->ldw, a->rows, a->in, a->out, reinterpret_cast<float *>(ws + b.off_dx));
-    dx.epi = Epilogue{nullptr, nullptr, nullptr, a->dx, 0, 0, a->lddx, CADA_ACT_NONE};
-    dir = dir && direct_kc(a->w, a->ldw, sizeof(T)) && direct_kc(dz, lddz, sizeof(T));
+    dx.epi.out = a->dx; dx.epi.ldo = a->lddx;
+    dx.pre = a->pre; dx.ldpre = a->ldpre; dx.act = a->act;
   }
   if (a->dw) {
     lay(&dw, b.dw, a->x, a->ldx, dz, lddz, a->in, a->out, a->rows, reinterpret_cast<float *>(ws + b.off_dw));
-    dw.epi = Epilogue{nullptr, nullptr, nullptr, a->dw, 0, 0, a->lddw, CADA_ACT_NONE};
-    dw.b_cols = own_dz ? b.lddz : a->out;
-    dir = dir && direct_oc(a->x, a->ldx, a->in, sizeof(T)) && direct_oc(dz, lddz, dw.b_cols, sizeof(T));
+    if (b.own_dz) dw.b_cols = b.lddz;      // (dz's rows in the workspace are filled with zeros up to whole pieces)
+    dw.epi.out = a->dw; dw.epi.ldo = a->lddw;
+    dw.pre = a->pre; dw.ldpre = a->ldpre; dw.act = a->act;
+    if (b.small) { dw.db = a->db; dw.db_part = db_part; }
   }
-  if (products) if (int rc = launch_backward<T>(dx, dw, a->dx ? b.dx.tile : b.dw.tile, dir, st)) return rc;
+  if (a->dx || a->dw) {
+    const int tile = a->dx ? b.dx.tile : b.dw.tile;
+    if (b.small) k_backward_small<T><<<(unsigned)(ceil_div(tiles_of(dx) + tiles_of(dw), 8) * 8), 256, 0, st>>>(dx, dw);
+    else if (tile == 64) backward_tiles<T, 64, 2>(dx, dw, b.direct, st);
+    if constexpr (sizeof(T) == 2) {
+      if (!b.small && tile == 128) backward_tiles<T, 128, 2>(dx, dw, b.direct, st);
+      if (!b.small && tile == 256) backward_tiles<T, 256, 4>(dx, dw, b.direct, st);
+    }
+    if (int rc = ops_launched("linear gradients")) return rc;
+  }
   Join j{};
   j.p[0] = dx; j.p[1] = dw;
-  if (a->db) { j.db_part = reinterpret_cast<float *>(ws + b.off_db); j.db = a->db; j.db_parts = (int)b.row_blocks; j.db_n = (int)a->out; }
+  if (a->db && (!b.small || b.dw.splits > 1)) { j.db_part = db_part; j.db = a->db; j.db_parts = (int)b.row_blocks; j.db_n = (int)a->out; }
   return launch_join<T>(j, st);
 }
-
-template <typename T>
-int forward(const cada_linear *a) {
-  hipStream_t st = static_cast<hipStream_t>(a->stream);
-  const Cut c = cut(a->rows, a->out, a->in, kStep<T>);
-  Product p{};
-  lay(&p, c, a->x, a->ldx, a->w, a->ldw, a->rows, a->out, a->in, static_cast<float *>(a->workspace));
-  p.epi = Epilogue{a->bias, a->residual, a->pre, a->y, a->ldr, a->ldpre, a->ldy, a->act};
-  const bool dir = direct_kc(a->x, a->ldx, sizeof(T)) && direct_oc(a->w, a->ldw, a->out, sizeof(T));
-  if (int rc = launch_forward<T>(p, c.tile, dir, st)) return rc;
-  Join j{};
-  j.p[0] = p;
-  return launch_join<T>(j, st);
-}
-
-size_t forward_workspace(const cada_linear *a) {
-  if (a->rows == 0) return 0;
-  return partial_bytes(cut(a->rows, a->out, a->in, kStepBytes / (int)type_bytes(a->type)), a->rows, a->out);
-}
-size_t backward_workspace(const cada_linear_grad *a) { return a->rows == 0 ? 0 : plan_backward(a->rows, a->in, a->out, a->type).bytes; }
 
 }  // namespace
 
@@ -581,7 +845,7 @@ extern "C" {
 int cada_linear_forward_workspace(cada_linear *a) {
   if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
   if (!check_shape(a->rows, a->in, a->out, a->type, a->act)) return CADA_EINVAL;
-  a->workspace_bytes = forward_workspace(a);
+  a->workspace_bytes = plan_forward(a).bytes;
   return CADA_OK;
 }
 
@@ -593,14 +857,15 @@ int cada_linear_forward(const cada_linear *a) {
   if (a->bias && !check_table("bias", a->bias, a->out, a->out, a->type)) return CADA_EINVAL;
   if (a->residual && !check_table("residual", a->residual, a->ldr, a->out, a->type)) return CADA_EINVAL;
   if (a->pre && !check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
-  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, forward_workspace(a))) return rc;
-  return a->type == CADA_BF16 ? forward<bf16>(a) : forward<float>(a);
+  const ForwardPlan f = plan_forward(a);
+  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, f.bytes)) return rc;
+  return a->type == CADA_BF16 ? forward<bf16>(a, f) : forward<float>(a, f);
 }
 
 int cada_linear_backward_workspace(cada_linear_grad *a) {
   if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
   if (!check_shape(a->rows, a->in, a->out, a->type, a->act)) return CADA_EINVAL;
-  a->workspace_bytes = backward_workspace(a);
+  a->workspace_bytes = plan_backward(a).bytes;
   return CADA_OK;
 }
 
@@ -612,11 +877,12 @@ int cada_linear_backward(const cada_linear_grad *a) {
     if ((a->dx || a->dw || a->db) && a->act != CADA_ACT_NONE && !check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
     if (a->dx && (!check_table("w", a->w, a->ldw, a->out, a->type) || !check_table("dx", a->dx, a->lddx, a->in, a->type))) return CADA_EINVAL;
     if (a->dw && !check_table("x", a->x, a->ldx, a->in, a->type)) return CADA_EINVAL;
-    if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, backward_workspace(a))) return rc;
   }
   if (a->dw && !check_table("dw", a->dw, a->lddw, a->out, a->type)) return CADA_EINVAL;
   if (a->db && !check_table("db", a->db, a->out, a->out, a->type)) return CADA_EINVAL;
-  return a->type == CADA_BF16 ? backward<bf16>(a) : backward<float>(a);
+  const BackwardPlan b = plan_backward(a);
+  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, b.bytes)) return rc;
+  return a->type == CADA_BF16 ? backward<bf16>(a, b) : backward<float>(a, b);
 }
 
 }  // extern "C"

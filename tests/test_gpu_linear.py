@@ -76,14 +76,37 @@ def test_backward(shape, dtype):
         dx, dw, db = ops.linear_backward(dy, x, w, pre=pre, act=act)
         dz = dy.double() * (slope64(pre.double(), act) if pre is not None else 1)
         dz_abs, r = dy.double().abs() * 1.2, 2.0 ** -8 if dtype == "bf16" and act != "none" else 0.0      # (a slope near zero is off by a few U of its terms, not of itself)
-        close(dx, dz @ w.double().t(), ((n + 16) * U + r) * (dz_abs @ w.double().abs().t()), dtype)
-        close(dw, x.double().t() @ dz, ((rows + 16) * U + r) * (x.double().abs().t() @ dz_abs), dtype)
-        close(db, dz.sum(0), (rows + 16) * U * dz_abs.sum(0), dtype)
-        # each output alone is what it is with the others
+        want = (dz @ w.double().t(), x.double().t() @ dz, dz.sum(0))
+        bound = (((n + 16) * U + r) * (dz_abs @ w.double().abs().t()), ((rows + 16) * U + r) * (x.double().abs().t() @ dz_abs), (rows + 16) * U * dz_abs.sum(0))
+        for got, v, bd in zip((dx, dw, db), want, bound):
+            close(got, v, bd, dtype)
+        # each output alone (the contractions may be cut otherwise)
         for need in ((True, False, False), (False, True, False), (False, False, True)):
             alone = ops.linear_backward(dy, x, w, pre=pre, act=act, need_dx=need[0], need_dw=need[1], need_db=need[2])
-            for wanted, a, b in zip(need, alone, (dx, dw, db)):
-                assert torch.equal(a, b) if wanted else a is None
+            for wanted, got, v, bd in zip(need, alone, want, bound):
+                if wanted:
+                    close(got, v, bd, dtype)
+                else:
+                    assert got is None
+
+
+# Large enough for every tile that the library has (bf16; float32 has one), with and without 16-byte rows, and contractions that end inside a step.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(8200, 2056, 4104), (4100, 1032, 1032), (2056, 520, 2056), (3001, 1001, 1003), (300, 4100, 520)], ids=str)
+def test_large(shape, dtype):
+    rows, k, n = shape
+    gen = torch.Generator(device="cuda"); gen.manual_seed(rows)
+    x, w, b, r = table(rows, k, dtype, gen), table(k, n, dtype, gen, scale=1 / math.sqrt(k)), table(1, n, dtype, gen)[0], table(rows, n, dtype, gen)
+    y, pre = ops.linear_forward(x, w, b, residual=r, act="gelu", keep_pre=True)
+    z = x.double() @ w.double() + b.double()
+    bound = (k + 8) * U * (x.double().abs() @ w.double().abs() + b.double().abs())
+    close(pre, z, bound, dtype)
+    close(y, act64(z, "gelu") + r.double(), bound + U * r.double().abs(), dtype)
+    dx, dw, db = ops.linear_backward(r, x, w, pre=pre, act="gelu")
+    dz, extra = r.double() * slope64(pre.double(), "gelu"), 2.0 ** -8 if dtype == "bf16" else 0.0
+    close(dx, dz @ w.double().t(), ((n + 16) * U + extra) * (r.double().abs() @ w.double().abs().t()), dtype)
+    close(dw, x.double().t() @ dz, ((rows + 16) * U + extra) * (x.double().abs().t() @ r.double().abs()), dtype)
+    close(db, dz.sum(0), (rows + 16) * U * r.double().abs().sum(0) * 1.2, dtype)
 
 
 @pytest.mark.parametrize("act", ["gelu", "silu"])
