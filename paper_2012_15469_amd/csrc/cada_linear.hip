@@ -69,17 +69,32 @@ template <typename T, bool KC, int BO, int TH> struct Side {
   }
 };
 
-// The general way: through registers, any alignment, whatever lies outside [0, left) x [.., k_end) zero.
+// The general way: through registers, any alignment, whatever lies outside [0, left) x [.., k_end) zero.  A piece is one load wherever 16 bytes from its start
+// lie before the table's last element (behind a row's end lies the next row, and is masked); else its elements one by one.
 template <typename T, bool KC, int BO, int TH>
-__device__ __forceinline__ void fetch(u32x4v (&reg)[BO * 8 / TH], const T *src, int64_t ld, int64_t left, int64_t k_left, int t) {
+__device__ __forceinline__ void fetch(u32x4v (&reg)[BO * 8 / TH], const T *src, int64_t ld, int64_t left, int64_t k_left, const T *end, int t) {
   typedef Side<T, KC, BO, TH> S;
+  constexpr int E = S::E;
 #pragma unroll
   for (int i = 0; i < S::kPieces; ++i) {
     int row, piece;
     S::place(i, t, row, piece);
-    const int64_t along = KC ? k_left - piece * S::E : left - piece * S::E;        // elements from the piece's first to the row's end
-    const bool row_in = KC ? row < left : row < k_left;
-    reg[i] = load16_n(src + (int64_t)row * ld + piece * S::E, row_in ? along : 0);
+    const int64_t along = (KC ? k_left : left) - piece * E;        // elements from the piece's first to the row's end
+    const bool any = (KC ? row < left : row < k_left) && along > 0;
+    const T *at = src + (int64_t)row * ld + piece * E;
+    u32x4v x = {0, 0, 0, 0};
+    if (any) {
+      if (at + E <= end) x = load16(at);
+      else x = load16_n(at, along);
+    }
+    if (along < E) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        if constexpr (E == 8) x[d] &= along >= 2 * d + 2 ? 0xFFFFFFFFu : along == 2 * d + 1 ? 0xFFFFu : 0u;
+        else x[d] = along > d ? x[d] : 0u;
+      }
+    }
+    reg[i] = x;
   }
 }
 // dz = dy * act'(pre) in place of dy, and its sums per element of a piece (the pieces of a thread of an oc table are the same columns of different rows).
@@ -213,6 +228,9 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   const int64_t n_left = p.N - n0, k0 = split * p.k_per_split, k1 = min(p.K, k0 + p.k_per_split);
   const T *a = static_cast<const T *>(p.a) + (AKC ? m0 * p.lda + k0 : k0 * p.lda + m0);
   const T *b = static_cast<const T *>(p.b) + (BKC ? n0 * p.ldb + k0 : k0 * p.ldb + n0);
+  // (one past the tables' last elements)
+  const T *a_end = static_cast<const T *>(p.a) + (AKC ? (p.M - 1) * p.lda + p.K : (p.K - 1) * p.lda + p.M);
+  const T *b_end = static_cast<const T *>(p.b) + (BKC ? ((int64_t)p.N - 1) * p.ldb + p.K : (p.K - 1) * p.ldb + p.N);
   const int64_t a_step = AKC ? BK : BK * p.lda, b_step = BKC ? BK : BK * p.ldb;
   const int steps = (int)((k1 - k0 + BK - 1) / BK), whole = (int)((k1 - k0) / BK);
 
@@ -226,12 +244,14 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   float column_sum[Elem<T>::kPer16] = {};
   auto ask = [&](int s) __attribute__((always_inline)) {
     const int64_t k_left = k1 - k0 - (int64_t)s * BK;
-    fetch<T, AKC, BM, TH>(ra, a + s * a_step, p.lda, m_left, k_left, t);
-    fetch<T, BKC, BN, TH>(rb, b + s * b_step, p.ldb, n_left, k_left, t);
+    fetch<T, AKC, BM, TH>(ra, a + s * a_step, p.lda, m_left, k_left, a_end, t);
+    fetch<T, BKC, BN, TH>(rb, b + s * b_step, p.ldb, n_left, k_left, b_end, t);
     if constexpr (SIGNAL == A_SIGNAL) {
-      if (p.act != CADA_ACT_NONE) fetch<T, AKC, BM, TH>(rp, static_cast<const T *>(p.pre) + m0 * p.ldpre + k0 + (int64_t)s * BK, p.ldpre, m_left, k_left, t);
+      if (p.act != CADA_ACT_NONE) fetch<T, AKC, BM, TH>(rp, static_cast<const T *>(p.pre) + m0 * p.ldpre + k0 + (int64_t)s * BK, p.ldpre, m_left, k_left,
+                                                                static_cast<const T *>(p.pre) + (p.M - 1) * p.ldpre + p.K, t);
     } else if constexpr (SIGNAL == B_SIGNAL) {
-      if (p.act != CADA_ACT_NONE) fetch<T, BKC, BN, TH>(rp, static_cast<const T *>(p.pre) + (k0 + (int64_t)s * BK) * p.ldpre + n0, p.ldpre, n_left, k_left, t);
+      if (p.act != CADA_ACT_NONE) fetch<T, BKC, BN, TH>(rp, static_cast<const T *>(p.pre) + (k0 + (int64_t)s * BK) * p.ldpre + n0, p.ldpre, n_left, k_left,
+                                                                static_cast<const T *>(p.pre) + (p.K - 1) * p.ldpre + p.N, t);
     }
   };
   auto put_step = [&](unsigned char *dst) __attribute__((always_inline)) {
@@ -278,9 +298,11 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
     }
   };
   if constexpr (DIRECT) {
-    // Whole steps; what is left of the contraction comes through registers behind them.
+    // Whole steps; what is left of the contraction comes through registers behind them, asked for first where the tile leaves registers for it.
+    constexpr bool kEarly = BM < 256;
     if (whole > 0) {
       load_step(0, lds);
+      if (kEarly && whole < steps) ask(whole);
       landed();
       if (whole > 1) load_step(1, lds + kHalf);
       read_fragments(fa[0], fb[0], lds, 0);
@@ -301,7 +323,7 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       }
     }
     if (whole < steps) {
-      ask(whole);
+      if (!kEarly || whole == 0) ask(whole);
       __syncthreads();
       put_step(lds);
       __syncthreads();
@@ -376,10 +398,10 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   }
 }
 
-// Tiles of a launch, dealt to the eight XCDs in consecutive eighths (each has an L2 of its own).
-__device__ __forceinline__ uint32_t tile_of_block(uint32_t total) {
-  const uint32_t per = (total + 7) / 8, t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  return (blockIdx.x >> 3) < per && t < total ? t : ~0u;
+// Tiles of a launch, dealt to the eight XCDs in consecutive eighths (each has an L2 of its own).  `first`: workgroups of an XCD that have other tiles.
+__device__ __forceinline__ uint32_t tile_of_block(uint32_t total, uint32_t first = 0) {
+  const uint32_t per = (total + 7) / 8, i = (blockIdx.x >> 3) - first, t = (blockIdx.x & 7) * per + i;
+  return i < per && t < total ? t : ~0u;
 }
 
 template <typename T, int BM, int BN, int WY, int WX, bool DIRECT>
@@ -460,22 +482,22 @@ __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
 template <typename T, int BM, int BN, int WY, int WX, bool DIRECT>
 __global__ __launch_bounds__(64 * WY * WX) void k_backward(const Product dx, const Product dw) {
   __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (BM + BN)];
-  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits;
-  const uint32_t tile = tile_of_block(n_dw + n_dx);
+  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
+  const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
   if (tile == ~0u) return;
-  if (tile < n_dw) tile_product<T, BM, BN, WY, WX, false, false, DIRECT>(dw, tile, lds);
-  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT>(dx, tile - n_dw, lds);
+  if ((blockIdx.x >> 3) < first) tile_product<T, BM, BN, WY, WX, false, false, DIRECT>(dw, tile, lds);
+  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT>(dx, tile, lds);
 }
 
 // The same for small gradients: any alignment, and dz formed on the way (dy's and pre's rows in the place of dz's).
 template <typename T>
 __global__ __launch_bounds__(256) void k_backward_small(const Product dx, const Product dw) {
   __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (64 + 64)];
-  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits;
-  const uint32_t tile = tile_of_block(n_dw + n_dx);
+  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
+  const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
   if (tile == ~0u) return;
-  if (tile < n_dw) tile_product<T, 64, 64, 2, 2, false, false, false, B_SIGNAL>(dw, tile, lds);
-  else tile_product<T, 64, 64, 2, 2, true, true, false, A_SIGNAL>(dx, tile - n_dw, lds);
+  if ((blockIdx.x >> 3) < first) tile_product<T, 64, 64, 2, 2, false, false, false, B_SIGNAL>(dw, tile, lds);
+  else tile_product<T, 64, 64, 2, 2, true, true, false, A_SIGNAL>(dx, tile, lds);
 }
 
 // Joins the sums of a split contraction, in the order of the splits, and finishes them; eight columns per thread.
@@ -485,13 +507,14 @@ struct Join {
   const float *db_part;      // [db_parts][N of the second product] or null
   void *db;
   int db_parts, db_n;
+  unsigned db_block;         // the first workgroup of the column sums
 };
 template <typename T>
 __global__ __launch_bounds__(256) void k_join(const Join j) {
   int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (g < j.groups[i]) {
+    if (blockIdx.x < j.db_block && g < j.groups[i]) {
       const Product &p = j.p[i];
       const int per = (p.N + 7) / 8;
       const int64_t m = g / per;
@@ -510,10 +533,22 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
     }
     g -= j.groups[i];
   }
-  if (j.db_part && g < j.db_n) {
-    float s = 0.f;
-    for (int i = 0; i < j.db_parts; ++i) s += j.db_part[(int64_t)i * j.db_n + g];
-    static_cast<T *>(j.db)[g] = from_f32<T>(s);
+  if (blockIdx.x < j.db_block) return;
+  if (!j.db_part) return;
+  // Column sums of dz: a workgroup of its own takes 32 columns, eight lanes of each every eighth part.
+  __shared__ float part[8][32];
+  const int c = (int)(blockIdx.x - j.db_block) * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
+  float s = 0.f;
+  if (c < j.db_n) {
+#pragma unroll 8
+    for (int i = lane; i < j.db_parts; i += 8) s += j.db_part[(int64_t)i * j.db_n + c];
+  }
+  part[lane][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (lane == 0 && c < j.db_n) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x];
+    static_cast<T *>(j.db)[c] = from_f32<T>(s);
   }
 }
 
@@ -681,13 +716,15 @@ void forward_tiles(const Product &p, bool dir, hipStream_t st) {
 
 template <typename T>
 int launch_join(Join &j, hipStream_t st) {
-  int64_t total = j.db_part ? j.db_n : 0;
+  int64_t total = 0;
   for (int i = 0; i < 2; ++i) {
     j.groups[i] = j.p[i].splits > 1 ? j.p[i].M * ceil_div(j.p[i].N, 8) : 0;
     total += j.groups[i];
   }
-  if (total == 0) return CADA_OK;
-  k_join<T><<<(unsigned)ceil_div(total, 256), 256, 0, st>>>(j);
+  j.db_block = (unsigned)ceil_div(total, 256);
+  const unsigned grid = j.db_block + (j.db_part ? (unsigned)ceil_div(j.db_n, 32) : 0);
+  if (grid == 0) return CADA_OK;
+  k_join<T><<<grid, 256, 0, st>>>(j);
   return ops_launched("linear join");
 }
 
@@ -745,7 +782,8 @@ BackwardPlan plan_backward(const cada_linear_grad *a) {
   else if (a->dx) { cut(s, 1, a->type, largest, c); b.dx = c[0]; }
   else if (a->dw) { cut(s + 1, 1, a->type, largest, c); b.dw = c[0]; }
   b.lddz = ceil_div(out, 8) * 8;
-  b.rows_per_block = std::max<int64_t>(32, ceil_div(ceil_div(rows, 64), 8) * 8);
+  // (workgroups for every CU several times over, but no more parts of the column sums than rows / 16)
+  b.rows_per_block = std::max<int64_t>(16, ceil_div(ceil_div(rows * ceil_div(out, 256), 2048), 8) * 8);
   b.row_blocks = b.small ? b.dw.splits : ceil_div(rows, b.rows_per_block);
   size_t off = b.own_dz ? ops_align((size_t)rows * b.lddz * elem) : 0;
   b.off_db = off;
@@ -766,7 +804,7 @@ int zero_table(void *p, int64_t ld, int64_t rows, int64_t n, hipStream_t st) {
 
 template <typename T, int E, int W>
 void backward_tiles(const Product &dx, const Product &dw, bool dir, hipStream_t st) {
-  const unsigned grid = (unsigned)(ceil_div(tiles_of(dx) + tiles_of(dw), 8) * 8);
+  const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);
   if (dir) k_backward<T, E, E, 2, W, true><<<grid, 128 * W, 0, st>>>(dx, dw);
   else if constexpr (E == 64) k_backward<T, E, E, 2, W, false><<<grid, 128 * W, 0, st>>>(dx, dw);
 }
@@ -806,7 +844,7 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   }
   if (a->dx || a->dw) {
     const int tile = a->dx ? b.dx.tile : b.dw.tile;
-    if (b.small) k_backward_small<T><<<(unsigned)(ceil_div(tiles_of(dx) + tiles_of(dw), 8) * 8), 256, 0, st>>>(dx, dw);
+    if (b.small) k_backward_small<T><<<(unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8), 256, 0, st>>>(dx, dw);
     else if (tile == 64) backward_tiles<T, 64, 2>(dx, dw, b.direct, st);
     if constexpr (sizeof(T) == 2) {
       if (!b.small && tile == 128) backward_tiles<T, 128, 2>(dx, dw, b.direct, st);
