@@ -6,6 +6,7 @@
 // BM x BN outputs and walks the contraction in steps of 128 bytes per row, both operands' next step on its way into the other half
 // of LDS while the matrix instructions (32x32x16 bf16, 32x32x2 f32; float32 accumulators) take this one.
 #include <algorithm>
+#include <cmath>
 
 #include "cada_ops_internal.h"
 
@@ -69,32 +70,49 @@ template <typename T, bool KC, int BO, int TH> struct Side {
   }
 };
 
-// The general way: through registers, any alignment, whatever lies outside [0, left) x [.., k_end) zero.  A piece is one load wherever 16 bytes from its start
-// lie before the table's last element (behind a row's end lies the next row, and is masked); else its elements one by one.
+// The general way: through registers, any alignment, whatever lies outside [0, left) x [.., k_end) zero.  A piece is always one load and no branch (a branch
+// per piece makes the compiler wait for one piece before it asks for the next): behind a row's end it reads the next row, and past the
+// table's last element (`end`) the 16 bytes before that, so a table holds 16 bytes at least.  What does not belong to the row is masked, and what was read
+// from before its place is shifted there, when the piece is put into LDS, a step or two later.
 template <typename T, bool KC, int BO, int TH>
-__device__ __forceinline__ void fetch(u32x4v (&reg)[BO * 8 / TH], const T *src, int64_t ld, int64_t left, int64_t k_left, const T *end, int t) {
+__device__ __forceinline__ void piece_offsets(uint32_t (&off)[BO * 8 / TH], int64_t ld, int t) {
   typedef Side<T, KC, BO, TH> S;
-  constexpr int E = S::E;
 #pragma unroll
   for (int i = 0; i < S::kPieces; ++i) {
     int row, piece;
     S::place(i, t, row, piece);
-    const int64_t along = (KC ? k_left : left) - piece * E;        // elements from the piece's first to the row's end
-    const bool any = (KC ? row < left : row < k_left) && along > 0;
-    const T *at = src + (int64_t)row * ld + piece * E;
-    u32x4v x = {0, 0, 0, 0};
-    if (any) {
-      if (at + E <= end) x = load16(at);
-      else x = load16_n(at, along);
-    }
-    if (along < E) {
+    off[i] = (uint32_t)(((int64_t)row * ld + piece * S::E) * (int64_t)sizeof(T));
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void fetch(u32x4v (&reg)[N], const T *src, const uint32_t (&off)[N], const T *end) {
+  const T *last = end - Elem<T>::kPer16, *base = src < last ? src : last;
+  const uint32_t most = (uint32_t)min((int64_t)0xFFFFFFF0, (last - base) * (int64_t)sizeof(T));
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        if constexpr (E == 8) x[d] &= along >= 2 * d + 2 ? 0xFFFFFFFFu : along == 2 * d + 1 ? 0xFFFFu : 0u;
-        else x[d] = along > d ? x[d] : 0u;
-      }
+  for (int i = 0; i < N; ++i) reg[i] = load16(reinterpret_cast<const T *>(reinterpret_cast<const unsigned char *>(base) + min(off[i], most)));
+}
+template <typename T, bool KC, int BO, int TH>
+__device__ __forceinline__ void mask(u32x4v (&reg)[BO * 8 / TH], const T *src, int64_t ld, const T *end, int left, int k_left, int t) {
+  typedef Side<T, KC, BO, TH> S;
+  if (left >= BO && k_left >= kStep<T>) return;
+#pragma unroll
+  for (int i = 0; i < S::kPieces; ++i) {
+    int row, piece;
+    S::place(i, t, row, piece);
+    const int along = (KC ? row < left : row < k_left) ? (KC ? k_left : left) - piece * S::E : 0;        // elements of the piece that exist
+    const int64_t over = src + (int64_t)row * ld + piece * S::E + S::E - end;
+    if (along > 0 && over > 0) {
+      const int bits = (int)over * 8 * (int)sizeof(T);        // < 128, as the piece's first element exists
+      uint64_t lo = (uint64_t)reg[i][1] << 32 | reg[i][0], hi = (uint64_t)reg[i][3] << 32 | reg[i][2];
+      if (bits >= 64) { lo = hi >> (bits - 64); hi = 0; }
+      else { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
+      reg[i] = u32x4v{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
     }
-    reg[i] = x;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      if constexpr (S::E == 8) reg[i][d] &= along >= 2 * d + 2 ? 0xFFFFFFFFu : along == 2 * d + 1 ? 0xFFFFu : 0u;
+      else reg[i][d] = along > d ? reg[i][d] : 0u;
+    }
   }
 }
 // dz = dy * act'(pre) in place of dy, and its sums per element of a piece (the pieces of a thread of an oc table are the same columns of different rows).
@@ -150,8 +168,8 @@ __device__ __forceinline__ void direct(const unsigned char *lds, const void *src
 #pragma unroll
   for (int i = 0; i < N; ++i) direct_kilobyte(at + i * (TH * 16), base, off[i]);
 }
-// Everything that this wavefront has asked for has arrived, in registers and in LDS; then so for the others.
-__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// What this wavefront has asked for, but for the last N loads, has arrived, in registers and in LDS; then so for the others.
+template <int N> __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
 // ---- fragments ----
 // Sub-step ks of four: lane l holds outer index l % 32; bf16: 8 contraction indices from 16 ks + 8 (l / 32) on; float32: 4 from 8 ks + 4 (l / 32) on, one
@@ -212,7 +230,7 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int
 }
 
 enum { NO_SIGNAL = 0, A_SIGNAL = 1, B_SIGNAL = 2 };
-template <typename T, int BM, int BN, int WY, int WX, bool AKC, bool BKC, bool DIRECT, int SIGNAL = NO_SIGNAL>
+template <typename T, int BM, int BN, int WY, int WX, bool AKC, bool BKC, bool DIRECT, int STAGES, int SIGNAL = NO_SIGNAL>
 __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, unsigned char *lds) {
   constexpr int TH = 64 * WY * WX;
   typedef Side<T, AKC, BM, TH> SA;
@@ -234,31 +252,48 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   const int64_t a_step = AKC ? BK : BK * p.lda, b_step = BKC ? BK : BK * p.ldb;
   const int steps = (int)((k1 - k0 + BK - 1) / BK), whole = (int)((k1 - k0) / BK);
 
-  uint32_t oa[SA::kPieces], ob[SB::kPieces];
+  uint32_t oa[SA::kPieces], ob[SB::kPieces], op[SIGNAL == A_SIGNAL ? SA::kPieces : SIGNAL == B_SIGNAL ? SB::kPieces : 1];
   if constexpr (DIRECT) {
     direct_offsets<T, AKC, BM, TH>(oa, p.lda, AKC ? m_left : p.a_cols - m0, t);
     direct_offsets<T, BKC, BN, TH>(ob, p.ldb, BKC ? n_left : p.b_cols - n0, t);
+  } else {
+    piece_offsets<T, AKC, BM, TH>(oa, p.lda, t);
+    piece_offsets<T, BKC, BN, TH>(ob, p.ldb, t);
   }
   // The way through registers: asked for early, put into LDS where the step before has been read.
-  u32x4v ra[SA::kPieces], rb[SB::kPieces], rp[SIGNAL == A_SIGNAL ? SA::kPieces : SIGNAL == B_SIGNAL ? SB::kPieces : 1];
+  struct Pieces { u32x4v a[SA::kPieces], b[SB::kPieces], pre[SIGNAL == A_SIGNAL ? SA::kPieces : SIGNAL == B_SIGNAL ? SB::kPieces : 1]; };
   float column_sum[Elem<T>::kPer16] = {};
-  auto ask = [&](int s) __attribute__((always_inline)) {
-    const int64_t k_left = k1 - k0 - (int64_t)s * BK;
-    fetch<T, AKC, BM, TH>(ra, a + s * a_step, p.lda, m_left, k_left, a_end, t);
-    fetch<T, BKC, BN, TH>(rb, b + s * b_step, p.ldb, n_left, k_left, b_end, t);
-    if constexpr (SIGNAL == A_SIGNAL) {
-      if (p.act != CADA_ACT_NONE) fetch<T, AKC, BM, TH>(rp, static_cast<const T *>(p.pre) + m0 * p.ldpre + k0 + (int64_t)s * BK, p.ldpre, m_left, k_left,
-                                                                static_cast<const T *>(p.pre) + (p.M - 1) * p.ldpre + p.K, t);
-    } else if constexpr (SIGNAL == B_SIGNAL) {
-      if (p.act != CADA_ACT_NONE) fetch<T, BKC, BN, TH>(rp, static_cast<const T *>(p.pre) + (k0 + (int64_t)s * BK) * p.ldpre + n0, p.ldpre, n_left, k_left,
-                                                                static_cast<const T *>(p.pre) + (p.K - 1) * p.ldpre + p.N, t);
-    }
+  const int m_in = (int)min(m_left, (int64_t)BM), n_in = (int)min(n_left, (int64_t)BN);
+  auto k_in = [&](int s) __attribute__((always_inline)) { return (int)min(k1 - k0 - (int64_t)s * BK, (int64_t)BK); };
+  // (without an activation there is no pre: the signal itself is read again, and not used, rather than a branch among the loads)
+  const bool no_act = SIGNAL == NO_SIGNAL || p.act == CADA_ACT_NONE;
+  const int64_t ldpre = no_act ? (SIGNAL == A_SIGNAL ? p.lda : p.ldb) : p.ldpre;
+  const T *pre = static_cast<const T *>(no_act ? (SIGNAL == A_SIGNAL ? p.a : p.b) : p.pre), *pre_end = pre;
+  if constexpr (SIGNAL != NO_SIGNAL) {
+    pre_end += SIGNAL == A_SIGNAL ? (p.M - 1) * ldpre + p.K : (p.K - 1) * ldpre + p.N;
+    pre += SIGNAL == A_SIGNAL ? m0 * ldpre + k0 : k0 * ldpre + n0;
+  }
+  const int64_t pre_step = SIGNAL == A_SIGNAL ? BK : BK * ldpre;
+  if constexpr (SIGNAL == A_SIGNAL) piece_offsets<T, AKC, BM, TH>(op, ldpre, t);
+  if constexpr (SIGNAL == B_SIGNAL) piece_offsets<T, BKC, BN, TH>(op, ldpre, t);
+  auto ask = [&](Pieces &r, int s) __attribute__((always_inline)) {
+    fetch(r.a, a + s * a_step, oa, a_end);
+    fetch(r.b, b + s * b_step, ob, b_end);
+    if constexpr (SIGNAL != NO_SIGNAL) fetch(r.pre, pre + s * pre_step, op, pre_end);
   };
-  auto put_step = [&](unsigned char *dst) __attribute__((always_inline)) {
-    if constexpr (SIGNAL == A_SIGNAL) signal<T>(ra, rp, p.act, column_sum);
-    if constexpr (SIGNAL == B_SIGNAL) signal<T>(rb, rp, p.act, column_sum);
-    put<SA::kPieces, TH>(dst, ra, t);
-    put<SB::kPieces, TH>(dst + SA::kBytes, rb, t);
+  auto put_step = [&](Pieces &r, int s, unsigned char *dst) __attribute__((always_inline)) {
+    const int k = k_in(s);
+    mask<T, AKC, BM, TH>(r.a, a + s * a_step, p.lda, a_end, m_in, k, t);
+    mask<T, BKC, BN, TH>(r.b, b + s * b_step, p.ldb, b_end, n_in, k, t);
+    if constexpr (SIGNAL == A_SIGNAL) {
+      mask<T, AKC, BM, TH>(r.pre, pre + s * pre_step, ldpre, pre_end, m_in, k, t);
+      signal<T>(r.a, r.pre, p.act, column_sum);
+    } else if constexpr (SIGNAL == B_SIGNAL) {
+      mask<T, BKC, BN, TH>(r.pre, pre + s * pre_step, ldpre, pre_end, n_in, k, t);
+      signal<T>(r.b, r.pre, p.act, column_sum);
+    }
+    put<SA::kPieces, TH>(dst, r.a, t);
+    put<SB::kPieces, TH>(dst + SA::kBytes, r.b, t);
   };
   auto load_step = [&](int s, unsigned char *dst) __attribute__((always_inline)) {
     direct<SA::kPieces, TH>(dst, a + s * a_step, oa, wave);
@@ -288,6 +323,7 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       for (int j = 0; j < FN; ++j) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);
   };
   Frag fa[2][FM], fb[2][FN];
+  Pieces reg[2];
   auto whole_step = [&](const unsigned char *src) __attribute__((always_inline)) {
     read_fragments(fa[0], fb[0], src, 0);
 #pragma unroll
@@ -300,21 +336,34 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   if constexpr (DIRECT) {
     // Whole steps; what is left of the contraction comes through registers behind them, asked for first where the tile leaves registers for it.
     constexpr bool kEarly = BM < 256;
+    auto ask_tail = [&]() __attribute__((always_inline)) {
+      uint32_t ta[SA::kPieces], tb[SB::kPieces];
+      piece_offsets<T, AKC, BM, TH>(ta, p.lda, t);
+      piece_offsets<T, BKC, BN, TH>(tb, p.ldb, t);
+      fetch(reg[0].a, a + whole * a_step, ta, a_end);
+      fetch(reg[0].b, b + whole * b_step, tb, b_end);
+    };
     if (whole > 0) {
-      load_step(0, lds);
-      if (kEarly && whole < steps) ask(whole);
-      landed();
-      if (whole > 1) load_step(1, lds + kHalf);
+      constexpr int P = SA::kPieces + SB::kPieces;
+#pragma unroll
+      for (int q = 0; q < STAGES; ++q) {
+        if (q < whole) load_step(q, lds + q * kHalf);
+        if (q == 0 && kEarly && whole < steps) ask_tail();
+      }
+      if (whole >= STAGES) landed<(STAGES - 1) * P>();
+      else landed<0>();
       read_fragments(fa[0], fb[0], lds, 0);
       for (int s = 0; s < whole; ++s) {
-        unsigned char *here = lds + (s & 1) * kHalf, *there = lds + ((s + 1) & 1) * kHalf;
+        unsigned char *here = lds + (s & (STAGES - 1)) * kHalf, *there = lds + ((s + 1) & (STAGES - 1)) * kHalf;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
           if (ks < 3) {
             read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
           } else {
-            landed();               // the next step is there, and everybody has read this one
-            if (s + 2 < whole) load_step(s + 2, here);
+            // the next step is there, and everybody has read this one
+            if (STAGES > 2 && s + STAGES - 1 < whole) landed<(STAGES - 2) * P>();
+            else landed<0>();
+            if (s + STAGES < whole) load_step(s + STAGES, here);
             read_fragments(fa[0], fb[0], there, 0);        // (past the last step: what nobody uses)
           }
           __builtin_amdgcn_sched_barrier(0);        // (the reads of the next sub-step go out before this one's products, not between them)
@@ -323,21 +372,39 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       }
     }
     if (whole < steps) {
-      if (!kEarly || whole == 0) ask(whole);
+      if (!kEarly || whole == 0) ask_tail();
       __syncthreads();
-      put_step(lds);
+      put_step(reg[0], whole, lds);
       __syncthreads();
       whole_step(lds);
     }
   } else {
-    ask(0);
-    put_step(lds);
-    __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-      if (s + 1 < steps) ask(s + 1);
-      whole_step(lds + (s & 1) * kHalf);
-      if (s + 1 < steps) put_step(lds + ((s + 1) & 1) * kHalf);
-      __syncthreads();
+    // Two steps ahead in registers (asked for also where there is no such step: the loads are in bounds, and a branch around them would be waited at); the next
+    // step is put into LDS between this one's products.
+    ask(reg[0], 0);
+    ask(reg[1], 1);
+    put_step(reg[0], 0, lds);
+    lds_sync();
+    read_fragments(fa[0], fb[0], lds, 0);
+    auto one = [&](Pieces &next, Pieces &after, int s) __attribute__((always_inline)) {
+      unsigned char *here = lds + (s & 1) * kHalf, *there = lds + ((s + 1) & 1) * kHalf;
+      ask(after, s + 2);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        if (ks < 3) {
+          read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
+        } else {
+          lds_sync();
+          read_fragments(fa[0], fb[0], there, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply_all(fa[ks & 1], fb[ks & 1]);
+        if (ks == 1) put_step(next, s + 1, there);
+      }
+    };
+    for (int s = 0; s < steps; s += 2) {
+      one(reg[1], reg[0], s);
+      if (s + 1 < steps) one(reg[0], reg[1], s + 1);
     }
   }
   __syncthreads();
@@ -404,11 +471,11 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t total, uint32_t first
   return i < per && t < total ? t : ~0u;
 }
 
-template <typename T, int BM, int BN, int WY, int WX, bool DIRECT>
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES>
 __global__ __launch_bounds__(64 * WY * WX) void k_forward(const Product p) {
-  __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (BM + BN)];
+  __shared__ __align__(16) unsigned char lds[STAGES * kStepBytes * (BM + BN)];
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n * p.splits);
-  if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT>(p, tile, lds);
+  if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT, STAGES>(p, tile, lds);
 }
 
 // A few rows (a single sample answered): a read of the weights.  A workgroup takes 64 columns, a lane eight of them (one line of memory per eight lanes and weight row), and
@@ -479,14 +546,14 @@ __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
 }
 
 // dx and dw in one launch (either may have no tiles).
-template <typename T, int BM, int BN, int WY, int WX, bool DIRECT>
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES>
 __global__ __launch_bounds__(64 * WY * WX) void k_backward(const Product dx, const Product dw) {
-  __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (BM + BN)];
+  __shared__ __align__(16) unsigned char lds[STAGES * kStepBytes * (BM + BN)];
   const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
   const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
   if (tile == ~0u) return;
-  if ((blockIdx.x >> 3) < first) tile_product<T, BM, BN, WY, WX, false, false, DIRECT>(dw, tile, lds);
-  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT>(dx, tile, lds);
+  if ((blockIdx.x >> 3) < first) tile_product<T, BM, BN, WY, WX, false, false, DIRECT, STAGES>(dw, tile, lds);
+  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT, STAGES>(dx, tile, lds);
 }
 
 // The same for small gradients: any alignment, and dz formed on the way (dy's and pre's rows in the place of dz's).
@@ -496,8 +563,31 @@ __global__ __launch_bounds__(256) void k_backward_small(const Product dx, const 
   const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
   const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
   if (tile == ~0u) return;
-  if ((blockIdx.x >> 3) < first) tile_product<T, 64, 64, 2, 2, false, false, false, B_SIGNAL>(dw, tile, lds);
-  else tile_product<T, 64, 64, 2, 2, true, true, false, A_SIGNAL>(dx, tile, lds);
+  if ((blockIdx.x >> 3) < first) tile_product<T, 64, 64, 2, 2, false, false, false, 2, B_SIGNAL>(dw, tile, lds);
+  else tile_product<T, 64, 64, 2, 2, true, true, false, 2, A_SIGNAL>(dx, tile, lds);
+}
+
+// Tables of less than 16 bytes (the contraction has few terms, or there are few outputs in a row or column), and rows so far apart that a tile's
+// do not lie within 4 GB: a thread per output.
+template <typename T, bool AKC, bool BKC, int SIGNAL>
+__global__ __launch_bounds__(256) void k_by_element(const Product p) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= p.M * p.N) return;
+  const int64_t m = i / p.N, n = i - m * p.N;
+  float sum = 0.f, column = 0.f;
+  for (int64_t k = 0; k < p.K; ++k) {
+    float a = to_f32(static_cast<const T *>(p.a)[AKC ? m * p.lda + k : k * p.lda + m]), b = to_f32(static_cast<const T *>(p.b)[BKC ? n * p.ldb + k : k * p.ldb + n]);
+    if constexpr (SIGNAL != NO_SIGNAL) {
+      float &dz = SIGNAL == A_SIGNAL ? a : b;
+      if (p.act != CADA_ACT_NONE) dz *= activation_slope<T>(to_f32(static_cast<const T *>(p.pre)[SIGNAL == A_SIGNAL ? m * p.ldpre + k : k * p.ldpre + n]), p.act);
+      column += dz;
+      dz = to_f32(from_f32<T>(dz));
+    }
+    sum = fmaf(a, b, sum);
+  }
+  float f[8] = {sum};
+  finish8<T>(p.epi, m, (int)n, 1, f);
+  if (SIGNAL == B_SIGNAL && p.db && m == 0) static_cast<T *>(p.db)[n] = from_f32<T>(column);
 }
 
 // Joins the sums of a split contraction, in the order of the splits, and finishes them; eight columns per thread.
@@ -596,6 +686,21 @@ __global__ __launch_bounds__(256) void k_signal(const Signal a) {
   }
 }
 
+// Tables whose rows start on no 16-byte boundary, copied to rows that do (filled up with zeros), for products large enough to be worth it.
+struct Pack { const void *src; void *dst; int64_t ld, rows, cols, ldd; };
+struct Packs { Pack p[2]; int64_t pieces[2]; };
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack(const Packs a) {
+  constexpr int E = Elem<T>::kPer16;
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int q = i < a.pieces[0] ? 0 : 1;
+  i -= q ? a.pieces[0] : 0;
+  if (i >= a.pieces[q]) return;
+  const Pack &p = a.p[q];
+  const int64_t per = p.ldd / E, row = i / per, col = (i - row * per) * E;
+  *reinterpret_cast<u32x4v *>(static_cast<T *>(p.dst) + row * p.ldd + col) = load16_n(static_cast<const T *>(p.src) + row * p.ld + col, p.cols - col);
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void k_zero(T *p, int64_t ld, int64_t rows, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * n; i += (int64_t)gridDim.x * 256) {
@@ -611,54 +716,69 @@ constexpr int kCUs = 256;
 // How a product is cut: the tile's edge, and into how many parts its contraction.
 struct Cut { int tile, splits; int64_t k_per_split; };
 
-// What a tile costs, in microseconds, measured (one product of random values, whole tiles, operands in the caches): a step alone on its CU and with all CUs at work, a
-// step's share of a full CU, and the tile's way in and out.  At 8192 x 4096 x 4096 bf16: 256 x 256 tiles 1220 TFLOP/s, 128 x 128 1060, 64 x 64 640.  Float32 is
-// bound by the matrix instructions at any of them (146 TFLOP/s, 64 x 64 as 128 x 128), so it takes the smallest.
+// What a tile costs, in microseconds, measured (one product of random values, whole tiles, operands in the caches): a step alone on its CU, what all CUs at work add to
+// it, a step's share of a full CU, and the tile's way in and out.  At 8192 x 4096 x 4096 bf16: 256 x 256 tiles 1220 TFLOP/s, 128 x 128 1080, 64 x 64 640; a single
+// tile per CU: 870 (128), 460 (64).  Float32 is bound by the matrix instructions at any of them (146 TFLOP/s, 64 x 64 as 128 x 128), so it takes the smallest.
 struct TileCost { int tile, slots; double alone, crowd, share, ends; };
-constexpr TileCost kCostBf16[] = {{64, 5, 0.22, 0.25, 0.235, 1.7}, {128, 2, 0.45, 0.37, 0.49, 3.8}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
+constexpr TileCost kCostBf16[] = {{64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
 constexpr TileCost kCostF32[] = {{64, 5, 0.5, 0.1, 0.46, 1.7}};
+// Through registers (64 x 64 only): 8192 x 4001 x 2003 bf16 340 us where 4000 x 2000 takes 108 directly, float32 1100 and 960.
+constexpr TileCost kCostBf16Registers[] = {{64, 5, 0.45, 0.1, 0.335, 1.9}}, kCostF32Registers[] = {{64, 5, 0.8, 0.1, 0.54, 1.9}};
 constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct Shape { int64_t M, N, K; };
-// Estimated time of one or two products in one launch with this tile and these splits.
-double estimate(const TileCost &c, const Shape *s, const int *splits, int n, int step) {
-  int64_t tiles = 0, most = 0;
-  double work = 0, join = 0;
-  for (int i = 0; i < n; ++i) {
-    const int64_t t = ceil_div(s[i].M, c.tile) * ceil_div(s[i].N, c.tile) * splits[i], k = ceil_div(ceil_div(s[i].K, step), splits[i]);
-    tiles += t;
-    work += (double)t * k;
-    most = std::max(most, k);
-    if (splits[i] > 1) join += (splits[i] * 4.0 + 2.0) * (double)s[i].M * s[i].N / kJoinBytesPerUs;
-  }
-  if (join > 0) join += kJoinLaunch;
-  const double per_cu = (double)ceil_div(tiles, kCUs);
-  return std::max(most * (c.alone + c.crowd * std::min(1.0, (double)tiles / kCUs)), per_cu * (work / tiles) * c.share) + c.ends * std::ceil(per_cu / c.slots) + join;
-}
-constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
-// The cheapest cut of one or two products (one tile for both), by that estimate; with `largest` = 64 only the smallest tile.
-void cut(const Shape *s, int n, int type, int largest, Cut *out) {
-  const int step = kStepBytes / (int)type_bytes(type);
-  const TileCost *costs = type == CADA_BF16 ? kCostBf16 : kCostF32;
-  const int n_costs = type == CADA_BF16 ? 3 : 1;
+// The cheapest cut of one or two products in one launch (one tile for both) by that estimate, which it returns.
+double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
+  const int64_t step = kStepBytes / (int64_t)type_bytes(type);
+  const TileCost *costs = type == CADA_BF16 ? (direct ? kCostBf16 : kCostBf16Registers) : direct ? kCostF32 : kCostF32Registers;
+  const int n_costs = type == CADA_BF16 && direct ? 3 : 1;
+  int64_t steps[2] = {0, 0};
+  for (int i = 0; i < n; ++i) steps[i] = ceil_div(s[i].K, step);
   double best = 1e300;
-  for (int c = 0; c < n_costs && costs[c].tile <= largest; ++c) {
-    for (int s0 : kSplits) {
-      if (s0 > 1 && ceil_div(s[0].K, step) < 2 * s0) break;
-      for (int s1 : kSplits) {
-        if (s1 > 1 && (n < 2 || ceil_div(s[1].K, step) < 2 * s1)) break;
-        const int splits[2] = {s0, s1};
-        const double e = estimate(costs[c], s, splits, n, step);
-        if (e < best) {
-          best = e;
-          for (int i = 0; i < n; ++i) {
-            const int64_t steps = ceil_div(s[i].K, step), per = ceil_div(steps, splits[i]);
-            out[i] = Cut{costs[c].tile, (int)ceil_div(steps, per), per * step};
-          }
+  for (int c = 0; c < n_costs; ++c) {
+    const TileCost &t = costs[c];
+    // each product's splits that may help (none that leave less than two steps, or make more tiles than two for every CU), with tiles, steps and the join's time
+    struct Option { int splits; double tiles, steps, join; } opt[2][16];
+    int n_opt[2] = {0, 0};
+    for (int i = 0; i < n; ++i) {
+      const int64_t tiles = ceil_div(s[i].M, t.tile) * ceil_div(s[i].N, t.tile);
+      for (int k : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+        if (k > 1 && (steps[i] < 2 * k || tiles * k > 2 * kCUs)) break;
+        opt[i][n_opt[i]++] = Option{k, (double)(tiles * k), (double)ceil_div(steps[i], k), k > 1 ? (k * 4.0 + 2.0) * (double)s[i].M * (double)s[i].N / kJoinBytesPerUs : 0.0};
+      }
+    }
+    for (int i = 0; i < n_opt[0]; ++i) {
+      for (int j = 0; j < (n > 1 ? n_opt[1] : 1); ++j) {
+        const Option &a = opt[0][i], *b = n > 1 ? &opt[1][j] : nullptr;
+        const double tiles = a.tiles + (b ? b->tiles : 0.0), most = b ? std::max(a.steps, b->steps) : a.steps, join = a.join + (b ? b->join : 0.0);
+        const double mean = (a.tiles * a.steps + (b ? b->tiles * b->steps : 0.0)) / tiles, per_cu = std::ceil(tiles / kCUs);
+        const double e = std::max(most * (t.alone + t.crowd * std::min(1.0, tiles / kCUs)), per_cu * mean * t.share) + t.ends * std::ceil(per_cu / t.slots) + (join > 0.0 ? join + kJoinLaunch : 0.0);
+        if (e >= best) continue;
+        best = e;
+        for (int q = 0; q < n; ++q) {
+          const int64_t per = ceil_div(steps[q], (q == 0 ? a : *b).splits);
+          out[q] = Cut{t.tile, (int)ceil_div(steps[q], per), per * step};
         }
       }
     }
   }
+  return best;
+}
+// What a copy of a table to aligned rows costs, in the same microseconds (a launch for one or two of them).
+constexpr double kPackLaunch = 4.0, kPackBytesPerUs = 3.5e6;
+double pack_cost(int64_t rows, int64_t cols, size_t elem) { return 2.0 * elem * (double)rows * (double)cols / kPackBytesPerUs; }
+int64_t packed_ld(int64_t cols) { return ceil_div(cols, 8) * 8; }
+size_t packed_bytes(int64_t rows, int64_t cols, size_t elem) { return ops_align((size_t)rows * packed_ld(cols) * elem); }
+template <typename T>
+int launch_pack(Packs &a, hipStream_t st) {
+  int64_t total = 0;
+  for (int i = 0; i < 2; ++i) {
+    a.pieces[i] = a.p[i].src ? a.p[i].rows * (a.p[i].ldd / Elem<T>::kPer16) : 0;
+    total += a.pieces[i];
+  }
+  if (total == 0) return CADA_OK;
+  k_pack<T><<<(unsigned)ceil_div(total, 256), 256, 0, st>>>(a);
+  return ops_launched("linear pack");
 }
 size_t partial_bytes(const Cut &c, int64_t M, int64_t N) { return c.splits > 1 ? ops_align((size_t)c.splits * M * N * 4) : 0; }
 
@@ -692,26 +812,50 @@ bool check_table(const char *name, const void *p, int64_t ld, int64_t cols, int 
 
 // ---- forward ----
 
-struct ForwardPlan { bool few, direct; Cut cut; size_t bytes; };
+// Whether a table is too small for a read of 16 bytes, or a tile of it too large for offsets in 32 bits.
+bool no_tiles(int64_t rows, int64_t ld, int64_t cols, size_t elem) { return ((rows - 1) * ld + cols) * (int64_t)elem < 16 || 64 * ld * (int64_t)elem >= (int64_t)1 << 32; }
+
+struct ForwardPlan { bool few, by_element, direct, pack_x, pack_w; Cut cut; size_t off_x, off_w, bytes; };
 ForwardPlan plan_forward(const cada_linear *a) {
   ForwardPlan f{};
   if (a->rows == 0) return f;
   f.few = a->rows <= kFewRows;
   f.cut = Cut{64, 1, a->in};
-  if (f.few) return f;
   const size_t elem = type_bytes(a->type);
-  f.direct = direct_kc(a->x, a->ldx, elem) && direct_oc(a->w, a->ldw, a->out, elem);
+  f.by_element = no_tiles(a->rows, a->ldx, a->in, elem) || no_tiles(a->in, a->ldw, a->out, elem);
+  if (f.few || f.by_element) return f;
+  const bool x_direct = direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, a->out, elem);
   const Shape s = {a->rows, a->out, a->in};
-  cut(&s, 1, a->type, f.direct ? 256 : 64, &f.cut);
-  f.bytes = partial_bytes(f.cut, a->rows, a->out);
+  f.direct = x_direct && w_direct;
+  const double time = cut(&s, 1, a->type, f.direct, &f.cut);
+  if (!f.direct) {
+    Cut c;
+    const double packed = cut(&s, 1, a->type, true, &c) + kPackLaunch + (x_direct ? 0 : pack_cost(a->rows, a->in, elem)) + (w_direct ? 0 : pack_cost(a->in, a->out, elem));
+    if (packed < time) {
+      f.direct = true; f.pack_x = !x_direct; f.pack_w = !w_direct;
+      f.cut = c;
+    }
+  }
+  f.off_x = partial_bytes(f.cut, a->rows, a->out);
+  f.off_w = f.off_x + (f.pack_x ? packed_bytes(a->rows, a->in, elem) : 0);
+  f.bytes = f.off_w + (f.pack_w ? packed_bytes(a->in, a->out, elem) : 0);
   return f;
 }
+
+// Four steps on their way where LDS has room for them (few tiles: long contractions come from memory, 64 x 64 x 4096 with one tile per CU 32 -> 18.5 us); two, and more
+// workgroups on a CU, where there are many tiles (64 x 64 x 1024 with four per CU 17 -> 15.5 us).
+bool deep(int tile, int64_t tiles) { return tiles <= (tile == 64 ? 2 : 1) * kCUs; }
 
 template <typename T, int E, int W>
 void forward_tiles(const Product &p, bool dir, hipStream_t st) {
   const unsigned grid = (unsigned)(ceil_div(tiles_of(p), 8) * 8);
-  if (dir) k_forward<T, E, E, 2, W, true><<<grid, 128 * W, 0, st>>>(p);
-  else if constexpr (E == 64) k_forward<T, E, E, 2, W, false><<<grid, 128 * W, 0, st>>>(p);
+  if constexpr (E == 64) {
+    if (!dir) { k_forward<T, E, E, 2, W, false, 2><<<grid, 128 * W, 0, st>>>(p); return; }
+  }
+  if constexpr (E < 256) {
+    if (deep(E, tiles_of(p))) { k_forward<T, E, E, 2, W, true, 4><<<grid, 128 * W, 0, st>>>(p); return; }
+  }
+  k_forward<T, E, E, 2, W, true, 2><<<grid, 128 * W, 0, st>>>(p);
 }
 
 template <typename T>
@@ -733,6 +877,19 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   Product p{};
   lay(&p, f.cut, a->x, a->ldx, a->w, a->ldw, a->rows, a->out, a->in, static_cast<float *>(a->workspace));
+  if (f.pack_x || f.pack_w) {
+    Packs k{};
+    char *ws = static_cast<char *>(a->workspace);
+    if (f.pack_x) {
+      k.p[0] = Pack{a->x, ws + f.off_x, a->ldx, a->rows, a->in, packed_ld(a->in)};
+      p.a = k.p[0].dst; p.lda = k.p[0].ldd;
+    }
+    if (f.pack_w) {
+      k.p[1] = Pack{a->w, ws + f.off_w, a->ldw, a->in, a->out, packed_ld(a->out)};
+      p.b = k.p[1].dst; p.ldb = p.b_cols = k.p[1].ldd;
+    }
+    if (int rc = launch_pack<T>(k, st)) return rc;
+  }
   p.epi = Epilogue{a->bias, a->residual, a->pre, a->y, a->ldr, a->ldpre, a->ldy, a->act};
   if (f.few) {
     const unsigned grid = (unsigned)ceil_div(a->out, 64);
@@ -741,9 +898,13 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
     else k_few_rows<T, 4><<<grid, kFewThreads, 0, st>>>(p);
     return ops_launched("linear");
   }
+  if (f.by_element) {
+    k_by_element<T, true, false, NO_SIGNAL><<<(unsigned)ceil_div(a->rows * a->out, 256), 256, 0, st>>>(p);
+    return ops_launched("linear");
+  }
   if (f.cut.tile == 64) forward_tiles<T, 64, 2>(p, f.direct, st);
   if constexpr (sizeof(T) == 2) {
-    if (f.cut.tile == 128) forward_tiles<T, 128, 2>(p, f.direct, st);
+    if (f.cut.tile == 128) forward_tiles<T, 128, 4>(p, f.direct, st);
     if (f.cut.tile == 256) forward_tiles<T, 256, 4>(p, f.direct, st);
   }
   if (int rc = ops_launched("linear")) return rc;
@@ -760,10 +921,10 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
 constexpr double kSmallGradients = 4e9;
 
 struct BackwardPlan {
-  bool small, own_dz, direct;
+  bool small, by_element, own_dz, direct, pack_x, pack_w;
   Cut dx, dw;
   int64_t lddz, rows_per_block, row_blocks;
-  size_t off_db, off_dx, off_dw, bytes;
+  size_t off_db, off_dx, off_dw, off_x, off_w, bytes;
 };
 BackwardPlan plan_backward(const cada_linear_grad *a) {
   BackwardPlan b{};
@@ -771,16 +932,33 @@ BackwardPlan plan_backward(const cada_linear_grad *a) {
   const int64_t rows = a->rows, in = a->in, out = a->out;
   const size_t elem = type_bytes(a->type);
   const bool products = a->dx || a->dw;
+  // (dy and pre are met as operands, w in dx and x in dw)
+  b.by_element = no_tiles(rows, a->lddy, out, elem) || (a->act != CADA_ACT_NONE && no_tiles(rows, a->ldpre, out, elem)) || (a->dx && no_tiles(in, a->ldw, out, elem)) || (a->dw && no_tiles(rows, a->ldx, in, elem));
+  b.dx = Cut{64, 1, out};
+  b.dw = Cut{64, 1, rows};
+  if (b.by_element && (a->dw || !a->db)) return b;
+  b.by_element = false;
   b.small = products && (a->dw || !a->db) && 4.0 * rows * in * out < kSmallGradients;
   // dz in the workspace, unless dy itself will do
   b.own_dz = products && !b.small && (a->act != CADA_ACT_NONE || !direct_oc(a->dy, a->lddy, out, elem));
-  b.direct = !b.small && (!a->dx || direct_kc(a->w, a->ldw, elem)) && (!a->dw || direct_oc(a->x, a->ldx, in, elem));
+  const bool w_direct = !a->dx || direct_kc(a->w, a->ldw, elem), x_direct = !a->dw || direct_oc(a->x, a->ldx, in, elem);
+  b.direct = !b.small && w_direct && x_direct;
   const Shape s[2] = {{rows, in, out}, {in, out, rows}};
-  Cut c[2];
-  const int largest = b.direct ? 256 : 64;
-  if (a->dx && a->dw) { cut(s, 2, a->type, largest, c); b.dx = c[0]; b.dw = c[1]; }
-  else if (a->dx) { cut(s, 1, a->type, largest, c); b.dx = c[0]; }
-  else if (a->dw) { cut(s + 1, 1, a->type, largest, c); b.dw = c[0]; }
+  const int n = (a->dx ? 1 : 0) + (a->dw ? 1 : 0);
+  Cut c[2], d[2];
+  if (n > 0) {
+    const Shape *first = a->dx ? s : s + 1;
+    const double time = cut(first, n, a->type, b.direct, c);
+    if (!b.small && !b.direct) {
+      const double packed = cut(first, n, a->type, true, d) + kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, out, elem));
+      if (packed < time) {
+        b.direct = true; b.pack_x = !x_direct; b.pack_w = !w_direct;
+        c[0] = d[0]; c[1] = d[1];
+      }
+    }
+    if (a->dx) b.dx = c[0];
+    if (a->dw) b.dw = c[n - 1];
+  }
   b.lddz = ceil_div(out, 8) * 8;
   // (workgroups for every CU several times over, but no more parts of the column sums than rows / 16)
   b.rows_per_block = std::max<int64_t>(16, ceil_div(ceil_div(rows * ceil_div(out, 256), 2048), 8) * 8);
@@ -792,6 +970,10 @@ BackwardPlan plan_backward(const cada_linear_grad *a) {
   if (a->dx) off += partial_bytes(b.dx, rows, in);
   b.off_dw = off;
   if (a->dw) off += partial_bytes(b.dw, in, out);
+  b.off_x = off;
+  if (b.pack_x) off += packed_bytes(rows, in, elem);
+  b.off_w = off;
+  if (b.pack_w) off += packed_bytes(in, out, elem);
   b.bytes = off;
   return b;
 }
@@ -805,8 +987,13 @@ int zero_table(void *p, int64_t ld, int64_t rows, int64_t n, hipStream_t st) {
 template <typename T, int E, int W>
 void backward_tiles(const Product &dx, const Product &dw, bool dir, hipStream_t st) {
   const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);
-  if (dir) k_backward<T, E, E, 2, W, true><<<grid, 128 * W, 0, st>>>(dx, dw);
-  else if constexpr (E == 64) k_backward<T, E, E, 2, W, false><<<grid, 128 * W, 0, st>>>(dx, dw);
+  if constexpr (E == 64) {
+    if (!dir) { k_backward<T, E, E, 2, W, false, 2><<<grid, 128 * W, 0, st>>>(dx, dw); return; }
+  }
+  if constexpr (E < 256) {
+    if (deep(E, tiles_of(dx) + tiles_of(dw))) { k_backward<T, E, E, 2, W, true, 4><<<grid, 128 * W, 0, st>>>(dx, dw); return; }
+  }
+  k_backward<T, E, E, 2, W, true, 2><<<grid, 128 * W, 0, st>>>(dx, dw);
 }
 
 template <typename T>
@@ -819,7 +1006,7 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   }
   char *ws = static_cast<char *>(a->workspace);
   float *db_part = reinterpret_cast<float *>(ws + b.off_db);
-  if (b.own_dz || (a->db && !b.small)) {
+  if (b.own_dz || (a->db && !b.small && !b.by_element)) {
     Signal s{};
     s.dy = a->dy; s.lddy = a->lddy; s.pre = a->pre; s.ldpre = a->ldpre; s.rows = a->rows; s.rows_per_block = b.rows_per_block; s.n = (int32_t)a->out; s.act = a->act;
     s.dz = b.own_dz ? ws : nullptr; s.lddz = b.lddz;
@@ -840,14 +1027,31 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
     if (b.own_dz) dw.b_cols = b.lddz;      // (dz's rows in the workspace are filled with zeros up to whole pieces)
     dw.epi.out = a->dw; dw.epi.ldo = a->lddw;
     dw.pre = a->pre; dw.ldpre = a->ldpre; dw.act = a->act;
-    if (b.small) { dw.db = a->db; dw.db_part = db_part; }
+    if (b.small || b.by_element) { dw.db = a->db; dw.db_part = db_part; }
+  }
+  if (b.pack_x || b.pack_w) {
+    Packs k{};
+    if (b.pack_x) {
+      k.p[0] = Pack{a->x, ws + b.off_x, a->ldx, a->rows, a->in, packed_ld(a->in)};
+      dw.a = k.p[0].dst; dw.lda = dw.a_cols = k.p[0].ldd;
+    }
+    if (b.pack_w) {
+      k.p[1] = Pack{a->w, ws + b.off_w, a->ldw, a->in, a->out, packed_ld(a->out)};
+      dx.b = k.p[1].dst; dx.ldb = k.p[1].ldd;
+    }
+    if (int rc = launch_pack<T>(k, st)) return rc;
   }
   if (a->dx || a->dw) {
     const int tile = a->dx ? b.dx.tile : b.dw.tile;
+    if (b.by_element) {
+      if (a->dx) k_by_element<T, true, true, A_SIGNAL><<<(unsigned)ceil_div(a->rows * a->in, 256), 256, 0, st>>>(dx);
+      if (a->dw) k_by_element<T, false, false, B_SIGNAL><<<(unsigned)ceil_div(a->in * a->out, 256), 256, 0, st>>>(dw);
+      return ops_launched("linear gradients");
+    }
     if (b.small) k_backward_small<T><<<(unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8), 256, 0, st>>>(dx, dw);
     else if (tile == 64) backward_tiles<T, 64, 2>(dx, dw, b.direct, st);
     if constexpr (sizeof(T) == 2) {
-      if (!b.small && tile == 128) backward_tiles<T, 128, 2>(dx, dw, b.direct, st);
+      if (!b.small && tile == 128) backward_tiles<T, 128, 4>(dx, dw, b.direct, st);
       if (!b.small && tile == 256) backward_tiles<T, 256, 4>(dx, dw, b.direct, st);
     }
     if (int rc = ops_launched("linear gradients")) return rc;
