@@ -1,8 +1,9 @@
 // Softmax cross-entropy over any number of classes, with its gradient (cada_ops.h).
 //
-// A row's logits are read once and stay in registers between the statistics and the gradient: max, then sum of exp(z - max) with the
-// classes that are left and their logits' sum (smoothing), then softmax - target.  A group of 16, 64, 256 or 1024 lanes takes a row, by its length;
-// rows beyond what 1024 lanes hold are read again for the gradient.
+// A row's logits are read once and stay in registers, as they were read, between the statistics and the gradient: max, then sum of exp(z - max) with the
+// classes that are left and their logits' mean (smoothing), then softmax - target.  A group of 4 to 1024 lanes takes a row, by its length; rows beyond what
+// 1024 lanes hold (131072 bf16, 65536 float32) are read again.  Two launches: the rows that count, which every gradient is divided by, and the rows, the last
+// workgroup of which adds the losses up in the rows' order.
 #include <algorithm>
 
 #include "cada_ops_internal.h"
@@ -10,11 +11,12 @@
 namespace cada {
 namespace {
 
+struct Head { int64_t count; uint32_t done; };      // rows that are not ignored; workgroups whose losses are written
 struct Xent {
   const void *logits, *labels;
   void *grad;
-  float *loss;
-  const int64_t *count;       // rows that are not ignored
+  float *loss, *mean;
+  Head *head;
   int64_t rows, ldz, ldg, ignore;
   int32_t classes, label_bytes;
   float smoothing, keep, scale;      // keep = 1 - smoothing, rounded once
@@ -24,9 +26,10 @@ __device__ __forceinline__ int64_t label_at(const void *labels, int bytes, int64
   return bytes == 8 ? static_cast<const int64_t *>(labels)[r] : (int64_t)static_cast<const int32_t *>(labels)[r];
 }
 
-__global__ __launch_bounds__(1024) void k_count(const void *labels, int bytes, int64_t rows, int64_t ignore, int64_t *count) {
+__global__ __launch_bounds__(1024) void k_count(const void *labels, int bytes, int64_t rows, int64_t ignore, Head *head, float *mean) {
   __shared__ int64_t part[16];
   int64_t n = 0;
+#pragma unroll 4
   for (int64_t r = threadIdx.x; r < rows; r += 1024) n += label_at(labels, bytes, r) != ignore;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
@@ -35,21 +38,9 @@ __global__ __launch_bounds__(1024) void k_count(const void *labels, int bytes, i
   if (threadIdx.x == 0) {
     n = 0;
     for (int i = 0; i < 16; ++i) n += part[i];
-    *count = n;
-  }
-}
-
-__global__ __launch_bounds__(1024) void k_mean(const float *loss, int64_t rows, const int64_t *count, float *mean) {
-  __shared__ double part[16];
-  double s = 0.0;
-  for (int64_t r = threadIdx.x; r < rows; r += 1024) s += (double)loss[r];
-  s = wave_sum_f64(s);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s = 0.0;
-    for (int i = 0; i < 16; ++i) s += part[i];
-    *mean = (float)(s / (double)max(*count, (int64_t)1));
+    head->count = n;
+    head->done = 0;
+    if (rows == 0 && mean) *mean = 0.f;
   }
 }
 
@@ -73,115 +64,162 @@ __device__ __forceinline__ float group_reduce(float x, float *part, OP op) {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_inff();
 
-// Eight logits of a row from class c on; classes beyond the last are -inf.
-template <typename T>
-__device__ __forceinline__ void logits8(const T *z, int c, int classes, float (&f)[8]) {
-  load8_n(z + c, classes - c, f);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) if (c + i >= classes) f[i] = -kInf;
-}
+// A row in pieces of 16 bytes, which the lanes take in turn, and the few classes behind the last whole piece, one per lane.  Pieces and classes that do not exist are -inf.
+template <typename T> constexpr uint32_t kInfBits = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
 
-template <typename T, int LANES, int V>
+// LANES lanes for a row, V pieces each; V = 0: as many as it takes, read again for each use.
+template <typename T, int LANES, int V, bool SMOOTH>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a) {
-  constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
+  constexpr int kRows = LANES < 256 ? 256 / LANES : 1, E = Elem<T>::kPer16;
   __shared__ float part[16];
+  __shared__ bool last;
   const int lane = threadIdx.x % LANES;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
   const bool here = row < a.rows;
   const int64_t r = here ? row : a.rows - 1;
   const T *z = static_cast<const T *>(a.logits) + r * a.ldz;
   T *g = a.grad ? static_cast<T *>(a.grad) + r * a.ldg : nullptr;
-  const int64_t label = label_at(a.labels, a.label_bytes, r);
-  const bool used = label != a.ignore, known = label >= 0 && label < a.classes;
-  const float zy = used && known ? to_f32(z[label]) : 0.f;      // (read before the gradient may overwrite it)
-  const float inv = a.scale / (float)max(*a.count, (int64_t)1);
-
-  float f[V > 0 ? V : 1][8];
-  float top = -kInf;
-  auto bigger = [](float x, float y) { return fmaxf(x, y); };      // (a NaN is in the sum below)
-  auto plus = [](float x, float y) { return x + y; };
+  static_assert(LANES >= E, "one class per lane behind the last piece");
+  const int whole = a.classes / E * E;
+  u32x4v raw[V > 0 ? V : 1];
   if constexpr (V > 0) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      logits8(z, (v * LANES + lane) * 8, a.classes, f[v]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, f[v][i]);
-    }
-  } else {
-    for (int c = lane * 8; c < a.classes; c += LANES * 8) {
-      logits8(z, c, a.classes, f[0]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, f[0][i]);
+      const int c = (v * LANES + lane) * E;
+      raw[v] = u32x4v{kInfBits<T>, kInfBits<T>, kInfBits<T>, kInfBits<T>};
+      if (c < whole) raw[v] = load16(z + c);
     }
   }
-  top = group_reduce<LANES>(top, part, bigger);
+  const float behind = lane < a.classes - whole ? to_f32(z[whole + lane]) : -kInf;
+  const int64_t label = label_at(a.labels, a.label_bytes, r);
+  const bool used = label != a.ignore, known = label >= 0 && label < a.classes;
+  const float zy = used && known ? to_f32(z[label]) : 0.f;      // (read before the gradient may overwrite it)
+  const float inv = a.scale / (float)max(a.head->count, (int64_t)1);
+
+  // Calls f(class of the first, logits) for each piece of this lane.  (The empty asm keeps the compiler from holding all pieces as float32 from one
+  // use to the next, which is twice the registers and spills.)
+  auto pieces = [&](auto f) __attribute__((always_inline)) {
+    float x[E];
+    if constexpr (V > 0) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        asm volatile("" : "+v"(raw[v]));
+        unpack<T>(raw[v], x);
+        f((v * LANES + lane) * E, x);
+      }
+    } else {
+      for (int c = lane * E; c < whole; c += LANES * E) {
+        unpack<T>(load16(z + c), x);
+        f(c, x);
+      }
+    }
+  };
+  float top = -kInf;
+  pieces([&](int, const float (&x)[E]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) top = fmaxf(top, x[i]);
+  });
+  top = fmaxf(top, behind);
+  top = group_reduce<LANES>(top, part, [](float x, float y) { return fmaxf(x, y); });      // (a NaN is in the sum below)
   // Differences to the largest first, so that a mask of the type's lowest value (or a row of nothing else) overflows nowhere.  A row with
   // nothing left has top = -inf; its exponentials are taken against 0, so that they are 0 and not NaN.
   const bool none = top == -kInf;
   const float base = none ? 0.f : top, share = 1.f / (float)a.classes;
   float total = 0.f, left = 0.f, mean_left = 0.f;        // mean_left: first the sum of (z - top) / classes, which cannot overflow
-  auto statistics = [&](const float (&x)[8]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float d = x[i] - base;
-      total += __builtin_amdgcn_exp2f(d * kLog2e);
-      left += x[i] != -kInf ? 1.f : 0.f;
-      mean_left = fmaf(x[i] != -kInf ? d : 0.f, share, mean_left);
+  auto statistics = [&](float x) __attribute__((always_inline)) {
+    const float d = x - base;
+    total += __builtin_amdgcn_exp2f(d * kLog2e);
+    if constexpr (SMOOTH) {
+      const bool in = x != -kInf;
+      left += in ? 1.f : 0.f;
+      mean_left = fmaf(in ? d : 0.f, share, mean_left);
     }
   };
-  if constexpr (V > 0) {
+  pieces([&](int, const float (&x)[E]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) statistics(f[v]);
-  } else {
-    for (int c = lane * 8; c < a.classes; c += LANES * 8) { logits8(z, c, a.classes, f[0]); statistics(f[0]); }
-  }
+    for (int i = 0; i < E; ++i) statistics(x[i]);
+  });
+  statistics(behind);
+  auto plus = [](float x, float y) { return x + y; };
   total = group_reduce<LANES>(total, part, plus);
-  if (a.smoothing != 0.f) {
+  if constexpr (SMOOTH) {
     left = group_reduce<LANES>(left, part, plus);
     mean_left = group_reduce<LANES>(mean_left, part, plus) * ((float)a.classes / left);
   }
   if (here && lane == 0 && a.loss) {
     // log(sum exp z) - keep z_y - smoothing mean_left z, with top taken out of all three
-    float l = logf(total) - a.keep * (zy - base) - (a.smoothing != 0.f ? a.smoothing * mean_left : 0.f);
+    float l = logf(total) - a.keep * (zy - base) - (SMOOTH ? a.smoothing * mean_left : 0.f);
     if (none) l = kInf;
     if (!known) l = __builtin_nanf("");
-    a.loss[r] = used ? l : 0.f;
+    // (to where every XCD sees it, for the last workgroup)
+    __hip_atomic_store(a.loss + r, used ? l : 0.f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  if (!g) return;
-  const bool flat = !used || !known || none;      // no gradient
-  const float f_total = flat ? 0.f : inv / total, f_keep = a.keep * inv, f_each = a.smoothing != 0.f ? a.smoothing / left * inv : 0.f;
-  auto gradient = [&](int c, float (&x)[8]) __attribute__((always_inline)) {
-    if (c >= a.classes) return;
+  if (g) {
+    const bool flat = !used || !known || none;      // no gradient
+    const float f_total = inv / total, f_keep = a.keep * inv, f_each = SMOOTH ? a.smoothing / left * inv : 0.f;
+    auto gradient = [&](float x) __attribute__((always_inline)) {
+      float p = __builtin_amdgcn_exp2f((x - base) * kLog2e) * f_total;
+      if constexpr (SMOOTH) p -= x != -kInf ? f_each : 0.f;
+      return p;
+    };
+    pieces([&](int c, float (&x)[E]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float p = __builtin_amdgcn_exp2f((x[i] - base) * kLog2e) * f_total;
-      if (x[i] != -kInf) p -= f_each;
-      if (label == c + i) p -= f_keep;
-      x[i] = flat ? 0.f : p;
-    }
-    if (here) store8_n(g + c, a.classes - c, x);
-  };
-  if constexpr (V > 0) {
+      for (int i = 0; i < E; ++i) x[i] = gradient(x[i]);
+      if (label >= c && label < c + E) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) gradient((v * LANES + lane) * 8, f[v]);
-  } else {
-    for (int c = lane * 8; c < a.classes; c += LANES * 8) { logits8(z, c, a.classes, f[0]); gradient(c, f[0]); }
+        for (int i = 0; i < E; ++i) if (label == c + i) x[i] -= f_keep;
+      }
+      if (flat) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = 0.f;
+      }
+      if (here && c < whole) store16(g + c, pack<T>(x));
+    });
+    if (here && lane < a.classes - whole) g[whole + lane] = from_f32<T>(flat ? 0.f : gradient(behind) - (label == whole + lane ? f_keep : 0.f));
+  }
+  if (!a.mean) return;
+  // The losses that this workgroup wrote are where the last one reads them before it counts itself (no fence: it would write back the gradient's lines).
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(&a.head->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  constexpr int TH = LANES < 256 ? 256 : LANES;
+  __shared__ double sums[TH / 64];
+  double s = 0.0;
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < a.rows; i += TH) s += (double)__hip_atomic_load(a.loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  s = wave_sum_f64(s);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int i = 0; i < TH / 64; ++i) s += sums[i];
+    *a.mean = (float)(s / (double)max(a.head->count, (int64_t)1));
   }
 }
 
 template <typename T, int LANES, int V>
 void launch_rows(const Xent &x, hipStream_t st) {
   constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
-  k_rows<T, LANES, V><<<(unsigned)ceil_div(x.rows, kRows), LANES < 256 ? 256 : LANES, 0, st>>>(x);
+  const unsigned grid = (unsigned)ceil_div(x.rows, kRows), threads = LANES < 256 ? 256 : LANES;
+  if (x.smoothing != 0.f) k_rows<T, LANES, V, true><<<grid, threads, 0, st>>>(x);
+  else k_rows<T, LANES, V, false><<<grid, threads, 0, st>>>(x);
 }
+// Lanes and pieces by the row's length: few lanes for a few classes, so that a wavefront holds several rows; beyond that as many as keep a lane's pieces in at
+// most 64 registers, so that two workgroups of 512 fit a CU and one reads while the other computes.
 template <typename T>
 int rows(const Xent &x, hipStream_t st) {
-  const int c = x.classes;
-  if (c <= 16 * 8) launch_rows<T, 16, 1>(x, st);
-  else if (c <= 64 * 8) launch_rows<T, 64, 1>(x, st);
-  else if (c <= 64 * 32) launch_rows<T, 64, 4>(x, st);
-  else if (c <= 256 * 32) launch_rows<T, 256, 4>(x, st);
-  else if (c <= 1024 * 32) launch_rows<T, 1024, 4>(x, st);
+  const int64_t n = ceil_div(x.classes, Elem<T>::kPer16);
+  if (n <= Elem<T>::kPer16) launch_rows<T, Elem<T>::kPer16, 1>(x, st);
+  else if (n <= 16) launch_rows<T, 16, 1>(x, st);
+  else if (n <= 64) launch_rows<T, 64, 1>(x, st);
+  else if (n <= 256) launch_rows<T, 64, 4>(x, st);
+  else if (n <= 1024) launch_rows<T, 256, 4>(x, st);
+  else if (n <= 2048) launch_rows<T, 256, 8>(x, st);
+  else if (n <= 4096) launch_rows<T, 512, 8>(x, st);
+  else if (n <= 8192) launch_rows<T, 512, 16>(x, st);
+  else if (n <= 16384) launch_rows<T, 1024, 16>(x, st);
   else launch_rows<T, 1024, 0>(x, st);
   return ops_launched("cross-entropy");
 }
@@ -222,21 +260,17 @@ int cada_cross_entropy(const cada_xent *a) {
   }
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, workspace(a))) return rc;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
-  int64_t *count = static_cast<int64_t *>(a->workspace);
+  Head *head = static_cast<Head *>(a->workspace);
   Xent x{};
   x.logits = a->logits; x.labels = a->labels; x.grad = a->grad;
   x.loss = a->loss ? a->loss : a->mean ? reinterpret_cast<float *>(static_cast<char *>(a->workspace) + kOpsAlign) : nullptr;
-  x.count = count; x.rows = a->rows; x.ldz = a->ldz; x.ldg = a->ldg; x.ignore = a->ignore_index;
+  x.mean = a->mean; x.head = head; x.rows = a->rows; x.ldz = a->ldz; x.ldg = a->ldg; x.ignore = a->ignore_index;
   x.classes = (int32_t)a->classes; x.label_bytes = a->label_bytes;
   x.smoothing = (float)a->smoothing; x.keep = (float)(1.0 - a->smoothing); x.scale = (float)a->scale;
-  k_count<<<1, 1024, 0, st>>>(a->labels, a->label_bytes, a->rows, a->ignore_index, count);
+  k_count<<<1, 1024, 0, st>>>(a->labels, a->label_bytes, a->rows, a->ignore_index, head, a->mean);
   if (int rc = ops_launched("cross-entropy count")) return rc;
-  if (a->rows > 0) if (int rc = a->type == CADA_BF16 ? rows<bf16>(x, st) : rows<float>(x, st)) return rc;
-  if (a->mean) {
-    k_mean<<<1, 1024, 0, st>>>(x.loss, a->rows, count, a->mean);
-    return ops_launched("cross-entropy mean");
-  }
-  return CADA_OK;
+  if (a->rows == 0) return CADA_OK;
+  return a->type == CADA_BF16 ? rows<bf16>(x, st) : rows<float>(x, st);
 }
 
 }  // extern "C"
