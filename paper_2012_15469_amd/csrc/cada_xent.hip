@@ -11,7 +11,10 @@
 namespace cada {
 namespace {
 
-struct Head { int64_t count; uint32_t done; };      // rows that are not ignored; workgroups whose losses are written
+// Rows that are not ignored, and workgroups whose losses are written: counted in kCounters places of a line each, and those that are full in one more (one
+// counter for all takes 12 ns per workgroup: 205 us for 16384).
+constexpr uint32_t kCounters = 64, kLineWords = 32;
+struct Head { int64_t count; uint32_t pad[kLineWords - 2]; uint32_t full[kLineWords]; uint32_t done[kCounters * kLineWords]; };
 struct Xent {
   const void *logits, *labels;
   void *grad;
@@ -35,11 +38,12 @@ __global__ __launch_bounds__(1024) void k_count(const void *labels, int bytes, i
   for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
   __syncthreads();
+  if (threadIdx.x < kCounters) head->done[threadIdx.x * kLineWords] = 0;
   if (threadIdx.x == 0) {
+    head->full[0] = 0;
     n = 0;
     for (int i = 0; i < 16; ++i) n += part[i];
     head->count = n;
-    head->done = 0;
     if (rows == 0 && mean) *mean = 0.f;
   }
 }
@@ -181,7 +185,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a
   // The losses that this workgroup wrote are where the last one reads them before it counts itself (no fence: it would write back the gradient's lines).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(&a.head->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  if (threadIdx.x == 0) {
+    const uint32_t c = blockIdx.x % kCounters, of_mine = (gridDim.x - c + kCounters - 1) / kCounters, counters = min(gridDim.x, kCounters);
+    last = __hip_atomic_fetch_add(&a.head->done[c * kLineWords], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of_mine - 1 &&
+           __hip_atomic_fetch_add(&a.head->full[0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == counters - 1;
+  }
   __syncthreads();
   if (!last) return;
   constexpr int TH = LANES < 256 ? 256 : LANES;
@@ -230,7 +238,7 @@ bool check(const cada_xent *a) {
   return true;
 }
 
-size_t workspace(const cada_xent *a) { return kOpsAlign + (a->mean && !a->loss ? ops_align((size_t)a->rows * 4) : 0); }
+size_t workspace(const cada_xent *a) { return ops_align(sizeof(Head)) + (a->mean && !a->loss ? ops_align((size_t)a->rows * 4) : 0); }
 
 }  // namespace
 }  // namespace cada
@@ -263,7 +271,7 @@ int cada_cross_entropy(const cada_xent *a) {
   Head *head = static_cast<Head *>(a->workspace);
   Xent x{};
   x.logits = a->logits; x.labels = a->labels; x.grad = a->grad;
-  x.loss = a->loss ? a->loss : a->mean ? reinterpret_cast<float *>(static_cast<char *>(a->workspace) + kOpsAlign) : nullptr;
+  x.loss = a->loss ? a->loss : a->mean ? reinterpret_cast<float *>(static_cast<char *>(a->workspace) + ops_align(sizeof(Head))) : nullptr;
   x.mean = a->mean; x.head = head; x.rows = a->rows; x.ldz = a->ldz; x.ldg = a->ldg; x.ignore = a->ignore_index;
   x.classes = (int32_t)a->classes; x.label_bytes = a->label_bytes;
   x.smoothing = (float)a->smoothing; x.keep = (float)(1.0 - a->smoothing); x.scale = (float)a->scale;
