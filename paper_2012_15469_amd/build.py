@@ -42,8 +42,28 @@ def build_libcada() -> str:
     return LIBCADA
 
 
+OPS_BINDING = os.path.join(HERE, "_ops.so")
+
+
+def build_ops_binding() -> str:
+    """The Python module of the operators (host code on torch's C++ tensors), next to libcada.so, which it links to."""
+    import sysconfig
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-I", os.path.join(ROOT, "include"), "-isystem", sysconfig.get_paths()["include"]]
+    for p in include_paths():
+        cmd += ["-isystem", p]
+    cmd += ["-o", OPS_BINDING, os.path.join(HERE, "csrc", "ops_binding.cpp"), "-L", HERE, "-l:libcada.so", "-Wl,-rpath,$ORIGIN"]
+    for p in library_paths():
+        cmd += ["-L", p]
+    _run(cmd + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
+    return OPS_BINDING
+
+
 def build_all() -> None:
     build_libcada()
+    build_ops_binding()
 
 
 if __name__ == "__main__":

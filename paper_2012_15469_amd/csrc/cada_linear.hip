@@ -916,9 +916,10 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
 
 // ---- backward ----
 
-// Below this many products of numbers (both gradients), dz is formed on its way into the products' tiles: one launch less, for tiles that read their operands
-// through registers and each form the part of dz that they need.
-constexpr double kSmallGradients = 4e9;
+// Below this many operations (both gradients), dz is formed on its way into the products' tiles: one launch for three, with tiles that read their operands
+// through registers and each form the part of dz that they need.  bf16, us (the three launches): 128 x 362 x 286 12.0 (14.2), 16 x 128 x 128 7.6 (8.6); above it the
+// other way round: 120 x 784 x 500 18.3 (15.9), 128 x 784 x 512 15.6 (10.0).
+constexpr double kSmallGradients = 1e8;
 
 struct BackwardPlan {
   bool small, by_element, own_dz, direct, pack_x, pack_w;

@@ -12,11 +12,17 @@ handed in; like outputs allocated here it belongs to the current stream, so with
 from __future__ import annotations
 
 import ctypes as C
-from typing import List, Optional, Sequence, Tuple, Union
+from typing import Optional, Sequence, Tuple, Union
 
 import torch
 
-from .binding import _check, _lib
+from .binding import CadaError, _check, _lib
+
+try:
+    from . import _ops
+except ImportError as e:
+    raise ImportError("_ops.so is not built: run `python -m paper_2012_15469_amd.build` (no fallback exists)") from e
+_ops.set_error_class(CadaError)
 
 F32, BF16 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -72,56 +78,17 @@ def _need(ok: bool, text: str):
         raise ValueError(text)
 
 
-def _table(name: str, t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, device: torch.device) -> Tuple[int, int]:
-    """(address, elements from one row to the next) of a [rows, cols] tensor."""
-    if t.dim() != 2 or t.shape != (rows, cols):
-        raise ValueError("%s must be [%d, %d], it is %s" % (name, rows, cols, list(t.shape)))
-    if t.dtype != dtype or t.device != device:
-        raise ValueError("%s must be %s on %s like the other operands, it is %s on %s" % (name, dtype, device, t.dtype, t.device))
-    s0, s1 = t.stride()
-    if cols > 1 and s1 != 1 or rows > 1 and s0 < cols:
-        raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, t.stride()))
-    return t.data_ptr(), s0 if rows > 1 else max(s0, cols)
-
-
-def _first(x: torch.Tensor, name: str):
-    if not x.is_cuda or x.dtype not in _TYPES or x.dim() != 2:
-        raise ValueError("%s must be a two-dimensional float32 or bfloat16 tensor on a GPU, it is %s %s on %s" % (name, list(x.shape), x.dtype, x.device))
-
-
-def _vector(name: str, t: torch.Tensor, n: int, like: torch.Tensor) -> int:
-    if t.shape != (n,) or t.dtype != like.dtype or t.device != like.device or (n > 1 and t.stride(0) != 1):
-        raise ValueError("%s must be a contiguous %s [%d] on %s" % (name, like.dtype, n, like.device))
-    return t.data_ptr()
-
-
-def _activation(act: str) -> int:
-    if act not in ACTIVATIONS:
-        raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
-    return ACTIVATIONS[act]
-
-
-def _enqueue(a, size_of, call, device, workspace, stream):
-    """Workspace and stream of a call, and the call."""
-    if workspace is None:
-        r = C.byref(a)
-        _check(size_of(r))
-        if a.workspace_bytes:
-            workspace = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=device)      # (the allocator's blocks start on 512 bytes)
-            a.workspace = workspace.data_ptr()
-    elif workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 tensor on %s" % device)
-    else:
-        r = C.byref(a)
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    index = device.index
-    # (the raw handle: torch.cuda.current_stream() makes an object, 2 us of a call that takes 8)
-    a.stream = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
+def _call(call, tensor, stream, *args):
+    """call(*args, stream handle) with the tensor's device current.  (The raw handle and device index: torch.cuda's own functions make objects, 2 us of a call
+    that takes six.)"""
+    index = tensor.get_device() if isinstance(tensor, torch.Tensor) else -1
+    if index < 0:
+        return call(*args, 0)          # (refused there)
+    handle = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
     if index == torch._C._cuda_getDevice():
-        _check(call(r))
-    else:
-        with torch.cuda.device(device):
-            _check(call(r))
+        return call(*args, handle)
+    with torch.cuda.device(index):
+        return call(*args, handle)
 
 
 def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None, act: str = "none",
@@ -131,28 +98,9 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
 
     x [rows, in], w [in, out] (the layout of the engine's parameters), bias [out], residual [rows, out], all of one type; rows contiguous, any
     distance apart.  ``out`` may be ``residual``."""
-    _first(x, "x")
-    a = cada_linear()
-    rows, k = x.shape
-    dt, dev = x.dtype, x.device
-    _need(w.dim() == 2, "w must be [in, out]")
-    n = w.shape[1]
-    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[dt], _activation(act)
-    a.x, a.ldx = _table("x", x, rows, k, dt, dev)
-    a.w, a.ldw = _table("w", w, k, n, dt, dev)
-    if bias is not None:
-        a.bias = _vector("bias", bias, n, x)
-    if residual is not None:
-        a.residual, a.ldr = _table("residual", residual, rows, n, dt, dev)
-    if out is None:
-        out = torch.empty(rows, n, dtype=dt, device=dev)
-    a.y, a.ldy = _table("out", out, rows, n, dt, dev)
-    if pre is None and keep_pre:
-        pre = torch.empty(rows, n, dtype=dt, device=dev)
-    if pre is not None:
-        a.pre, a.ldpre = _table("pre", pre, rows, n, dt, dev)
-    _enqueue(a, _lib.cada_linear_forward_workspace, _lib.cada_linear_forward, dev, workspace, stream)
-    return out, pre
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
+    return _call(_ops.linear_forward, x, stream, x, w, bias, residual, ACTIVATIONS[act], bool(keep_pre), out, pre, workspace)
 
 
 def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, pre: Optional[torch.Tensor] = None, act: str = "none", need_dx: bool = True,
@@ -161,30 +109,9 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, pre: 
                     ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
     """(dx, dw, db) of a layer from the gradient of its output; the residual's gradient is dy itself.  ``pre`` is what
     linear_forward kept (not needed for act="none").  Outputs handed in are written, not added to."""
-    _first(dy, "dy")
-    a = cada_linear_grad()
-    rows, n = dy.shape
-    dt, dev = dy.dtype, dy.device
-    _need(x.dim() == 2 and w.dim() == 2, "x must be [rows, in] and w [in, out]")
-    k = x.shape[1]
-    a.rows, a.in_, a.out, a.type, a.act = rows, k, n, _TYPES[dt], _activation(act)
-    a.dy, a.lddy = _table("dy", dy, rows, n, dt, dev)
-    a.x, a.ldx = _table("x", x, rows, k, dt, dev)
-    a.w, a.ldw = _table("w", w, k, n, dt, dev)
-    if act != "none":
-        _need(pre is not None, "act=%r needs pre" % act)
-        a.pre, a.ldpre = _table("pre", pre, rows, n, dt, dev)
-    if need_dx:
-        dx = torch.empty(rows, k, dtype=dt, device=dev) if dx is None else dx
-        a.dx, a.lddx = _table("dx", dx, rows, k, dt, dev)
-    if need_dw:
-        dw = torch.empty(k, n, dtype=dt, device=dev) if dw is None else dw
-        a.dw, a.lddw = _table("dw", dw, k, n, dt, dev)
-    if need_db:
-        db = torch.empty(n, dtype=dt, device=dev) if db is None else db
-        a.db = _vector("db", db, n, dy)
-    _enqueue(a, _lib.cada_linear_backward_workspace, _lib.cada_linear_backward, dev, workspace, stream)
-    return dx if need_dx else None, dw if need_dw else None, db if need_db else None
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
+    return _call(_ops.linear_backward, dy, stream, dy, x, w, pre, ACTIVATIONS[act], bool(need_dx), bool(need_dw), bool(need_db), dx, dw, db, workspace)
 
 
 def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, *, smoothing: float = 0.0, ignore_index: int = -100, scale: float = 1.0, need_grad: bool = True,
@@ -194,25 +121,7 @@ def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, *, smoothing: floa
 
     logits [rows, classes]; labels int32 or int64 [rows].  Rows labelled ``ignore_index`` count nowhere; classes at -inf are ruled out.  ``grad`` may be
     the logits themselves.  Losses are float32, the gradient has the logits' type."""
-    _first(logits, "logits")
-    a = cada_xent()
-    rows, n = logits.shape
-    dt, dev = logits.dtype, logits.device
-    a.rows, a.classes, a.type = rows, n, _TYPES[dt]
-    a.logits, a.ldz = _table("logits", logits, rows, n, dt, dev)
-    if labels.dtype not in (torch.int32, torch.int64) or labels.shape != (rows,) or labels.device != logits.device or (rows > 1 and labels.stride(0) != 1):
-        raise ValueError("labels must be a contiguous int32 or int64 [%d] on %s" % (rows, logits.device))
-    a.labels, a.label_bytes = labels.data_ptr(), labels.element_size()
-    a.ignore_index, a.smoothing, a.scale = ignore_index, smoothing, scale
-    stats = torch.empty(rows + 1, dtype=torch.float32, device=logits.device)
-    loss, mean = stats[:rows], stats[rows]
-    a.loss, a.mean = stats.data_ptr(), stats.data_ptr() + 4 * rows
-    if grad is None and need_grad:
-        grad = torch.empty(rows, n, dtype=dt, device=dev)
-    if grad is not None:
-        a.grad, a.ldg = _table("grad", grad, rows, n, dt, dev)
-    _enqueue(a, _lib.cada_xent_workspace, _lib.cada_cross_entropy, dev, workspace, stream)
-    return mean, loss, grad
+    return _call(_ops.cross_entropy, logits, stream, logits, labels, smoothing, ignore_index, scale, bool(need_grad), grad, workspace)
 
 
 class AdamW:

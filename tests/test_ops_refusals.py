@@ -10,7 +10,7 @@ from paper_2012_15469_amd.binding import _lib, cada_last_error
 FAKE = 1 << 20          # an aligned address that nobody reads
 
 
-LONG = dict(in_=100000, ldx=100000)          # few tiles of a long contraction: split, with its parts in a workspace
+LONG = dict(rows=64, in_=100000, ldx=100000)          # few tiles of a long contraction: split, with its parts in a workspace
 
 
 def linear(**kw):
@@ -34,7 +34,7 @@ def test_linear_forward(kw, code, text):
 @pytest.mark.parametrize("kw,code,text", [
     (dict(rows=-1), -1, "rows"), (dict(type=5), -1, "type"), (dict(act=-1), -1, "act"), (dict(dy=None), -1, "dy is NULL"), (dict(lddy=1), -1, "row length of dy"), (dict(act=1), -1, "pre is NULL"),
     (dict(x=None), -1, "x is NULL"), (dict(w=None), -1, "w is NULL"), (dict(lddx=1), -1, "row length of dx"), (dict(lddw=1), -1, "row length of dw"), (dict(db=FAKE + 1), -1, "db"),
-    (dict(workspace_bytes=0), -2, "too small")])
+    (dict(rows=100000, workspace_bytes=0), -2, "too small")])
 def test_linear_backward(kw, code, text):
     a = ops.cada_linear_grad()
     a.rows, a.in_, a.out, a.type, a.act = 4, 8, 16, 1, 0
