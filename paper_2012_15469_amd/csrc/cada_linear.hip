@@ -59,7 +59,7 @@ template <typename T, bool KC, int BO, int TH> struct Side {
   static constexpr int kPieces = BO * 8 / TH;                   // per thread
   static constexpr int kRow16 = KC ? 8 : BO / E;                // pieces per row in LDS
   static constexpr int kBytes = kStepBytes * BO;
-  __device__ static __forceinline__ int swizzle(int krow) { return sizeof(T) == 4 ? 0 : BO >= 128 ? (krow & 3) << 1 : krow & 2; }
+  __device__ static __forceinline__ int swizzle(int krow) { return sizeof(T) == 4 || BO < 64 ? 0 : BO >= 128 ? (krow & 3) << 1 : krow & 2; }
   // row of LDS and source piece in it of thread t's i-th piece
   __device__ static __forceinline__ void place(int i, int t, int &row, int &piece) {
     const int q = i * TH + t;
@@ -229,14 +229,17 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int
   store8_n(static_cast<T *>(e.out) + m * e.ldo + n, left, f);
 }
 
+// WY x WX wavefronts share the tile; with KW = 4 four wavefronts each take the whole (32 x 32) tile and one of the four sub-steps of every step, and their sums are joined
+// on the way out: short steps for few outputs.
 enum { NO_SIGNAL = 0, A_SIGNAL = 1, B_SIGNAL = 2 };
-template <typename T, int BM, int BN, int WY, int WX, bool AKC, bool BKC, bool DIRECT, int STAGES, int SIGNAL = NO_SIGNAL>
+template <typename T, int BM, int BN, int WY, int WX, bool AKC, bool BKC, bool DIRECT, int STAGES, int KW = 1, int SIGNAL = NO_SIGNAL>
 __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, unsigned char *lds) {
-  constexpr int TH = 64 * WY * WX;
+  constexpr int TH = 64 * WY * WX * KW, NK = 4 / KW;
   typedef Side<T, AKC, BM, TH> SA;
   typedef Side<T, BKC, BN, TH> SB;
   constexpr int WM = BM / WY, WN = BN / WX, FM = WM / 32, FN = WN / 32, kHalf = SA::kBytes + SB::kBytes, BK = kStep<T>;
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WX * WM, wn = wave % WX * WN;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int place = wave % (WY * WX), kw = wave / (WY * WX), wm = place / WX * WM, wn = place % WX * WN;
   // Tiles in bands of eight rows of tiles, columns slowest in a band: the tiles that run together share operands.
   const uint32_t per_split = (uint32_t)p.tiles_m * p.tiles_n, band_tiles = 8u * p.tiles_n;
   const uint32_t split = tile / per_split, r = tile - split * per_split, band = r / band_tiles, in_band = r - band * band_tiles;
@@ -311,9 +314,9 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   typedef decltype(fragment<AKC, BM>(lds, 0, 0, 0, T())) Frag;
   auto read_fragments = [&](Frag (&fa)[FM], Frag (&fb)[FN], const unsigned char *src, int ks) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) fa[i] = fragment<AKC, BM>(src, wm + 32 * i, ks, lane, T());
+    for (int i = 0; i < FM; ++i) fa[i] = fragment<AKC, BM>(src, wm + 32 * i, ks * KW + kw, lane, T());
 #pragma unroll
-    for (int j = 0; j < FN; ++j) fb[j] = fragment<BKC, BN>(src + SA::kBytes, wn + 32 * j, ks, lane, T());
+    for (int j = 0; j < FN; ++j) fb[j] = fragment<BKC, BN>(src + SA::kBytes, wn + 32 * j, ks * KW + kw, lane, T());
   };
   // (lane: row l % 32 of the tile, four consecutive columns at a time)
   auto multiply_all = [&](const Frag (&fa)[FM], const Frag (&fb)[FN]) __attribute__((always_inline)) {
@@ -327,10 +330,21 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   auto whole_step = [&](const unsigned char *src) __attribute__((always_inline)) {
     read_fragments(fa[0], fb[0], src, 0);
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      if (ks < 3) read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], src, ks + 1);
+    for (int ks = 0; ks < NK; ++ks) {
+      if (ks < NK - 1) read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], src, ks + 1);
       __builtin_amdgcn_sched_barrier(0);
       multiply_all(fa[ks & 1], fb[ks & 1]);
+    }
+  };
+  // The last sub-step of a step, when the next step can be read: its first fragments on their way, then the products.
+  auto last_of_step = [&](const unsigned char *there) __attribute__((always_inline)) {
+    constexpr int next = NK == 1 ? 1 : 0;
+    read_fragments(fa[next], fb[next], there, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply_all(fa[(NK - 1) & 1], fb[(NK - 1) & 1]);
+    if constexpr (NK == 1) {
+      fa[0][0] = fa[1][0];
+      fb[0][0] = fb[1][0];
     }
   };
   if constexpr (DIRECT) {
@@ -356,19 +370,16 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       for (int s = 0; s < whole; ++s) {
         unsigned char *here = lds + (s & (STAGES - 1)) * kHalf, *there = lds + ((s + 1) & (STAGES - 1)) * kHalf;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          if (ks < 3) {
-            read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
-          } else {
-            // the next step is there, and everybody has read this one
-            if (STAGES > 2 && s + STAGES - 1 < whole) landed<(STAGES - 2) * P>();
-            else landed<0>();
-            if (s + STAGES < whole) load_step(s + STAGES, here);
-            read_fragments(fa[0], fb[0], there, 0);        // (past the last step: what nobody uses)
-          }
+        for (int ks = 0; ks < NK - 1; ++ks) {
+          read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
           __builtin_amdgcn_sched_barrier(0);        // (the reads of the next sub-step go out before this one's products, not between them)
           multiply_all(fa[ks & 1], fb[ks & 1]);
         }
+        // the next step is there, and everybody has read this one
+        if (STAGES > 2 && s + STAGES - 1 < whole) landed<(STAGES - 2) * P>();
+        else landed<0>();
+        if (s + STAGES < whole) load_step(s + STAGES, here);
+        last_of_step(there);        // (past the last step: fragments that nobody uses)
       }
     }
     if (whole < steps) {
@@ -390,17 +401,15 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       unsigned char *here = lds + (s & 1) * kHalf, *there = lds + ((s + 1) & 1) * kHalf;
       ask(after, s + 2);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        if (ks < 3) {
-          read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
-        } else {
-          lds_sync();
-          read_fragments(fa[0], fb[0], there, 0);
-        }
+      for (int ks = 0; ks < NK - 1; ++ks) {
+        read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
         __builtin_amdgcn_sched_barrier(0);
         multiply_all(fa[ks & 1], fb[ks & 1]);
         if (ks == 1) put_step(next, s + 1, there);
       }
+      if constexpr (NK == 1) put_step(next, s + 1, there);
+      lds_sync();
+      last_of_step(there);
     };
     for (int s = 0; s < steps; s += 2) {
       one(reg[1], reg[0], s);
@@ -430,10 +439,31 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
     }
   }
 
+  if constexpr (KW > 1) {
+    // The wavefronts' sums side by side in LDS; four lanes for each row join them.
+    static_assert(FM == 1 && FN == 1 && BM == 32 && BN == 32 && KW == 4, "");
+    constexpr int kLd = BN + 4;
+    float *sums = reinterpret_cast<float *>(lds), *mine = sums + kw * BM * kLd + (lane & 31) * kLd + 4 * (lane >> 5);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<v4s *>(mine + 8 * q) = v4s{acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
+    __syncthreads();
+    if (t < BM * 4 && m0 + t / 4 < p.M) {
+      const float *src = sums + t / 4 * kLd + (t & 3) * 8;
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = (src[e] + src[BM * kLd + e]) + (src[2 * BM * kLd + e] + src[3 * BM * kLd + e]);
+      const int64_t m = m0 + t / 4, left = (int64_t)p.N - n0 - (t & 3) * 8;
+      const int n = n0 + (t & 3) * 8;
+      if (p.splits > 1) store8_n(p.partial + ((int64_t)split * p.M + m) * p.N + n, left, f);
+      else finish8<T>(p.epi, m, n, left, f);
+    }
+    return;
+  }
+
   // Out through LDS, 32 rows of the wavefront's tile at a time, so that memory is met in eight consecutive columns per lane.  (One copy of the code
   // behind it: with one for every group of rows a 256 x 256 tile spent 8 us fetching instructions.)
   constexpr int kLd = WN + 4, kLanes = WN / 8, kRows = 64 / kLanes;
-  static_assert(WY * WX * 32 * kLd * 4 <= 2 * kHalf, "the wavefronts' strips fit the operands' LDS");
+  static_assert(KW > 1 || WY * WX * 32 * kLd * 4 <= 2 * kHalf, "the wavefronts' strips fit the operands' LDS");
   float *strip = reinterpret_cast<float *>(lds) + wave * 32 * kLd;
   const int n = n0 + wn + lane % kLanes * 8;
   const int64_t left = (int64_t)p.N - n;
@@ -471,11 +501,14 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t total, uint32_t first
   return i < per && t < total ? t : ~0u;
 }
 
-template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES>
-__global__ __launch_bounds__(64 * WY * WX) void k_forward(const Product p) {
-  __shared__ __align__(16) unsigned char lds[STAGES * kStepBytes * (BM + BN)];
+// LDS of a tile: the ring of steps, or what the four wavefronts of KW = 4 leave there.
+constexpr int tile_lds(int bm, int bn, int stages, int kw) { return kw > 1 && stages * kStepBytes * (bm + bn) < kw * bm * (bn + 4) * 4 ? kw * bm * (bn + 4) * 4 : stages * kStepBytes * (bm + bn); }
+
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
+__global__ __launch_bounds__(64 * WY * WX * KW) void k_forward(const Product p) {
+  __shared__ __align__(16) unsigned char lds[tile_lds(BM, BN, STAGES, KW)];
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n * p.splits);
-  if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT, STAGES>(p, tile, lds);
+  if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT, STAGES, KW>(p, tile, lds);
 }
 
 // A few rows (a single sample answered): a read of the weights.  A workgroup takes 64 columns, a lane eight of them (one line of memory per eight lanes and weight row), and
@@ -546,25 +579,25 @@ __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
 }
 
 // dx and dw in one launch (either may have no tiles).
-template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES>
-__global__ __launch_bounds__(64 * WY * WX) void k_backward(const Product dx, const Product dw) {
-  __shared__ __align__(16) unsigned char lds[STAGES * kStepBytes * (BM + BN)];
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
+__global__ __launch_bounds__(64 * WY * WX * KW) void k_backward(const Product dx, const Product dw) {
+  __shared__ __align__(16) unsigned char lds[tile_lds(BM, BN, STAGES, KW)];
   const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
   const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
   if (tile == ~0u) return;
-  if ((blockIdx.x >> 3) < first) tile_product<T, BM, BN, WY, WX, false, false, DIRECT, STAGES>(dw, tile, lds);
-  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT, STAGES>(dx, tile, lds);
+  if ((blockIdx.x >> 3) < first) tile_product<T, BM, BN, WY, WX, false, false, DIRECT, STAGES, KW>(dw, tile, lds);
+  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT, STAGES, KW>(dx, tile, lds);
 }
 
 // The same for small gradients: any alignment, and dz formed on the way (dy's and pre's rows in the place of dz's).
-template <typename T>
+template <typename T, int E, int W, int KW>
 __global__ __launch_bounds__(256) void k_backward_small(const Product dx, const Product dw) {
-  __shared__ __align__(16) unsigned char lds[2 * kStepBytes * (64 + 64)];
+  __shared__ __align__(16) unsigned char lds[tile_lds(E, E, 2, KW)];
   const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
   const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
   if (tile == ~0u) return;
-  if ((blockIdx.x >> 3) < first) tile_product<T, 64, 64, 2, 2, false, false, false, 2, B_SIGNAL>(dw, tile, lds);
-  else tile_product<T, 64, 64, 2, 2, true, true, false, 2, A_SIGNAL>(dx, tile, lds);
+  if ((blockIdx.x >> 3) < first) tile_product<T, E, E, W, W, false, false, false, 2, KW, B_SIGNAL>(dw, tile, lds);
+  else tile_product<T, E, E, W, W, true, true, false, 2, KW, A_SIGNAL>(dx, tile, lds);
 }
 
 // Tables of less than 16 bytes (the contraction has few terms, or there are few outputs in a row or column), and rows so far apart that a tile's
@@ -720,10 +753,10 @@ struct Cut { int tile, splits; int64_t k_per_split; };
 // it, a step's share of a full CU, and the tile's way in and out.  At 8192 x 4096 x 4096 bf16: 256 x 256 tiles 1220 TFLOP/s, 128 x 128 1080, 64 x 64 640; a single
 // tile per CU: 870 (128), 460 (64).  Float32 is bound by the matrix instructions at any of them (146 TFLOP/s, 64 x 64 as 128 x 128), so it takes the smallest.
 struct TileCost { int tile, slots; double alone, crowd, share, ends; };
-constexpr TileCost kCostBf16[] = {{64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
-constexpr TileCost kCostF32[] = {{64, 5, 0.5, 0.1, 0.46, 1.7}};
+constexpr TileCost kCostBf16[] = {{32, 5, 0.12, 0.03, 0.09, 1.0}, {64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
+constexpr TileCost kCostF32[] = {{32, 5, 0.16, 0.04, 0.13, 1.0}, {64, 5, 0.5, 0.1, 0.46, 1.7}};
 // Through registers (64 x 64 only): 8192 x 4001 x 2003 bf16 340 us where 4000 x 2000 takes 108 directly, float32 1100 and 960.
-constexpr TileCost kCostBf16Registers[] = {{64, 5, 0.45, 0.1, 0.335, 1.9}}, kCostF32Registers[] = {{64, 5, 0.8, 0.1, 0.54, 1.9}};
+constexpr TileCost kCostBf16Registers[] = {{32, 5, 0.25, 0.05, 0.15, 1.2}, {64, 5, 0.45, 0.1, 0.335, 1.9}}, kCostF32Registers[] = {{32, 5, 0.3, 0.05, 0.2, 1.2}, {64, 5, 0.8, 0.1, 0.54, 1.9}};
 constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct Shape { int64_t M, N, K; };
@@ -731,7 +764,7 @@ struct Shape { int64_t M, N, K; };
 double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
   const int64_t step = kStepBytes / (int64_t)type_bytes(type);
   const TileCost *costs = type == CADA_BF16 ? (direct ? kCostBf16 : kCostBf16Registers) : direct ? kCostF32 : kCostF32Registers;
-  const int n_costs = type == CADA_BF16 && direct ? 3 : 1;
+  const int n_costs = type == CADA_BF16 && direct ? 4 : 2;
   int64_t steps[2] = {0, 0};
   for (int i = 0; i < n; ++i) steps[i] = ceil_div(s[i].K, step);
   double best = 1e300;
@@ -844,18 +877,18 @@ ForwardPlan plan_forward(const cada_linear *a) {
 
 // Four steps on their way where LDS has room for them (few tiles: long contractions come from memory, 64 x 64 x 4096 with one tile per CU 32 -> 18.5 us); two, and more
 // workgroups on a CU, where there are many tiles (64 x 64 x 1024 with four per CU 17 -> 15.5 us).
-bool deep(int tile, int64_t tiles) { return tiles <= (tile == 64 ? 2 : 1) * kCUs; }
+bool deep(int tile, int64_t tiles) { return tiles <= (tile <= 64 ? 2 : 1) * kCUs; }
 
-template <typename T, int E, int W>
+template <typename T, int E, int WY, int WX, int KW>
 void forward_tiles(const Product &p, bool dir, hipStream_t st) {
   const unsigned grid = (unsigned)(ceil_div(tiles_of(p), 8) * 8);
-  if constexpr (E == 64) {
-    if (!dir) { k_forward<T, E, E, 2, W, false, 2><<<grid, 128 * W, 0, st>>>(p); return; }
+  if constexpr (E <= 64) {
+    if (!dir) { k_forward<T, E, E, WY, WX, false, 2, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(p); return; }
   }
   if constexpr (E < 256) {
-    if (deep(E, tiles_of(p))) { k_forward<T, E, E, 2, W, true, 4><<<grid, 128 * W, 0, st>>>(p); return; }
+    if (deep(E, tiles_of(p))) { k_forward<T, E, E, WY, WX, true, 4, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(p); return; }
   }
-  k_forward<T, E, E, 2, W, true, 2><<<grid, 128 * W, 0, st>>>(p);
+  k_forward<T, E, E, WY, WX, true, 2, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(p);
 }
 
 template <typename T>
@@ -902,10 +935,11 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
     k_by_element<T, true, false, NO_SIGNAL><<<(unsigned)ceil_div(a->rows * a->out, 256), 256, 0, st>>>(p);
     return ops_launched("linear");
   }
-  if (f.cut.tile == 64) forward_tiles<T, 64, 2>(p, f.direct, st);
+  if (f.cut.tile == 32) forward_tiles<T, 32, 1, 1, 4>(p, f.direct, st);
+  if (f.cut.tile == 64) forward_tiles<T, 64, 2, 2, 1>(p, f.direct, st);
   if constexpr (sizeof(T) == 2) {
-    if (f.cut.tile == 128) forward_tiles<T, 128, 4>(p, f.direct, st);
-    if (f.cut.tile == 256) forward_tiles<T, 256, 4>(p, f.direct, st);
+    if (f.cut.tile == 128) forward_tiles<T, 128, 2, 4, 1>(p, f.direct, st);
+    if (f.cut.tile == 256) forward_tiles<T, 256, 2, 4, 1>(p, f.direct, st);
   }
   if (int rc = ops_launched("linear")) return rc;
   if (p.splits == 1) return CADA_OK;
@@ -985,16 +1019,16 @@ int zero_table(void *p, int64_t ld, int64_t rows, int64_t n, hipStream_t st) {
   return ops_launched("linear clear");
 }
 
-template <typename T, int E, int W>
+template <typename T, int E, int WY, int WX, int KW>
 void backward_tiles(const Product &dx, const Product &dw, bool dir, hipStream_t st) {
   const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);
-  if constexpr (E == 64) {
-    if (!dir) { k_backward<T, E, E, 2, W, false, 2><<<grid, 128 * W, 0, st>>>(dx, dw); return; }
+  if constexpr (E <= 64) {
+    if (!dir) { k_backward<T, E, E, WY, WX, false, 2, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw); return; }
   }
   if constexpr (E < 256) {
-    if (deep(E, tiles_of(dx) + tiles_of(dw))) { k_backward<T, E, E, 2, W, true, 4><<<grid, 128 * W, 0, st>>>(dx, dw); return; }
+    if (deep(E, tiles_of(dx) + tiles_of(dw))) { k_backward<T, E, E, WY, WX, true, 4, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw); return; }
   }
-  k_backward<T, E, E, 2, W, true, 2><<<grid, 128 * W, 0, st>>>(dx, dw);
+  k_backward<T, E, E, WY, WX, true, 2, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw);
 }
 
 template <typename T>
@@ -1049,11 +1083,14 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
       if (a->dw) k_by_element<T, false, false, B_SIGNAL><<<(unsigned)ceil_div(a->in * a->out, 256), 256, 0, st>>>(dw);
       return ops_launched("linear gradients");
     }
-    if (b.small) k_backward_small<T><<<(unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8), 256, 0, st>>>(dx, dw);
-    else if (tile == 64) backward_tiles<T, 64, 2>(dx, dw, b.direct, st);
+    const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);
+    if (b.small && tile == 32) k_backward_small<T, 32, 1, 4><<<grid, 256, 0, st>>>(dx, dw);
+    else if (b.small) k_backward_small<T, 64, 2, 1><<<grid, 256, 0, st>>>(dx, dw);
+    else if (tile == 32) backward_tiles<T, 32, 1, 1, 4>(dx, dw, b.direct, st);
+    else if (tile == 64) backward_tiles<T, 64, 2, 2, 1>(dx, dw, b.direct, st);
     if constexpr (sizeof(T) == 2) {
-      if (!b.small && tile == 128) backward_tiles<T, 128, 4>(dx, dw, b.direct, st);
-      if (!b.small && tile == 256) backward_tiles<T, 256, 4>(dx, dw, b.direct, st);
+      if (!b.small && tile == 128) backward_tiles<T, 128, 2, 4, 1>(dx, dw, b.direct, st);
+      if (!b.small && tile == 256) backward_tiles<T, 256, 2, 4, 1>(dx, dw, b.direct, st);
     }
     if (int rc = ops_launched("linear gradients")) return rc;
   }
