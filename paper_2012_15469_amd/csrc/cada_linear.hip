@@ -578,26 +578,32 @@ __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
   }
 }
 
-// dx and dw in one launch (either may have no tiles).
+// dx and dw in one launch (either may have no tiles), the one with the longer contraction first: its tiles would be the launch's tail.
+struct Turn { uint32_t tile; bool dw; };
+__device__ __forceinline__ Turn backward_tile(const Product &dx, const Product &dw) {
+  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits;
+  const bool dw_first = dw.k_per_split >= dx.k_per_split;
+  const uint32_t n_first = dw_first ? n_dw : n_dx, n_second = dw_first ? n_dx : n_dw, first = (n_first + 7) / 8;
+  const bool in_first = (blockIdx.x >> 3) < first;
+  return Turn{in_first ? tile_of_block(n_first) : tile_of_block(n_second, first), in_first == dw_first};
+}
 template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_backward(const Product dx, const Product dw) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BN, STAGES, KW)];
-  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
-  const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
-  if (tile == ~0u) return;
-  if ((blockIdx.x >> 3) < first) tile_product<T, BM, BN, WY, WX, false, false, DIRECT, STAGES, KW>(dw, tile, lds);
-  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT, STAGES, KW>(dx, tile, lds);
+  const Turn turn = backward_tile(dx, dw);
+  if (turn.tile == ~0u) return;
+  if (turn.dw) tile_product<T, BM, BN, WY, WX, false, false, DIRECT, STAGES, KW>(dw, turn.tile, lds);
+  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT, STAGES, KW>(dx, turn.tile, lds);
 }
 
 // The same for small gradients: any alignment, and dz formed on the way (dy's and pre's rows in the place of dz's).
 template <typename T, int E, int W, int KW>
 __global__ __launch_bounds__(256) void k_backward_small(const Product dx, const Product dw) {
   __shared__ __align__(16) unsigned char lds[tile_lds(E, E, 2, KW)];
-  const uint32_t n_dw = (uint32_t)dw.tiles_m * dw.tiles_n * dw.splits, n_dx = (uint32_t)dx.tiles_m * dx.tiles_n * dx.splits, first = (n_dw + 7) / 8;
-  const uint32_t tile = (blockIdx.x >> 3) < first ? tile_of_block(n_dw) : tile_of_block(n_dx, first);
-  if (tile == ~0u) return;
-  if ((blockIdx.x >> 3) < first) tile_product<T, E, E, W, W, false, false, false, 2, KW, B_SIGNAL>(dw, tile, lds);
-  else tile_product<T, E, E, W, W, true, true, false, 2, KW, A_SIGNAL>(dx, tile, lds);
+  const Turn turn = backward_tile(dx, dw);
+  if (turn.tile == ~0u) return;
+  if (turn.dw) tile_product<T, E, E, W, W, false, false, false, 2, KW, B_SIGNAL>(dw, turn.tile, lds);
+  else tile_product<T, E, E, W, W, true, true, false, 2, KW, A_SIGNAL>(dx, turn.tile, lds);
 }
 
 // Tables of less than 16 bytes (the contraction has few terms, or there are few outputs in a row or column), and rows so far apart that a tile's
@@ -753,10 +759,10 @@ struct Cut { int tile, splits; int64_t k_per_split; };
 // it, a step's share of a full CU, and the tile's way in and out.  At 8192 x 4096 x 4096 bf16: 256 x 256 tiles 1220 TFLOP/s, 128 x 128 1080, 64 x 64 640; a single
 // tile per CU: 870 (128), 460 (64).  Float32 is bound by the matrix instructions at any of them (146 TFLOP/s, 64 x 64 as 128 x 128), so it takes the smallest.
 struct TileCost { int tile, slots; double alone, crowd, share, ends; };
-constexpr TileCost kCostBf16[] = {{32, 5, 0.12, 0.03, 0.09, 1.0}, {64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
-constexpr TileCost kCostF32[] = {{32, 5, 0.16, 0.04, 0.13, 1.0}, {64, 5, 0.5, 0.1, 0.46, 1.7}};
+constexpr TileCost kCostBf16[] = {{32, 5, 0.135, 0.05, 0.13, 1.0}, {64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
+constexpr TileCost kCostF32[] = {{32, 5, 0.21, 0.02, 0.14, 1.1}, {64, 5, 0.51, 0.05, 0.47, 1.3}};
 // Through registers (64 x 64 only): 8192 x 4001 x 2003 bf16 340 us where 4000 x 2000 takes 108 directly, float32 1100 and 960.
-constexpr TileCost kCostBf16Registers[] = {{32, 5, 0.25, 0.05, 0.15, 1.2}, {64, 5, 0.45, 0.1, 0.335, 1.9}}, kCostF32Registers[] = {{32, 5, 0.3, 0.05, 0.2, 1.2}, {64, 5, 0.8, 0.1, 0.54, 1.9}};
+constexpr TileCost kCostBf16Registers[] = {{32, 5, 0.30, 0.03, 0.16, 1.7}, {64, 5, 0.35, 0.1, 0.30, 2.1}}, kCostF32Registers[] = {{32, 5, 0.44, 0.03, 0.20, 1.3}, {64, 5, 0.69, 0.05, 0.53, 2.2}};
 constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct Shape { int64_t M, N, K; };
