@@ -47,7 +47,7 @@ enum {
  * formed in float32 and rounded once. */
 typedef struct cada_linear {
   int64_t rows;         /* >= 0 (0: nothing to do) */
-  int64_t in, out;      /* 1 .. CADA_MAX_WIDTH */
+  int64_t in, out;      /* 1 .. CADA_MAX_WIDTH; of the tables' products, at most 2^23 - 8 tiles of 64 x 64 */
   int32_t type;         /* CADA_F32 or CADA_BF16 */
   int32_t act;          /* CADA_ACT_* */
   const void *x;        /* [rows, in] */
@@ -126,7 +126,7 @@ typedef struct cada_xent {
   void *stream;
 } cada_xent;
 
-int cada_xent_workspace(cada_xent *a); /* rows, mean and loss are read */
+int cada_xent_workspace(cada_xent *a); /* rows, classes, type, mean and loss are read */
 int cada_cross_entropy(const cada_xent *a);
 
 /* AdamW over many tensors in one launch (two with clipping).  Step t = 1, 2, ... of tensor p with gradient g:

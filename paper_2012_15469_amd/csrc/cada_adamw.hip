@@ -5,6 +5,7 @@
 // Bound by memory: every element is read and written once.  Each operation is rounded by itself (no contraction), as the header says, so that
 // codes do not depend on how a compiler joins operations.
 #include <cmath>
+#include <exception>
 #include <new>
 #include <vector>
 
@@ -207,10 +208,10 @@ bool sizes(const cada_adamw_config *cfg, int64_t *elements, int64_t *chunks) {
   int64_t e = 0, c = 0;
   for (int i = 0; i < cfg->n_tensors; ++i) {
     const int64_t n = cfg->tensors[i].n;
-    if (n < 0 || n > (int64_t)1 << 41) { set_error("tensor %d: n must be in [0, 2^41] (got %lld)", i, (long long)n); return false; }
+    if (n < 0 || n > (int64_t)1 << 34) { set_error("tensor %d: n must be in [0, 2^34] (got %lld)", i, (long long)n); return false; }
     e += ceil_div(n, CADA_MOMENT_BLOCK) * CADA_MOMENT_BLOCK;
     c += ceil_div(n, kChunk);
-    if (c > (int64_t)1 << 30) { set_error("more than 2^41 elements in all"); return false; }
+    if (c > (int64_t)1 << 23) { set_error("more than 2^34 elements in all"); return false; }
   }
   *elements = e;
   *chunks = c;
@@ -302,7 +303,7 @@ int cada_adamw_init(const cada_adamw_config *cfg, cada_adamw **out) {
     s.beta1 = (float)cfg->beta1; s.beta2 = (float)cfg->beta2; s.omb1 = (float)(1.0 - cfg->beta1); s.omb2 = (float)(1.0 - cfg->beta2); s.eps = (float)cfg->eps;
     const hipError_t e = hipMemcpyAsync(ws, p.host.data(), p.host.size(), hipMemcpyHostToDevice, p.stream);
     if (e != hipSuccess) { set_error("hipMemcpyAsync: %s", hipGetErrorString(e)); delete h; return CADA_EHIP; }
-  } catch (const std::bad_alloc &) {
+  } catch (const std::exception &) {      // (memory, or a size that no vector has)
     delete h;
     set_error("out of host memory");
     return CADA_EINVAL;

@@ -610,23 +610,23 @@ __global__ __launch_bounds__(256) void k_backward_small(const Product dx, const 
 // do not lie within 4 GB: a thread per output.
 template <typename T, bool AKC, bool BKC, int SIGNAL>
 __global__ __launch_bounds__(256) void k_by_element(const Product p) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= p.M * p.N) return;
-  const int64_t m = i / p.N, n = i - m * p.N;
-  float sum = 0.f, column = 0.f;
-  for (int64_t k = 0; k < p.K; ++k) {
-    float a = to_f32(static_cast<const T *>(p.a)[AKC ? m * p.lda + k : k * p.lda + m]), b = to_f32(static_cast<const T *>(p.b)[BKC ? n * p.ldb + k : k * p.ldb + n]);
-    if constexpr (SIGNAL != NO_SIGNAL) {
-      float &dz = SIGNAL == A_SIGNAL ? a : b;
-      if (p.act != CADA_ACT_NONE) dz *= activation_slope<T>(to_f32(static_cast<const T *>(p.pre)[SIGNAL == A_SIGNAL ? m * p.ldpre + k : k * p.ldpre + n]), p.act);
-      column += dz;
-      dz = to_f32(from_f32<T>(dz));
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.M * p.N; i += (int64_t)gridDim.x * 256) {
+    const int64_t m = i / p.N, n = i - m * p.N;
+    float sum = 0.f, column = 0.f;
+    for (int64_t k = 0; k < p.K; ++k) {
+      float a = to_f32(static_cast<const T *>(p.a)[AKC ? m * p.lda + k : k * p.lda + m]), b = to_f32(static_cast<const T *>(p.b)[BKC ? n * p.ldb + k : k * p.ldb + n]);
+      if constexpr (SIGNAL != NO_SIGNAL) {
+        float &dz = SIGNAL == A_SIGNAL ? a : b;
+        if (p.act != CADA_ACT_NONE) dz *= activation_slope<T>(to_f32(static_cast<const T *>(p.pre)[SIGNAL == A_SIGNAL ? m * p.ldpre + k : k * p.ldpre + n]), p.act);
+        column += dz;
+        dz = to_f32(from_f32<T>(dz));
+      }
+      sum = fmaf(a, b, sum);
     }
-    sum = fmaf(a, b, sum);
+    float f[8] = {sum};
+    finish8<T>(p.epi, m, (int)n, 1, f);
+    if (SIGNAL == B_SIGNAL && p.db && m == 0) static_cast<T *>(p.db)[n] = from_f32<T>(column);
   }
-  float f[8] = {sum};
-  finish8<T>(p.epi, m, (int)n, 1, f);
-  if (SIGNAL == B_SIGNAL && p.db && m == 0) static_cast<T *>(p.db)[n] = from_f32<T>(column);
 }
 
 // Joins the sums of a split contraction, in the order of the splits, and finishes them; eight columns per thread.
@@ -731,13 +731,13 @@ struct Packs { Pack p[2]; int64_t pieces[2]; };
 template <typename T>
 __global__ __launch_bounds__(256) void k_pack(const Packs a) {
   constexpr int E = Elem<T>::kPer16;
-  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int q = i < a.pieces[0] ? 0 : 1;
-  i -= q ? a.pieces[0] : 0;
-  if (i >= a.pieces[q]) return;
-  const Pack &p = a.p[q];
-  const int64_t per = p.ldd / E, row = i / per, col = (i - row * per) * E;
-  *reinterpret_cast<u32x4v *>(static_cast<T *>(p.dst) + row * p.ldd + col) = load16_n(static_cast<const T *>(p.src) + row * p.ld + col, p.cols - col);
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < a.pieces[0] + a.pieces[1]; at += (int64_t)gridDim.x * 256) {
+    const int q = at < a.pieces[0] ? 0 : 1;
+    const int64_t i = at - (q ? a.pieces[0] : 0);
+    const Pack &p = a.p[q];
+    const int64_t per = p.ldd / E, row = i / per, col = (i - row * per) * E;
+    *reinterpret_cast<u32x4v *>(static_cast<T *>(p.dst) + row * p.ldd + col) = load16_n(static_cast<const T *>(p.src) + row * p.ld + col, p.cols - col);
+  }
 }
 
 template <typename T>
@@ -766,6 +766,7 @@ constexpr TileCost kCostBf16Registers[] = {{32, 5, 0.30, 0.03, 0.16, 1.7}, {64, 
 constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct Shape { int64_t M, N, K; };
+constexpr int64_t kMostTiles = ((int64_t)1 << 23) - 8;        // of a product: 512 threads each, two products, less than 2^32 threads in a launch
 // The cheapest cut of one or two products in one launch (one tile for both) by that estimate, which it returns.
 double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
   const int64_t step = kStepBytes / (int64_t)type_bytes(type);
@@ -783,9 +784,11 @@ double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
       const int64_t tiles = ceil_div(s[i].M, t.tile) * ceil_div(s[i].N, t.tile);
       for (int k : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
         if (k > 1 && (steps[i] < 2 * k || tiles * k > 2 * kCUs)) break;
+        if (tiles > kMostTiles) break;
         opt[i][n_opt[i]++] = Option{k, (double)(tiles * k), (double)ceil_div(steps[i], k), k > 1 ? (k * 4.0 + 2.0) * (double)s[i].M * (double)s[i].N / kJoinBytesPerUs : 0.0};
       }
     }
+    if (n_opt[0] == 0 || (n > 1 && n_opt[1] == 0)) continue;      // (too many of the smallest tiles for one launch)
     for (int i = 0; i < n_opt[0]; ++i) {
       for (int j = 0; j < (n > 1 ? n_opt[1] : 1); ++j) {
         const Option &a = opt[0][i], *b = n > 1 ? &opt[1][j] : nullptr;
@@ -808,6 +811,8 @@ constexpr double kPackLaunch = 4.0, kPackBytesPerUs = 3.5e6;
 double pack_cost(int64_t rows, int64_t cols, size_t elem) { return 2.0 * elem * (double)rows * (double)cols / kPackBytesPerUs; }
 int64_t packed_ld(int64_t cols) { return ceil_div(cols, 8) * 8; }
 size_t packed_bytes(int64_t rows, int64_t cols, size_t elem) { return ops_align((size_t)rows * packed_ld(cols) * elem); }
+// Workgroups of 256 threads for so many items, which the kernel's loop takes on from there.
+unsigned many(int64_t items) { return (unsigned)std::min<int64_t>(ceil_div(items, 256), 1 << 20); }
 template <typename T>
 int launch_pack(Packs &a, hipStream_t st) {
   int64_t total = 0;
@@ -816,7 +821,7 @@ int launch_pack(Packs &a, hipStream_t st) {
     total += a.pieces[i];
   }
   if (total == 0) return CADA_OK;
-  k_pack<T><<<(unsigned)ceil_div(total, 256), 256, 0, st>>>(a);
+  k_pack<T><<<many(total), 256, 0, st>>>(a);
   return ops_launched("linear pack");
 }
 size_t partial_bytes(const Cut &c, int64_t M, int64_t N) { return c.splits > 1 ? ops_align((size_t)c.splits * M * N * 4) : 0; }
@@ -839,7 +844,7 @@ bool check_shape(int64_t rows, int64_t in, int64_t out, int type, int act) {
   if (type != CADA_F32 && type != CADA_BF16) { set_error("type must be CADA_F32 or CADA_BF16 (got %d)", type); return false; }
   if (act < CADA_ACT_NONE || act > CADA_ACT_SILU) { set_error("act must be one of CADA_ACT_* (got %d)", act); return false; }
   const int64_t t = std::max({ceil_div(rows, 64) * ceil_div(out, 64), ceil_div(rows, 64) * ceil_div(in, 64), ceil_div(in, 64) * ceil_div(out, 64)});
-  if (t > (int64_t)1 << 28) { set_error("more than 2^28 tiles of 64 x 64 outputs"); return false; }
+  if (t > kMostTiles) { set_error("more than %lld tiles of 64 x 64 outputs", (long long)kMostTiles); return false; }
   return true;
 }
 bool check_table(const char *name, const void *p, int64_t ld, int64_t cols, int type) {
@@ -938,7 +943,7 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
     return ops_launched("linear");
   }
   if (f.by_element) {
-    k_by_element<T, true, false, NO_SIGNAL><<<(unsigned)ceil_div(a->rows * a->out, 256), 256, 0, st>>>(p);
+    k_by_element<T, true, false, NO_SIGNAL><<<many(a->rows * a->out), 256, 0, st>>>(p);
     return ops_launched("linear");
   }
   if (f.cut.tile == 32) forward_tiles<T, 32, 1, 1, 4>(p, f.direct, st);
@@ -1085,8 +1090,8 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   if (a->dx || a->dw) {
     const int tile = a->dx ? b.dx.tile : b.dw.tile;
     if (b.by_element) {
-      if (a->dx) k_by_element<T, true, true, A_SIGNAL><<<(unsigned)ceil_div(a->rows * a->in, 256), 256, 0, st>>>(dx);
-      if (a->dw) k_by_element<T, false, false, B_SIGNAL><<<(unsigned)ceil_div(a->in * a->out, 256), 256, 0, st>>>(dw);
+      if (a->dx) k_by_element<T, true, true, A_SIGNAL><<<many(a->rows * a->in), 256, 0, st>>>(dx);
+      if (a->dw) k_by_element<T, false, false, B_SIGNAL><<<many(a->in * a->out), 256, 0, st>>>(dw);
       return ops_launched("linear gradients");
     }
     const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);

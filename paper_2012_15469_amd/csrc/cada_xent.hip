@@ -73,7 +73,7 @@ template <typename T> constexpr uint32_t kInfBits = sizeof(T) == 2 ? 0xFF80FF80u
 
 // LANES lanes for a row, V pieces each; V = 0: as many as it takes, read again for each use.
 template <typename T, int LANES, int V, bool SMOOTH>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a) {
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES >= 512 ? 4 : 2) void k_rows(const Xent a) {
   constexpr int kRows = LANES < 256 ? 256 / LANES : 1, E = Elem<T>::kPer16;
   __shared__ float part[16];
   __shared__ bool last;
@@ -98,18 +98,30 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a
   const int64_t label = label_at(a.labels, a.label_bytes, r);
   const bool used = label != a.ignore, known = label >= 0 && label < a.classes;
   const float zy = used && known ? to_f32(z[label]) : 0.f;      // (read before the gradient may overwrite it)
-  const float inv = a.scale / (float)max(a.head->count, (int64_t)1);
+  // (a launch of one workgroup counts its rows itself, and no other kernel runs)
+  const bool alone = gridDim.x == 1;
+  int64_t count;
+  if (alone) {
+    const float n = group_reduce<(LANES < 256 ? 256 : LANES)>(here && lane == 0 && used ? 1.f : 0.f, part, [](float x, float y) { return x + y; });
+    count = (int64_t)n;
+  } else {
+    count = a.head->count;
+  }
+  const float inv = a.scale / (float)max(count, (int64_t)1);
 
   // Calls f(class of the first, logits) for each piece of this lane.  (The empty asm keeps the compiler from holding all pieces as float32 from one
   // use to the next, which is twice the registers and spills.)
   auto pieces = [&](auto f) __attribute__((always_inline)) {
     float x[E];
     if constexpr (V > 0) {
+      int first = lane * E;
+      asm volatile("" : "+v"(first));        // (nor which pieces exist, in scalar registers)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         asm volatile("" : "+v"(raw[v]));
         unpack<T>(raw[v], x);
-        f((v * LANES + lane) * E, x);
+        f(v * LANES * E + first, x);
+        if constexpr (V >= 16) __builtin_amdgcn_sched_barrier(0);        // (piece by piece: interleaved, the comparisons' results spill)
       }
     } else {
       for (int c = lane * E; c < whole; c += LANES * E) {
@@ -129,13 +141,16 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a
   // nothing left has top = -inf; its exponentials are taken against 0, so that they are 0 and not NaN.
   const bool none = top == -kInf;
   const float base = none ? 0.f : top, share = 1.f / (float)a.classes;
+  constexpr bool kBallot = LANES >= 64;        // a wavefront's lanes have one row: the classes left are counted by the scalar unit
+  uint32_t wave_left = 0;
   float total = 0.f, left = 0.f, mean_left = 0.f;        // mean_left: first the sum of (z - top) / classes, which cannot overflow
   auto statistics = [&](float x) __attribute__((always_inline)) {
     const float d = x - base;
     total += __builtin_amdgcn_exp2f(d * kLog2e);
     if constexpr (SMOOTH) {
       const bool in = x != -kInf;
-      left += in ? 1.f : 0.f;
+      if constexpr (kBallot) wave_left += (uint32_t)__popcll(__ballot(in));
+      else left += in ? 1.f : 0.f;
       mean_left = fmaf(in ? d : 0.f, share, mean_left);
     }
   };
@@ -147,6 +162,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a
   auto plus = [](float x, float y) { return x + y; };
   total = group_reduce<LANES>(total, part, plus);
   if constexpr (SMOOTH) {
+    if constexpr (kBallot) left = lane % 64 == 0 ? (float)wave_left : 0.f;
     left = group_reduce<LANES>(left, part, plus);
     mean_left = group_reduce<LANES>(mean_left, part, plus) * ((float)a.classes / left);
   }
@@ -185,7 +201,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a
   // The losses that this workgroup wrote are where the last one reads them before it counts itself (no fence: it would write back the gradient's lines).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && alone) last = true;
+  if (threadIdx.x == 0 && !alone) {
     const uint32_t c = blockIdx.x % kCounters, of_mine = (gridDim.x - c + kCounters - 1) / kCounters, counters = min(gridDim.x, kCounters);
     last = __hip_atomic_fetch_add(&a.head->done[c * kLineWords], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of_mine - 1 &&
            __hip_atomic_fetch_add(&a.head->full[0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == counters - 1;
@@ -203,42 +220,47 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(const Xent a
   if (threadIdx.x == 0) {
     s = 0.0;
     for (int i = 0; i < TH / 64; ++i) s += sums[i];
-    *a.mean = (float)(s / (double)max(a.head->count, (int64_t)1));
+    *a.mean = (float)(s / (double)max(count, (int64_t)1));
   }
 }
 
+int rows_together(int lanes) { return lanes < 256 ? 256 / lanes : 1; }      // of a workgroup
 template <typename T, int LANES, int V>
 void launch_rows(const Xent &x, hipStream_t st) {
-  constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
-  const unsigned grid = (unsigned)ceil_div(x.rows, kRows), threads = LANES < 256 ? 256 : LANES;
+  const unsigned grid = (unsigned)ceil_div(x.rows, rows_together(LANES)), threads = LANES < 256 ? 256 : LANES;
   if (x.smoothing != 0.f) k_rows<T, LANES, V, true><<<grid, threads, 0, st>>>(x);
   else k_rows<T, LANES, V, false><<<grid, threads, 0, st>>>(x);
 }
 // Lanes and pieces by the row's length: few lanes for a few classes, so that a wavefront holds several rows; beyond that as many as keep a lane's pieces in at
 // most 64 registers, so that two workgroups of 512 fit a CU and one reads while the other computes.
+int lanes_for(int64_t classes, int per16) {
+  const int64_t n = ceil_div(classes, per16);
+  return n <= per16 ? per16 : n <= 16 ? 16 : n <= 256 ? 64 : n <= 2048 ? 256 : n <= 8192 ? 512 : 1024;
+}
 template <typename T>
 int rows(const Xent &x, hipStream_t st) {
   const int64_t n = ceil_div(x.classes, Elem<T>::kPer16);
-  if (n <= Elem<T>::kPer16) launch_rows<T, Elem<T>::kPer16, 1>(x, st);
-  else if (n <= 16) launch_rows<T, 16, 1>(x, st);
-  else if (n <= 64) launch_rows<T, 64, 1>(x, st);
-  else if (n <= 256) launch_rows<T, 64, 4>(x, st);
-  else if (n <= 1024) launch_rows<T, 256, 4>(x, st);
-  else if (n <= 2048) launch_rows<T, 256, 8>(x, st);
-  else if (n <= 4096) launch_rows<T, 512, 8>(x, st);
-  else if (n <= 8192) launch_rows<T, 512, 16>(x, st);
-  else if (n <= 16384) launch_rows<T, 1024, 16>(x, st);
-  else launch_rows<T, 1024, 0>(x, st);
+  switch (lanes_for(x.classes, Elem<T>::kPer16)) {
+    case Elem<T>::kPer16: launch_rows<T, Elem<T>::kPer16, 1>(x, st); break;
+    case 16: launch_rows<T, 16, 1>(x, st); break;
+    case 64: if (n <= 64) launch_rows<T, 64, 1>(x, st); else launch_rows<T, 64, 4>(x, st); break;
+    case 256: if (n <= 1024) launch_rows<T, 256, 4>(x, st); else launch_rows<T, 256, 8>(x, st); break;
+    case 512: if (n <= 4096) launch_rows<T, 512, 8>(x, st); else launch_rows<T, 512, 16>(x, st); break;
+    default: if (n <= 16384) launch_rows<T, 1024, 16>(x, st); else launch_rows<T, 1024, 0>(x, st);
+  }
   return ops_launched("cross-entropy");
 }
 
 bool check(const cada_xent *a) {
   if (!a) { set_error("the arguments are NULL"); return false; }
   if (a->rows < 0 || a->rows > (int64_t)1 << 30) { set_error("rows must be in [0, 2^30] (got %lld)", (long long)a->rows); return false; }
+  if (a->classes < 1 || a->classes > 0x7fffffff - (1 << 20)) { set_error("classes must be in [1, 2^31 - 2^20) (got %lld)", (long long)a->classes); return false; }
+  if (a->type != CADA_F32 && a->type != CADA_BF16) { set_error("type must be CADA_F32 or CADA_BF16 (got %d)", a->type); return false; }
   return true;
 }
 
-size_t workspace(const cada_xent *a) { return ops_align(sizeof(Head)) + (a->mean && !a->loss ? ops_align((size_t)a->rows * 4) : 0); }
+bool one_workgroup(const cada_xent *a) { return a->rows > 0 && a->rows <= rows_together(lanes_for(a->classes, 16 / (int)type_bytes(a->type))); }
+size_t workspace(const cada_xent *a) { return (one_workgroup(a) ? 0 : ops_align(sizeof(Head))) + (a->mean && !a->loss ? ops_align((size_t)a->rows * 4) : 0); }
 
 }  // namespace
 }  // namespace cada
@@ -255,8 +277,6 @@ int cada_xent_workspace(cada_xent *a) {
 
 int cada_cross_entropy(const cada_xent *a) {
   if (!check(a)) return CADA_EINVAL;
-  if (a->classes < 1 || a->classes > 0x7fffffff - (1 << 20)) { set_error("classes must be in [1, 2^31 - 2^20) (got %lld)", (long long)a->classes); return CADA_EINVAL; }
-  if (a->type != CADA_F32 && a->type != CADA_BF16) { set_error("type must be CADA_F32 or CADA_BF16 (got %d)", a->type); return CADA_EINVAL; }
   if (a->label_bytes != 4 && a->label_bytes != 8) { set_error("label_bytes must be 4 or 8 (got %d)", a->label_bytes); return CADA_EINVAL; }
   if (!(a->smoothing >= 0.0 && a->smoothing < 1.0)) { set_error("smoothing must be in [0, 1)"); return CADA_EINVAL; }
   if (a->rows > 0) {
@@ -266,17 +286,21 @@ int cada_cross_entropy(const cada_xent *a) {
     if (reinterpret_cast<uintptr_t>(a->logits) % type_bytes(a->type) != 0 || reinterpret_cast<uintptr_t>(a->grad) % type_bytes(a->type) != 0 ||
         reinterpret_cast<uintptr_t>(a->labels) % a->label_bytes != 0) { set_error("logits, grad or labels are not aligned to their elements"); return CADA_EINVAL; }
   }
+  const int lanes = lanes_for(a->classes, 16 / (int)type_bytes(a->type));
+  if (ceil_div(a->rows, rows_together(lanes)) * std::max(lanes, 256) >= (int64_t)1 << 32) { set_error("%lld rows of %lld classes are more than one launch takes", (long long)a->rows, (long long)a->classes); return CADA_EINVAL; }
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, workspace(a))) return rc;
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   Head *head = static_cast<Head *>(a->workspace);
   Xent x{};
   x.logits = a->logits; x.labels = a->labels; x.grad = a->grad;
-  x.loss = a->loss ? a->loss : a->mean ? reinterpret_cast<float *>(static_cast<char *>(a->workspace) + ops_align(sizeof(Head))) : nullptr;
+  x.loss = a->loss ? a->loss : a->mean ? reinterpret_cast<float *>(static_cast<char *>(a->workspace) + (one_workgroup(a) ? 0 : ops_align(sizeof(Head)))) : nullptr;
   x.mean = a->mean; x.head = head; x.rows = a->rows; x.ldz = a->ldz; x.ldg = a->ldg; x.ignore = a->ignore_index;
   x.classes = (int32_t)a->classes; x.label_bytes = a->label_bytes;
   x.smoothing = (float)a->smoothing; x.keep = (float)(1.0 - a->smoothing); x.scale = (float)a->scale;
-  k_count<<<1, 1024, 0, st>>>(a->labels, a->label_bytes, a->rows, a->ignore_index, head, a->mean);
-  if (int rc = ops_launched("cross-entropy count")) return rc;
+  if (!one_workgroup(a)) {
+    k_count<<<1, 1024, 0, st>>>(a->labels, a->label_bytes, a->rows, a->ignore_index, head, a->mean);
+    if (int rc = ops_launched("cross-entropy count")) return rc;
+  }
   if (a->rows == 0) return CADA_OK;
   return a->type == CADA_BF16 ? rows<bf16>(x, st) : rows<float>(x, st);
 }

@@ -5,9 +5,8 @@
 ``AdamW``: the step over many tensors at once, moments in 32 or in 8 bits.
 
 Tensors are float32 or bfloat16 on one GPU.  Work goes to ``stream``, by default the device's current stream, and nothing
-synchronises the host.  Outputs that are not handed in are allocated.  A call's workspace comes from torch's caching allocator, unless one is
-handed in; like outputs allocated here it belongs to the current stream, so with a ``stream`` of one's own hand both in, or make it current
-(``with torch.cuda.stream(s)``).
+synchronises the host; inputs must be ready there.  Outputs that are not handed in, and a call's workspace unless one is, come from torch's caching
+allocator and belong to that stream.
 """
 from __future__ import annotations
 
@@ -84,7 +83,10 @@ def _call(call, tensor, stream, *args):
     index = tensor.get_device() if isinstance(tensor, torch.Tensor) else -1
     if index < 0:
         return call(*args, 0)          # (refused there)
-    handle = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
+    if stream is not None:
+        with torch.cuda.stream(stream):          # (so that what is allocated belongs to it)
+            return call(*args, stream.cuda_stream)
+    handle = torch._C._cuda_getCurrentRawStream(index)
     if index == torch._C._cuda_getDevice():
         return call(*args, handle)
     with torch.cuda.device(index):
@@ -148,6 +150,7 @@ class AdamW:
         _need(dev.type == "cuda", "params must be on a GPU")
         self.params, self.grads, self.copies = list(params), list(grads), list(copies) if copies is not None else [None] * n
         self.lr, self.t, self.state_bits = lr, 0, state_bits
+        self.stream = stream or torch.cuda.current_stream(dev)
         tensors = (cada_adamw_tensor * n)()
         self.offsets, total = [], 0
         for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
@@ -161,9 +164,11 @@ class AdamW:
             t.param_type, t.grad_type, t.weight_decay = _TYPES[p.dtype], _TYPES[g.dtype], decay[i]
             self.offsets.append(total)
             total += -(-p.numel() // MOMENT_BLOCK) * MOMENT_BLOCK
-        if moments is None:
-            moments = tuple((torch.zeros(total, dtype=dt, device=dev), torch.zeros(total // MOMENT_BLOCK, device=dev)) for dt in (torch.int8, torch.uint8)) \
-                if state_bits == 8 else (torch.zeros(total, device=dev), torch.zeros(total, device=dev))
+        with torch.cuda.stream(self.stream):          # (what is made here is ready for the steps)
+            self.norm = torch.zeros((), device=dev)
+            if moments is None:
+                moments = tuple((torch.zeros(total, dtype=dt, device=dev), torch.zeros(total // MOMENT_BLOCK, device=dev)) for dt in (torch.int8, torch.uint8)) \
+                    if state_bits == 8 else (torch.zeros(total, device=dev), torch.zeros(total, device=dev))
         self.m, self.v = moments
         for name, t, dt in (("m", self.m, torch.int8), ("v", self.v, torch.uint8)):
             parts = (t[0], t[1]) if state_bits == 8 else (t,)
@@ -171,7 +176,6 @@ class AdamW:
             for part, (dtype, size) in zip(parts, want):
                 _need(part.device == dev and part.dtype == dtype and part.is_contiguous() and part.numel() == size,
                       "%s must hold contiguous %s of %d elements on %s" % (name, dtype, size, dev))
-        self.norm = torch.zeros((), device=dev)
         cfg = cada_adamw_config()
         cfg.tensors, cfg.n_tensors, cfg.moment_bits = tensors, n, state_bits
         if state_bits == 8:
@@ -181,8 +185,8 @@ class AdamW:
         cfg.norm = self.norm.data_ptr()
         cfg.beta1, cfg.beta2, cfg.eps, cfg.max_norm = beta1, beta2, eps, max_norm
         _check(_lib.cada_adamw_workspace(C.byref(cfg)))
-        self.workspace = torch.empty(cfg.workspace_bytes, dtype=torch.uint8, device=dev)
-        self.stream = stream or torch.cuda.current_stream(dev)
+        with torch.cuda.stream(self.stream):
+            self.workspace = torch.empty(cfg.workspace_bytes, dtype=torch.uint8, device=dev)
         cfg.workspace, cfg.stream = self.workspace.data_ptr(), self.stream.cuda_stream
         plan = C.c_void_p()
         with torch.cuda.device(dev):
@@ -207,8 +211,8 @@ class AdamW:
         """(m, v) as float32 values, laid out as ``offsets`` says: the moments themselves with 32 bits, decoded copies with 8."""
         if self.state_bits == 32:
             return self.m, self.v
-        m, v = (torch.empty(self.m[0].numel(), dtype=torch.float32, device=self.device) for _ in range(2))
-        with torch.cuda.device(self.device):
+        with torch.cuda.stream(self.stream):
+            m, v = (torch.empty(self.m[0].numel(), dtype=torch.float32, device=self.device) for _ in range(2))
             _check(_lib.cada_adamw_moments(self.plan, m.data_ptr(), v.data_ptr()))
         return m, v
 

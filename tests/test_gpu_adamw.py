@@ -171,8 +171,7 @@ def test_one_step_of_a_captured_graph():
     a, b = ops.AdamW(params, grads, max_norm=1.0, state_bits=8), ops.AdamW(other, grads, max_norm=1.0, state_bits=8)
     s = torch.cuda.Stream()
     a.close()
-    with torch.cuda.stream(s):
-        a = ops.AdamW(params, grads, max_norm=1.0, state_bits=8)
+    a = ops.AdamW(params, grads, max_norm=1.0, state_bits=8, stream=s)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=s):

@@ -194,6 +194,11 @@ def test_other_stream_and_graph():
         got = ops.linear_backward(dy, x, w, pre=pre2, act="gelu")
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(y, y2) and all(torch.equal(p, q) for p, q in zip(want, got))
+    s.wait_stream(torch.cuda.current_stream())
+    y2, pre2 = ops.linear_forward(x, w, b, act="gelu", keep_pre=True, stream=s)
+    got = ops.linear_backward(dy, x, w, pre=pre2, act="gelu", stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(y, y2) and all(torch.equal(p, q) for p, q in zip(want, got))
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         y3, pre3 = ops.linear_forward(x, w, b, act="gelu", keep_pre=True)

@@ -51,7 +51,7 @@ def test_linear_backward(kw, code, text):
     (dict(ldz=9), -1, "row length"), (dict(ldg=9), -1, "row length"), (dict(ldg=12, grad=FAKE), -1, "in the place"), (dict(labels=FAKE + 4), -1, "not aligned"), (dict(workspace=None), -2, "NULL")])
 def test_cross_entropy(kw, code, text):
     a = ops.cada_xent()
-    a.rows, a.classes, a.type, a.label_bytes, a.logits, a.ldz, a.labels, a.grad, a.ldg = 4, 10, 0, 8, FAKE, 10, FAKE, FAKE + 4096, 10
+    a.rows, a.classes, a.type, a.label_bytes, a.logits, a.ldz, a.labels, a.grad, a.ldg = 1000, 10, 0, 8, FAKE, 10, FAKE, FAKE + 4096, 10
     a.workspace, a.workspace_bytes = FAKE, 1 << 20
     for k, v in kw.items():
         setattr(a, k, v)
