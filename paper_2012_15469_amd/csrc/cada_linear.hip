@@ -36,7 +36,7 @@ struct Product {
   int64_t a_cols, b_cols;    // oc tables: columns that lie in memory (>= M, N), whole pieces where they are read directly
   int64_t k_per_split;       // a multiple of the step
   int32_t N, tiles_m, tiles_n, splits;
-  float *partial;            // [splits][M][N] where splits > 1: the sums are joined by k_join
+  float *partial;            // [splits][M][N up to whole groups of eight] where splits > 1: the sums are joined by k_join
   Epilogue epi;
   // small gradients: the operand that is the signal is read as dy, and dz = dy * act'(pre) is formed on its way into LDS
   const void *pre;
@@ -115,6 +115,32 @@ __device__ __forceinline__ void mask(u32x4v (&reg)[BO * 8 / TH], const T *src, i
     }
   }
 }
+// The same for a whole step, whose contraction indices all exist: rows (kc) or columns (oc) beyond the table, which are the same ones in every step.
+template <typename T, bool KC, int BO, int TH> struct Edge {
+  typedef Side<T, KC, BO, TH> S;
+  uint32_t keep[KC ? S::kPieces : 4];
+  __device__ __forceinline__ Edge(int left, int t) {
+    int row, piece;
+    if constexpr (KC) {
+#pragma unroll
+      for (int i = 0; i < S::kPieces; ++i) {
+        S::place(i, t, row, piece);
+        keep[i] = row < left ? 0xFFFFFFFFu : 0u;
+      }
+    } else {
+      S::place(0, t, row, piece);        // (a thread's pieces are the same columns of different rows)
+      const int along = left - piece * S::E;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) keep[d] = S::E == 8 ? (along >= 2 * d + 2 ? 0xFFFFFFFFu : along == 2 * d + 1 ? 0xFFFFu : 0u) : along > d ? 0xFFFFFFFFu : 0u;
+    }
+  }
+  __device__ __forceinline__ void cut(u32x4v (&reg)[S::kPieces]) const {
+#pragma unroll
+    for (int i = 0; i < S::kPieces; ++i)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) reg[i][d] &= keep[KC ? i : d];
+  }
+};
 // dz = dy * act'(pre) in place of dy, and its sums per element of a piece (the pieces of a thread of an oc table are the same columns of different rows).
 template <typename T, int N>
 __device__ __forceinline__ void signal(u32x4v (&dy)[N], const u32x4v (&pre)[N], int act, float (&sum)[Elem<T>::kPer16]) {
@@ -206,6 +232,8 @@ __device__ __forceinline__ f32x16 multiply(v4s a, v4s b, f32x16 c) {
   return c;
 }
 
+__host__ __device__ constexpr int64_t eights(int64_t n) { return (n + 7) / 8 * 8; }
+
 // Eight consecutive columns n .. of row m of a finished sum; `left` of them exist.
 template <typename T>
 __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int64_t left, float (&f)[8]) {
@@ -284,17 +312,27 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
     fetch(r.b, b + s * b_step, ob, b_end);
     if constexpr (SIGNAL != NO_SIGNAL) fetch(r.pre, pre + s * pre_step, op, pre_end);
   };
+  const Edge<T, AKC, BM, TH> a_edge(m_in, t);
+  const Edge<T, BKC, BN, TH> b_edge(n_in, t);
   auto put_step = [&](Pieces &r, int s, unsigned char *dst) __attribute__((always_inline)) {
     const int k = k_in(s);
-    mask<T, AKC, BM, TH>(r.a, a + s * a_step, p.lda, a_end, m_in, k, t);
-    mask<T, BKC, BN, TH>(r.b, b + s * b_step, p.ldb, b_end, n_in, k, t);
-    if constexpr (SIGNAL == A_SIGNAL) {
-      mask<T, AKC, BM, TH>(r.pre, pre + s * pre_step, ldpre, pre_end, m_in, k, t);
-      signal<T>(r.a, r.pre, p.act, column_sum);
-    } else if constexpr (SIGNAL == B_SIGNAL) {
-      mask<T, BKC, BN, TH>(r.pre, pre + s * pre_step, ldpre, pre_end, n_in, k, t);
-      signal<T>(r.b, r.pre, p.act, column_sum);
+    if (DIRECT || k0 + (int64_t)(s + 1) * BK >= p.K) {        // (the contraction's last step, which may end inside, and read up to the tables' ends)
+      mask<T, AKC, BM, TH>(r.a, a + s * a_step, p.lda, a_end, m_in, k, t);
+      mask<T, BKC, BN, TH>(r.b, b + s * b_step, p.ldb, b_end, n_in, k, t);
+      if constexpr (SIGNAL == A_SIGNAL) mask<T, AKC, BM, TH>(r.pre, pre + s * pre_step, ldpre, pre_end, m_in, k, t);
+      if constexpr (SIGNAL == B_SIGNAL) mask<T, BKC, BN, TH>(r.pre, pre + s * pre_step, ldpre, pre_end, n_in, k, t);
+    } else {
+      if (m_in < BM) {
+        a_edge.cut(r.a);
+        if constexpr (SIGNAL == A_SIGNAL) a_edge.cut(r.pre);
+      }
+      if (n_in < BN) {
+        b_edge.cut(r.b);
+        if constexpr (SIGNAL == B_SIGNAL) b_edge.cut(r.pre);
+      }
     }
+    if constexpr (SIGNAL == A_SIGNAL) signal<T>(r.a, r.pre, p.act, column_sum);
+    if constexpr (SIGNAL == B_SIGNAL) signal<T>(r.b, r.pre, p.act, column_sum);
     put<SA::kPieces, TH>(dst, r.a, t);
     put<SB::kPieces, TH>(dst + SA::kBytes, r.b, t);
   };
@@ -393,21 +431,21 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
     // Two steps ahead in registers (asked for also where there is no such step: the loads are in bounds, and a branch around them would be waited at); the next
     // step is put into LDS between this one's products.
     ask(reg[0], 0);
-    ask(reg[1], 1);
+    if (steps > 1) ask(reg[1], 1);
     put_step(reg[0], 0, lds);
     lds_sync();
     read_fragments(fa[0], fb[0], lds, 0);
     auto one = [&](Pieces &next, Pieces &after, int s) __attribute__((always_inline)) {
       unsigned char *here = lds + (s & 1) * kHalf, *there = lds + ((s + 1) & 1) * kHalf;
-      ask(after, s + 2);
+      if (steps > 1) ask(after, s + 2);
 #pragma unroll
       for (int ks = 0; ks < NK - 1; ++ks) {
         read_fragments(fa[(ks + 1) & 1], fb[(ks + 1) & 1], here, ks + 1);
         __builtin_amdgcn_sched_barrier(0);
         multiply_all(fa[ks & 1], fb[ks & 1]);
-        if (ks == 1) put_step(next, s + 1, there);
+        if (ks == 1 && s + 1 < steps) put_step(next, s + 1, there);
       }
-      if constexpr (NK == 1) put_step(next, s + 1, there);
+      if (NK == 1 && s + 1 < steps) put_step(next, s + 1, there);
       lds_sync();
       last_of_step(there);
     };
@@ -454,7 +492,7 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       for (int e = 0; e < 8; ++e) f[e] = (src[e] + src[BM * kLd + e]) + (src[2 * BM * kLd + e] + src[3 * BM * kLd + e]);
       const int64_t m = m0 + t / 4, left = (int64_t)p.N - n0 - (t & 3) * 8;
       const int n = n0 + (t & 3) * 8;
-      if (p.splits > 1) store8_n(p.partial + ((int64_t)split * p.M + m) * p.N + n, left, f);
+      if (p.splits > 1) store8_n(p.partial + ((int64_t)split * p.M + m) * eights(p.N) + n, left > 0 ? 8 : 0, f);
       else finish8<T>(p.epi, m, n, left, f);
     }
     return;
@@ -487,7 +525,7 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       const v4s x = *reinterpret_cast<const v4s *>(src), y = *reinterpret_cast<const v4s *>(src + 4);
       float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
       if (m < p.M) {
-        if (p.splits > 1) store8_n(p.partial + ((int64_t)split * p.M + m) * p.N + n, left, f);
+        if (p.splits > 1) store8_n(p.partial + ((int64_t)split * p.M + m) * eights(p.N) + n, left > 0 ? 8 : 0, f);
         else finish8<T>(p.epi, m, n, left, f);
       }
     }
@@ -648,15 +686,23 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
       const int per = (p.N + 7) / 8;
       const int64_t m = g / per;
       const int n = (int)(g - m * per) * 8;
-      const float *src = p.partial + m * p.N + n;
-      const int64_t left = (int64_t)p.N - n;
-      float f[8], o[8];
-      load8_n(src, left, f);
-      for (int s = 1; s < p.splits; ++s) {
-        load8_n(src + (int64_t)s * p.M * p.N, left, o);
+      const int64_t left = (int64_t)p.N - n, apart = p.M * per * 8 / 4;        // (four floats apart)
+      const v4s *src = reinterpret_cast<const v4s *>(p.partial + (m * per * 8 + n));
+      v4s lo = src[0], hi = src[1];
+      for (int s = 1; s < p.splits; s += 8) {        // eight parts on their way at once
+        v4s l[8], h[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) f[q] += o[q];
+        for (int u = 0; u < 8; ++u) {
+          const v4s *at = src + (int64_t)min(s + u, p.splits - 1) * apart;
+          l[u] = at[0];
+          h[u] = at[1];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          if (s + u < p.splits) { lo += l[u]; hi += h[u]; }
+        }
       }
+      float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       finish8<T>(p.epi, m, n, left, f);
       return;
     }
@@ -760,9 +806,9 @@ struct Cut { int tile, splits; int64_t k_per_split; };
 // tile per CU: 870 (128), 460 (64).  Float32 is bound by the matrix instructions at any of them (146 TFLOP/s, 64 x 64 as 128 x 128), so it takes the smallest.
 struct TileCost { int tile, slots; double alone, crowd, share, ends; };
 constexpr TileCost kCostBf16[] = {{32, 5, 0.135, 0.05, 0.13, 1.0}, {64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
-constexpr TileCost kCostF32[] = {{32, 5, 0.21, 0.02, 0.14, 1.1}, {64, 5, 0.51, 0.05, 0.47, 1.3}};
+constexpr TileCost kCostF32[] = {{32, 5, 0.21, 0.02, 0.155, 1.1}, {64, 5, 0.51, 0.05, 0.50, 1.3}};
 // Through registers (64 x 64 only): 8192 x 4001 x 2003 bf16 340 us where 4000 x 2000 takes 108 directly, float32 1100 and 960.
-constexpr TileCost kCostBf16Registers[] = {{32, 5, 0.30, 0.03, 0.16, 1.7}, {64, 5, 0.35, 0.1, 0.30, 2.1}}, kCostF32Registers[] = {{32, 5, 0.44, 0.03, 0.20, 1.3}, {64, 5, 0.69, 0.05, 0.53, 2.2}};
+constexpr TileCost kCostBf16Registers[] = {{32, 5, 0.30, 0.03, 0.16, 1.7}, {64, 5, 0.35, 0.1, 0.30, 2.1}}, kCostF32Registers[] = {{32, 5, 0.44, 0.03, 0.24, 1.3}, {64, 5, 0.69, 0.05, 0.57, 2.2}};
 constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct Shape { int64_t M, N, K; };
@@ -824,7 +870,7 @@ int launch_pack(Packs &a, hipStream_t st) {
   k_pack<T><<<many(total), 256, 0, st>>>(a);
   return ops_launched("linear pack");
 }
-size_t partial_bytes(const Cut &c, int64_t M, int64_t N) { return c.splits > 1 ? ops_align((size_t)c.splits * M * N * 4) : 0; }
+size_t partial_bytes(const Cut &c, int64_t M, int64_t N) { return c.splits > 1 ? ops_align((size_t)c.splits * M * eights(N) * 4) : 0; }
 
 void lay(Product *p, const Cut &c, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, float *partial) {
   p->a_cols = M; p->b_cols = N;
@@ -1006,8 +1052,8 @@ BackwardPlan plan_backward(const cada_linear_grad *a) {
     if (a->dw) b.dw = c[n - 1];
   }
   b.lddz = ceil_div(out, 8) * 8;
-  // (workgroups for every CU several times over, but no more parts of the column sums than rows / 16)
-  b.rows_per_block = std::max<int64_t>(16, ceil_div(ceil_div(rows * ceil_div(out, 256), 2048), 8) * 8);
+  // (workgroups for every CU several times over, but no more parts of the column sums than rows / 8)
+  b.rows_per_block = std::max<int64_t>(8, ceil_div(ceil_div(rows * ceil_div(out, 256), 2048), 8) * 8);
   b.row_blocks = b.small ? b.dw.splits : ceil_div(rows, b.rows_per_block);
   size_t off = b.own_dz ? ops_align((size_t)rows * b.lddz * elem) : 0;
   b.off_db = off;

@@ -29,27 +29,6 @@ MOMENT_BLOCK = 256
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-class cada_linear(C.Structure):
-    _fields_ = [("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("type", C.c_int32), ("act", C.c_int32),
-                ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
-                ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64), ("pre", C.c_void_p), ("ldpre", C.c_int64),
-                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
-
-
-class cada_linear_grad(C.Structure):
-    _fields_ = [("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("type", C.c_int32), ("act", C.c_int32),
-                ("dy", C.c_void_p), ("lddy", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64),
-                ("pre", C.c_void_p), ("ldpre", C.c_int64), ("dx", C.c_void_p), ("lddx", C.c_int64), ("dw", C.c_void_p), ("lddw", C.c_int64),
-                ("db", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
-
-
-class cada_xent(C.Structure):
-    _fields_ = [("rows", C.c_int64), ("classes", C.c_int64), ("type", C.c_int32), ("label_bytes", C.c_int32), ("logits", C.c_void_p), ("ldz", C.c_int64),
-                ("labels", C.c_void_p), ("ignore_index", C.c_int64), ("smoothing", C.c_double), ("scale", C.c_double), ("mean", C.c_void_p),
-                ("loss", C.c_void_p), ("grad", C.c_void_p), ("ldg", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
-                ("stream", C.c_void_p)]
-
-
 class cada_adamw_tensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32),
                 ("weight_decay", C.c_double)]
@@ -61,10 +40,7 @@ class cada_adamw_config(C.Structure):
                 ("max_norm", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
 
 
-for _name, _res, _args in (("cada_linear_forward_workspace", C.c_int, [C.POINTER(cada_linear)]), ("cada_linear_forward", C.c_int, [C.POINTER(cada_linear)]),
-                           ("cada_linear_backward_workspace", C.c_int, [C.POINTER(cada_linear_grad)]), ("cada_linear_backward", C.c_int, [C.POINTER(cada_linear_grad)]),
-                           ("cada_xent_workspace", C.c_int, [C.POINTER(cada_xent)]), ("cada_cross_entropy", C.c_int, [C.POINTER(cada_xent)]),
-                           ("cada_adamw_moment_elements", C.c_int64, [C.POINTER(cada_adamw_config)]), ("cada_adamw_workspace", C.c_int, [C.POINTER(cada_adamw_config)]),
+for _name, _res, _args in (("cada_adamw_moment_elements", C.c_int64, [C.POINTER(cada_adamw_config)]), ("cada_adamw_workspace", C.c_int, [C.POINTER(cada_adamw_config)]),
                            ("cada_adamw_init", C.c_int, [C.POINTER(cada_adamw_config), C.POINTER(C.c_void_p)]),
                            ("cada_adamw_step", C.c_int, [C.c_void_p, C.c_int64, C.c_double, C.c_void_p]),
                            ("cada_adamw_moments", C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]), ("cada_adamw_destroy", None, [C.c_void_p])):
@@ -211,9 +187,11 @@ class AdamW:
         """(m, v) as float32 values, laid out as ``offsets`` says: the moments themselves with 32 bits, decoded copies with 8."""
         if self.state_bits == 32:
             return self.m, self.v
-        with torch.cuda.stream(self.stream):
-            m, v = (torch.empty(self.m[0].numel(), dtype=torch.float32, device=self.device) for _ in range(2))
-            _check(_lib.cada_adamw_moments(self.plan, m.data_ptr(), v.data_ptr()))
+        if torch._C._cuda_getCurrentRawStream(self.device.index) != self.stream.cuda_stream:
+            with torch.cuda.stream(self.stream):          # (so that what is allocated belongs to it)
+                return self.moments()
+        m, v = (torch.empty_like(self.m[0], dtype=torch.float32) for _ in range(2))
+        _check(_lib.cada_adamw_moments(self.plan, m.data_ptr(), v.data_ptr()))
         return m, v
 
     def close(self):

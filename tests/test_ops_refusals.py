@@ -4,6 +4,7 @@ import ctypes as C
 import pytest
 import torch
 
+from common_ops import cada_linear, cada_linear_grad, cada_xent
 from paper_2012_15469_amd import ops
 from paper_2012_15469_amd.binding import _lib, cada_last_error
 
@@ -14,7 +15,7 @@ LONG = dict(rows=64, in_=100000, ldx=100000)          # few tiles of a long cont
 
 
 def linear(**kw):
-    a = ops.cada_linear()
+    a = cada_linear()
     a.rows, a.in_, a.out, a.type, a.act = 4, 8, 16, 1, 0
     a.x, a.ldx, a.w, a.ldw, a.y, a.ldy, a.workspace, a.workspace_bytes = FAKE, 8, FAKE, 16, FAKE, 16, FAKE, 1 << 30
     for k, v in kw.items():
@@ -36,7 +37,7 @@ def test_linear_forward(kw, code, text):
     (dict(x=None), -1, "x is NULL"), (dict(w=None), -1, "w is NULL"), (dict(lddx=1), -1, "row length of dx"), (dict(lddw=1), -1, "row length of dw"), (dict(db=FAKE + 1), -1, "db"),
     (dict(rows=100000, workspace_bytes=0), -2, "too small")])
 def test_linear_backward(kw, code, text):
-    a = ops.cada_linear_grad()
+    a = cada_linear_grad()
     a.rows, a.in_, a.out, a.type, a.act = 4, 8, 16, 1, 0
     a.dy, a.lddy, a.x, a.ldx, a.w, a.ldw, a.dx, a.lddx, a.dw, a.lddw, a.db = FAKE, 16, FAKE, 8, FAKE, 16, FAKE, 8, FAKE, 16, FAKE
     a.workspace, a.workspace_bytes = FAKE, 1 << 30
@@ -50,7 +51,7 @@ def test_linear_backward(kw, code, text):
     (dict(smoothing=1.0), -1, "smoothing"), (dict(smoothing=float("nan")), -1, "smoothing"), (dict(logits=None), -1, "device pointers"), (dict(labels=None), -1, "device pointers"),
     (dict(ldz=9), -1, "row length"), (dict(ldg=9), -1, "row length"), (dict(ldg=12, grad=FAKE), -1, "in the place"), (dict(labels=FAKE + 4), -1, "not aligned"), (dict(workspace=None), -2, "NULL")])
 def test_cross_entropy(kw, code, text):
-    a = ops.cada_xent()
+    a = cada_xent()
     a.rows, a.classes, a.type, a.label_bytes, a.logits, a.ldz, a.labels, a.grad, a.ldg = 1000, 10, 0, 8, FAKE, 10, FAKE, FAKE + 4096, 10
     a.workspace, a.workspace_bytes = FAKE, 1 << 20
     for k, v in kw.items():
