@@ -727,25 +727,25 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
   }
 }
 
-// dz = dy * act'(pre), written in the operands' type with rows on 16-byte boundaries, and its column sums per block of rows.  A workgroup takes 256 columns:
-// 32 lanes of eight columns each by eight rows at a time.
+// dz = dy * act'(pre), written in the operands' type with rows on 16-byte boundaries, and its column sums per block of rows.  A workgroup is 2^lanes threads
+// of eight columns each, as many as the columns need up to 32, by as many rows at a time.
 struct Signal {
   const void *dy, *pre;
   int64_t lddy, ldpre, rows, rows_per_block;
-  int32_t n, act;
+  int32_t n, act, lanes;
   void *dz;                  // or null
   int64_t lddz;
   float *db_part;            // [blocks of rows][n] or null
 };
 template <typename T>
 __global__ __launch_bounds__(256) void k_signal(const Signal a) {
-  __shared__ float part[8][32][9];
-  const int t = threadIdx.x, cx = t & 31, ry = t >> 5;
-  const int n = (blockIdx.x * 32 + cx) * 8;
+  __shared__ float part[256 * 9];
+  const int t = threadIdx.x, width = 1 << a.lanes, cx = t & (width - 1), ry = t >> a.lanes, high = 256 >> a.lanes;
+  const int n = (blockIdx.x * width + cx) * 8;
   const int64_t left = (int64_t)a.n - n, r0 = (int64_t)blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   float sum[8] = {};
   if (left > 0) {
-    for (int64_t r = r0 + ry; r < r1; r += 8) {
+    for (int64_t r = r0 + ry; r < r1; r += high) {
       float f[8], z[8];
       load8_n(static_cast<const T *>(a.dy) + r * a.lddy + n, left, f);
       if (a.act != CADA_ACT_NONE) {
@@ -760,13 +760,12 @@ __global__ __launch_bounds__(256) void k_signal(const Signal a) {
   }
   if (!a.db_part) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) part[ry][cx][i] = sum[i];
+  for (int i = 0; i < 8; ++i) part[t * 9 + i] = sum[i];
   __syncthreads();
-  const int c = blockIdx.x * 256 + t;
-  if (c < a.n) {
+  const int c = blockIdx.x * width * 8 + t;
+  if (t < width * 8 && c < a.n) {
     float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += part[i][t >> 3][t & 7];
+    for (int i = 0; i < high; ++i) s += part[((i << a.lanes) + (t >> 3)) * 9 + (t & 7)];
     a.db_part[(int64_t)blockIdx.y * a.n + c] = s;
   }
 }
@@ -823,13 +822,13 @@ double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
   double best = 1e300;
   for (int c = 0; c < n_costs; ++c) {
     const TileCost &t = costs[c];
-    // each product's splits that may help (none that leave less than two steps, or make more tiles than two for every CU), with tiles, steps and the join's time
+    // each product's splits that may help (none that leave less than two steps, or make more tiles than two, for a product alone six, for every CU), with tiles, steps and the join's time
     struct Option { int splits; double tiles, steps, join; } opt[2][16];
     int n_opt[2] = {0, 0};
     for (int i = 0; i < n; ++i) {
       const int64_t tiles = ceil_div(s[i].M, t.tile) * ceil_div(s[i].N, t.tile);
-      for (int k : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-        if (k > 1 && (steps[i] < 2 * k || tiles * k > 2 * kCUs)) break;
+      for (int k : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 24, 32}) {
+        if (k > 1 && (steps[i] < 2 * k || tiles * k > (n == 1 ? 6 : 2) * kCUs)) break;
         if (tiles > kMostTiles) break;
         opt[i][n_opt[i]++] = Option{k, (double)(tiles * k), (double)ceil_div(steps[i], k), k > 1 ? (k * 4.0 + 2.0) * (double)s[i].M * (double)s[i].N / kJoinBytesPerUs : 0.0};
       }
@@ -1015,7 +1014,8 @@ constexpr double kSmallGradients = 1e8;
 struct BackwardPlan {
   bool small, by_element, own_dz, direct, pack_x, pack_w;
   Cut dx, dw;
-  int64_t lddz, rows_per_block, row_blocks;
+  int signal_lanes;
+  int64_t signal_columns, lddz, rows_per_block, row_blocks;
   size_t off_db, off_dx, off_dw, off_x, off_w, bytes;
 };
 BackwardPlan plan_backward(const cada_linear_grad *a) {
@@ -1052,8 +1052,11 @@ BackwardPlan plan_backward(const cada_linear_grad *a) {
     if (a->dw) b.dw = c[n - 1];
   }
   b.lddz = ceil_div(out, 8) * 8;
-  // (workgroups for every CU several times over, but no more parts of the column sums than rows / 8)
-  b.rows_per_block = std::max<int64_t>(8, ceil_div(ceil_div(rows * ceil_div(out, 256), 2048), 8) * 8);
+  // (workgroups for every CU several times over, but no more parts of the column sums than a workgroup's rows at a time, or two, make)
+  while (b.signal_lanes < 5 && (8 << b.signal_lanes) < out) ++b.signal_lanes;
+  const int64_t high = 256 >> b.signal_lanes;
+  b.signal_columns = ceil_div(out, 8 << b.signal_lanes);
+  b.rows_per_block = std::max<int64_t>(b.signal_lanes == 5 ? high : 2 * high, ceil_div(ceil_div(rows * b.signal_columns, 2048), high) * high);
   b.row_blocks = b.small ? b.dw.splits : ceil_div(rows, b.rows_per_block);
   size_t off = b.own_dz ? ops_align((size_t)rows * b.lddz * elem) : 0;
   b.off_db = off;
@@ -1100,10 +1103,10 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   float *db_part = reinterpret_cast<float *>(ws + b.off_db);
   if (b.own_dz || (a->db && !b.small && !b.by_element)) {
     Signal s{};
-    s.dy = a->dy; s.lddy = a->lddy; s.pre = a->pre; s.ldpre = a->ldpre; s.rows = a->rows; s.rows_per_block = b.rows_per_block; s.n = (int32_t)a->out; s.act = a->act;
+    s.dy = a->dy; s.lddy = a->lddy; s.pre = a->pre; s.ldpre = a->ldpre; s.rows = a->rows; s.rows_per_block = b.rows_per_block; s.n = (int32_t)a->out; s.act = a->act; s.lanes = b.signal_lanes;
     s.dz = b.own_dz ? ws : nullptr; s.lddz = b.lddz;
     s.db_part = a->db ? db_part : nullptr;
-    k_signal<T><<<dim3((unsigned)ceil_div(a->out, 256), (unsigned)b.row_blocks), 256, 0, st>>>(s);
+    k_signal<T><<<dim3((unsigned)b.signal_columns, (unsigned)b.row_blocks), 256, 0, st>>>(s);
     if (int rc = ops_launched("linear signal")) return rc;
   }
   const void *dz = b.own_dz ? ws : a->dy;
