@@ -806,7 +806,7 @@ struct Cut { int tile, splits; int64_t k_per_split; };
 struct TileCost { int tile, slots; double alone, crowd, share, ends; };
 constexpr TileCost kCostBf16[] = {{32, 5, 0.135, 0.05, 0.13, 1.0}, {64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
 constexpr TileCost kCostF32[] = {{32, 5, 0.21, 0.02, 0.155, 1.1}, {64, 5, 0.51, 0.05, 0.50, 1.3}};
-// Through registers (64 x 64 only): 8192 x 4001 x 2003 bf16 340 us where 4000 x 2000 takes 108 directly, float32 1100 and 960.
+// Through registers (up to 64 x 64): 8192 x 4001 x 2003 bf16 340 us where 4000 x 2000 takes 108 directly, float32 1100 and 960.
 constexpr TileCost kCostBf16Registers[] = {{32, 5, 0.30, 0.03, 0.16, 1.7}, {64, 5, 0.35, 0.1, 0.30, 2.1}}, kCostF32Registers[] = {{32, 5, 0.44, 0.03, 0.24, 1.3}, {64, 5, 0.69, 0.05, 0.57, 2.2}};
 constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 

@@ -3,7 +3,7 @@
 // A row's logits are read once and stay in registers, as they were read, between the statistics and the gradient: max, then sum of exp(z - max) with the
 // classes that are left and their logits' mean (smoothing), then softmax - target.  A group of 4 to 1024 lanes takes a row, by its length; rows beyond what
 // 1024 lanes hold (131072 bf16, 65536 float32) are read again.  Two launches: the rows that count, which every gradient is divided by, and the rows, the last
-// workgroup of which adds the losses up in the rows' order.
+// workgroup of which adds the losses up in the rows' order; rows that fit one workgroup are counted there, in one launch.
 #include <algorithm>
 
 #include "cada_ops_internal.h"
