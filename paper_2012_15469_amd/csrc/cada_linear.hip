@@ -549,71 +549,82 @@ __global__ __launch_bounds__(64 * WY * WX * KW) void k_forward(const Product p) 
   if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT, STAGES, KW>(p, tile, lds);
 }
 
-// A few rows (a single sample answered): a read of the weights.  A workgroup takes 64 columns, a lane eight of them (one line of memory per eight lanes and weight row), and
-// 128 weight rows at a time; the rows of x wait in LDS; the sums over the 128 lanes of a column are joined at the end.  One launch, no workspace.
-constexpr int kFewRows = 4, kFewThreads = 1024, kFewChunk = 2048;
-template <typename T, int R>
+// A few rows (a single sample answered): a read of the weights.  A workgroup takes C columns, a lane eight of them, and 1024 or 512 weight rows at a time, asked for
+// together with x, which waits in LDS; a column's lanes exchange halves of their sums until each has one (four rows of 784 x 512 bf16 6.4 us; with sums of all
+// values over all lanes 10.3), and the wavefronts' sums are added in their order.  One launch, unless the contraction is split.  What bounds it: a launch and two trips to memory, one of
+// them the kernel's own (1 x 1024 x 4096 bf16 5.0 us, from memory 7.4; 8192 x 16384 54.9 us, 4.9 TB/s).
+constexpr int kFewRows = 4, kFewThreads = 1024;
+template <typename T, int R, int C>
 __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
-  __shared__ float xs[R][kFewChunk];
-  __shared__ float part[16][R][64];
-  constexpr int kVecs = 8 / Elem<T>::kPer16;        // of 16 bytes in eight columns
-  const int t = threadIdx.x, cg = t & 7, kl = t >> 3, n0 = blockIdx.x * 64, n = n0 + cg * 8;
-  const int64_t left = (int64_t)p.N - n;
+  constexpr int E = Elem<T>::kPer16, kVecs = 8 / E;        // loads of eight columns
+  constexpr int kLanes = C / 8, kApart = kFewThreads / kLanes, U = 8 / kVecs, kFewStep = U * kApart;
+  __shared__ float xs[R][kFewStep], part[16][R][C];
+  const int t = threadIdx.x, lane = t & 63, cg = t % kLanes, kl = t / kLanes, n0 = blockIdx.x * C, n = n0 + cg * 8;
+  const int64_t left = (int64_t)p.N - n, k_end = min(p.K, (blockIdx.y + 1) * p.k_per_split);
   const T *w = static_cast<const T *>(p.b) + n, *x = static_cast<const T *>(p.a);
   float acc[R][8] = {};
-  for (int64_t k0 = 0; k0 < p.K; k0 += kFewChunk) {
-    const int here = (int)min((int64_t)kFewChunk, p.K - k0);
-    if (k0 > 0) __syncthreads();
+  for (int64_t k0 = blockIdx.y * p.k_per_split; k0 < k_end; k0 += kFewStep) {
+    const int here = (int)min((int64_t)kFewStep, k_end - k0);
+    float xv[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      for (int i = t; i < here; i += kFewThreads) xs[r][i] = r < p.M ? to_f32(x[r * p.lda + k0 + i]) : 0.f;
+    for (int r = 0; r < R; ++r) xv[r] = r < p.M && t < here ? to_f32(x[r * p.lda + k0 + t]) : 0.f;
+    u32x4v raw[U][kVecs];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) raw[u][v] = load16_n(w + (k0 + kl + u * kApart) * p.ldb + v * E, kl + u * kApart < here ? left - v * E : 0);
     __syncthreads();
-    if (left > 0) {
-      const T *wk = w + k0 * p.ldb;
-      constexpr int U = 32 / kVecs / 4;        // weight rows on their way at once
-      for (int k = kl; k < here; k += U * 128) {
-        u32x4v raw[U][kVecs];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+    for (int r = 0; r < R; ++r) if (t < kFewStep) xs[r][t] = xv[r];
+    __syncthreads();
 #pragma unroll
-          for (int v = 0; v < kVecs; ++v) raw[u][v] = load16_n(wk + (int64_t)(k + u * 128) * p.ldb + v * Elem<T>::kPer16, k + u * 128 < here ? left - v * Elem<T>::kPer16 : 0);
+    for (int u = 0; u < U; ++u) {
+      if (kl + u * kApart >= here) break;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (k + u * 128 >= here) break;
-          float xv[R];
+      for (int r = 0; r < R; ++r) xv[r] = xs[r][kl + u * kApart];
 #pragma unroll
-          for (int r = 0; r < R; ++r) xv[r] = xs[r][k + u * 128];
+      for (int v = 0; v < kVecs; ++v) {
+        float f[E];
+        unpack<T>(raw[u][v], f);
 #pragma unroll
-          for (int v = 0; v < kVecs; ++v) {
-            float f[Elem<T>::kPer16];
-            unpack<T>(raw[u][v], f);
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-              for (int e = 0; e < Elem<T>::kPer16; ++e) acc[r][v * Elem<T>::kPer16 + e] = fmaf(xv[r], f[e], acc[r][v * Elem<T>::kPer16 + e]);
-          }
-        }
+          for (int e = 0; e < E; ++e) acc[r][v * E + e] = fmaf(xv[r], f[e], acc[r][v * E + e]);
       }
     }
   }
 #pragma unroll
-  for (int r = 0; r < R; ++r)
+  for (int r = 0; r < R; ++r) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float v = acc[r][e];
-      v += __shfl_xor(v, 8, 64);
-      v += __shfl_xor(v, 16, 64);
-      v += __shfl_xor(v, 32, 64);
-      if ((t & 56) == 0) part[t >> 6][r][cg * 8 + e] = v;
+    for (int o = kLanes; o < 8; o *= 2)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[r][e] += __shfl_xor(acc[r][e], o, 64);
+#pragma unroll
+    for (int h = 4; h > 0; h /= 2) {        // lanes 8 h apart: the upper one goes on with the upper half
+      const bool upper = lane & 8 * h;
+#pragma unroll
+      for (int e = 0; e < h; ++e) {
+        const float mine = upper ? acc[r][e + h] : acc[r][e], other = upper ? acc[r][e] : acc[r][e + h];
+        acc[r][e] = mine + __shfl_xor(other, 8 * h, 64);
+      }
     }
-  __syncthreads();
-  if (t < R * 8 && (t >> 3) < p.M) {
-    float f[8] = {};
-    for (int i = 0; i < 16; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] += part[i][t >> 3][cg * 8 + e];
-    finish8<T>(p.epi, t >> 3, n, left, f);
+    if ((lane & 7) < kLanes) part[t >> 6][r][cg * 8 + (lane >> 5) * 4 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1)] = acc[r][0];
   }
+  __syncthreads();
+  if (t < R * C) {
+    float v = part[0][t / C][t % C];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += part[i][t / C][t % C];
+    part[0][t / C][t % C] = v;
+  }
+  __syncthreads();
+  const int m = t / kLanes;
+  if (m >= R || m >= p.M) return;
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = part[0][m][cg * 8 + e];
+  if (p.splits > 1) store8_n(p.partial + ((int64_t)blockIdx.y * p.M + m) * eights(p.N) + n, left > 0 ? 8 : 0, f);
+  else finish8<T>(p.epi, m, n, left, f);
 }
 
 // dx and dw in one launch (either may have no tiles), the one with the longer contraction first: its tiles would be the launch's tail.
@@ -904,14 +915,26 @@ bool check_table(const char *name, const void *p, int64_t ld, int64_t cols, int 
 // Whether a table is too small for a read of 16 bytes, or a tile of it too large for offsets in 32 bits.
 bool no_tiles(int64_t rows, int64_t ld, int64_t cols, size_t elem) { return ((rows - 1) * ld + cols) * (int64_t)elem < 16 || 64 * ld * (int64_t)elem >= (int64_t)1 << 32; }
 
+// Columns of a workgroup that answers a few rows: a line of memory of bf16 weights (half a line each from two: 4096 x 4096 17 us, not 11); of float32 ones a line,
+// for twice the workgroups, or two lines where that leaves one for every CU (4096 x 1024, single row, from memory 28 us with 32 columns and 36 with 64; 8192 x 16384 127 and 104).
+int few_columns(size_t elem, int64_t out) { return elem == 2 || out >= 64 * kCUs ? 64 : 32; }
+// Their contraction is split where CUs would stand idle and a workgroup have more than two reads of memory one after the other: a join costs 3 us, 1024 rows of weights 4 where they
+// come from memory (single row, bf16, from memory: 4096 x 1024 19.5 -> 11.2 us, 3000 x 1000 17.0 -> 11.5, 16384 x 4096 71 -> 32; 2048 x 2048 11.8 -> 11.1, and within L2 7.0 -> 8.7).
+Cut cut_few(size_t elem, int64_t in, int64_t out) {
+  const int64_t groups = ceil_div(out, few_columns(elem, out)), most = in <= 2 * 1024 ? 1 : std::min(kCUs / groups, ceil_div(in, 1024));
+  const int64_t per = ceil_div(ceil_div(in, std::clamp<int64_t>(most, 1, 16)), 1024) * 1024;
+  return Cut{64, (int)ceil_div(in, per), per};
+}
+
 struct ForwardPlan { bool few, by_element, direct, pack_x, pack_w; Cut cut; size_t off_x, off_w, bytes; };
 ForwardPlan plan_forward(const cada_linear *a) {
   ForwardPlan f{};
   if (a->rows == 0) return f;
   f.few = a->rows <= kFewRows;
-  f.cut = Cut{64, 1, a->in};
   const size_t elem = type_bytes(a->type);
+  f.cut = f.few ? cut_few(elem, a->in, a->out) : Cut{64, 1, a->in};
   f.by_element = no_tiles(a->rows, a->ldx, a->in, elem) || no_tiles(a->in, a->ldw, a->out, elem);
+  if (f.few) f.bytes = partial_bytes(f.cut, a->rows, a->out);
   if (f.few || f.by_element) return f;
   const bool x_direct = direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, a->out, elem);
   const Shape s = {a->rows, a->out, a->in};
@@ -961,6 +984,13 @@ int launch_join(Join &j, hipStream_t st) {
   return ops_launched("linear join");
 }
 
+template <typename T, int C>
+void launch_few(const Product &p, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(p.N, C), p.splits);
+  if (p.M <= 2) k_few_rows<T, 2, C><<<grid, kFewThreads, 0, st>>>(p);
+  else k_few_rows<T, 4, C><<<grid, kFewThreads, 0, st>>>(p);
+}
+
 template <typename T>
 int forward(const cada_linear *a, const ForwardPlan &f) {
   hipStream_t st = static_cast<hipStream_t>(a->stream);
@@ -981,19 +1011,15 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
   }
   p.epi = Epilogue{a->bias, a->residual, a->pre, a->y, a->ldr, a->ldpre, a->ldy, a->act};
   if (f.few) {
-    const unsigned grid = (unsigned)ceil_div(a->out, 64);
-    if (a->rows == 1) k_few_rows<T, 1><<<grid, kFewThreads, 0, st>>>(p);
-    else if (a->rows == 2) k_few_rows<T, 2><<<grid, kFewThreads, 0, st>>>(p);
-    else k_few_rows<T, 4><<<grid, kFewThreads, 0, st>>>(p);
-    return ops_launched("linear");
-  }
-  if (f.by_element) {
+    if (few_columns(sizeof(T), a->out) == 64) launch_few<T, 64>(p, st);
+    else if constexpr (sizeof(T) == 4) launch_few<T, 32>(p, st);
+  } else if (f.by_element) {
     k_by_element<T, true, false, NO_SIGNAL><<<many(a->rows * a->out), 256, 0, st>>>(p);
-    return ops_launched("linear");
-  }
-  if (f.cut.tile == 32) forward_tiles<T, 32, 1, 1, 4>(p, f.direct, st);
-  if (f.cut.tile == 64) forward_tiles<T, 64, 2, 2, 1>(p, f.direct, st);
-  if constexpr (sizeof(T) == 2) {
+  } else if (f.cut.tile == 32) {
+    forward_tiles<T, 32, 1, 1, 4>(p, f.direct, st);
+  } else if (f.cut.tile == 64) {
+    forward_tiles<T, 64, 2, 2, 1>(p, f.direct, st);
+  } else if constexpr (sizeof(T) == 2) {
     if (f.cut.tile == 128) forward_tiles<T, 128, 2, 4, 1>(p, f.direct, st);
     if (f.cut.tile == 256) forward_tiles<T, 256, 2, 4, 1>(p, f.direct, st);
   }

@@ -225,3 +225,20 @@ def test_offsets_past_32_bits(dtype):
     assert torch.equal(ops.linear_forward(x, w)[0], ops.linear_forward(small, w)[0])
     for a, b in zip(ops.linear_backward(dy, x, w), ops.linear_backward(dy, small, w)):
         assert torch.allclose(a.float(), b.float(), rtol=2 * rounding(dtype), atol=1e-4)
+
+
+# One to four rows: contractions that end inside a read, that are split, and outputs that take either number of columns for a workgroup.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1023, 31), (1, 1025, 65), (2, 2049, 10), (1, 4096, 1024), (3, 5001, 1003), (4, 4097, 4100), (1, 20011, 129), (4, 40, 16640), (2, 2050, 16390)], ids=str)
+def test_few_rows(shape, dtype):
+    rows, k, n = shape
+    gen = torch.Generator(device="cuda"); gen.manual_seed(rows * 13 + n)
+    for act, pad, shift in (("none", 0, 0), ("gelu", 3, 1)):
+        x, w = table(rows, k, dtype, gen, pad, shift), table(k, n, dtype, gen, pad, shift, 1 / math.sqrt(k))
+        b, r = table(1, n, dtype, gen)[0], table(rows, n, dtype, gen, pad, shift)
+        y, pre = ops.linear_forward(x, w, b, residual=r, act=act, keep_pre=True)
+        assert torch.equal(y, ops.linear_forward(x, w, b, residual=r, act=act)[0])
+        z = x.double() @ w.double() + b.double()
+        bound = (k + 8) * U * (x.double().abs() @ w.double().abs() + b.double().abs())
+        close(pre, z, bound, dtype)
+        close(y, act64(z, act) + r.double(), bound + U * r.double().abs(), dtype)
