@@ -549,14 +549,14 @@ __global__ __launch_bounds__(64 * WY * WX * KW) void k_forward(const Product p) 
   if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT, STAGES, KW>(p, tile, lds);
 }
 
-// A few rows (a single sample answered): a read of the weights.  A workgroup takes C columns, a lane eight of them, and 1024 or 512 weight rows at a time, asked for
-// together with x, which waits in LDS; a column's lanes exchange halves of their sums until each has one (four rows of 784 x 512 bf16 6.4 us; with sums of all
-// values over all lanes 10.3), and the wavefronts' sums are added in their order.  One launch, unless the contraction is split.  What bounds it: a launch and two trips to memory, one of
-// them the kernel's own (1 x 1024 x 4096 bf16 5.0 us, from memory 7.4; 8192 x 16384 54.9 us, 4.9 TB/s).
-constexpr int kFewRows = 4, kFewThreads = 1024;
-template <typename T, int R, int C>
+// One or two rows (a single sample answered): a read of the weights.  A workgroup takes C columns, a lane eight of them, and 1024 or 512 weight rows at a time, asked
+// for together with x, which waits in LDS; a column's lanes exchange halves of their sums until each has one, and the wavefronts' sums are added in their order
+// (1 x 784 x 512 bf16 4.9 us; with sums of all values over all lanes, and weights asked for behind x, 5.6).  One launch, unless the contraction is split.  What bounds
+// it: a launch and two trips to memory, one of them the kernel's own (1 x 1024 x 4096 bf16 5.0 us, from memory 7.4; 8192 x 16384 54.9 us, 4.9 TB/s).
+constexpr int kFewRows = 2, kFewThreads = 1024;
+template <typename T, int C>
 __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
-  constexpr int E = Elem<T>::kPer16, kVecs = 8 / E;        // loads of eight columns
+  constexpr int R = kFewRows, E = Elem<T>::kPer16, kVecs = 8 / E;        // kVecs: loads of eight columns
   constexpr int kLanes = C / 8, kApart = kFewThreads / kLanes, U = 8 / kVecs, kFewStep = U * kApart;
   __shared__ float xs[R][kFewStep], part[16][R][C];
   const int t = threadIdx.x, lane = t & 63, cg = t % kLanes, kl = t / kLanes, n0 = blockIdx.x * C, n = n0 + cg * 8;
@@ -915,9 +915,12 @@ bool check_table(const char *name, const void *p, int64_t ld, int64_t cols, int 
 // Whether a table is too small for a read of 16 bytes, or a tile of it too large for offsets in 32 bits.
 bool no_tiles(int64_t rows, int64_t ld, int64_t cols, size_t elem) { return ((rows - 1) * ld + cols) * (int64_t)elem < 16 || 64 * ld * (int64_t)elem >= (int64_t)1 << 32; }
 
-// Columns of a workgroup that answers a few rows: a line of memory of bf16 weights (half a line each from two: 4096 x 4096 17 us, not 11); of float32 ones a line,
-// for twice the workgroups, or two lines where that leaves one for every CU (4096 x 1024, single row, from memory 28 us with 32 columns and 36 with 64; 8192 x 16384 127 and 104).
-int few_columns(size_t elem, int64_t out) { return elem == 2 || out >= 64 * kCUs ? 64 : 32; }
+// Rows and outputs that are a read of the weights; more rows cost little or no more as 32 x 32 tiles (4 x 1024 x 4096 bf16 7.4 us as rows, 6.0 as tiles, from memory 9.8 and 7.9; float32 8.5 and 10.8, 13.4 and 13.3), and
+// more outputs would make a second workgroup for some CUs (1 x 4096 x 50000 bf16 118 us as rows, 91 as tiles; float32 186 and 157).
+bool few_rows(int64_t rows, int64_t out) { return rows <= kFewRows && out <= 64 * kCUs; }
+// Columns of a workgroup there: a line of memory of bf16 weights (half a line each from two: 4096 x 4096 17 us, not 11); of float32 ones a line, for twice the workgroups, or
+// two lines where that fills the CUs (single row from memory: 4096 x 1024 28 us with 32 columns and 36 with 64, 8192 x 16384 127 and 104).
+int few_columns(size_t elem, int64_t out) { return elem == 2 || out > 32 * kCUs ? 64 : 32; }
 // Their contraction is split where CUs would stand idle and a workgroup have more than two reads of memory one after the other: a join costs 3 us, 1024 rows of weights 4 where they
 // come from memory (single row, bf16, from memory: 4096 x 1024 19.5 -> 11.2 us, 3000 x 1000 17.0 -> 11.5, 16384 x 4096 71 -> 32; 2048 x 2048 11.8 -> 11.1, and within L2 7.0 -> 8.7).
 Cut cut_few(size_t elem, int64_t in, int64_t out) {
@@ -930,7 +933,7 @@ struct ForwardPlan { bool few, by_element, direct, pack_x, pack_w; Cut cut; size
 ForwardPlan plan_forward(const cada_linear *a) {
   ForwardPlan f{};
   if (a->rows == 0) return f;
-  f.few = a->rows <= kFewRows;
+  f.few = few_rows(a->rows, a->out);
   const size_t elem = type_bytes(a->type);
   f.cut = f.few ? cut_few(elem, a->in, a->out) : Cut{64, 1, a->in};
   f.by_element = no_tiles(a->rows, a->ldx, a->in, elem) || no_tiles(a->in, a->ldw, a->out, elem);
@@ -984,13 +987,6 @@ int launch_join(Join &j, hipStream_t st) {
   return ops_launched("linear join");
 }
 
-template <typename T, int C>
-void launch_few(const Product &p, hipStream_t st) {
-  const dim3 grid((unsigned)ceil_div(p.N, C), p.splits);
-  if (p.M <= 2) k_few_rows<T, 2, C><<<grid, kFewThreads, 0, st>>>(p);
-  else k_few_rows<T, 4, C><<<grid, kFewThreads, 0, st>>>(p);
-}
-
 template <typename T>
 int forward(const cada_linear *a, const ForwardPlan &f) {
   hipStream_t st = static_cast<hipStream_t>(a->stream);
@@ -1011,8 +1007,10 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
   }
   p.epi = Epilogue{a->bias, a->residual, a->pre, a->y, a->ldr, a->ldpre, a->ldy, a->act};
   if (f.few) {
-    if (few_columns(sizeof(T), a->out) == 64) launch_few<T, 64>(p, st);
-    else if constexpr (sizeof(T) == 4) launch_few<T, 32>(p, st);
+    const int columns = few_columns(sizeof(T), a->out);
+    const dim3 grid((unsigned)ceil_div(a->out, columns), p.splits);
+    if (columns == 64) k_few_rows<T, 64><<<grid, kFewThreads, 0, st>>>(p);
+    else if constexpr (sizeof(T) == 4) k_few_rows<T, 32><<<grid, kFewThreads, 0, st>>>(p);
   } else if (f.by_element) {
     k_by_element<T, true, false, NO_SIGNAL><<<many(a->rows * a->out), 256, 0, st>>>(p);
   } else if (f.cut.tile == 32) {
