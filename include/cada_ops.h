@@ -19,7 +19,8 @@
  *     not; a captured cada_adamw_step repeats its t and lr).
  *   - Tables have rows of contiguous elements, ld... elements apart (ld >= the row's length).
  *     Element alignment is enough; rows that start on 16-byte boundaries and have a multiple of 16
- *     bytes are faster.  Outputs overlap no operand except where it says so.
+ *     bytes are faster.  Outputs share memory with no operand except where it says so (CADA_EINVAL;
+ *     columns side by side in one wider table are apart), and the workspace with neither.
  *   - Sums, statistics and moments are formed in float32 or more; values are rounded to nearest
  *     even where they are written as bf16.
  *   - Results do not depend on timing: the same call on the same operands gives the same bits.

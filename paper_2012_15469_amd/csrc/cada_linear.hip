@@ -1186,6 +1186,17 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
 
 }  // namespace
 
+bool ops_apart(const Span &out, const Span &other, size_t elem) {
+  if (!out.at || !other.at) return true;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(out.at), b = reinterpret_cast<uintptr_t>(other.at);
+  if (a + ((out.rows - 1) * out.ld + out.cols) * elem <= b || b + ((other.rows - 1) * other.ld + other.cols) * elem <= a) return true;
+  if (out.rows > 1 && other.rows > 1 && out.ld == other.ld) {
+    const int64_t row = out.ld * (int64_t)elem, between = ((int64_t)(b - a) % row + row) % row;      // bytes from out's column to the other's in a row of both
+    if (between >= out.cols * (int64_t)elem && between + other.cols * (int64_t)elem <= row) return true;
+  }
+  set_error("%s and %s share memory", out.name, other.name);
+  return false;
+}
 int ops_check_workspace(const void *ws, size_t given, size_t need) {
   if (need == 0) return CADA_OK;
   if (!ws) { set_error("workspace is NULL"); return CADA_EWORKSPACE; }
@@ -1223,6 +1234,13 @@ int cada_linear_forward(const cada_linear *a) {
   if (a->pre && !check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
   const ForwardPlan f = plan_forward(a);
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, f.bytes)) return rc;
+  const size_t elem = type_bytes(a->type);
+  const Span y{"y", a->y, a->rows, a->ldy, a->out}, pre{"pre", a->pre, a->rows, a->ldpre, a->out}, residual{"residual", a->residual, a->rows, a->ldr, a->out};
+  const Span ins[] = {{"x", a->x, a->rows, a->ldx, a->in}, {"w", a->w, a->in, a->ldw, a->out}, {"bias", a->bias, 1, a->out, a->out}};
+  for (const Span &in : ins)
+    if (!ops_apart(y, in, elem) || !ops_apart(pre, in, elem)) return CADA_EINVAL;
+  const bool in_place = a->residual == a->y && (a->ldr == a->ldy || a->rows == 1);
+  if (!ops_apart(y, pre, elem) || !ops_apart(pre, residual, elem) || (!in_place && !ops_apart(y, residual, elem))) return CADA_EINVAL;
   return a->type == CADA_BF16 ? forward<bf16>(a, f) : forward<float>(a, f);
 }
 
@@ -1246,6 +1264,16 @@ int cada_linear_backward(const cada_linear_grad *a) {
   if (a->db && !check_table("db", a->db, a->out, a->out, a->type)) return CADA_EINVAL;
   const BackwardPlan b = plan_backward(a);
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, b.bytes)) return rc;
+  const size_t elem = type_bytes(a->type);
+  const Span outs[] = {{"dx", a->rows ? a->dx : nullptr, a->rows, a->lddx, a->in}, {"dw", a->dw, a->in, a->lddw, a->out}, {"db", a->db, 1, a->out, a->out}};
+  const Span ins[] = {{"dy", a->dy, a->rows, a->lddy, a->out}, {"x", a->dw ? a->x : nullptr, a->rows, a->ldx, a->in}, {"w", a->dx ? a->w : nullptr, a->in, a->ldw, a->out},
+                      {"pre", a->act != CADA_ACT_NONE ? a->pre : nullptr, a->rows, a->ldpre, a->out}};
+  for (int i = 0; i < 3; ++i) {
+    for (const Span &in : ins)
+      if (a->rows && !ops_apart(outs[i], in, elem)) return CADA_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (!ops_apart(outs[i], outs[j], elem)) return CADA_EINVAL;
+  }
   return a->type == CADA_BF16 ? backward<bf16>(a, b) : backward<float>(a, b);
 }
 

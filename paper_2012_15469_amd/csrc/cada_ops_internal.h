@@ -126,6 +126,9 @@ inline size_t ops_align(size_t x) { return (x + kOpsAlign - 1) / kOpsAlign * kOp
 inline size_t type_bytes(int type) { return type == CADA_BF16 ? 2 : 4; }
 inline bool aligned16(const void *p, int64_t ld, size_t elem) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * (int64_t)elem) % 16 == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Whether an output shares no memory with another table, which an error names otherwise.  Columns side by side of one wider table (one row length) are apart.
+struct Span { const char *name; const void *at; int64_t rows, ld, cols; };
+bool ops_apart(const Span &out, const Span &other, size_t elem);      // cada_linear.hip
 int ops_check_workspace(const void *ws, size_t given, size_t need);      // cada_linear.hip
 int ops_launched(const char *what);
 

@@ -184,7 +184,7 @@ class AdamW:
         self.t = t
 
     def moments(self) -> Tuple[torch.Tensor, torch.Tensor]:
-        """(m, v) as float32 values, laid out as ``offsets`` says: the moments themselves with 32 bits, decoded copies with 8."""
+        """(m, v) as float32 values, laid out as ``offsets`` says: the moments themselves with 32 bits, decoded copies with 8; ready on the plan's stream."""
         if self.state_bits == 32:
             return self.m, self.v
         if torch._C._cuda_getCurrentRawStream(self.device.index) != self.stream.cuda_stream:

@@ -242,3 +242,31 @@ def test_few_rows(shape, dtype):
         bound = (k + 8) * U * (x.double().abs() @ w.double().abs() + b.double().abs())
         close(pre, z, bound, dtype)
         close(y, act64(z, act) + r.double(), bound + U * r.double().abs(), dtype)
+
+
+def test_columns_of_one_table():
+    """Operands and outputs that lie side by side in the rows of one wider table share no memory."""
+    gen = torch.Generator(device="cuda"); gen.manual_seed(5)
+    both = torch.randn(70, 96, generator=gen, device="cuda")
+    w = torch.randn(40, 56, generator=gen, device="cuda")
+    want = both[:, :40].double() @ w.double()
+    y, _ = ops.linear_forward(both[:, :40], w, out=both[:, 40:])
+    close(y, want, 48 * U * (both[:, :40].double().abs() @ w.double().abs()), "f32")
+    with pytest.raises(Exception, match="share memory"):
+        ops.linear_forward(both[:, :40], w, out=both[:, 39:95])
+
+
+@pytest.mark.parametrize("make,text", [
+    (lambda x, w: ops.linear_forward(x.double(), w), "x must be"), (lambda x, w: ops.linear_forward(x[0], w), "x must be"), (lambda x, w: ops.linear_forward(x, w.bfloat16()), "w must be"),
+    (lambda x, w: ops.linear_forward(x, w.t()), "w must be"), (lambda x, w: ops.linear_forward(x.t().contiguous().t(), w), "contiguous rows"), (lambda x, w: ops.linear_forward(x, w, w[0, :3]), "bias"),
+    (lambda x, w: ops.linear_forward(x, w, w[:, 0].repeat(9)[:9]), "bias"), (lambda x, w: ops.linear_forward(x, w, residual=x), "residual must be"), (lambda x, w: ops.linear_forward(x, w, out=x), "out must be"),
+    (lambda x, w: ops.linear_forward(x, w, act="tanh"), "act"), (lambda x, w: ops.linear_forward(x[:1].expand(4, 8), w), "overlap"), (lambda x, w: ops.linear_forward(x, w.cpu()), "w must be"),
+    (lambda x, w: ops.linear_forward(x, w, workspace=w), "workspace"), (lambda x, w: ops.linear_backward(x, x, w), "w must be"), (lambda x, w: ops.linear_backward(x @ w, x, w, act="gelu"), "needs pre"),
+    (lambda x, w: ops.linear_backward(x @ w, x[:2], w), "x must be"), (lambda x, w: ops.linear_backward(x @ w, x, w, dw=w.t()), "dw must be"), (lambda x, w: ops.linear_backward(x @ w, x, w, db=w[0, :3]), "db must be"),
+    (lambda x, w: ops.cross_entropy(x, torch.zeros(4, device="cuda")), "labels"), (lambda x, w: ops.cross_entropy(x, torch.zeros(3, device="cuda", dtype=torch.int64)), "labels"),
+    (lambda x, w: ops.cross_entropy(x, torch.zeros(4, dtype=torch.int64)), "labels"), (lambda x, w: ops.cross_entropy(x.half(), torch.zeros(4, device="cuda", dtype=torch.int64)), "logits must be"),
+    (lambda x, w: ops.AdamW([x], [x.t()]), "grad 0"), (lambda x, w: ops.AdamW([x], [w]), "shape"), (lambda x, w: ops.AdamW([x], [x.clone()], copies=[x]), "copy 0"),
+    (lambda x, w: ops.AdamW([x], [x.clone()], moments=(x, x)), "m must hold")])
+def test_tensors_that_do_not_fit(make, text):
+    with pytest.raises(ValueError, match=text):
+        make(torch.zeros(4, 8, device="cuda"), torch.zeros(8, 5, device="cuda"))

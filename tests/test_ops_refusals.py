@@ -106,3 +106,35 @@ def test_sizes_without_gpu():
 def test_tensors_that_are_not_on_a_gpu(call, text):
     with pytest.raises(ValueError, match=text):
         call(torch.zeros(4, 4))
+
+
+MB = 1 << 20
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(y=1 * MB), "y and x"), (dict(y=2 * MB), "y and w"), (dict(y=2 * MB + 8 * 32 - 2), "y and w"), (dict(bias=3 * MB + 32), "y and bias"), (dict(pre=3 * MB, ldpre=16), "y and pre"),
+    (dict(pre=1 * MB, ldpre=16), "pre and x"), (dict(residual=3 * MB + 2, ldr=16), "y and residual"), (dict(residual=3 * MB, ldr=17), "y and residual"),
+    (dict(pre=5 * MB, ldpre=16, residual=5 * MB, ldr=16), "pre and residual"), (dict(y=1 * MB + 14, ldy=24, ldx=24), "y and x"), (dict(y=1 * MB + 18, ldy=24, ldx=24), "y and x")])
+def test_linear_forward_in_place(kw, text):
+    a = linear(**{**dict(x=1 * MB, w=2 * MB, y=3 * MB), **kw})
+    assert _lib.cada_linear_forward(C.byref(a)) == -1 and text + " share memory" in cada_last_error()
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(dx=1 * MB), "dx and dy"), (dict(dw=2 * MB), "dw and x"), (dict(dw=3 * MB), "dw and w"), (dict(db=1 * MB), "db and dy"), (dict(dx=3 * MB), "dx and w"), (dict(dx=7 * MB, lddx=8), "dx and pre"),
+    (dict(dw=4 * MB), "dw and dx"), (dict(db=5 * MB + 8 * 32 - 2), "db and dw")])
+def test_linear_backward_in_place(kw, text):
+    a = cada_linear_grad()
+    a.rows, a.in_, a.out, a.type, a.act = 4, 8, 16, 1, 1
+    a.dy, a.lddy, a.x, a.ldx, a.w, a.ldw, a.dx, a.lddx, a.dw, a.lddw, a.db, a.pre, a.ldpre = 1 * MB, 16, 2 * MB, 8, 3 * MB, 16, 4 * MB, 8, 5 * MB, 16, 6 * MB, 7 * MB, 16
+    a.workspace, a.workspace_bytes = 8 * MB, 1 << 30
+    for k, v in kw.items():
+        setattr(a, k, v)
+    assert _lib.cada_linear_backward(C.byref(a)) == -1 and text + " share memory" in cada_last_error()
+
+
+def test_cross_entropy_partly_in_place():
+    a = cada_xent()
+    a.rows, a.classes, a.type, a.label_bytes, a.logits, a.ldz, a.labels, a.grad, a.ldg = 1000, 10, 0, 8, MB, 10, 2 * MB, MB + 4, 10
+    a.workspace, a.workspace_bytes = 4 * MB, 1 << 20
+    assert _lib.cada_cross_entropy(C.byref(a)) == -1 and "grad and logits share memory" in cada_last_error()
