@@ -115,7 +115,7 @@ __device__ __forceinline__ void mask(u32x4v (&reg)[BO * 8 / TH], const T *src, i
     }
   }
 }
-// The same for a whole step, whose contraction indices all exist: rows (kc) or columns (oc) beyond the table, which are the same ones in every step.
+// The same for a whole step that no piece leaves the table in: rows (kc) or columns (oc) beyond the table, which are the same ones in every step.
 template <typename T, bool KC, int BO, int TH> struct Edge {
   typedef Side<T, KC, BO, TH> S;
   uint32_t keep[KC ? S::kPieces : 4];
@@ -312,11 +312,16 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
     fetch(r.b, b + s * b_step, ob, b_end);
     if constexpr (SIGNAL != NO_SIGNAL) fetch(r.pre, pre + s * pre_step, op, pre_end);
   };
+  // Rows of a table that is read across the contraction whose pieces may pass the table's last element, where fetch takes the 16 bytes before that and only mask() shifts them to their
+  // place: the last one, and as many as a piece of a narrow table reaches over.  Tables read along the contraction meet their ends in its last step.
+  const int64_t whole_piece = SB::E;
+  const int narrowest = (int)min(min(AKC ? whole_piece : p.lda, BKC ? whole_piece : p.ldb), min(SIGNAL == B_SIGNAL ? ldpre : whole_piece, whole_piece));
+  const int64_t k_inner = p.K - (SB::E - 2 + narrowest) / narrowest;
   const Edge<T, AKC, BM, TH> a_edge(m_in, t);
   const Edge<T, BKC, BN, TH> b_edge(n_in, t);
   auto put_step = [&](Pieces &r, int s, unsigned char *dst) __attribute__((always_inline)) {
     const int k = k_in(s);
-    if (DIRECT || k0 + (int64_t)(s + 1) * BK >= p.K) {        // (the contraction's last step, which may end inside, and read up to the tables' ends)
+    if (DIRECT || k0 + (int64_t)(s + 1) * BK > k_inner) {        // (the contraction's last step, which may end inside, and steps that read up to the tables' ends)
       mask<T, AKC, BM, TH>(r.a, a + s * a_step, p.lda, a_end, m_in, k, t);
       mask<T, BKC, BN, TH>(r.b, b + s * b_step, p.ldb, b_end, n_in, k, t);
       if constexpr (SIGNAL == A_SIGNAL) mask<T, AKC, BM, TH>(r.pre, pre + s * pre_step, ldpre, pre_end, m_in, k, t);

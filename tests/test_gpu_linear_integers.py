@@ -1,0 +1,55 @@
+"""A layer's product and its gradients of small integers, which must come out exactly.
+
+Operands are -2, -1, 1 or 2 (and 0 where an activation makes it), so every product, every partial sum (below 2^24) and every bf16 operand is exact in whatever order and however
+many parts a contraction is summed; what is written is that integer, rounded once where the tables are bf16.  No tolerance: a term that is lost, doubled or taken from
+another place shows, however long the contraction."""
+import pytest
+import torch
+
+from paper_2012_15469_amd import ops
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def ints(rows, cols, dtype, gen, pad=0):
+    t = torch.randint(0, 4, (rows, cols + pad), generator=gen, device="cuda") - 2
+    return (t + (t >= 0)).to(DT[dtype])[:, :cols]
+
+
+def rounded(x, dtype):
+    return x.to(torch.float32).to(DT[dtype])        # (integers below 2^24: the first step is exact)
+
+
+def layer(rows, k, n, dtype, gen, pad=0):
+    x, w, b, r = ints(rows, k, dtype, gen, pad), ints(k, n, dtype, gen, pad), ints(1, n, dtype, gen)[0], ints(rows, n, dtype, gen, pad)
+    y, pre = ops.linear_forward(x, w, b, residual=r, act="relu", keep_pre=True)
+    z = x.double() @ w.double() + b.double()
+    assert torch.equal(pre, rounded(z, dtype)) and torch.equal(y, rounded(z.clamp(min=0) + r.double(), dtype))
+    sign = ints(rows, n, dtype, gen, pad)        # (a pre whose slopes are 0 and 1)
+    for act, p in (("none", None), ("relu", sign)):
+        dx, dw, db = ops.linear_backward(r, x, w, pre=p, act=act)
+        dz = r.double() * ((sign > 0).double() if p is not None else 1.0)
+        assert torch.equal(dx, rounded(dz @ w.double().t(), dtype))
+        assert torch.equal(dw, rounded(x.double().t().contiguous() @ dz, dtype))
+        assert torch.equal(db, rounded(dz.sum(0), dtype))
+
+
+# Rows shorter than a piece of 16 bytes, and contractions that end at, before and a few indices past a step (64 bf16, 32 float32), with one part and with several.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [1, 2, 3, 4, 5, 6, 7, 8, 9])
+def test_narrow_outputs(width, dtype):
+    gen = torch.Generator(device="cuda"); gen.manual_seed(width)
+    for k in (31, 32, 33, 34, 35, 63, 64, 65, 66, 67, 69, 70, 71, 129, 130, 134, 257, 1025, 4097, 20002):
+        for rows, pad in ((3, 0), (8, 0), (70, 0), (256, 0), (5, 1), (9, 2)):
+            layer(rows, k, width, dtype, gen, pad)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [1, 2, 3, 4, 5, 7, 8])
+def test_narrow_inputs_and_short_batches(width, dtype):
+    gen = torch.Generator(device="cuda"); gen.manual_seed(20 + width)
+    for rows in (31, 33, 34, 65, 66, 67, 69, 70, 71, 129, 134, 257, 1025, 4097, 20002):
+        for n, pad in ((40, 0), (1000, 0), (3, 0), (2, 1)):
+            layer(rows, width, n, dtype, gen, pad)
+            layer(rows, 40, width, dtype, gen, pad)
