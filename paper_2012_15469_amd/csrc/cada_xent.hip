@@ -136,11 +136,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES >= 512 ? 4 : 2) vo
     for (int i = 0; i < E; ++i) top = fmaxf(top, x[i]);
   });
   top = fmaxf(top, behind);
-  top = group_reduce<LANES>(top, part, [](float x, float y) { return fmaxf(x, y); });      // (a NaN is in the sum below)
-  // Differences to the largest first, so that a mask of the type's lowest value (or a row of nothing else) overflows nowhere.  A row with
-  // nothing left has top = -inf; its exponentials are taken against 0, so that they are 0 and not NaN.
-  const bool none = top == -kInf;
-  const float base = none ? 0.f : top, share = 1.f / (float)a.classes;
+  top = group_reduce<LANES>(top, part, [](float x, float y) { return fmaxf(x, y); });      // (a NaN, which this drops, is in the sum below)
+  // Differences to the largest first, so that a mask of the type's lowest value (or a row of nothing else) overflows nowhere.  A row of nothing but -inf and
+  // NaN has top = -inf; its exponentials are taken against 0, so that those of -inf are 0 and only a NaN makes the sum NaN.
+  const float base = top == -kInf ? 0.f : top, share = 1.f / (float)a.classes;
   constexpr bool kBallot = LANES >= 64;        // a wavefront's lanes have one row: the classes left are counted by the scalar unit
   uint32_t wave_left = 0;
   float total = 0.f, left = 0.f, mean_left = 0.f;        // mean_left: first the sum of (z - top) / classes, which cannot overflow
@@ -161,6 +160,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES >= 512 ? 4 : 2) vo
   statistics(behind);
   auto plus = [](float x, float y) { return x + y; };
   total = group_reduce<LANES>(total, part, plus);
+  const bool none = top == -kInf && total == 0.f;        // no class left
   if constexpr (SMOOTH) {
     if constexpr (kBallot) left = lane % 64 == 0 ? (float)wave_left : 0.f;
     left = group_reduce<LANES>(left, part, plus);
