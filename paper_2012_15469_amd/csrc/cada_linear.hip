@@ -1053,32 +1053,35 @@ BackwardPlan plan_backward(const cada_linear_grad *a) {
   const int64_t rows = a->rows, in = a->in, out = a->out;
   const size_t elem = type_bytes(a->type);
   const bool products = a->dx || a->dw;
-  // (dy and pre are met as operands, w in dx and x in dw)
-  b.by_element = no_tiles(rows, a->lddy, out, elem) || (a->act != CADA_ACT_NONE && no_tiles(rows, a->ldpre, out, elem)) || (a->dx && no_tiles(in, a->ldw, out, elem)) || (a->dw && no_tiles(rows, a->ldx, in, elem));
   b.dx = Cut{64, 1, out};
   b.dw = Cut{64, 1, rows};
-  if (b.by_element && (a->dw || !a->db)) return b;
-  b.by_element = false;
-  b.small = products && (a->dw || !a->db) && 4.0 * rows * in * out < kSmallGradients;
-  // dz in the workspace, unless dy itself will do
-  b.own_dz = products && !b.small && (a->act != CADA_ACT_NONE || !direct_oc(a->dy, a->lddy, out, elem));
-  const bool w_direct = !a->dx || direct_kc(a->w, a->ldw, elem), x_direct = !a->dw || direct_oc(a->x, a->ldx, in, elem);
-  b.direct = !b.small && w_direct && x_direct;
-  const Shape s[2] = {{rows, in, out}, {in, out, rows}};
-  const int n = (a->dx ? 1 : 0) + (a->dw ? 1 : 0);
-  Cut c[2], d[2];
-  if (n > 0) {
-    const Shape *first = a->dx ? s : s + 1;
-    const double time = cut(first, n, a->type, b.direct, c);
-    if (!b.small && !b.direct) {
-      const double packed = cut(first, n, a->type, true, d) + kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, out, elem));
-      if (packed < time) {
-        b.direct = true; b.pack_x = !x_direct; b.pack_w = !w_direct;
-        c[0] = d[0]; c[1] = d[1];
+  // What dx and dw read by tiles: w and x, and dy and pre, but for dx and db without dw, where the pass that sums db writes dz as well (or dy itself will do: then its rows are whole pieces).
+  const bool signal_too_small = no_tiles(rows, a->lddy, out, elem) || (a->act != CADA_ACT_NONE && no_tiles(rows, a->ldpre, out, elem)), w_too_small = a->dx && no_tiles(in, a->ldw, out, elem);
+  b.by_element = a->dw ? signal_too_small || w_too_small || no_tiles(rows, a->ldx, in, elem) : w_too_small || (a->dx && !a->db && signal_too_small);
+  if (b.by_element) {
+    if (a->dw || !a->db) return b;
+  } else {
+    b.small = products && (a->dw || !a->db) && 4.0 * rows * in * out < kSmallGradients;
+    // dz in the workspace, unless dy itself will do
+    b.own_dz = products && !b.small && (a->act != CADA_ACT_NONE || !direct_oc(a->dy, a->lddy, out, elem));
+    const bool w_direct = !a->dx || direct_kc(a->w, a->ldw, elem), x_direct = !a->dw || direct_oc(a->x, a->ldx, in, elem);
+    b.direct = !b.small && w_direct && x_direct;
+    const Shape s[2] = {{rows, in, out}, {in, out, rows}};
+    const int n = (a->dx ? 1 : 0) + (a->dw ? 1 : 0);
+    Cut c[2], d[2];
+    if (n > 0) {
+      const Shape *first = a->dx ? s : s + 1;
+      const double time = cut(first, n, a->type, b.direct, c);
+      if (!b.small && !b.direct) {
+        const double packed = cut(first, n, a->type, true, d) + kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, out, elem));
+        if (packed < time) {
+          b.direct = true; b.pack_x = !x_direct; b.pack_w = !w_direct;
+          c[0] = d[0]; c[1] = d[1];
+        }
       }
+      if (a->dx) b.dx = c[0];
+      if (a->dw) b.dw = c[n - 1];
     }
-    if (a->dx) b.dx = c[0];
-    if (a->dw) b.dw = c[n - 1];
   }
   b.lddz = ceil_div(out, 8) * 8;
   // (workgroups for every CU several times over, but no more parts of the column sums than a workgroup's rows at a time, or two, make)
@@ -1130,7 +1133,8 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   }
   char *ws = static_cast<char *>(a->workspace);
   float *db_part = reinterpret_cast<float *>(ws + b.off_db);
-  if (b.own_dz || (a->db && !b.small && !b.by_element)) {
+  const bool db_by_products = b.small || (b.by_element && a->dw);
+  if (b.own_dz || (a->db && !db_by_products)) {
     Signal s{};
     s.dy = a->dy; s.lddy = a->lddy; s.pre = a->pre; s.ldpre = a->ldpre; s.rows = a->rows; s.rows_per_block = b.rows_per_block; s.n = (int32_t)a->out; s.act = a->act; s.lanes = b.signal_lanes;
     s.dz = b.own_dz ? ws : nullptr; s.lddz = b.lddz;
@@ -1151,7 +1155,7 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
     if (b.own_dz) dw.b_cols = b.lddz;      // (dz's rows in the workspace are filled with zeros up to whole pieces)
     dw.epi.out = a->dw; dw.epi.ldo = a->lddw;
     dw.pre = a->pre; dw.ldpre = a->ldpre; dw.act = a->act;
-    if (b.small || b.by_element) { dw.db = a->db; dw.db_part = db_part; }
+    if (db_by_products) { dw.db = a->db; dw.db_part = db_part; }
   }
   if (b.pack_x || b.pack_w) {
     Packs k{};
@@ -1167,25 +1171,27 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   }
   if (a->dx || a->dw) {
     const int tile = a->dx ? b.dx.tile : b.dw.tile;
+    const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);
     if (b.by_element) {
       if (a->dx) k_by_element<T, true, true, A_SIGNAL><<<many(a->rows * a->in), 256, 0, st>>>(dx);
       if (a->dw) k_by_element<T, false, false, B_SIGNAL><<<many(a->in * a->out), 256, 0, st>>>(dw);
-      return ops_launched("linear gradients");
-    }
-    const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);
-    if (b.small && tile == 32) k_backward_small<T, 32, 1, 4><<<grid, 256, 0, st>>>(dx, dw);
-    else if (b.small) k_backward_small<T, 64, 2, 1><<<grid, 256, 0, st>>>(dx, dw);
-    else if (tile == 32) backward_tiles<T, 32, 1, 1, 4>(dx, dw, b.direct, st);
-    else if (tile == 64) backward_tiles<T, 64, 2, 2, 1>(dx, dw, b.direct, st);
-    if constexpr (sizeof(T) == 2) {
-      if (!b.small && tile == 128) backward_tiles<T, 128, 2, 4, 1>(dx, dw, b.direct, st);
-      if (!b.small && tile == 256) backward_tiles<T, 256, 2, 4, 1>(dx, dw, b.direct, st);
+    } else if (b.small && tile == 32) {
+      k_backward_small<T, 32, 1, 4><<<grid, 256, 0, st>>>(dx, dw);
+    } else if (b.small) {
+      k_backward_small<T, 64, 2, 1><<<grid, 256, 0, st>>>(dx, dw);
+    } else if (tile == 32) {
+      backward_tiles<T, 32, 1, 1, 4>(dx, dw, b.direct, st);
+    } else if (tile == 64) {
+      backward_tiles<T, 64, 2, 2, 1>(dx, dw, b.direct, st);
+    } else if constexpr (sizeof(T) == 2) {
+      if (tile == 128) backward_tiles<T, 128, 2, 4, 1>(dx, dw, b.direct, st);
+      if (tile == 256) backward_tiles<T, 256, 2, 4, 1>(dx, dw, b.direct, st);
     }
     if (int rc = ops_launched("linear gradients")) return rc;
   }
   Join j{};
   j.p[0] = dx; j.p[1] = dw;
-  if (a->db && (!b.small || b.dw.splits > 1)) { j.db_part = db_part; j.db = a->db; j.db_parts = (int)b.row_blocks; j.db_n = (int)a->out; }
+  if (a->db && (!db_by_products || b.dw.splits > 1)) { j.db_part = db_part; j.db = a->db; j.db_parts = (int)b.row_blocks; j.db_n = (int)a->out; }
   return launch_join<T>(j, st);
 }
 
