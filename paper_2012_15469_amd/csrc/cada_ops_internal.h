@@ -2,7 +2,7 @@
 #pragma once
 
 #include "cada_internal.h"
-#include "cada_ops.h"
+#include "cada_ops_sizes.h"
 
 namespace cada {
 
@@ -121,11 +121,6 @@ template <typename T> __device__ __forceinline__ float activation_slope(float z,
 }
 
 // ---- host ----
-constexpr size_t kOpsAlign = 256;
-inline size_t ops_align(size_t x) { return (x + kOpsAlign - 1) / kOpsAlign * kOpsAlign; }
-inline size_t type_bytes(int type) { return type == CADA_BF16 ? 2 : 4; }
-inline bool aligned16(const void *p, int64_t ld, size_t elem) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * (int64_t)elem) % 16 == 0; }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Whether an output shares no memory with another table, which an error names otherwise.  Columns side by side of one wider table (one row length) are apart.
 struct Span { const char *name; const void *at; int64_t rows, ld, cols; };
 bool ops_apart(const Span &out, const Span &other, size_t elem);      // cada_linear.hip
