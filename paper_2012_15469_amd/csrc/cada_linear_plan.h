@@ -30,8 +30,8 @@ constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct Shape { int64_t M, N, K; };
 constexpr int64_t kMostTiles = ((int64_t)1 << 23) - 8;        // of a product: 512 threads each, two products, less than 2^32 threads in a launch
-// The cheapest cut of one or two products in one launch (one tile for both) by that estimate, which it returns.
-inline double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
+// The cheapest cut of one or two products in one launch (one tile for both) by that estimate, which it returns; tiles up to `widest`.
+inline double cut(const Shape *s, int n, int type, bool direct, int widest, Cut *out) {
   const int64_t step = kStepBytes / (int64_t)type_bytes(type);
   const TileCost *costs = type == CADA_BF16 ? (direct ? kCostBf16 : kCostBf16Registers) : direct ? kCostF32 : kCostF32Registers;
   const int n_costs = type == CADA_BF16 && direct ? 4 : 2;
@@ -40,6 +40,7 @@ inline double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
   double best = 1e300;
   for (int c = 0; c < n_costs; ++c) {
     const TileCost &t = costs[c];
+    if (t.tile > widest) break;
     // each product's splits that may help (none that leave less than two steps, or make more tiles than two, for a product alone six, for every CU), with tiles, steps and the join's time
     struct Option { int splits; double tiles, steps, join; } opt[2][16];
     int n_opt[2] = {0, 0};
@@ -73,6 +74,8 @@ inline double cut(const Shape *s, int n, int type, bool direct, Cut *out) {
 constexpr double kPackLaunch = 4.0, kPackBytesPerUs = 3.5e6;
 inline double pack_cost(int64_t rows, int64_t cols, size_t elem) { return 2.0 * elem * (double)rows * (double)cols / kPackBytesPerUs; }
 inline int64_t packed_ld(int64_t cols) { return ceil_div(cols, 8) * 8; }
+// Tiles whose rows of a copy (or of dz) lie within offsets of 32 bits; those of up to 128 do at any width that a call may have (2^24).
+inline int widest_tile(int64_t cols, size_t elem) { return 256 * packed_ld(cols) * (int64_t)elem < (int64_t)1 << 32 ? 256 : 128; }
 inline size_t packed_bytes(int64_t rows, int64_t cols, size_t elem) { return ops_align((size_t)rows * packed_ld(cols) * elem); }
 
 inline size_t partial_bytes(const Cut &c, int64_t M, int64_t N) { return c.splits > 1 ? ops_align((size_t)c.splits * M * eights(N) * 4) : 0; }
@@ -111,10 +114,11 @@ inline ForwardPlan plan_forward(const cada_linear *a) {
   const bool x_direct = direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, a->out, elem);
   const Shape s = {a->rows, a->out, a->in};
   f.direct = x_direct && w_direct;
-  const double time = cut(&s, 1, a->type, f.direct, &f.cut);
+  const int widest = widest_tile(a->in, elem);
+  const double time = cut(&s, 1, a->type, f.direct, widest, &f.cut);
   if (!f.direct) {
     Cut c;
-    const double packed = cut(&s, 1, a->type, true, &c) + kPackLaunch + (x_direct ? 0 : pack_cost(a->rows, a->in, elem)) + (w_direct ? 0 : pack_cost(a->in, a->out, elem));
+    const double packed = cut(&s, 1, a->type, true, widest, &c) + kPackLaunch + (x_direct ? 0 : pack_cost(a->rows, a->in, elem)) + (w_direct ? 0 : pack_cost(a->in, a->out, elem));
     if (packed < time) {
       f.direct = true; f.pack_x = !x_direct; f.pack_w = !w_direct;
       f.cut = c;
@@ -162,9 +166,10 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
     Cut c[2], d[2];
     if (n > 0) {
       const Shape *first = a->dx ? s : s + 1;
-      const double time = cut(first, n, a->type, b.direct, c);
+      const int widest = a->dx ? widest_tile(out, elem) : 256;
+      const double time = cut(first, n, a->type, b.direct, widest, c);
       if (!b.small && !b.direct) {
-        const double packed = cut(first, n, a->type, true, d) + kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, out, elem));
+        const double packed = cut(first, n, a->type, true, widest, d) + kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, out, elem));
         if (packed < time) {
           b.direct = true; b.pack_x = !x_direct; b.pack_w = !w_direct;
           c[0] = d[0]; c[1] = d[1];
