@@ -1017,8 +1017,9 @@ bool ops_apart(const Span &out, const Span &other, size_t elem) {
   if (!out.at || !other.at) return true;
   const uintptr_t a = reinterpret_cast<uintptr_t>(out.at), b = reinterpret_cast<uintptr_t>(other.at);
   if (a + ((out.rows - 1) * out.ld + out.cols) * elem <= b || b + ((other.rows - 1) * other.ld + other.cols) * elem <= a) return true;
-  if (out.rows > 1 && other.rows > 1 && out.ld == other.ld) {
-    const int64_t row = out.ld * (int64_t)elem, between = ((int64_t)(b - a) % row + row) % row;      // bytes from out's column to the other's in a row of both
+  // (both lie in rows of one length: a single row in those of the other)
+  if (out.rows == 1 || other.rows == 1 || out.ld == other.ld) {
+    const int64_t row = (out.rows > 1 ? out.ld : other.ld) * (int64_t)elem, between = ((int64_t)(b - a) % row + row) % row;      // bytes from out's column to the other's in a row of both
     if (between >= out.cols * (int64_t)elem && between + other.cols * (int64_t)elem <= row) return true;
   }
   set_error("%s and %s share memory", out.name, other.name);

@@ -121,7 +121,7 @@ template <typename T> __device__ __forceinline__ float activation_slope(float z,
 }
 
 // ---- host ----
-// Whether an output shares no memory with another table, which an error names otherwise.  Columns side by side of one wider table (one row length) are apart.
+// Whether an output shares no memory with another table, which an error names otherwise.  Columns side by side of one wider table (one row length, or a single row among them) are apart.
 struct Span { const char *name; const void *at; int64_t rows, ld, cols; };
 bool ops_apart(const Span &out, const Span &other, size_t elem);      // cada_linear.hip
 int ops_check_workspace(const void *ws, size_t given, size_t need);      // cada_linear.hip
