@@ -147,7 +147,7 @@ int cada_cross_entropy(const cada_xent *a);
 enum { CADA_MOMENTS_32 = 32, CADA_MOMENTS_8 = 8 };
 #define CADA_MOMENT_BLOCK 256
 typedef struct cada_adamw_tensor {
-  void *param;          /* [n] contiguous, updated in place */
+  void *param;          /* [n] contiguous, updated in place; no tensor of a plan may be listed twice (gradients may) */
   const void *grad;     /* [n] contiguous */
   void *copy;           /* [n] bf16 or NULL: the new value rounded to bf16 (for float32 masters) */
   int64_t n;            /* >= 0 */

@@ -283,6 +283,27 @@ int check_config(const cada_adamw_config *cfg, int64_t *elements, int64_t *chunk
   return CADA_OK;
 }
 
+// Whether parameters, copies, moments, norm and workspace, which a step writes, share memory with nothing: workgroups meet them in no order.
+bool apart(const cada_adamw_config *cfg, int64_t elements, size_t workspace_bytes) {
+  std::vector<Range> r;
+  r.reserve((size_t)cfg->n_tensors * 3 + 6);
+  for (int i = 0; i < cfg->n_tensors; ++i) {
+    const cada_adamw_tensor &t = cfg->tensors[i];
+    r.push_back(Range{"param", i, t.param, (size_t)t.n * type_bytes(t.param_type), true});
+    r.push_back(Range{"grad", i, t.grad, (size_t)t.n * type_bytes(t.grad_type), false});
+    r.push_back(Range{"copy", i, t.copy, (size_t)t.n * 2, true});
+  }
+  const bool eight = cfg->moment_bits == CADA_MOMENTS_8;
+  const size_t size = (size_t)elements * (eight ? 1 : 4), scales = eight ? (size_t)elements / CADA_MOMENT_BLOCK * 4 : 0;
+  r.push_back(Range{"m", -1, cfg->m, size, true});
+  r.push_back(Range{"v", -1, cfg->v, size, true});
+  r.push_back(Range{"m_scale", -1, cfg->m_scale, scales, true});
+  r.push_back(Range{"v_scale", -1, cfg->v_scale, scales, true});
+  r.push_back(Range{"norm", -1, cfg->norm, cfg->max_norm > 0.0 ? sizeof(float) : 0, true});
+  r.push_back(Range{"workspace", -1, cfg->workspace, workspace_bytes, true});
+  return ops_apart(r.data(), r.size());
+}
+
 }  // namespace
 }  // namespace cada
 
@@ -313,6 +334,7 @@ int cada_adamw_init(const cada_adamw_config *cfg, cada_adamw **out) {
   if (int rc = ops_check_workspace(cfg->workspace, cfg->workspace_bytes, l.bytes)) return rc;
   cada_adamw *h = nullptr;
   try {
+    if (!apart(cfg, elements, l.bytes)) return CADA_EINVAL;
     h = new cada_adamw();
     Plan &p = h->p;
     p.host.resize(l.norm);

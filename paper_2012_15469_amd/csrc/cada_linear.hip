@@ -7,6 +7,7 @@
 // of LDS while the matrix instructions (32x32x16 bf16, 32x32x2 f32; float32 accumulators) take this one.
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
 
 #include "cada_linear_plan.h"
 #include "cada_ops_internal.h"
@@ -1024,6 +1025,28 @@ bool ops_apart(const Span &out, const Span &other, size_t elem) {
   }
   set_error("%s and %s share memory", out.name, other.name);
   return false;
+}
+bool ops_apart(Range *ranges, size_t n) {
+  std::sort(ranges, ranges + n, [](const Range &x, const Range &y) { return x.at != y.at ? reinterpret_cast<uintptr_t>(x.at) < reinterpret_cast<uintptr_t>(y.at) : x.index < y.index; });
+  auto end = [](const Range &r) { return reinterpret_cast<uintptr_t>(r.at) + r.bytes; };
+  const Range *last = nullptr, *last_written = nullptr;      // of those that begin no later, the ones that end last
+  for (const Range *r = ranges; r < ranges + n; ++r) {
+    if (!r->at || r->bytes == 0) continue;
+    const Range *other = r->written ? last : last_written;
+    if (other && end(*other) > reinterpret_cast<uintptr_t>(r->at)) {
+      char text[2][64];
+      for (int i = 0; i < 2; ++i) {
+        const Range &x = i == 0 ? *other : *r;
+        if (x.index >= 0) snprintf(text[i], sizeof(text[i]), "%s %d", x.name, x.index);
+        else snprintf(text[i], sizeof(text[i]), "%s", x.name);
+      }
+      set_error("%s and %s share memory", text[0], text[1]);
+      return false;
+    }
+    if (!last || end(*r) > end(*last)) last = r;
+    if (r->written && (!last_written || end(*r) > end(*last_written))) last_written = r;
+  }
+  return true;
 }
 int ops_check_workspace(const void *ws, size_t given, size_t need) {
   if (need == 0) return CADA_OK;

@@ -4,6 +4,7 @@ import ctypes as C
 import pytest
 
 from common_ops import cada_linear
+from paper_2012_15469_amd import ops
 from paper_2012_15469_amd.binding import _lib, cada_last_error
 
 MB = 1 << 20
@@ -18,3 +19,40 @@ def test_a_single_row_beside_columns(y, bias, apart):
     a.pre, a.ldpre, a.residual, a.ldr = 6 * MB, 40, 6 * MB, 40
     assert _lib.cada_linear_forward(C.byref(a)) == -1
     assert ("pre and residual" if apart else "y and bias") + " share memory" in cada_last_error()
+
+
+def adamw(n=1000, bits=32, count=3, max_norm=0.0, **kw):
+    """Three tensors whose parts lie one MB after the other; `kw` moves parts: "param2", "copy0", "m", ..."""
+    t = (ops.cada_adamw_tensor * count)()
+    for i in range(count):
+        t[i].param, t[i].grad, t[i].copy, t[i].n = MB * (10 * i + 1), MB * (10 * i + 2), MB * (10 * i + 3), n
+    cfg = ops.cada_adamw_config()
+    cfg.tensors, cfg.n_tensors, cfg.moment_bits, cfg.beta1, cfg.beta2, cfg.eps, cfg.max_norm = t, count, bits, 0.9, 0.999, 1e-8, max_norm
+    cfg.m, cfg.v, cfg.m_scale, cfg.v_scale, cfg.norm, cfg.workspace, cfg.workspace_bytes = (MB * i for i in (100, 101, 102, 103, 104, 105, 1))
+    for k, v in kw.items():
+        if k[-1].isdigit():
+            setattr(t[int(k[-1])], k[:-1], v)
+        else:
+            setattr(cfg, k, v)
+    out = C.c_void_p()
+    rc = _lib.cada_adamw_init(C.byref(cfg), C.byref(out))
+    assert rc == -1 and not out.value
+    return cada_last_error()
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(param1=1 * MB), "param 0 and param 1"), (dict(param2=1 * MB + 3996), "param 0 and param 2"), (dict(copy0=1 * MB), "0 and "), (dict(copy1=11 * MB + 3998), "param 1 and copy 1"),
+    (dict(param0=2 * MB), "0 and "), (dict(grad2=1 * MB + 4), "param 0 and grad 2"), (dict(grad0=3 * MB), "0 and "), (dict(copy2=3 * MB), "0 and copy"), (dict(m=1 * MB), " and "), (dict(v=100 * MB + 3 * 4096 - 16), "m and v"),
+    (dict(v=2 * MB + 16), "grad 0 and v"), (dict(workspace=23 * MB), " and "), (dict(norm=1 * MB + 8, max_norm=1.0), "param 0 and norm"), (dict(m_scale=100 * MB + 2048, bits=8), "m and m_scale"),
+    (dict(v_scale=102 * MB + 44, bits=8), "m_scale and v_scale")])
+def test_adamw(kw, text):
+    error = adamw(**kw)
+    assert "share memory" in error and text in error
+
+
+def test_what_a_step_only_reads_or_does_not_touch_may_be_shared():
+    """Gradients of several tensors, ends that meet, moments of 8 bits where 32 would not fit, a norm without clipping, parts of no elements: the fault that is named is the one planted last."""
+    last = dict(param2=11 * MB)
+    for kw in (dict(grad1=2 * MB, grad2=2 * MB + 4), dict(grad1=1 * MB + 4000), dict(v=100 * MB + 3 * 1024, bits=8), dict(norm=1 * MB), dict(m_scale=1 * MB, v_scale=1 * MB)):
+        assert "param 1 and param 2 share memory" in adamw(**{**kw, **last}), kw
+    assert "share memory" in adamw(n=1, param1=1 * MB)
