@@ -108,6 +108,8 @@ __device__ __forceinline__ float half_max(float x) {
   return __uint_as_float(u);
 }
 
+__device__ __forceinline__ float finite_or_nan(float x) { return x < __builtin_inff() ? x : __builtin_nanf(""); }
+
 template <int BITS>
 __global__ __launch_bounds__(256) void k_adamw(const Step a) {
 #pragma clang fp contract(off)
@@ -177,8 +179,9 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a) {
       sm = __uint_as_float(max(__float_as_uint(sm), __float_as_uint(fabsf(m[i]))));
       sv = __uint_as_float(max(__float_as_uint(sv), __float_as_uint(fabsf(r[i]))));
     }
-    sm = half_max(sm);
-    sv = half_max(sv);
+    // (a block with an infinity becomes NaN: codes of infinity are zero or infinite, and sqrt(v) would go on dividing by it)
+    sm = finite_or_nan(half_max(sm));
+    sv = finite_or_nan(half_max(sv));
     const float im = sm >= kScaleMin ? kMomentMax / sm : 0.f, iv = sv >= kScaleMin ? kRootMax / sv : 0.f;
     uint64_t qm = 0, qv = 0;
 #pragma unroll
