@@ -164,6 +164,10 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a) {
     r[i] = sqrtf(v[i]);
     p[i] = (p[i] - p[i] * decay) - (m[i] * a.step_size) / (r[i] * a.root + a.eps);
   }
+  if (left < 8) {        // (the fill's gradients are zero, but a factor that is not finite would make them NaN)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i >= left) m[i] = v[i] = r[i] = 0.f;
+  }
   if (t.types & 1) store8_n(static_cast<bf16 *>(t.param) + e, left, p); else store8_n(static_cast<float *>(t.param) + e, left, p);
   if (t.copy) store8_n(reinterpret_cast<bf16 *>(t.copy) + e, left, p);
   if constexpr (BITS == 32) {
