@@ -1014,14 +1014,14 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
 
 }  // namespace
 
-bool ops_apart(const Span &out, const Span &other, size_t elem) {
+bool ops_apart(const Span &out, const Span &other) {
   if (!out.at || !other.at) return true;
   const uintptr_t a = reinterpret_cast<uintptr_t>(out.at), b = reinterpret_cast<uintptr_t>(other.at);
-  if (a + ((out.rows - 1) * out.ld + out.cols) * elem <= b || b + ((other.rows - 1) * other.ld + other.cols) * elem <= a) return true;
+  if (a + ((out.rows - 1) * out.ld + out.cols) <= b || b + ((other.rows - 1) * other.ld + other.cols) <= a) return true;
   // (both lie in rows of one length: a single row in those of the other)
   if (out.rows == 1 || other.rows == 1 || out.ld == other.ld) {
-    const int64_t row = (out.rows > 1 ? out.ld : other.ld) * (int64_t)elem, between = ((int64_t)(b - a) % row + row) % row;      // bytes from out's column to the other's in a row of both
-    if (between >= out.cols * (int64_t)elem && between + other.cols * (int64_t)elem <= row) return true;
+    const int64_t row = out.rows > 1 ? out.ld : other.ld, between = ((int64_t)(b - a) % row + row) % row;      // from out's column to the other's in a row of both
+    if (between >= out.cols && between + other.cols <= row) return true;
   }
   set_error("%s and %s share memory", out.name, other.name);
   return false;
@@ -1086,12 +1086,12 @@ int cada_linear_forward(const cada_linear *a) {
   const ForwardPlan f = plan_forward(a);
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, f.bytes)) return rc;
   const size_t elem = type_bytes(a->type);
-  const Span y{"y", a->y, a->rows, a->ldy, a->out}, pre{"pre", a->pre, a->rows, a->ldpre, a->out}, residual{"residual", a->residual, a->rows, a->ldr, a->out};
-  const Span ins[] = {{"x", a->x, a->rows, a->ldx, a->in}, {"w", a->w, a->in, a->ldw, a->out}, {"bias", a->bias, 1, a->out, a->out}};
+  const Span y = span("y", a->y, a->rows, a->ldy, a->out, elem), pre = span("pre", a->pre, a->rows, a->ldpre, a->out, elem), residual = span("residual", a->residual, a->rows, a->ldr, a->out, elem);
+  const Span ins[] = {span("x", a->x, a->rows, a->ldx, a->in, elem), span("w", a->w, a->in, a->ldw, a->out, elem), span("bias", a->bias, 1, a->out, a->out, elem)};
   for (const Span &in : ins)
-    if (!ops_apart(y, in, elem) || !ops_apart(pre, in, elem)) return CADA_EINVAL;
+    if (!ops_apart(y, in) || !ops_apart(pre, in)) return CADA_EINVAL;
   const bool in_place = a->residual == a->y && (a->ldr == a->ldy || a->rows == 1);
-  if (!ops_apart(y, pre, elem) || !ops_apart(pre, residual, elem) || (!in_place && !ops_apart(y, residual, elem))) return CADA_EINVAL;
+  if (!ops_apart(y, pre) || !ops_apart(pre, residual) || (!in_place && !ops_apart(y, residual))) return CADA_EINVAL;
   return a->type == CADA_BF16 ? forward<bf16>(a, f) : forward<float>(a, f);
 }
 
@@ -1116,14 +1116,14 @@ int cada_linear_backward(const cada_linear_grad *a) {
   const BackwardPlan b = plan_backward(a);
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, b.bytes)) return rc;
   const size_t elem = type_bytes(a->type);
-  const Span outs[] = {{"dx", a->rows ? a->dx : nullptr, a->rows, a->lddx, a->in}, {"dw", a->dw, a->in, a->lddw, a->out}, {"db", a->db, 1, a->out, a->out}};
-  const Span ins[] = {{"dy", a->dy, a->rows, a->lddy, a->out}, {"x", a->dw ? a->x : nullptr, a->rows, a->ldx, a->in}, {"w", a->dx ? a->w : nullptr, a->in, a->ldw, a->out},
-                      {"pre", a->act != CADA_ACT_NONE ? a->pre : nullptr, a->rows, a->ldpre, a->out}};
+  const Span outs[] = {span("dx", a->rows ? a->dx : nullptr, a->rows, a->lddx, a->in, elem), span("dw", a->dw, a->in, a->lddw, a->out, elem), span("db", a->db, 1, a->out, a->out, elem)};
+  const Span ins[] = {span("dy", a->dy, a->rows, a->lddy, a->out, elem), span("x", a->dw ? a->x : nullptr, a->rows, a->ldx, a->in, elem), span("w", a->dx ? a->w : nullptr, a->in, a->ldw, a->out, elem),
+                      span("pre", a->act != CADA_ACT_NONE ? a->pre : nullptr, a->rows, a->ldpre, a->out, elem)};
   for (int i = 0; i < 3; ++i) {
     for (const Span &in : ins)
-      if (a->rows && !ops_apart(outs[i], in, elem)) return CADA_EINVAL;
+      if (a->rows && !ops_apart(outs[i], in)) return CADA_EINVAL;
     for (int j = 0; j < i; ++j)
-      if (!ops_apart(outs[i], outs[j], elem)) return CADA_EINVAL;
+      if (!ops_apart(outs[i], outs[j])) return CADA_EINVAL;
   }
   return a->type == CADA_BF16 ? backward<bf16>(a, b) : backward<float>(a, b);
 }

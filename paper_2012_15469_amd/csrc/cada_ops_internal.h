@@ -122,8 +122,10 @@ template <typename T> __device__ __forceinline__ float activation_slope(float z,
 
 // ---- host ----
 // Whether an output shares no memory with another table, which an error names otherwise.  Columns side by side of one wider table (one row length, or a single row among them) are apart.
-struct Span { const char *name; const void *at; int64_t rows, ld, cols; };
-bool ops_apart(const Span &out, const Span &other, size_t elem);      // cada_linear.hip
+struct Span { const char *name; const void *at; int64_t rows, ld, cols; };      // (in bytes)
+inline Span span(const char *name, const void *at, int64_t rows, int64_t ld, int64_t cols, size_t elem) { return Span{name, at, rows, ld * (int64_t)elem, cols * (int64_t)elem}; }
+inline Span span(const char *name, const void *at, size_t bytes) { return Span{name, bytes > 0 ? at : nullptr, 1, (int64_t)bytes, (int64_t)bytes}; }
+bool ops_apart(const Span &out, const Span &other);      // cada_linear.hip
 // The same of any number of ranges of memory: no written one shares memory with another.  `index`: which tensor of a list, or -1.
 struct Range { const char *name; int index; const void *at; size_t bytes; bool written; };
 bool ops_apart(Range *ranges, size_t n);      // cada_linear.hip (puts them in order; none may throw)

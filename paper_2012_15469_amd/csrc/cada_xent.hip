@@ -289,7 +289,16 @@ int cada_cross_entropy(const cada_xent *a) {
   const int lanes = lanes_for(a->classes, 16 / (int)type_bytes(a->type));
   if (ceil_div(a->rows, rows_together(lanes)) * std::max(lanes, 256) >= (int64_t)1 << 32) { set_error("%lld rows of %lld classes are more than one launch takes", (long long)a->rows, (long long)a->classes); return CADA_EINVAL; }
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, workspace(a))) return rc;
-  if (a->rows > 0 && a->grad != a->logits && !ops_apart(Span{"grad", a->grad, a->rows, a->ldg, a->classes}, Span{"logits", a->logits, a->rows, a->ldz, a->classes}, type_bytes(a->type))) return CADA_EINVAL;
+  const size_t elem = type_bytes(a->type);
+  const bool any = a->rows > 0;
+  const Span logits = span("logits", any ? a->logits : nullptr, a->rows, a->ldz, a->classes, elem), labels = span("labels", a->labels, (size_t)a->rows * a->label_bytes);
+  const Span outs[] = {span("grad", any ? a->grad : nullptr, a->rows, a->ldg, a->classes, elem), span("loss", a->loss, (size_t)a->rows * sizeof(float)), span("mean", a->mean, sizeof(float)),
+                       span("workspace", a->workspace, workspace(a))};
+  for (int i = 0; i < 4; ++i) {
+    if ((!(i == 0 && a->grad == a->logits) && !ops_apart(outs[i], logits)) || !ops_apart(outs[i], labels)) return CADA_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (!ops_apart(outs[i], outs[j])) return CADA_EINVAL;
+  }
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   Head *head = static_cast<Head *>(a->workspace);
   Xent x{};

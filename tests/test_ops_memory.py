@@ -3,7 +3,7 @@ import ctypes as C
 
 import pytest
 
-from common_ops import cada_linear
+from common_ops import cada_linear, cada_xent
 from paper_2012_15469_amd import ops
 from paper_2012_15469_amd.binding import _lib, cada_last_error
 
@@ -56,3 +56,17 @@ def test_what_a_step_only_reads_or_does_not_touch_may_be_shared():
     for kw in (dict(grad1=2 * MB, grad2=2 * MB + 4), dict(grad1=1 * MB + 4000), dict(v=100 * MB + 3 * 1024, bits=8), dict(norm=1 * MB), dict(m_scale=1 * MB, v_scale=1 * MB)):
         assert "param 1 and param 2 share memory" in adamw(**{**kw, **last}), kw
     assert "share memory" in adamw(n=1, param1=1 * MB)
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(loss=1 * MB + 39996), "loss and logits"), (dict(mean=1 * MB), "mean and logits"), (dict(workspace=1 * MB - 256), "workspace and logits"), (dict(grad=2 * MB - 40000 + 4), "grad and labels"),
+    (dict(loss=2 * MB), "loss and labels"), (dict(mean=2 * MB + 7996), "mean and labels"), (dict(loss=5 * MB), "loss and grad"), (dict(mean=6 * MB + 3996), "mean and loss"),
+    (dict(mean=5 * MB + 16), "mean and grad"), (dict(workspace=2 * MB), "workspace and labels"), (dict(workspace=5 * MB), "workspace and grad"), (dict(workspace=6 * MB), "workspace and loss"),
+    (dict(mean=8 * MB + 64), "workspace and mean"), (dict(loss=1 * MB + 40, ldz=10 + 999), "loss and logits"), (dict(labels=1 * MB, grad=1 * MB), "grad and labels"), (dict(rows=0, mean=8 * MB), "workspace and mean")])
+def test_cross_entropy(kw, text):
+    a = cada_xent()
+    a.rows, a.classes, a.type, a.label_bytes, a.logits, a.ldz, a.labels, a.grad, a.ldg = 1000, 10, 0, 8, MB, 10, 2 * MB, 5 * MB, 10
+    a.loss, a.mean, a.workspace, a.workspace_bytes = 6 * MB, 7 * MB, 8 * MB, 1 << 20
+    for k, v in kw.items():
+        setattr(a, k, v)
+    assert _lib.cada_cross_entropy(C.byref(a)) == -1 and text + " share memory" in cada_last_error()
