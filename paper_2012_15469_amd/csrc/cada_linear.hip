@@ -1092,6 +1092,9 @@ int cada_linear_forward(const cada_linear *a) {
     if (!ops_apart(y, in) || !ops_apart(pre, in)) return CADA_EINVAL;
   const bool in_place = a->residual == a->y && (a->ldr == a->ldy || a->rows == 1);
   if (!ops_apart(y, pre) || !ops_apart(pre, residual) || (!in_place && !ops_apart(y, residual))) return CADA_EINVAL;
+  const Span workspace = span("workspace", a->workspace, f.bytes);
+  for (const Span &other : {ins[0], ins[1], ins[2], y, pre, residual})
+    if (!ops_apart(workspace, other)) return CADA_EINVAL;
   return a->type == CADA_BF16 ? forward<bf16>(a, f) : forward<float>(a, f);
 }
 
@@ -1125,6 +1128,9 @@ int cada_linear_backward(const cada_linear_grad *a) {
     for (int j = 0; j < i; ++j)
       if (!ops_apart(outs[i], outs[j])) return CADA_EINVAL;
   }
+  const Span workspace = span("workspace", a->workspace, b.bytes);        // (none without rows)
+  for (const Span &other : {ins[0], ins[1], ins[2], ins[3], outs[0], outs[1], outs[2]})
+    if (!ops_apart(workspace, other)) return CADA_EINVAL;
   return a->type == CADA_BF16 ? backward<bf16>(a, b) : backward<float>(a, b);
 }
 

@@ -3,7 +3,7 @@ import ctypes as C
 
 import pytest
 
-from common_ops import cada_linear, cada_xent
+from common_ops import cada_linear, cada_linear_grad, cada_xent
 from paper_2012_15469_amd import ops
 from paper_2012_15469_amd.binding import _lib, cada_last_error
 
@@ -70,3 +70,28 @@ def test_cross_entropy(kw, text):
     for k, v in kw.items():
         setattr(a, k, v)
     assert _lib.cada_cross_entropy(C.byref(a)) == -1 and text + " share memory" in cada_last_error()
+
+
+@pytest.mark.parametrize("part,cols", [("x", 4096), ("w", 10), ("bias", 10), ("y", 10), ("pre", 10), ("residual", 10)])
+def test_workspace_of_a_layer(part, cols):
+    """A long contraction, whose parts lie in the workspace."""
+    a = cada_linear()
+    a.rows, a.in_, a.out, a.type, a.act = 64, 4096, 10, 0, 0
+    a.x, a.ldx, a.w, a.ldw, a.bias, a.y, a.ldy, a.pre, a.ldpre, a.residual, a.ldr = 10 * MB, 4096, 20 * MB, 10, 30 * MB, 40 * MB, 10, 50 * MB, 10, 60 * MB, 10
+    a.workspace = 70 * MB
+    assert _lib.cada_linear_forward_workspace(C.byref(a)) == 0 and 256 < a.workspace_bytes < MB
+    setattr(a, part, a.workspace + a.workspace_bytes - 256)
+    assert _lib.cada_linear_forward(C.byref(a)) == -1 and "workspace and %s share memory" % part in cada_last_error()
+
+
+@pytest.mark.parametrize("part", ["dy", "x", "w", "pre", "dx", "dw", "db"])
+def test_workspace_of_a_layers_gradients(part):
+    a = cada_linear_grad()
+    a.rows, a.in_, a.out, a.type, a.act = 512, 512, 512, 1, 1
+    for i, name in enumerate(("dy", "x", "w", "pre", "dx", "dw")):
+        setattr(a, name, 10 * (i + 1) * MB)
+        setattr(a, "ld" + name, 512)
+    a.db, a.workspace = 80 * MB, 90 * MB
+    assert _lib.cada_linear_backward_workspace(C.byref(a)) == 0 and 512 * 512 * 2 < a.workspace_bytes < 10 * MB
+    setattr(a, part, a.workspace + 1024)
+    assert _lib.cada_linear_backward(C.byref(a)) == -1 and "workspace and %s share memory" % part in cada_last_error()
