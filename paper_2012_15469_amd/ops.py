@@ -187,8 +187,8 @@ class AdamW:
         """(m, v) as float32 values, laid out as ``offsets`` says: the moments themselves with 32 bits, decoded copies with 8; ready on the plan's stream."""
         if self.state_bits == 32:
             return self.m, self.v
-        if torch._C._cuda_getCurrentRawStream(self.device.index) != self.stream.cuda_stream:
-            with torch.cuda.stream(self.stream):          # (so that what is allocated belongs to it)
+        if self.device.index != torch._C._cuda_getDevice() or torch._C._cuda_getCurrentRawStream(self.device.index) != self.stream.cuda_stream:
+            with torch.cuda.stream(self.stream):          # (its device too; so that what is allocated belongs to it)
                 return self.moments()
         m, v = (torch.empty_like(self.m[0], dtype=torch.float32) for _ in range(2))
         _check(_lib.cada_adamw_moments(self.plan, m.data_ptr(), v.data_ptr()))
