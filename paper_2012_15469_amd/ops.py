@@ -60,6 +60,7 @@ def _call(call, tensor, stream, *args):
     if index < 0:
         return call(*args, 0)          # (refused there)
     if stream is not None:
+        _need(stream.device.index == index, "stream must be one of cuda:%d's" % index)
         with torch.cuda.stream(stream):          # (so that what is allocated belongs to it)
             return call(*args, stream.cuda_stream)
     handle = torch._C._cuda_getCurrentRawStream(index)
@@ -127,6 +128,7 @@ class AdamW:
         self.params, self.grads, self.copies = list(params), list(grads), list(copies) if copies is not None else [None] * n
         self.lr, self.t, self.state_bits = lr, 0, state_bits
         self.stream = stream or torch.cuda.current_stream(dev)
+        _need(self.stream.device == dev, "stream must be one of %s's" % dev)
         tensors = (cada_adamw_tensor * n)()
         self.offsets, total = [], 0
         for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
