@@ -400,6 +400,10 @@ int cada_adamw_moments(cada_adamw *plan, float *m, float *v) {
   if (!plan) { set_error("plan is NULL"); return CADA_EINVAL; }
   const Plan &p = plan->p;
   if (p.elements == 0 || (!m && !v)) return CADA_OK;
+  const size_t values = (size_t)p.elements * sizeof(float), held = p.bits == 32 ? values : (size_t)p.elements, scales = p.bits == 32 ? 0 : values / CADA_MOMENT_BLOCK;
+  Range r[] = {{"the values of m", -1, m, values, true}, {"the values of v", -1, v, values, true}, {"m", -1, p.step.m, held, false}, {"v", -1, p.step.v, held, false},
+               {"m_scale", -1, p.step.m_scale, scales, false}, {"v_scale", -1, p.step.v_scale, scales, false}, {"workspace", -1, p.step.tensors, p.host.size(), false}};
+  if (!ops_apart(r, sizeof(r) / sizeof(r[0]))) return CADA_EINVAL;
   const unsigned grid = (unsigned)ceil_div(p.elements, 2048);
   if (p.bits == 32) k_moments<32><<<grid, 256, 0, p.stream>>>(p.step.m, p.step.v, nullptr, nullptr, m, v, p.elements);
   else k_moments<8><<<grid, 256, 0, p.stream>>>(p.step.m, p.step.v, p.step.m_scale, p.step.v_scale, m, v, p.elements);
