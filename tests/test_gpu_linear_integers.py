@@ -53,3 +53,25 @@ def test_narrow_inputs_and_short_batches(width, dtype):
         for n, pad in ((40, 0), (1000, 0), (3, 0), (2, 1)):
             layer(rows, width, n, dtype, gen, pad)
             layer(rows, 40, width, dtype, gen, pad)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 20011, 129), (2, 2050, 16390), (1, 4096, 1024), (3, 5001, 1003), (4, 40, 16640), (5, 8200, 10), (520, 2050, 640), (300, 4100, 520),
+                                   (4097, 136, 24), (3001, 1001, 1003), (4100, 1032, 1032), (2056, 520, 2056), (8200, 2056, 4104)], ids=str)
+def test_long_contractions(shape, dtype):
+    gen = torch.Generator(device="cuda"); gen.manual_seed(sum(shape))
+    layer(*shape, dtype, gen)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("need", [(True, False, False), (False, True, False), (True, False, True), (False, True, True), (True, True, False)], ids=str)
+def test_some_of_the_gradients(need, dtype):
+    """The contractions are cut otherwise where not all are wanted."""
+    gen = torch.Generator(device="cuda"); gen.manual_seed(sum(need))
+    for rows, k, n in ((66, 65, 3), (70, 2, 130), (520, 2050, 640), (4097, 136, 24), (20002, 40, 8), (300, 4100, 520)):
+        x, w, dy, pre = ints(rows, k, dtype, gen), ints(k, n, dtype, gen), ints(rows, n, dtype, gen), ints(rows, n, dtype, gen)
+        dz = dy.double() * (pre.double() > 0)
+        want = dz @ w.double().t(), x.double().t().contiguous() @ dz, dz.sum(0)
+        got = ops.linear_backward(dy, x, w, pre=pre, act="relu", need_dx=need[0], need_dw=need[1], need_db=need[2])
+        for wanted, g, v in zip(need, got, want):
+            assert torch.equal(g, rounded(v, dtype)) if wanted else g is None
