@@ -61,12 +61,39 @@ def build_ops_binding() -> str:
     return OPS_BINDING
 
 
+def ops_binding_lacks() -> str:
+    """What the operators' Python module needs and is not here (torch with its C++ headers, Python's headers, a host compiler), or an empty text."""
+    import shutil
+    import sysconfig
+    try:
+        from torch.utils.cpp_extension import include_paths
+    except ImportError:
+        return "torch"
+    if not any(os.path.exists(os.path.join(p, "ATen", "ATen.h")) for p in include_paths()):
+        return "torch's C++ headers"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python's headers"
+    cxx = os.environ.get("CXX", "g++")
+    return "" if shutil.which(cxx.split()[0]) else "a host compiler (%s)" % cxx
+
+
 def build_all() -> None:
     build_libcada()
     build_ops_binding()
 
 
-if __name__ == "__main__":
-    build_all()
+def main() -> int:
+    """libcada.so, which the C ABI is all of, and the operators' Python module where what that needs is here."""
+    build_libcada()
     print("built", LIBCADA)
-    sys.exit(0)
+    lacks = ops_binding_lacks()
+    if lacks:
+        print("not built: %s, which needs %s (the C ABI does not need it)" % (OPS_BINDING, lacks), file=sys.stderr)
+    else:
+        build_ops_binding()
+        print("built", OPS_BINDING)
+    return 0
+
+
+if __name__ == "__main__":
+    sys.exit(main())
