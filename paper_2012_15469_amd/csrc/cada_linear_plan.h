@@ -150,9 +150,11 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
   const bool products = a->dx || a->dw;
   b.dx = Cut{64, 1, out};
   b.dw = Cut{64, 1, rows};
+  b.lddz = ceil_div(out, 8) * 8;
   // What dx and dw read by tiles: w and x, and dy and pre, but for dx and db without dw, where the pass that sums db writes dz as well (or dy itself will do: then its rows are whole pieces).
   const bool signal_too_small = no_tiles(rows, a->lddy, out, elem) || (a->act != CADA_ACT_NONE && no_tiles(rows, a->ldpre, out, elem)), w_too_small = a->dx && no_tiles(in, a->ldw, out, elem);
-  b.by_element = a->dw ? signal_too_small || w_too_small || no_tiles(rows, a->ldx, in, elem) : w_too_small || (a->dx && !a->db && signal_too_small);
+  const bool dz_too_small = ((rows - 1) * b.lddz + out) * (int64_t)elem < 16;
+  b.by_element = a->dw ? signal_too_small || w_too_small || no_tiles(rows, a->ldx, in, elem) : w_too_small || (a->dx && (a->db ? dz_too_small : signal_too_small));
   if (b.by_element) {
     if (a->dw || !a->db) return b;
   } else {
@@ -179,7 +181,6 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
       if (a->dw) b.dw = c[n - 1];
     }
   }
-  b.lddz = ceil_div(out, 8) * 8;
   // (workgroups for every CU several times over, but no more parts of the column sums than a workgroup's rows at a time, or two, make)
   while (b.signal_lanes < 5 && (8 << b.signal_lanes) < out) ++b.signal_lanes;
   const int64_t high = 256 >> b.signal_lanes;

@@ -113,3 +113,26 @@ def test_offsets_of_rows_far_apart(plan):
         lds = [max(w, int(2 ** rng.uniform(3, 28)) // 8 * 8 + rng.choice((0, 0, 3))) for w in (k, n, n)]
         check_forward(plan, rows, k, n, dtype, ldx=lds[0], ldw=lds[1])
         check_backward(plan, rows, k, n, dtype, rng.choice((0, 1)), rng.random() < 0.7, rng.random() < 0.7, rng.random() < 0.5, ldx=lds[0], ldw=lds[1], lddy=lds[2])
+
+
+def test_every_table_that_tiles_read_holds_a_piece(plan):
+    """A load through registers takes 16 bytes and is moved back from a table's end so as to lie in it: tables of less are read element by element."""
+    rng = random.Random(2)
+    spans = lambda rows, ld, cols, elem: ((rows - 1) * ld + cols) * elem
+    for _ in range(100000):
+        dtype = rng.choice((0, 1))
+        rows, k, n = (rng.choice((1, 1, 2, 3, rng.randint(1, 9), int(2 ** rng.uniform(0, 12)))) for _ in range(3))
+        pad, shift = [rng.choice((0, 0, 1, 8)) for _ in range(3)], rng.choice((0, ELEM[dtype]))
+        lds = [w + p for w, p in zip((k, n, n), pad)]
+        elem = ELEM[dtype]
+        p, a = forward(plan, rows, k, n, dtype, ldx=lds[0], ldw=lds[1], shift=shift)
+        if not p["few"] and not p["by_element"]:
+            assert spans(rows, plan.packed(k) if p["pack_x"] else lds[0], k, elem) >= 16 and spans(k, plan.packed(n) if p["pack_w"] else lds[1], n, elem) >= 16
+        dx, dw, db = (rng.random() < 0.6 for _ in range(3))
+        p, a = backward(plan, rows, k, n, dtype, rng.choice((0, 1)), dx, dw, db, ldx=lds[0], ldw=lds[1], lddy=lds[2], shift=shift)
+        if (dx or dw) and not p["by_element"]:
+            what = (rows, k, n, dtype, dx, dw, db, lds, p)
+            assert spans(rows, p["lddz"] if p["own_dz"] else lds[2], n, elem) >= 16, what
+            assert not p["small"] or a.act == 0 or spans(rows, n, n, elem) >= 16, what          # (pre)
+            assert not dx or spans(k, plan.packed(n) if p["pack_w"] else lds[1], n, elem) >= 16, what
+            assert not dw or spans(rows, plan.packed(k) if p["pack_x"] else lds[0], k, elem) >= 16, what
