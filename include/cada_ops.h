@@ -19,8 +19,9 @@
  *     not; a captured cada_adamw_step repeats its t and lr).
  *   - Tables have rows of contiguous elements, ld... elements apart (ld >= the row's length).
  *     Element alignment is enough; rows that start on 16-byte boundaries and have a multiple of 16
- *     bytes are faster.  Outputs share memory with no operand except where it says so (CADA_EINVAL;
- *     columns side by side in one wider table are apart), and the workspace with neither.
+ *     bytes are faster.  Outputs share memory with no operand except where it says so, and the
+ *     workspace with neither (CADA_EINVAL; columns side by side in one wider table are apart, and a
+ *     single row is beside a wider table's columns).
  *   - Sums, statistics and moments are formed in float32 or more; values are rounded to nearest
  *     even where they are written as bf16.
  *   - Results do not depend on timing: the same call on the same operands gives the same bits.
@@ -108,8 +109,8 @@ int cada_linear_backward(const cada_linear_grad *a);
  * gradient zero.  NaN and +inf among the logits give NaN.  A label that is neither ignore_index nor in [0, classes) gives loss NaN
  * and gradient zero. */
 typedef struct cada_xent {
-  int64_t rows;          /* >= 0 */
-  int64_t classes;       /* 1 .. 2^31 - 1 */
+  int64_t rows;          /* 0 .. 2^30, and no more than one launch takes (2^22 - 1 of the longest rows) */
+  int64_t classes;       /* 1 .. 2^31 - 1 - 2^20 */
   int32_t type;          /* of logits and grad */
   int32_t label_bytes;   /* 4 or 8: int32 or int64 labels */
   const void *logits;    /* [rows, classes] */
@@ -131,7 +132,8 @@ int cada_xent_workspace(cada_xent *a); /* rows, classes, type, mean and loss are
 int cada_cross_entropy(const cada_xent *a);
 
 /* AdamW over many tensors in one launch (two with clipping).  Step t = 1, 2, ... of tensor p with gradient g:
- *   g <- g * grad_scale * min(1, max_norm / norm)                 (norm: over grad_scale * all gradients; max_norm 0: no clipping)
+ *   g <- g * grad_scale * min(1, max_norm / norm)                 (norm: over grad_scale * all gradients; max_norm 0: no clipping;
+ *                                                                  a norm past float32 counts as infinite and leaves zeros)
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
  *   p <- (p - lr weight_decay p) - lr/(1 - beta1^t) m / (sqrt(v)/sqrt(1 - beta2^t) + eps)
  * in float32, each operation rounded by itself; p is rounded once if it is bf16.
@@ -142,15 +144,16 @@ int cada_cross_entropy(const cada_xent *a);
  *   m = q |q| s / 127^2,        q int8 in [-127, 127],  s = the block's largest |m|
  *   sqrt(v) = c^2 s / 255^2,    c uint8,                s = the block's largest sqrt(v)
  * The codes grow with the root, so that small values keep a relative precision; sqrt(v) is rounded to the nearest code but
- * never from something to zero, since it divides.  A block whose scale is below 1e-30 keeps no codes; NaN or an infinity in a
- * block makes the block NaN.  The update itself uses the moments before they are rounded to codes. */
+ * never from something to zero, since it divides.  A block whose scale is below 1e-30 keeps no codes (but the 1 of a sqrt(v)
+ * that is not zero); NaN or an infinity in a block makes the block NaN.  The update itself uses the moments before they are
+ * rounded to codes. */
 enum { CADA_MOMENTS_32 = 32, CADA_MOMENTS_8 = 8 };
 #define CADA_MOMENT_BLOCK 256
 typedef struct cada_adamw_tensor {
   void *param;          /* [n] contiguous, updated in place; no tensor of a plan may be listed twice (gradients may) */
   const void *grad;     /* [n] contiguous */
   void *copy;           /* [n] bf16 or NULL: the new value rounded to bf16 (for float32 masters) */
-  int64_t n;            /* >= 0 */
+  int64_t n;            /* >= 0; all tensors' together at most 2^34, each filled up to 2048 */
   int32_t param_type, grad_type; /* CADA_F32 or CADA_BF16 */
   double weight_decay;
 } cada_adamw_tensor;
@@ -174,9 +177,10 @@ int cada_adamw_workspace(cada_adamw_config *cfg); /* the tensors' n are read */
 /* Lays the plan out in the workspace.  Does not touch the moments: a new run starts from zeros (zero bytes: also
  * CADA_MOMENTS_8), a resumed one from what was saved. */
 int cada_adamw_init(const cada_adamw_config *cfg, cada_adamw **out);
-/* One step; t >= 1.  grad_scale: DEVICE [1] or NULL (1), read when the step runs. */
+/* One step, on the stream of the plan's config; t >= 1.  grad_scale: DEVICE [1] or NULL (1), read when the step runs, in nothing
+ * that the plan writes. */
 int cada_adamw_step(cada_adamw *plan, int64_t t, double lr, const float *grad_scale);
-/* The moments as float32 values, [cada_adamw_moment_elements()] each; either may be NULL. */
+/* The moments as float32 values, [cada_adamw_moment_elements()] each, on the plan's stream; either may be NULL. */
 int cada_adamw_moments(cada_adamw *plan, float *m, float *v);
 void cada_adamw_destroy(cada_adamw *plan);
 

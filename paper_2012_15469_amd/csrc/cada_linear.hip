@@ -2,9 +2,9 @@
 //
 // Three products of two tables: y = x w (contraction over x's columns), dx = dz w^T (over dz's columns) and dw = x^T dz (over
 // the rows of both).  A table is read either along the contraction ("kc": consecutive elements are consecutive
-// contraction indices) or across it ("oc").  One tile kernel serves all of them: a workgroup of four wavefronts (2 x 2) takes a tile of
-// BM x BN outputs and walks the contraction in steps of 128 bytes per row, both operands' next step on its way into the other half
-// of LDS while the matrix instructions (32x32x16 bf16, 32x32x2 f32; float32 accumulators) take this one.
+// contraction indices) or across it ("oc").  One tile kernel serves all of them: a workgroup of four or eight wavefronts takes a tile of
+// BM x BN outputs and walks the contraction in steps of 128 bytes per row, the next one to three steps of both operands on their way into a ring in
+// LDS while the matrix instructions (32x32x16 bf16, 32x32x2 f32; float32 accumulators) take this one.
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
@@ -556,7 +556,8 @@ __global__ __launch_bounds__(64 * WY * WX * KW) void k_forward(const Product p) 
 // One or two rows (a single sample answered): a read of the weights.  A workgroup takes C columns, a lane eight of them, and 1024 or 512 weight rows at a time, asked
 // for together with x, which waits in LDS; a column's lanes exchange halves of their sums until each has one, and the wavefronts' sums are added in their order
 // (1 x 784 x 512 bf16 4.9 us; with sums of all values over all lanes, and weights asked for behind x, 5.6).  One launch, unless the contraction is split.  What bounds
-// it: a launch and two trips to memory, one of them the kernel's own (1 x 1024 x 4096 bf16 5.0 us, from memory 7.4; 8192 x 16384 54.9 us, 4.9 TB/s).
+// it: a launch and two trips to memory, one of them the kernel's own (1 x 1024 x 4096 bf16 4.7 us, from memory 7.4; 8192 x 16384 53.2 us, 5.0 TB/s; float32 4.8, 9.9 and
+// 100.6 us, 5.3 TB/s; 4096 x 1024 in two launches, from memory, bf16 11.0 us, float32 13.8).
 constexpr int kFewThreads = 1024;
 template <typename T, int C>
 __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
@@ -743,7 +744,9 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
 }
 
 // dz = dy * act'(pre), written in the operands' type with rows on 16-byte boundaries, and its column sums per block of rows.  A workgroup is 2^lanes threads
-// of eight columns each, as many as the columns need up to 32, by as many rows at a time.
+// of eight columns each, as many as the columns need up to 32, by as many rows at a time.  Of bf16 tables dz is rounded to bf16, which the matrix
+// instructions' operands are (the way that forms it on its way into LDS rounds it alike): dx and dw are 2.3e-3 from 64 bits, relative in the 2-norm, where the rounding of the outputs alone leaves
+// 1.7e-3; two bf16 parts of dz would be twice the products.  The column sums are of dz before that.
 struct Signal {
   const void *dy, *pre;
   int64_t lddy, ldpre, rows, rows_per_block;

@@ -21,6 +21,8 @@ struct Cut { int tile, splits; int64_t k_per_split; };
 // What a tile costs, in microseconds, measured (one product of random values, whole tiles, operands in the caches): a step alone on its CU, what all CUs at work add to
 // it, a step's share of a full CU, and the tile's way in and out.  At 8192 x 4096 x 4096 bf16: 256 x 256 tiles 1220 TFLOP/s, 128 x 128 1080, 64 x 64 640; a single
 // tile per CU: 870 (128), 460 (64).  Float32 is bound by the matrix instructions at any of them (146 TFLOP/s, 64 x 64 as 128 x 128), so it takes the smallest.
+// These are of bare products: what an epilogue reads and writes is in none of them (8192 x 784 x 512 bf16 with z kept: 9.9 us by the estimate, 15.6 measured; the gradients of
+// 120 x 784 x 500 float32: 4.8 and 8.8), so times are compared with times, not with clocks.
 struct TileCost { int tile, slots; double alone, crowd, share, ends; };
 constexpr TileCost kCostBf16[] = {{32, 5, 0.135, 0.05, 0.13, 1.0}, {64, 5, 0.20, 0.05, 0.215, 1.7}, {128, 2, 0.40, 0.13, 0.46, 3.0}, {256, 1, 1.1, 0.57, 1.68, 7.5}};
 constexpr TileCost kCostF32[] = {{32, 5, 0.21, 0.02, 0.155, 1.1}, {64, 5, 0.51, 0.05, 0.50, 1.3}};
@@ -91,7 +93,7 @@ inline bool no_tiles(int64_t rows, int64_t ld, int64_t cols, size_t elem) { retu
 // more outputs would make a second workgroup for some CUs (1 x 4096 x 50000 bf16 118 us as rows, 91 as tiles; float32 186 and 157).
 inline bool few_rows(int64_t rows, int64_t out) { return rows <= kFewRows && out <= 64 * kCUs; }
 // Columns of a workgroup there: a line of memory of bf16 weights (half a line each from two: 4096 x 4096 17 us, not 11); of float32 ones a line, for twice the workgroups, or
-// two lines where that fills the CUs (single row from memory: 4096 x 1024 28 us with 32 columns and 36 with 64, 8192 x 16384 127 and 104).
+// two lines where that fills the CUs (single row from memory, contraction not split: 4096 x 1024 28 us with 32 columns and 36 with 64, 8192 x 16384 127 and 104).
 inline int few_columns(size_t elem, int64_t out) { return elem == 2 || out > 32 * kCUs ? 64 : 32; }
 // Their contraction is split where CUs would stand idle and a workgroup have more than two reads of memory one after the other: a join costs 3 us, 1024 rows of weights 4 where they
 // come from memory (single row, bf16, from memory: 4096 x 1024 19.5 -> 11.2 us, 3000 x 1000 17.0 -> 11.5, 16384 x 4096 71 -> 32; 2048 x 2048 11.8 -> 11.1, and within L2 7.0 -> 8.7).

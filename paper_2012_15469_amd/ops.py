@@ -4,9 +4,12 @@
 ``cross_entropy``: the softmax cross-entropy over any number of classes with its gradient.
 ``AdamW``: the step over many tensors at once, moments in 32 or in 8 bits.
 
-Tensors are float32 or bfloat16 on one GPU.  Work goes to ``stream``, by default the device's current stream, and nothing
-synchronises the host; inputs must be ready there.  Outputs that are not handed in, and a call's workspace unless one is, come from torch's caching
-allocator and belong to that stream.
+Tensors are float32 or bfloat16 on one GPU.  Work goes to ``stream``, by default the device's current stream at the call (AdamW: the one that was current when
+it was made, for its steps too), and nothing synchronises the host; inputs must be ready there.  Outputs that are not handed in, and a call's workspace
+unless one is, come from torch's caching allocator and belong to that stream.
+
+The calls do not take part in autograd: operands that require gradients are read as they are, outputs have no history, and what is written in place
+(outputs handed in, parameters) counts no version.  ``linear_backward`` and the gradient of ``cross_entropy`` are what a backward pass is made of.
 """
 from __future__ import annotations
 
@@ -109,7 +112,8 @@ class AdamW:
     params, grads: contiguous float32 or bfloat16 tensors, each param's type its own.  ``weight_decay``: one value or one per tensor.  ``max_norm`` > 0 clips
     the gradients to that norm over all of them (``norm`` holds the norm of the last step).  ``state_bits``: 32, or 8 for moments in
     8-bit codes.  ``copies``: bfloat16 tensors that receive the rounded parameters, or None each.  ``moments``: (m, v) to go on from, as ``m`` and ``v`` of another
-    AdamW, updated in place; zeros otherwise.
+    AdamW, updated in place; zeros otherwise.  Parameters, copies and moments share memory with nothing (gradients may with each other).  ``stream``: where every step runs, by
+    default the stream that is current here, whichever is current at the step; gradients must be ready there, and a step in a captured graph needs that graph's stream.
 
     ``m`` and ``v`` hold the moments of all tensors one after the other, each tensor's filled up to whole blocks of 256 (``offsets`` says where each
     starts): float32 tensors, or pairs of codes and scales.  ``moments()`` gives their values."""
