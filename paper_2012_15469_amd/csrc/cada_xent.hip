@@ -285,7 +285,7 @@ int cada_cross_entropy(const cada_xent *a) {
   if (a->rows > 0) {
     if (!a->logits || !a->labels) { set_error("logits and labels must be device pointers"); return CADA_EINVAL; }
     if (a->ldz < a->classes || (a->grad && a->ldg < a->classes)) { set_error("the row length of logits or grad is less than the %lld classes", (long long)a->classes); return CADA_EINVAL; }
-    if (a->grad == a->logits && a->ldg != a->ldz) { set_error("grad in the place of logits must have their row length"); return CADA_EINVAL; }
+    if (a->grad == a->logits && a->rows > 1 && a->ldg != a->ldz) { set_error("grad in the place of logits must have their row length"); return CADA_EINVAL; }
     if (reinterpret_cast<uintptr_t>(a->logits) % type_bytes(a->type) != 0 || reinterpret_cast<uintptr_t>(a->grad) % type_bytes(a->type) != 0 ||
         reinterpret_cast<uintptr_t>(a->labels) % a->label_bytes != 0) { set_error("logits, grad or labels are not aligned to their elements"); return CADA_EINVAL; }
   }

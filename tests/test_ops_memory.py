@@ -95,3 +95,12 @@ def test_workspace_of_a_layers_gradients(part):
     assert _lib.cada_linear_backward_workspace(C.byref(a)) == 0 and 512 * 512 * 2 < a.workspace_bytes < 10 * MB
     setattr(a, part, a.workspace + 1024)
     assert _lib.cada_linear_backward(C.byref(a)) == -1 and "workspace and %s share memory" % part in cada_last_error()
+
+
+@pytest.mark.parametrize("rows,text", [(1, "mean and labels share memory"), (2, "must have their row length")])
+def test_the_gradient_of_one_row_in_place(rows, text):
+    """One row has no distance to a next one."""
+    a = cada_xent()
+    a.rows, a.classes, a.type, a.label_bytes, a.logits, a.ldz, a.labels, a.grad, a.ldg = rows, 10, 0, 8, MB, 10, 2 * MB, MB, 12
+    a.mean, a.workspace, a.workspace_bytes = 2 * MB + 4, 8 * MB, 1 << 20
+    assert _lib.cada_cross_entropy(C.byref(a)) == -1 and text in cada_last_error()
