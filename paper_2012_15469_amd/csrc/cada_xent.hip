@@ -65,7 +65,7 @@ __device__ __forceinline__ float group_reduce(float x, float *part, OP op) {
   return x;
 }
 
-// Exponentials of either type are the hardware's exp2 of the difference times log2(e), both rounded to float32: off by (z - top) 2^-23 and an ulp or two, relative, where a
+// Exponentials of either type are the hardware's exp2 of the difference times log2(e), both rounded to float32: off by about (z - top) 2^-23 and an ulp or two, relative, where a
 // library's exponential would be off by an ulp.  Small probabilities take the larger errors, so that sums and gradients are off by less than float32's own sums leave
 // (ten classes: 5e-8 from 64 bits, relative in the 2-norm).
 constexpr float kLog2e = 1.4426950408889634f;
