@@ -1,7 +1,8 @@
 /*
  * cada_ops.h - C ABI of libcada's operators for networks of one's own: a layer's product with
- *              bias, activation and residual, its gradients, the softmax cross-entropy with its
- *              gradient, and the AdamW step over many tensors.
+ *              bias, activation and residual, its gradients, layer norm with its gradients, the
+ *              embedding lookup with its gradient, the softmax cross-entropy with its gradient, of
+ *              given logits or of a last layer's product, and the AdamW step over many tensors.
  *
  * The engine of cada.h trains the models that it knows.  With these a program trains and serves
  * any network of such layers by the plain (everybody uploads) Adam baseline, on the same device
@@ -98,6 +99,92 @@ typedef struct cada_linear_grad {
 
 int cada_linear_backward_workspace(cada_linear_grad *a); /* all but the pointers' contents and stream is read */
 int cada_linear_backward(const cada_linear_grad *a);
+
+/* Layer norm of the rows of a table.
+ *   mean = sum x / width,  rstd = 1 / sqrt(sum (x - mean)^2 / width + eps),  y = (x - mean) rstd weight + bias
+ * mean and rstd are in float32; y is formed in float32 and rounded once. */
+typedef struct cada_norm {
+  int64_t rows;         /* 0 .. 2^40 */
+  int64_t width;        /* 1 .. CADA_MAX_WIDTH */
+  int32_t type;         /* of all but the statistics */
+  double eps;           /* positive, also in float32 */
+  const void *x;        /* [rows, width] */
+  int64_t ldx;
+  const void *weight;   /* [width] or NULL (1) */
+  const void *bias;     /* [width] or NULL (0) */
+  void *y;              /* [rows, width]; may be x itself (then with its ld) */
+  int64_t ldy;
+  float *mean, *rstd;   /* [rows] or NULL: what the gradient reads */
+  void *stream;
+} cada_norm;
+
+int cada_layer_norm_forward(const cada_norm *a); /* needs no workspace */
+
+/* Its gradients.  With u = (x - mean) rstd and g = dy weight:
+ *   dx = rstd (g - sum g / width - u (sum g u) / width) + residual,  dw = sum over the rows of dy u,  db = of dy
+ * (residual: a gradient that comes around the layer).  Outputs that are NULL are not formed. */
+typedef struct cada_norm_grad {
+  int64_t rows, width;  /* as above; rows == 0 clears dw and db */
+  int32_t type;
+  const void *dy;       /* [rows, width] */
+  int64_t lddy;
+  const void *x;        /* [rows, width] */
+  int64_t ldx;
+  const float *mean, *rstd; /* [rows] */
+  const void *weight;   /* [width] or NULL (1) */
+  const void *residual; /* [rows, width] or NULL; not read unless dx is wanted */
+  int64_t ldr;
+  void *dx;             /* [rows, width] or NULL; may be dy or residual itself (then with its ld) */
+  int64_t lddx;
+  void *dw, *db;        /* [width] or NULL */
+  void *workspace;
+  size_t workspace_bytes;
+  void *stream;
+} cada_norm_grad;
+
+int cada_layer_norm_backward_workspace(cada_norm_grad *a); /* rows, width, type, and whether dw and db are wanted */
+int cada_layer_norm_backward(const cada_norm_grad *a);
+
+/* Rows of a table by integer tokens: y[i] = scale w[token i], in float32, rounded once.  The row of a token that is ignore_index is zero (also where
+ * ignore_index is in [0, vocab)); that of any other token outside [0, vocab) is NaN. */
+typedef struct cada_embedding {
+  int64_t rows;         /* 0 .. 2^30 */
+  int64_t vocab;        /* 1 .. 2^24 */
+  int64_t width;        /* 1 .. CADA_MAX_WIDTH */
+  int32_t type;         /* of w and y */
+  int32_t token_bytes;  /* 4 or 8: int32 or int64 tokens */
+  const void *tokens;   /* [rows] */
+  int64_t ignore_index;
+  const void *w;        /* [vocab, width] */
+  int64_t ldw;
+  double scale;         /* finite, also in float32 */
+  void *y;              /* [rows, width] */
+  int64_t ldy;
+  void *stream;
+} cada_embedding;
+
+int cada_embedding_forward(const cada_embedding *a); /* needs no workspace */
+
+/* Its gradient: dw[v] = scale times the sum of dy[i] over the tokens i that are v, in their order, in float32, rounded once.  All of dw is written: a row whose
+ * token does not occur is zero.  Tokens that are ignore_index or outside [0, vocab) add nothing. */
+typedef struct cada_embedding_grad {
+  int64_t rows, vocab, width; /* as above */
+  int32_t type;
+  int32_t token_bytes;
+  const void *tokens;   /* [rows] */
+  int64_t ignore_index;
+  const void *dy;       /* [rows, width] */
+  int64_t lddy;
+  double scale;
+  void *dw;             /* [vocab, width] */
+  int64_t lddw;
+  void *workspace;
+  size_t workspace_bytes;
+  void *stream;
+} cada_embedding_grad;
+
+int cada_embedding_backward_workspace(cada_embedding_grad *a); /* rows, vocab, width, type, token_bytes, scale */
+int cada_embedding_backward(const cada_embedding_grad *a);
 
 /* Softmax cross-entropy of rows of logits with integer labels, and its gradient, in one pass.
  * A class whose logit is -inf is ruled out: its probability and gradient are zero.  The target of a row is

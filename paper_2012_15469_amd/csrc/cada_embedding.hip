@@ -1,0 +1,394 @@
+// Embedding lookup with scaling, and its gradient by sorted tokens (cada_ops.h).
+//
+// The gradient sums, for each row of the table, the rows of dy whose token it is.  Positions are first sorted by token, equal ones in their own order, so that sums have
+// one order and no float is added by an atomic: each workgroup owns a range of tokens, goes over all of them and puts down the positions of those in its range (k_sort).  The
+// sorted positions are then taken in chunks of one length, however often a token occurs: a token's run that lies in one chunk is written to the table, the parts of one that
+// crosses a chunk's border are joined by k_join.  Table rows without a token are cleared next to that.
+#include <algorithm>
+
+#include "cada_ops_internal.h"
+
+namespace cada {
+namespace {
+
+struct Lookup {
+  const void *tokens, *w;
+  void *y;
+  int64_t rows, vocab, ignore, ldw, ldy;
+  int32_t width, token_bytes, lanes;
+  float scale;
+};
+
+__device__ __forceinline__ int64_t token_at(const void *tokens, int bytes, int64_t i) {
+  return bytes == 8 ? static_cast<const int64_t *>(tokens)[i] : (int64_t)static_cast<const int32_t *>(tokens)[i];
+}
+
+// Columns that a lane takes: pieces of 16 bytes, the last of which begins early enough to end with the row (its first columns are another lane's too, which writes the same).
+// Rows of less than a piece go element by element.
+template <typename T> __device__ __forceinline__ int first_column(int piece, int width) {
+  constexpr int E = Elem<T>::kPer16;
+  return max(0, min(piece * E, width - E));
+}
+template <typename T> __device__ __forceinline__ u32x4v load_piece(const T *p, int width) { return width >= Elem<T>::kPer16 ? load16(p) : load16_n(p, width); }
+template <typename T> __device__ __forceinline__ void store_piece(T *p, int width, const float (&f)[Elem<T>::kPer16]) {
+  if (width >= Elem<T>::kPer16) {
+    store16(p, pack<T>(f));
+  } else {
+#pragma unroll
+    for (int e = 0; e < Elem<T>::kPer16; ++e) if (e < width) p[e] = from_f32<T>(f[e]);
+  }
+}
+
+// 2^lanes threads along a row, the others of 256 on further rows, four rows of a thread on their way at once.
+constexpr int kLookupRows = 4;
+template <typename T>
+__global__ __launch_bounds__(256) void k_lookup(const Lookup a) {
+  constexpr int E = Elem<T>::kPer16, U = kLookupRows;
+  const int high = 256 >> a.lanes, piece = ((int)blockIdx.y << a.lanes) + (threadIdx.x & ((1 << a.lanes) - 1));
+  if (piece * E >= a.width) return;
+  const int c = first_column<T>(piece, a.width);
+  for (int64_t r0 = (int64_t)blockIdx.x * high * U + (threadIdx.x >> a.lanes); r0 < a.rows; r0 += (int64_t)gridDim.x * high * U) {
+    int64_t t[U];
+    u32x4v raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) t[u] = token_at(a.tokens, a.token_bytes, min(r0 + u * high, a.rows - 1));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool known = t[u] != a.ignore && t[u] >= 0 && t[u] < a.vocab;
+      raw[u] = load_piece(static_cast<const T *>(a.w) + (known ? t[u] : 0) * a.ldw + c, a.width);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = r0 + u * high;
+      if (r >= a.rows) break;
+      const bool known = t[u] >= 0 && t[u] < a.vocab;
+      float f[E];
+      unpack<T>(raw[u], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[e] = t[u] == a.ignore ? 0.f : known ? f[e] * a.scale : __builtin_nanf("");
+      store_piece(static_cast<T *>(a.y) + r * a.ldy + c, a.width, f);
+    }
+  }
+}
+
+// ---- gradient ----
+
+struct Scatter {
+  const void *tokens, *dy;
+  void *dw;
+  int32_t *start, *order, *key;        // [vocab + 1]; [rows] each, sorted
+  float *part;                         // [chunks][2][width]: of the run that comes from the chunk before, and of the one that goes on in the next
+  int64_t rows, ignore, lddy, lddw;
+  int32_t vocab, width, token_bytes, lanes, range, chunk;      // range: tokens of a workgroup of k_sort; chunk: sorted positions of one of k_sums
+  uint32_t chunk_blocks;
+  float scale;
+};
+
+// A workgroup's tokens are [first, first + range).  Each of its sixteen wavefronts goes over a sixteenth of the positions, twice: it counts its tokens, and, when all have
+// counted, puts their positions down behind those of the smaller tokens and of the wavefronts before it.  Smaller tokens outside the range are only counted.
+// Bound by the reads of all tokens from L2 by every workgroup.
+constexpr int kSortThreads = 1024, kSortWaves = 16;
+template <int RANGE>
+__global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
+  __shared__ int32_t count[kSortWaves][RANGE];
+  __shared__ int32_t wave_sum[2][kSortWaves];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int64_t first = (int64_t)blockIdx.x * a.range, range = min((int64_t)a.range, a.vocab - first);
+  const int64_t per = (a.rows + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64, from = wave * per, to = min(a.rows, from + per);
+  for (int i = t; i < kSortWaves * RANGE; i += kSortThreads) (&count[0][0])[i] = 0;
+  __syncthreads();
+  int32_t below = 0;
+#pragma unroll 8
+  for (int64_t i = from + lane; i < to; i += 64) {
+    const int64_t x = token_at(a.tokens, a.token_bytes, i);
+    if (x >= 0 && x != a.ignore) {
+      below += x < first;
+      if (x >= first && x - first < range) atomicAdd(&count[wave][x - first], 1);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o, 64);
+  if (lane == 0) wave_sum[0][wave] = below;
+  __syncthreads();
+  below = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) below += wave_sum[0][w];
+  // exclusive sums over the range's tokens, in turns of a token per thread
+  int32_t base = below;
+  for (int k0 = 0; k0 < RANGE; k0 += kSortThreads) {
+    const int k = k0 + t;
+    int32_t mine = 0;
+    if (k < RANGE) {
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) mine += count[w][k];
+    }
+    int32_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int32_t other = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += other;
+    }
+    __syncthreads();
+    if (lane == 63) wave_sum[1][wave] = sum;
+    __syncthreads();
+    int32_t before = base, all = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      before += w < wave ? wave_sum[1][w] : 0;
+      all += wave_sum[1][w];
+    }
+    int32_t at = before + sum - mine;
+    if (k < range) a.start[first + k] = at;
+    if (k < RANGE) {
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) {
+        const int32_t n = count[w][k];
+        count[w][k] = at;
+        at += n;
+      }
+    }
+    base += all;
+  }
+  if (t == 0 && first + range == a.vocab) a.start[a.vocab] = base;
+  __syncthreads();
+  volatile int32_t *mine = count[wave];
+  for (int64_t i0 = from; i0 < to; i0 += 64) {
+    const int64_t i = i0 + lane, x = i < to ? token_at(a.tokens, a.token_bytes, i) : -1;
+    const bool in = x >= first && x - first < range && x != a.ignore;
+    uint64_t left = __ballot(in);
+    const int32_t k = in ? (int32_t)(x - first) : -1;
+    while (left) {
+      const int32_t one = __builtin_amdgcn_readlane(k, __builtin_ctzll(left));
+      const uint64_t same = __ballot(k == one);
+      if (k == one) {
+        const int32_t at = mine[one] + __popcll(same & ((1ull << lane) - 1));
+        a.order[at] = (int32_t)i;
+        a.key[at] = (int32_t)x;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (lane == __builtin_ctzll(same)) mine[one] = mine[one] + (int32_t)__popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      left &= ~same;
+    }
+  }
+}
+
+// Sums of a chunk of sorted positions, in their order: 2^lanes threads along a row, one piece each (blockIdx.y: which of a wide row's), eight rows on their way; and zeros for
+// the table's rows that have none, by the workgroups behind the chunks'.
+template <typename T>
+__global__ __launch_bounds__(256) void k_sums(const Scatter a) {
+  constexpr int E = Elem<T>::kPer16, U = 8;
+  const int high = 256 >> a.lanes, group = threadIdx.x >> a.lanes, piece = ((int)blockIdx.y << a.lanes) + (threadIdx.x & ((1 << a.lanes) - 1));
+  if (piece * E >= a.width) return;
+  const int col = first_column<T>(piece, a.width);
+  T *dw = static_cast<T *>(a.dw) + col;
+  if (blockIdx.x >= a.chunk_blocks) {
+    const float zero[E] = {};
+    const int64_t stride = (int64_t)(gridDim.x - a.chunk_blocks) * high;
+#pragma unroll 4
+    for (int64_t v = (int64_t)(blockIdx.x - a.chunk_blocks) * high + group; v < a.vocab; v += stride)
+      if (a.start[v] == a.start[v + 1]) store_piece(dw + v * a.lddw, a.width, zero);
+    return;
+  }
+  const int64_t c = (int64_t)blockIdx.x * high + group, n = a.start[a.vocab], lo = c * a.chunk, hi = min(n, lo + a.chunk);
+  if (lo >= n) return;
+  float acc[E] = {};
+  int32_t now = a.key[lo];
+  bool from_before = lo > 0 && a.key[lo - 1] == now;
+  auto flush = [&](bool goes_on) __attribute__((always_inline)) {
+    if (!from_before && !goes_on) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] *= a.scale;
+      store_piece(dw + (int64_t)now * a.lddw, a.width, acc);
+    } else {
+      float *to = a.part + (2 * c + (from_before ? 0 : 1)) * a.width + col;
+#pragma unroll
+      for (int e = 0; e < E; ++e) if (e < a.width) to[e] = acc[e];
+    }
+  };
+  for (int64_t j = lo; j < hi; j += U) {
+    int32_t k[U], at[U];
+    u32x4v raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = min(j + u, hi - 1);
+      k[u] = a.key[i];
+      at[u] = a.order[i];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = load_piece(static_cast<const T *>(a.dy) + (int64_t)at[u] * a.lddy + col, a.width);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (j + u >= hi) break;
+      if (k[u] != now) {
+        flush(false);
+        from_before = false;
+        now = k[u];
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+      }
+      float f[E];
+      unpack<T>(raw[u], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += f[e];
+    }
+  }
+  flush(hi < n && a.key[hi] == now);
+}
+
+// A run that crosses borders: a workgroup at each border, which has something to do if it is the run's first.  64 columns, the parts dealt to four wavefronts.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join(const Scatter a) {
+  __shared__ float sums[4][64];
+  const int64_t b = (int64_t)blockIdx.x + 1, at = b * a.chunk, n = a.start[a.vocab];
+  if (at >= n) return;
+  const int32_t v = a.key[at];
+  if (a.key[at - 1] != v) return;
+  if (a.start[v] < at - a.chunk) return;
+  const int64_t last = (a.start[v + 1] - 1) / a.chunk, parts = last - b + 2;        // of chunk b - 1 what goes on, of the others what comes from before
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int64_t c0 = (int64_t)blockIdx.y * 64; c0 < a.width; c0 += (int64_t)gridDim.y * 64) {
+    const int64_t c = c0 + lane;
+    float s = 0.f;
+    if (c < a.width) {
+#pragma unroll 8
+      for (int64_t i = wave; i < parts; i += 4) s += a.part[(2 * (b - 1 + i) + (i == 0 ? 1 : 0)) * a.width + c];
+    }
+    __syncthreads();
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < a.width) static_cast<T *>(a.dw)[(int64_t)v * a.lddw + c] = from_f32<T>(((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane])) * a.scale);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_clear(T *p, int64_t ld, int64_t rows, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / n;
+    p[r * ld + (i - r * n)] = from_f32<T>(0.f);
+  }
+}
+
+// ---- host ----
+constexpr int64_t kMostVocab = 1 << 24, kMostRows = 1 << 30;
+
+bool check_shape(int64_t rows, int64_t vocab, int64_t width, int type, int token_bytes, double scale) {
+  if (rows < 0 || rows > kMostRows) { set_error("rows must be in [0, 2^30] (got %lld)", (long long)rows); return false; }
+  if (vocab < 1 || vocab > kMostVocab) { set_error("vocab must be in [1, 2^24] (got %lld)", (long long)vocab); return false; }
+  if (width < 1 || width > CADA_MAX_WIDTH) { set_error("width must be in [1, %d] (got %lld)", CADA_MAX_WIDTH, (long long)width); return false; }
+  if (type != CADA_F32 && type != CADA_BF16) { set_error("type must be CADA_F32 or CADA_BF16 (got %d)", type); return false; }
+  if (token_bytes != 4 && token_bytes != 8) { set_error("token_bytes must be 4 or 8 (got %d)", token_bytes); return false; }
+  if (!((float)scale - (float)scale == 0.f)) { set_error("scale must be finite in float32"); return false; }
+  return true;
+}
+bool check_tokens(const void *tokens, int bytes) {
+  if (!tokens) { set_error("tokens is NULL"); return false; }
+  if (reinterpret_cast<uintptr_t>(tokens) % bytes != 0) { set_error("tokens is not aligned to its elements"); return false; }
+  return true;
+}
+// Threads along a row, as a power of two up to a workgroup.
+int lanes_for(int64_t width, int per16) {
+  int lanes = 0;
+  while (lanes < 8 && ((int64_t)per16 << lanes) < width) ++lanes;
+  return lanes;
+}
+unsigned slices(int64_t width, int per16, int lanes) { return (unsigned)ceil_div(width, (int64_t)per16 << lanes); }
+
+struct ScatterPlan { int32_t range, chunk; int64_t chunks; size_t off_order, off_key, off_part, bytes; };
+ScatterPlan plan_scatter(const cada_embedding_grad *a) {
+  ScatterPlan p{};
+  if (a->rows == 0) return p;
+  // a workgroup's range of tokens: one for each CU, and no more than its counts have room for
+  p.range = (int32_t)std::min<int64_t>(2048, ceil_div(a->vocab, 256));
+  // chunks for every CU a few times over, where that leaves some rows to each
+  p.chunk = 16;
+  while (p.chunk < 128 && (int64_t)p.chunk * 1024 < a->rows) p.chunk *= 2;
+  p.chunks = ceil_div(a->rows, p.chunk);
+  p.off_order = ops_align((size_t)(a->vocab + 1) * 4);
+  p.off_key = p.off_order + ops_align((size_t)a->rows * 4);
+  p.off_part = p.off_key + ops_align((size_t)a->rows * 4);
+  p.bytes = p.off_part + (p.chunks > 1 ? ops_align((size_t)p.chunks * 2 * a->width * 4) : 0);
+  return p;
+}
+
+template <typename T>
+int lookup(const cada_embedding *a) {
+  constexpr int E = Elem<T>::kPer16;
+  Lookup l{};
+  l.tokens = a->tokens; l.w = a->w; l.y = a->y; l.rows = a->rows; l.vocab = a->vocab; l.ignore = a->ignore_index; l.ldw = a->ldw; l.ldy = a->ldy;
+  l.width = (int32_t)a->width; l.token_bytes = a->token_bytes; l.lanes = lanes_for(a->width, E); l.scale = (float)a->scale;
+  const int64_t high = 256 >> l.lanes;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a->rows, high * kLookupRows), 1 << 20), slices(a->width, E, l.lanes));
+  k_lookup<T><<<grid, 256, 0, static_cast<hipStream_t>(a->stream)>>>(l);
+  return ops_launched("embedding");
+}
+
+template <typename T>
+int scatter(const cada_embedding_grad *a, const ScatterPlan &p) {
+  constexpr int E = Elem<T>::kPer16;
+  hipStream_t st = static_cast<hipStream_t>(a->stream);
+  if (a->rows == 0) {
+    k_clear<T><<<(unsigned)std::min<int64_t>(ceil_div(a->vocab * a->width, 256), 1 << 16), 256, 0, st>>>(static_cast<T *>(a->dw), a->lddw, a->vocab, a->width);
+    return ops_launched("embedding clear");
+  }
+  char *ws = static_cast<char *>(a->workspace);
+  Scatter s{};
+  s.tokens = a->tokens; s.dy = a->dy; s.dw = a->dw; s.rows = a->rows; s.ignore = a->ignore_index; s.lddy = a->lddy; s.lddw = a->lddw;
+  s.start = reinterpret_cast<int32_t *>(ws); s.order = reinterpret_cast<int32_t *>(ws + p.off_order); s.key = reinterpret_cast<int32_t *>(ws + p.off_key); s.part = reinterpret_cast<float *>(ws + p.off_part);
+  s.vocab = (int32_t)a->vocab; s.width = (int32_t)a->width; s.token_bytes = a->token_bytes; s.lanes = lanes_for(a->width, E); s.range = p.range; s.chunk = p.chunk;
+  s.scale = (float)a->scale;
+  const unsigned groups = (unsigned)ceil_div(a->vocab, p.range);
+  if (p.range <= 256) k_sort<256><<<groups, kSortThreads, 0, st>>>(s);
+  else if (p.range <= 512) k_sort<512><<<groups, kSortThreads, 0, st>>>(s);
+  else k_sort<2048><<<groups, kSortThreads, 0, st>>>(s);
+  if (int rc = ops_launched("embedding sort")) return rc;
+  const int64_t high = 256 >> s.lanes;
+  s.chunk_blocks = (uint32_t)ceil_div(p.chunks, high);
+  const unsigned fill = (unsigned)std::min<int64_t>(ceil_div(a->vocab, high * 4), 4096), across = slices(a->width, E, s.lanes);
+  k_sums<T><<<dim3(s.chunk_blocks + fill, across), 256, 0, st>>>(s);
+  if (int rc = ops_launched("embedding gradient")) return rc;
+  if (p.chunks == 1) return CADA_OK;
+  k_join<T><<<dim3((unsigned)p.chunks - 1, (unsigned)std::min<int64_t>(ceil_div(a->width, 64), 1024)), 256, 0, st>>>(s);
+  return ops_launched("embedding join");
+}
+
+}  // namespace
+}  // namespace cada
+
+using namespace cada;
+
+extern "C" {
+
+int cada_embedding_forward(const cada_embedding *a) {
+  if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
+  if (!check_shape(a->rows, a->vocab, a->width, a->type, a->token_bytes, a->scale)) return CADA_EINVAL;
+  if (a->rows == 0) return CADA_OK;
+  if (!check_tokens(a->tokens, a->token_bytes) || !ops_check_table("w", a->w, a->ldw, a->width, a->type) || !ops_check_table("y", a->y, a->ldy, a->width, a->type)) return CADA_EINVAL;
+  const size_t elem = type_bytes(a->type);
+  const Span y = span("y", a->y, a->rows, a->ldy, a->width, elem);
+  if (!ops_apart(y, span("w", a->w, a->vocab, a->ldw, a->width, elem)) || !ops_apart(y, span("tokens", a->tokens, (size_t)a->rows * a->token_bytes))) return CADA_EINVAL;
+  return a->type == CADA_BF16 ? lookup<bf16>(a) : lookup<float>(a);
+}
+
+int cada_embedding_backward_workspace(cada_embedding_grad *a) {
+  if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
+  if (!check_shape(a->rows, a->vocab, a->width, a->type, a->token_bytes, a->scale)) return CADA_EINVAL;
+  a->workspace_bytes = plan_scatter(a).bytes;
+  return CADA_OK;
+}
+
+int cada_embedding_backward(const cada_embedding_grad *a) {
+  if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
+  if (!check_shape(a->rows, a->vocab, a->width, a->type, a->token_bytes, a->scale)) return CADA_EINVAL;
+  if (a->rows > 0 && (!check_tokens(a->tokens, a->token_bytes) || !ops_check_table("dy", a->dy, a->lddy, a->width, a->type))) return CADA_EINVAL;
+  if (!ops_check_table("dw", a->dw, a->lddw, a->width, a->type)) return CADA_EINVAL;
+  const ScatterPlan p = plan_scatter(a);
+  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, p.bytes)) return rc;
+  const size_t elem = type_bytes(a->type);
+  const Span dw = span("dw", a->dw, a->vocab, a->lddw, a->width, elem), dy = span("dy", a->rows ? a->dy : nullptr, a->rows, a->lddy, a->width, elem);
+  const Span tokens = span("tokens", a->tokens, (size_t)a->rows * a->token_bytes), workspace = span("workspace", a->workspace, p.bytes);
+  if (!ops_apart(dw, dy) || !ops_apart(dw, tokens) || !ops_apart(workspace, dw) || !ops_apart(workspace, dy) || !ops_apart(workspace, tokens)) return CADA_EINVAL;
+  return a->type == CADA_BF16 ? scatter<bf16>(a, p) : scatter<float>(a, p);
+}
+
+}  // extern "C"

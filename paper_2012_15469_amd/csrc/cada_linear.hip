@@ -843,13 +843,6 @@ bool check_shape(int64_t rows, int64_t in, int64_t out, int type, int act) {
   if (t > kMostTiles) { set_error("more than %lld tiles of 64 x 64 outputs", (long long)kMostTiles); return false; }
   return true;
 }
-bool check_table(const char *name, const void *p, int64_t ld, int64_t cols, int type) {
-  if (!p) { set_error("%s is NULL", name); return false; }
-  if (ld < cols) { set_error("the row length of %s (%lld) is less than its %lld columns", name, (long long)ld, (long long)cols); return false; }
-  if (reinterpret_cast<uintptr_t>(p) % type_bytes(type) != 0) { set_error("%s is not aligned to its elements", name); return false; }
-  return true;
-}
-
 // ---- forward ----
 
 // Four steps on their way where LDS has room for them (few tiles: long contractions come from memory, 64 x 64 x 4096 with one tile per CU 32 -> 18.5 us); two, and more
@@ -1017,6 +1010,12 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
 
 }  // namespace
 
+bool ops_check_table(const char *name, const void *p, int64_t ld, int64_t cols, int type) {
+  if (!p) { set_error("%s is NULL", name); return false; }
+  if (ld < cols) { set_error("the row length of %s (%lld) is less than its %lld columns", name, (long long)ld, (long long)cols); return false; }
+  if (reinterpret_cast<uintptr_t>(p) % type_bytes(type) != 0) { set_error("%s is not aligned to its elements", name); return false; }
+  return true;
+}
 bool ops_apart(const Span &out, const Span &other) {
   if (!out.at || !other.at) return true;
   const uintptr_t a = reinterpret_cast<uintptr_t>(out.at), b = reinterpret_cast<uintptr_t>(other.at);
@@ -1082,10 +1081,10 @@ int cada_linear_forward(const cada_linear *a) {
   if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
   if (!check_shape(a->rows, a->in, a->out, a->type, a->act)) return CADA_EINVAL;
   if (a->rows == 0) return CADA_OK;
-  if (!check_table("x", a->x, a->ldx, a->in, a->type) || !check_table("w", a->w, a->ldw, a->out, a->type) || !check_table("y", a->y, a->ldy, a->out, a->type)) return CADA_EINVAL;
-  if (a->bias && !check_table("bias", a->bias, a->out, a->out, a->type)) return CADA_EINVAL;
-  if (a->residual && !check_table("residual", a->residual, a->ldr, a->out, a->type)) return CADA_EINVAL;
-  if (a->pre && !check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
+  if (!ops_check_table("x", a->x, a->ldx, a->in, a->type) || !ops_check_table("w", a->w, a->ldw, a->out, a->type) || !ops_check_table("y", a->y, a->ldy, a->out, a->type)) return CADA_EINVAL;
+  if (a->bias && !ops_check_table("bias", a->bias, a->out, a->out, a->type)) return CADA_EINVAL;
+  if (a->residual && !ops_check_table("residual", a->residual, a->ldr, a->out, a->type)) return CADA_EINVAL;
+  if (a->pre && !ops_check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
   const ForwardPlan f = plan_forward(a);
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, f.bytes)) return rc;
   const size_t elem = type_bytes(a->type);
@@ -1112,13 +1111,13 @@ int cada_linear_backward(const cada_linear_grad *a) {
   if (!a) { set_error("the arguments are NULL"); return CADA_EINVAL; }
   if (!check_shape(a->rows, a->in, a->out, a->type, a->act)) return CADA_EINVAL;
   if (a->rows > 0) {
-    if ((a->dx || a->dw || a->db) && !check_table("dy", a->dy, a->lddy, a->out, a->type)) return CADA_EINVAL;
-    if ((a->dx || a->dw || a->db) && a->act != CADA_ACT_NONE && !check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
-    if (a->dx && (!check_table("w", a->w, a->ldw, a->out, a->type) || !check_table("dx", a->dx, a->lddx, a->in, a->type))) return CADA_EINVAL;
-    if (a->dw && !check_table("x", a->x, a->ldx, a->in, a->type)) return CADA_EINVAL;
+    if ((a->dx || a->dw || a->db) && !ops_check_table("dy", a->dy, a->lddy, a->out, a->type)) return CADA_EINVAL;
+    if ((a->dx || a->dw || a->db) && a->act != CADA_ACT_NONE && !ops_check_table("pre", a->pre, a->ldpre, a->out, a->type)) return CADA_EINVAL;
+    if (a->dx && (!ops_check_table("w", a->w, a->ldw, a->out, a->type) || !ops_check_table("dx", a->dx, a->lddx, a->in, a->type))) return CADA_EINVAL;
+    if (a->dw && !ops_check_table("x", a->x, a->ldx, a->in, a->type)) return CADA_EINVAL;
   }
-  if (a->dw && !check_table("dw", a->dw, a->lddw, a->out, a->type)) return CADA_EINVAL;
-  if (a->db && !check_table("db", a->db, a->out, a->out, a->type)) return CADA_EINVAL;
+  if (a->dw && !ops_check_table("dw", a->dw, a->lddw, a->out, a->type)) return CADA_EINVAL;
+  if (a->db && !ops_check_table("db", a->db, a->out, a->out, a->type)) return CADA_EINVAL;
   const BackwardPlan b = plan_backward(a);
   if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, b.bytes)) return rc;
   const size_t elem = type_bytes(a->type);

@@ -129,6 +129,7 @@ bool ops_apart(const Span &out, const Span &other);      // cada_linear.hip
 // The same of any number of ranges of memory: no written one shares memory with another.  `index`: which tensor of a list, or -1.
 struct Range { const char *name; int index; const void *at; size_t bytes; bool written; };
 bool ops_apart(Range *ranges, size_t n);      // cada_linear.hip (puts them in order; none may throw)
+bool ops_check_table(const char *name, const void *p, int64_t ld, int64_t cols, int type);      // cada_linear.hip: a pointer, its row length and its alignment
 int ops_check_workspace(const void *ws, size_t given, size_t need);      // cada_linear.hip
 int ops_launched(const char *what);
 

@@ -64,6 +64,22 @@ template <typename P> void vector(const char *name, const at::Tensor &t, int64_t
     refuse("%s must be a contiguous %s [%lld] on %s", name, type_name(like.scalar_type()), (long long)n, like.device().str().c_str());
   *ptr = t.data_ptr();
 }
+// A float32 value per row.
+float *statistics(const char *name, const at::Tensor &t, int64_t n, const at::Tensor &like) {
+  if (t.dim() != 1 || t.size(0) != n || t.scalar_type() != at::kFloat || t.device() != like.device() || (n > 1 && t.stride(0) != 1))
+    refuse("%s must be a contiguous Float [%lld] on %s", name, (long long)n, like.device().str().c_str());
+  return t.data_ptr<float>();
+}
+// Labels or tokens, n of them (any number if n < 0); how many there are.
+int64_t whole_numbers(const char *name, const at::Tensor &t, int64_t n, const at::Tensor &like, const void **ptr, int32_t *bytes) {
+  if ((t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) || t.dim() != 1 || (n >= 0 && t.size(0) != n) || t.device() != like.device() || (t.size(0) > 1 && t.stride(0) != 1)) {
+    if (n < 0) refuse("%s must be a contiguous one-dimensional int32 or int64 tensor on %s", name, like.device().str().c_str());
+    refuse("%s must be a contiguous int32 or int64 [%lld] on %s", name, (long long)n, like.device().str().c_str());
+  }
+  *ptr = t.data_ptr();
+  *bytes = (int32_t)t.element_size();
+  return t.size(0);
+}
 at::Tensor fresh(at::IntArrayRef size, const at::Tensor &like) { return at::empty(size, like.options()); }
 
 // Workspace of a call: the one handed in, or one of the size that it asks for (torch's blocks start on 512 bytes).
@@ -183,9 +199,7 @@ PyObject *cross_entropy(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     a.rows = z.size(0); a.classes = z.size(1); a.type = type_of(z);
     void *p;
     table("logits", z, a.rows, a.classes, z, &p, &a.ldz); a.logits = p;
-    if ((labels.scalar_type() != at::kInt && labels.scalar_type() != at::kLong) || labels.dim() != 1 || labels.size(0) != a.rows || labels.device() != z.device() || (a.rows > 1 && labels.stride(0) != 1))
-      refuse("labels must be a contiguous int32 or int64 [%lld] on %s", (long long)a.rows, z.device().str().c_str());
-    a.labels = labels.data_ptr(); a.label_bytes = (int)labels.element_size();
+    whole_numbers("labels", labels, a.rows, z, &a.labels, &a.label_bytes);
     a.smoothing = PyFloat_AsDouble(args[2]); a.ignore_index = PyLong_AsLongLong(args[3]); a.scale = PyFloat_AsDouble(args[4]);
     if (PyErr_Occurred()) throw Failed{};
     const at::Tensor loss = at::empty({a.rows}, z.options().dtype(at::kFloat)), mean = at::empty({}, z.options().dtype(at::kFloat));
@@ -203,6 +217,117 @@ PyObject *cross_entropy(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   });
 }
 
+// (x, weight, bias, eps, keep_stats, out, mean, rstd, stream) -> (y, mean, rstd)
+PyObject *layer_norm_forward(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject * {
+    if (n_args != 9) refuse("layer_norm_forward takes 9 arguments");
+    const at::Tensor &x = needed(args[0], "x");
+    first(x, "x");
+    cada_norm a{};
+    a.rows = x.size(0); a.width = x.size(1); a.type = type_of(x); a.eps = PyFloat_AsDouble(args[3]);
+    if (PyErr_Occurred()) throw Failed{};
+    void *p;
+    table("x", x, a.rows, a.width, x, &p, &a.ldx); a.x = p;
+    if (const at::Tensor *t = tensor(args[1], "weight")) { vector("weight", *t, a.width, x, &p); a.weight = p; }
+    if (const at::Tensor *t = tensor(args[2], "bias")) { vector("bias", *t, a.width, x, &p); a.bias = p; }
+    const at::Tensor *given = tensor(args[5], "out"), *given_stats[2] = {tensor(args[6], "mean"), tensor(args[7], "rstd")};
+    const at::Tensor y = given ? *given : fresh({a.rows, a.width}, x);
+    table("out", y, a.rows, a.width, x, &a.y, &a.ldy);
+    at::Tensor stats[2];
+    for (int i = 0; i < 2; ++i) {
+      if (!given_stats[i] && args[4] != Py_True) continue;
+      stats[i] = given_stats[i] ? *given_stats[i] : at::empty({a.rows}, x.options().dtype(at::kFloat));
+      (i == 0 ? a.mean : a.rstd) = statistics(i == 0 ? "mean" : "rstd", stats[i], a.rows, x);
+    }
+    a.stream = stream_of(args[8]);
+    check(cada_layer_norm_forward(&a));
+    return triple(y, stats[0], stats[1]);
+  });
+}
+
+// (dy, x, mean, rstd, weight, residual, need_dx, need_dw, need_db, dx, dw, db, workspace, stream) -> (dx, dw, db)
+PyObject *layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject * {
+    if (n_args != 14) refuse("layer_norm_backward takes 14 arguments");
+    const at::Tensor &dy = needed(args[0], "dy"), &x = needed(args[1], "x"), &mean = needed(args[2], "mean"), &rstd = needed(args[3], "rstd");
+    first(dy, "dy");
+    cada_norm_grad a{};
+    a.rows = dy.size(0); a.width = dy.size(1); a.type = type_of(dy);
+    void *p;
+    table("dy", dy, a.rows, a.width, dy, &p, &a.lddy); a.dy = p;
+    table("x", x, a.rows, a.width, dy, &p, &a.ldx); a.x = p;
+    a.mean = statistics("mean", mean, a.rows, dy);
+    a.rstd = statistics("rstd", rstd, a.rows, dy);
+    if (const at::Tensor *t = tensor(args[4], "weight")) { vector("weight", *t, a.width, dy, &p); a.weight = p; }
+    if (const at::Tensor *t = tensor(args[5], "residual")) { table("residual", *t, a.rows, a.width, dy, &p, &a.ldr); a.residual = p; }
+    at::Tensor dx, dw, db;
+    if (args[6] == Py_True) {
+      const at::Tensor *t = tensor(args[9], "dx");
+      dx = t ? *t : fresh({a.rows, a.width}, dy);
+      table("dx", dx, a.rows, a.width, dy, &a.dx, &a.lddx);
+    }
+    if (args[7] == Py_True) {
+      const at::Tensor *t = tensor(args[10], "dw");
+      dw = t ? *t : fresh({a.width}, dy);
+      vector("dw", dw, a.width, dy, &a.dw);
+    }
+    if (args[8] == Py_True) {
+      const at::Tensor *t = tensor(args[11], "db");
+      db = t ? *t : fresh({a.width}, dy);
+      vector("db", db, a.width, dy, &a.db);
+    }
+    const at::Tensor ws = workspace(&a, args[12], cada_layer_norm_backward_workspace, dy);
+    a.stream = stream_of(args[13]);
+    check(cada_layer_norm_backward(&a));
+    return triple(dx, dw, db);
+  });
+}
+
+// (tokens, w, scale, ignore_index, out, stream) -> y
+PyObject *embedding_forward(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject * {
+    if (n_args != 6) refuse("embedding_forward takes 6 arguments");
+    const at::Tensor &tokens = needed(args[0], "tokens"), &w = needed(args[1], "w");
+    first(w, "w");
+    cada_embedding a{};
+    a.rows = whole_numbers("tokens", tokens, -1, w, &a.tokens, &a.token_bytes);
+    a.vocab = w.size(0); a.width = w.size(1); a.type = type_of(w);
+    a.scale = PyFloat_AsDouble(args[2]); a.ignore_index = PyLong_AsLongLong(args[3]);
+    if (PyErr_Occurred()) throw Failed{};
+    void *p;
+    table("w", w, a.vocab, a.width, w, &p, &a.ldw); a.w = p;
+    const at::Tensor *given = tensor(args[4], "out");
+    const at::Tensor y = given ? *given : fresh({a.rows, a.width}, w);
+    table("out", y, a.rows, a.width, w, &a.y, &a.ldy);
+    a.stream = stream_of(args[5]);
+    check(cada_embedding_forward(&a));
+    return wrap(y);
+  });
+}
+
+// (dy, tokens, vocab, scale, ignore_index, dw, workspace, stream) -> dw
+PyObject *embedding_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject * {
+    if (n_args != 8) refuse("embedding_backward takes 8 arguments");
+    const at::Tensor &dy = needed(args[0], "dy"), &tokens = needed(args[1], "tokens");
+    first(dy, "dy");
+    cada_embedding_grad a{};
+    a.rows = dy.size(0); a.width = dy.size(1); a.type = type_of(dy);
+    whole_numbers("tokens", tokens, a.rows, dy, &a.tokens, &a.token_bytes);
+    a.vocab = PyLong_AsLongLong(args[2]); a.scale = PyFloat_AsDouble(args[3]); a.ignore_index = PyLong_AsLongLong(args[4]);
+    if (PyErr_Occurred()) throw Failed{};
+    void *p;
+    table("dy", dy, a.rows, a.width, dy, &p, &a.lddy); a.dy = p;
+    const at::Tensor ws = workspace(&a, args[6], cada_embedding_backward_workspace, dy);      // (checks the sizes)
+    const at::Tensor *given = tensor(args[5], "dw");
+    const at::Tensor dw = given ? *given : fresh({a.vocab, a.width}, dy);
+    table("dw", dw, a.vocab, a.width, dy, &a.dw, &a.lddw);
+    a.stream = stream_of(args[7]);
+    check(cada_embedding_backward(&a));
+    return wrap(dw);
+  });
+}
+
 PyObject *set_error_class(PyObject *, PyObject *o) {
   Py_INCREF(o);
   Py_XDECREF(g_error);
@@ -214,6 +339,10 @@ PyMethodDef methods[] = {
     {"linear_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(linear_forward)), METH_FASTCALL, nullptr},
     {"linear_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(linear_backward)), METH_FASTCALL, nullptr},
     {"cross_entropy", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cross_entropy)), METH_FASTCALL, nullptr},
+    {"layer_norm_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(layer_norm_forward)), METH_FASTCALL, nullptr},
+    {"layer_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(layer_norm_backward)), METH_FASTCALL, nullptr},
+    {"embedding_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(embedding_forward)), METH_FASTCALL, nullptr},
+    {"embedding_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(embedding_backward)), METH_FASTCALL, nullptr},
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

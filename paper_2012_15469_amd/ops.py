@@ -1,6 +1,8 @@
 """The operators of include/cada_ops.h on torch tensors: argument marshalling only.
 
 ``linear_forward`` / ``linear_backward``: a layer's product with bias, activation and residual, and its gradients.
+``layer_norm_forward`` / ``layer_norm_backward``: layer norm of the rows of a table, and its gradients.
+``embedding_forward`` / ``embedding_backward``: rows of a table by integer tokens, and the table's gradient.
 ``cross_entropy``: the softmax cross-entropy over any number of classes with its gradient.
 ``AdamW``: the step over many tensors at once, moments in 32 or in 8 bits.
 
@@ -9,7 +11,7 @@ it was made, for its steps too), and nothing synchronises the host; inputs must 
 unless one is, come from torch's caching allocator and belong to that stream.
 
 The calls do not take part in autograd: operands that require gradients are read as they are, outputs have no history, and what is written in place
-(outputs handed in, parameters) counts no version.  ``linear_backward`` and the gradient of ``cross_entropy`` are what a backward pass is made of.
+(outputs handed in, parameters) counts no version.  The ``..._backward`` functions and the gradient of ``cross_entropy`` are what a backward pass is made of.
 """
 from __future__ import annotations
 
@@ -94,6 +96,40 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, pre: 
     if act not in ACTIVATIONS:
         raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
     return _call(_ops.linear_backward, dy, stream, dy, x, w, pre, ACTIVATIONS[act], bool(need_dx), bool(need_dw), bool(need_db), dx, dw, db, workspace)
+
+
+def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *, eps: float = 1e-5, keep_stats: bool = False,
+                       out: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(y, mean, rstd) with y = (x - mean) rstd weight + bias for each row, rstd = 1 / sqrt(variance + eps); mean and rstd, float32 [rows], are None unless
+    ``keep_stats`` or tensors to write are given.
+
+    x [rows, width], weight and bias [width] or None, all of one type; rows contiguous, any distance apart.  ``out`` may be ``x``."""
+    return _call(_ops.layer_norm_forward, x, stream, x, weight, bias, eps, bool(keep_stats), out, mean, rstd)
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor] = None, *,
+                        residual: Optional[torch.Tensor] = None, need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
+                        dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                        ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dx, dw, db) of layer_norm_forward from the gradient of its output and the statistics that it kept; dw and db are those of weight and bias.
+    ``residual``, a gradient that comes around the layer, is added to dx.  ``dx`` may be ``dy`` or ``residual``.  Outputs handed in are written, not added to."""
+    return _call(_ops.layer_norm_backward, dy, stream, dy, x, mean, rstd, weight, residual, bool(need_dx), bool(need_dw), bool(need_db), dx, dw, db, workspace)
+
+
+def embedding_forward(tokens: torch.Tensor, w: torch.Tensor, *, scale: float = 1.0, ignore_index: int = -100, out: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """scale * w[tokens], [rows, width].
+
+    tokens int32 or int64 [rows], w [vocab, width] with contiguous rows.  Rows of tokens that are ``ignore_index`` are zero, those of other tokens outside the table NaN."""
+    return _call(_ops.embedding_forward, w, stream, tokens, w, scale, ignore_index, out)
+
+
+def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, *, scale: float = 1.0, ignore_index: int = -100, dw: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """dw [vocab, width] of embedding_forward from the gradient of its output: zero where a token does not occur.  Equal tokens' rows are added in their order."""
+    return _call(_ops.embedding_backward, dy, stream, dy, tokens, vocab, scale, ignore_index, dw, workspace)
 
 
 def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, *, smoothing: float = 0.0, ignore_index: int = -100, scale: float = 1.0, need_grad: bool = True,

@@ -1,0 +1,203 @@
+"""The embedding lookup, which comes out exactly, and its gradient against the definition in 64 bits.
+
+Tolerances of the gradient: n rows of a token are added in float32, one after the other or in parts, so a sum is off by n 2^-24 times the sum of magnitudes; the scale and the rounding to float32 add 2^-24 each,
+the rounding to bf16 2^-8 (bf16 has eight significant bits: half a step is 2^-8 of a value just above a power of two).  Sums of small integers are below 2^24 and come out exactly."""
+import math
+
+import pytest
+import torch
+
+from paper_2012_15469_amd import ops
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+E = 2.0 ** -24
+
+
+def tokens_of(gen, rows, vocab, bits, kind):
+    if kind == "one":
+        t = torch.full((rows,), vocab // 2, device="cuda")
+    elif kind == "few":
+        t = torch.randint(min(3, vocab), (rows,), generator=gen, device="cuda") * max(1, vocab // 3)
+    elif kind == "near":         # many different tokens of one workgroup's range
+        t = torch.randint(min(200, vocab), (rows,), generator=gen, device="cuda")
+    else:
+        t = torch.randint(vocab, (rows,), generator=gen, device="cuda")
+    return t.clamp(max=vocab - 1).to(bits)
+
+
+def forward_by_definition(tokens, w, scale, ignore):
+    known = (tokens >= 0) & (tokens < w.shape[0])
+    y = w[torch.where(known, tokens, 0).long()].float() * torch.tensor(scale, dtype=torch.float32, device="cuda")
+    y = torch.where(known[:, None], y, math.nan)
+    return torch.where((tokens == ignore)[:, None], 0.0, y).to(w.dtype)
+
+
+def check_backward(dy, tokens, vocab, scale=1.0, ignore=-100, exactly=False, **kw):
+    used = torch.nonzero((tokens != ignore) & (tokens >= 0) & (tokens < vocab))[:, 0]
+    at = tokens[used].long()
+    # (on the CPU: the GPU's additions to one row wait for each other)
+    cpu_at, cpu_dy = at.cpu(), dy[used].double().cpu()
+    want = torch.zeros(vocab, dy.shape[1], dtype=torch.float64).index_add_(0, cpu_at, cpu_dy).cuda()
+    size = want if exactly else torch.zeros(vocab, dy.shape[1], dtype=torch.float64).index_add_(0, cpu_at, cpu_dy.abs()).cuda()
+    count = torch.bincount(at, minlength=vocab).double()[:, None] if used.numel() else torch.zeros(vocab, 1, device="cuda")
+    dw = ops.embedding_backward(dy, tokens, vocab, scale=scale, ignore_index=ignore, **kw)
+    assert dw.dtype == dy.dtype and dw.shape == want.shape
+    if exactly:
+        same = torch.equal(dw, want.to(dy.dtype))
+        assert same
+    else:
+        limit = abs(scale) * size * (count + 2) * E + (2.0 ** -8 if dy.dtype == torch.bfloat16 else E) * 1.01 * (scale * want).abs()
+        worst = float(((dw.double() - scale * want).abs() / (limit + 1e-38)).max())
+        assert worst <= 1.0
+    return dw
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [1, 2, 3, 4, 5, 7, 8, 9, 33, 64, 301, 512, 1000, 2048, 2051, 5000, 9001])
+def test_lookup(width, dtype):
+    gen = torch.Generator(device="cuda"); gen.manual_seed(width)
+    for rows, vocab, bits, pad, scale in ((1, 5, torch.int64, 0, 1.0), (37, 1, torch.int32, 3, 2.5), (1000, 701, torch.int64, 8, math.sqrt(width)), (515, 33, torch.int32, 1, -0.37)):
+        w = torch.randn(vocab, width + pad, generator=gen, device="cuda").to(DT[dtype])[:, pad // 2:pad // 2 + width]
+        tokens = tokens_of(gen, rows, vocab, bits, "all")
+        if rows > 1:
+            tokens[3::7], tokens[4::9], tokens[5::11] = -100, vocab, -1
+        want = forward_by_definition(tokens, w, scale, -100)
+        wide = torch.full((rows + 1, width + 5), 7.0, dtype=w.dtype, device="cuda")
+        for out in (None, wide[:rows, 2:2 + width]):
+            y = ops.embedding_forward(tokens, w, scale=scale, out=out)
+            assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
+        wide[:rows, 2:2 + width] = 7.0
+        assert bool((wide == 7.0).all())
+    # an ignored token inside the table
+    y = ops.embedding_forward(torch.tensor([0, 2, 1], device="cuda"), w[:3], ignore_index=2)
+    assert torch.equal(y[0], w[0]) and torch.equal(y[2], w[1]) and not y[1].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [1, 3, 4, 7, 8, 9, 16, 64, 301, 1000, 2048, 2051, 5000])
+def test_gradient(width, dtype):
+    gen = torch.Generator(device="cuda"); gen.manual_seed(width)
+    for rows, vocab, bits, kind, pad, scale in ((1, 1, torch.int64, "all", 0, 1.0), (1, 77, torch.int32, "all", 3, 2.0), (16, 5, torch.int64, "all", 0, 0.5), (17, 300, torch.int64, "one", 1, 1.0), (64, 300, torch.int32, "few", 8, 1.0),
+                                                (257, 1001, torch.int32, "all", 3, math.sqrt(width)), (1000, 5000, torch.int64, "near", 0, 1.0), (2500, 257, torch.int64, "all", 0, -1.7), (3001, 700, torch.int64, "few", 5, 1.0)):
+        dy = torch.randn(rows, width + pad, generator=gen, device="cuda").to(DT[dtype])[:, pad // 2:pad // 2 + width]
+        tokens = tokens_of(gen, rows, vocab, bits, kind)
+        if rows > 1:
+            tokens[3::7], tokens[4::9], tokens[5::11] = -100, vocab, -1
+        first = check_backward(dy, tokens, vocab, scale)
+        wide = torch.full((vocab + 1, width + 5), 7.0, dtype=dy.dtype, device="cuda")
+        out = wide[:vocab, 2:2 + width]
+        assert ops.embedding_backward(dy, tokens, vocab, scale=scale, dw=out) is out and torch.equal(out, first)
+        out.fill_(7.0)
+        assert bool((wide == 7.0).all())
+
+
+@pytest.mark.parametrize("rows,vocab,kind", [
+    (20000, 50001, "all"), (20000, 50001, "one"), (20000, 50001, "near"), (20000, 65536, "few"), (40000, 65537, "all"), (40000, 131073, "near"), (16384, 600001, "all"), (150000, 4, "all"), (150000, 3000, "one"), (200000, 1, "one"),
+    (130000, 2, "few"), (1023, 70000, "all"), (1025, 70000, "near"), (5, 3000000, "all")])
+def test_gradient_exactly(rows, vocab, kind):
+    """Small integers: every count of tokens in a range and every length of a run, each sum exactly."""
+    gen = torch.Generator(device="cuda"); gen.manual_seed(rows)
+    for dtype, width in (("f32", 12), ("bf16", 24)):
+        dy = torch.randint(-8, 9, (rows, width), generator=gen, device="cuda").to(DT[dtype])
+        tokens = tokens_of(gen, rows, vocab, torch.int64, kind)
+        tokens[::13] = -100
+        check_backward(dy, tokens, vocab, exactly=True)
+        check_backward(dy, tokens.int(), vocab, exactly=True)
+
+
+@pytest.mark.parametrize("chunk_rows", [15, 16, 17, 31, 32, 33, 47, 48, 49])
+def test_runs_around_the_ends_of_chunks(chunk_rows):
+    """Tokens in order, each as often as given: runs that end at, before and behind the borders of sixteen sorted positions."""
+    tokens = torch.arange(40, device="cuda").repeat_interleave(chunk_rows)
+    dy = torch.randint(-8, 9, (tokens.numel(), 40), device="cuda").float()
+    for order in (torch.arange(tokens.numel(), device="cuda"), torch.randperm(tokens.numel(), device="cuda")):
+        check_backward(dy[order], tokens[order], 41, exactly=True)
+
+
+def test_the_order_of_a_sum():
+    """Equal tokens' rows are added in their order, chunk by chunk: a row of 2^24, ones that it swallows, and its negative."""
+    dy = torch.ones(6, 8, device="cuda")
+    dy[1], dy[4] = 2.0 ** 25, -2.0 ** 25
+    dw = ops.embedding_backward(dy, torch.tensor([1, 1, 1, 1, 1, 1], device="cuda"), 3)
+    assert bool((dw[1] == 1.0).all()) and not dw[0].any() and not dw[2].any()
+
+
+def test_nothing_counts():
+    for rows in (0, 5):
+        t = torch.full((rows,), 3, device="cuda")
+        dy = torch.randn(rows, 9, device="cuda")
+        dw = ops.embedding_backward(dy, t, 7, ignore_index=3)
+        assert dw.shape == (7, 9) and not dw.any()
+    assert ops.embedding_forward(torch.empty(0, dtype=torch.int64, device="cuda"), dy).shape == (0, 9)
+    # what is ignored is not looked at
+    dy[0] = math.nan
+    dy[1] = math.inf
+    t = torch.tensor([-100, 7, 2, 2, -3], device="cuda")
+    dw = ops.embedding_backward(dy, t, 7)
+    assert bool(torch.isfinite(dw).all()) and bool(dw[2].any())
+
+
+def test_gradient_against_differences():
+    w, dy, t, h = torch.randn(4, 5, device="cuda"), torch.randn(6, 5, device="cuda"), torch.tensor([2, 0, 2, -100, 3, 2], device="cuda"), 0.5
+    got = ops.embedding_backward(dy, t, 4, scale=1.5)
+    for i in range(4):
+        for j in range(5):
+            hi, lo = w.clone(), w.clone()
+            hi[i, j] += h
+            lo[i, j] -= h
+            want = sum(float((ops.embedding_forward(t, v, scale=1.5).double() * dy.double()).sum()) * s for v, s in ((hi, 1), (lo, -1))) / (2 * h)
+            assert abs(float(got[i, j]) - want) < 2e-5
+
+
+def test_graph_replays_and_another_stream():
+    w, t, dy = torch.randn(3000, 200, device="cuda").to(torch.bfloat16), torch.randint(3000, (2000,), device="cuda"), torch.randn(2000, 200, device="cuda").to(torch.bfloat16)
+
+    def both(**kw):
+        return ops.embedding_forward(t, w, scale=3.0, **kw), ops.embedding_backward(dy, t, 3000, scale=3.0, **kw)
+
+    both()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for i in range(4):
+        t.copy_(torch.randint(3000 if i % 2 else 3, (2000,), device="cuda"))
+        dy.copy_(torch.randn(2000, 200, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, both()))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    there = both(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(got, there))
+
+
+def test_rows_far_apart():
+    """Rows more than 4 GB apart, in every table."""
+    apart = (1 << 31) + 64
+    base = torch.empty(2 * apart + 1000, dtype=torch.bfloat16, device="cuda")
+    far = base.as_strided((3, 1000), (apart, 1))
+    far.copy_(torch.randn(3, 1000, device="cuda"))
+    near, t = far.contiguous(), torch.tensor([2, 0, 2, 1, -100], device="cuda")
+    assert torch.equal(ops.embedding_forward(t, far), ops.embedding_forward(t, near))
+    dw = ops.embedding_backward(near, t[:3].contiguous(), 3)
+    assert torch.equal(ops.embedding_backward(far, t[:3].contiguous(), 3), dw)
+    y = ops.embedding_forward(t[:3].contiguous(), near)
+    assert ops.embedding_forward(t[:3].contiguous(), near, out=far) is far and torch.equal(far, y)
+    assert torch.equal(ops.embedding_backward(near, t[:3].contiguous(), 3, dw=far), dw)
+
+
+def test_refusals():
+    w, t = torch.zeros(4, 8, device="cuda"), torch.zeros(6, dtype=torch.int64, device="cuda")
+    for bad in (t.float(), t[::2], t.cpu(), t[:, None]):
+        with pytest.raises(ValueError, match="tokens must be a contiguous"):
+            ops.embedding_forward(bad, w)
+    with pytest.raises(ValueError, match=r"int32 or int64 \[4\]"):
+        ops.embedding_backward(w, t, 9)
+    with pytest.raises(ValueError, match="out must be"):
+        ops.embedding_forward(t, w, out=torch.zeros(5, 8, device="cuda"))
+    with pytest.raises(ValueError, match="dw must be"):
+        ops.embedding_backward(w, t[:4], 9, dw=torch.zeros(9, 7, device="cuda"))
+    with pytest.raises(RuntimeError, match="vocab"):
+        ops.embedding_backward(w, t[:4], 0)
