@@ -218,6 +218,40 @@ typedef struct cada_xent {
 int cada_xent_workspace(cada_xent *a); /* rows, classes, type, mean and loss are read */
 int cada_cross_entropy(const cada_xent *a);
 
+/* The same loss of the logits z = x w + bias of a last layer, and its gradients, without the logits in memory: z is formed in float32 and goes into each row's statistics, and, for the
+ * gradients, again in pieces of the classes, whose (softmax - target) lies in the workspace in the operands' type while
+ *   dx = (softmax - target) w^T,  dw = x^T (softmax - target),  db = column sums of it (before it is rounded to that type)
+ * are formed, all times scale / max(1, number of rows that are not ignored).  A class is ruled out by a bias of -inf.  Rows that are ignored, or whose label is no class, get dx = 0
+ * and count nowhere, whatever x holds there.  Outputs that are NULL are not formed. */
+typedef struct cada_linear_xent {
+  int64_t rows;          /* 0 .. 2^30 */
+  int64_t in, classes;   /* 1 .. CADA_MAX_WIDTH; of the tables' products, at most 2^23 - 8 tiles of 64 x 64 */
+  int32_t type;          /* of all tables and the bias */
+  int32_t label_bytes;   /* 4 or 8: int32 or int64 labels */
+  const void *x;         /* [rows, in] */
+  int64_t ldx;
+  const void *w;         /* [in, classes] */
+  int64_t ldw;
+  const void *bias;      /* [classes] or NULL */
+  const void *labels;    /* [rows] */
+  int64_t ignore_index;
+  double smoothing;      /* [0, 1) */
+  double scale;          /* factor of the gradients (loss scaling) */
+  float *mean;           /* [1] or NULL */
+  float *loss;           /* [rows] or NULL */
+  void *dx;              /* [rows, in] or NULL */
+  int64_t lddx;
+  void *dw;              /* [in, classes] or NULL */
+  int64_t lddw;
+  void *db;              /* [classes] or NULL */
+  void *workspace;
+  size_t workspace_bytes;
+  void *stream;
+} cada_linear_xent;
+
+int cada_linear_xent_workspace(cada_linear_xent *a); /* all but the pointers' contents, mean, scale, ignore_index and stream is read */
+int cada_linear_cross_entropy(const cada_linear_xent *a);
+
 /* AdamW over many tensors in one launch (two with clipping).  Step t = 1, 2, ... of tensor p with gradient g:
  *   g <- g * grad_scale * min(1, max_norm / norm)                 (norm: over grad_scale * all gradients; max_norm 0: no clipping;
  *                                                                  a norm past float32 counts as infinite and leaves zeros)

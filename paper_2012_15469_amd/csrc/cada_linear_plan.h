@@ -33,7 +33,7 @@ constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 struct Shape { int64_t M, N, K; };
 constexpr int64_t kMostTiles = ((int64_t)1 << 23) - 8;        // of a product: 512 threads each, two products, less than 2^32 threads in a launch
 // The cheapest cut of one or two products in one launch (one tile for both) by that estimate, which it returns; tiles up to `widest`.
-inline double cut(const Shape *s, int n, int type, bool direct, int widest, Cut *out) {
+inline double cut(const Shape *s, int n, int type, bool direct, int widest, Cut *out, int most_splits = 32) {
   const int64_t step = kStepBytes / (int64_t)type_bytes(type);
   const TileCost *costs = type == CADA_BF16 ? (direct ? kCostBf16 : kCostBf16Registers) : direct ? kCostF32 : kCostF32Registers;
   const int n_costs = type == CADA_BF16 && direct ? 4 : 2;
@@ -49,7 +49,7 @@ inline double cut(const Shape *s, int n, int type, bool direct, int widest, Cut 
     for (int i = 0; i < n; ++i) {
       const int64_t tiles = ceil_div(s[i].M, t.tile) * ceil_div(s[i].N, t.tile);
       for (int k : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 24, 32}) {
-        if (k > 1 && (steps[i] < 2 * k || tiles * k > (n == 1 ? 6 : 2) * kCUs)) break;
+        if (k > most_splits || (k > 1 && (steps[i] < 2 * k || tiles * k > (n == 1 ? 6 : 2) * kCUs))) break;
         if (tiles > kMostTiles) break;
         opt[i][n_opt[i]++] = Option{k, (double)(tiles * k), (double)ceil_div(steps[i], k), k > 1 ? (k * 4.0 + 2.0) * (double)s[i].M * (double)s[i].N / kJoinBytesPerUs : 0.0};
       }
@@ -202,6 +202,77 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
   if (b.pack_w) off += packed_bytes(in, out, elem);
   b.bytes = off;
   return b;
+}
+
+// A last layer's loss: the product [rows, classes] is formed whole once, for each row's statistics, and again in pieces of the classes, whose signal (softmax - target, [rows, piece]) lies in the
+// workspace while both gradients' products read it.
+constexpr int64_t kSignalBytes = (int64_t)128 << 20, kPieceStep = 256;
+constexpr int kLossGroups = 256;        // workgroups of the rows' statistics, at most: each leaves a part of the losses' sum
+struct LossHead { uint32_t done; float inverse; uint32_t pad[62]; double loss[kLossGroups]; int64_t used[kLossGroups]; };
+constexpr int strip_columns(int tile) { return tile == 256 ? 64 : 32; }        // of a wavefront's strip of a tile, which has one entry in a row's statistics
+struct LossPlan {
+  bool grads, signal, direct, copy_x, copy_w;
+  Cut logits, piece_logits, dx, dw;
+  int64_t piece, pieces, chunks, ldz, strips;      // strips: of the signal's rows, each with a part of db
+  int stat_floats;
+  size_t off_stats, off_info, off_label, off_loss, off_signal, off_dx, off_dw, off_db, off_x, off_w, bytes;
+};
+inline LossPlan plan_loss(const cada_linear_xent *a) {
+  LossPlan f{};
+  if (a->rows == 0) return f;
+  const int64_t rows = a->rows, in = a->in, classes = a->classes;
+  const size_t elem = type_bytes(a->type);
+  f.signal = a->dx || a->dw || a->db;
+  f.grads = a->dx || a->dw;
+  f.pieces = 1;
+  f.piece = classes;
+  if (f.signal) {
+    const int64_t most = std::max<int64_t>(kSignalBytes / (rows * (int64_t)elem) / kPieceStep * kPieceStep, 4 * kPieceStep);
+    f.pieces = ceil_div(classes, most);
+    if (f.pieces > 1) {
+      f.piece = ceil_div(ceil_div(classes, f.pieces), kPieceStep) * kPieceStep;
+      f.pieces = ceil_div(classes, f.piece);
+    }
+  }
+  // x is read along the contraction for the logits and across it for dw, which takes a copy without the rows that do not count (what they hold is not looked at); w the other way round.
+  const bool x_direct = a->dw || direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, classes, elem);
+  const bool tiny = no_tiles(rows, a->ldx, in, elem) || no_tiles(in, a->ldw, classes, elem);
+  const Shape whole = {rows, classes, in}, part = {rows, f.piece, in}, grads[2] = {{rows, in, f.piece}, {in, f.piece, rows}};
+  const Shape *first = a->dx ? grads : grads + 1;
+  const int n = (a->dx ? 1 : 0) + (a->dw ? 1 : 0);
+  Cut c[2][4] = {};
+  double time[2];
+  for (int direct = 0; direct < 2; ++direct) {
+    time[direct] = cut(&whole, 1, a->type, direct, widest_tile(in, elem), &c[direct][0], 1);
+    if (f.signal) time[direct] += f.pieces * cut(&part, 1, a->type, direct, widest_tile(in, elem), &c[direct][1], 1);
+    if (n > 0) time[direct] += f.pieces * cut(first, n, a->type, direct, widest_tile(classes, elem), c[direct] + 2);
+  }
+  if (!x_direct || !w_direct) time[1] += kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, classes, elem));
+  f.direct = (x_direct && w_direct) || tiny || time[1] < time[0];
+  f.copy_x = a->dw || (f.direct && !x_direct) || tiny;
+  f.copy_w = (f.direct && !w_direct) || tiny;
+  const Cut *mine = c[f.direct];
+  f.logits = mine[0];
+  f.piece_logits = mine[1];
+  if (a->dx) f.dx = mine[2];
+  if (a->dw) f.dw = mine[2 + n - 1];
+  f.chunks = ceil_div(classes, f.logits.tile) * (f.logits.tile / strip_columns(f.logits.tile));
+  f.stat_floats = a->smoothing != 0.0 ? 4 : 2;
+  f.ldz = eights(f.piece);
+  if (f.signal) f.strips = 2 * ceil_div(rows, f.piece_logits.tile);
+  size_t off = ops_align(sizeof(LossHead));
+  f.off_stats = off; off += ops_align((size_t)f.chunks * rows * f.stat_floats * 4);
+  f.off_info = off; off += ops_align((size_t)rows * 16);
+  f.off_label = off; off += ops_align((size_t)rows * 4);
+  f.off_loss = off; off += a->loss ? 0 : ops_align((size_t)rows * 4);
+  f.off_signal = off; off += f.grads ? ops_align((size_t)rows * f.ldz * elem) : 0;
+  f.off_dx = off; off += a->dx && (f.pieces > 1 || f.dx.splits > 1) ? ops_align((size_t)f.dx.splits * rows * eights(in) * 4) : 0;
+  f.off_dw = off; off += a->dw ? partial_bytes(f.dw, in, f.piece) : 0;
+  f.off_db = off; off += a->db ? ops_align((size_t)f.strips * f.piece * 4) : 0;
+  f.off_x = off; off += f.copy_x ? packed_bytes(rows, in, elem) : 0;
+  f.off_w = off; off += f.copy_w ? packed_bytes(in, classes, elem) : 0;
+  f.bytes = off;
+  return f;
 }
 
 }  // namespace cada

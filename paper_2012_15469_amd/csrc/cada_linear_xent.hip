@@ -1,0 +1,450 @@
+// The softmax cross-entropy of a last layer's product, with its gradients, without the logits in memory (cada_ops.h).
+//
+// The logits' tiles (cada_linear_tiles.h) end in statistics: of each row, and of each strip of 32 or 64 columns, the largest logit and the sum of the exponentials of the
+// distances to it.  A row's strips are then joined, as one goes along, to the row's largest and its sum, which is its loss.  For the gradients the logits are formed again in
+// pieces of the classes; their tiles end in softmax - target in the operands' type, from which the products of a layer's gradients are taken while it is in the caches: dw is finished piece by
+// piece, dx is added up in float32.  That is four products where keeping the logits would take three, and memory for one piece instead of all.
+#include <algorithm>
+
+#include "cada_linear_tiles.h"
+
+namespace cada {
+namespace {
+
+struct Stat { float top, sum, distance, left; };      // distance: the sum of z - top over the classes that are left (smoothing), left: their number
+struct RowInfo { float base, f_total, f_each; int32_t label; };      // label: < 0 for a row without gradient
+struct Loss {
+  const void *labels, *bias;
+  LossHead *head;
+  float *stats;              // [chunks][rows][stat_floats]
+  RowInfo *info;
+  float *z_label, *loss, *mean;
+  void *signal;              // [rows, piece] or null
+  float *db_part;            // [strips][piece] or null
+  int64_t rows, ignore, ldz, chunks;
+  int32_t classes, label_bytes, first;      // first: the piece's first class
+  int32_t lanes;             // rows of a workgroup of k_rows, as a power of two
+  float smoothing, keep, scale;      // keep = 1 - smoothing, rounded once
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kInf = __builtin_inff();
+
+__device__ __forceinline__ int64_t label_at(const void *labels, int bytes, int64_t r) {
+  return bytes == 8 ? static_cast<const int64_t *>(labels)[r] : (int64_t)static_cast<const int32_t *>(labels)[r];
+}
+__device__ __forceinline__ bool counts(const Loss &q, int64_t label) { return label != q.ignore && label >= 0 && label < q.classes; }
+
+// Largest and sum over the LANES lanes (a power of two) that are next to each other.
+template <int LANES> __device__ __forceinline__ float lanes_max(float x) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  return x;
+}
+template <int LANES> __device__ __forceinline__ float lanes_sum(float x) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+
+// A tile's logits into statistics.
+template <int BM> struct ToStatistics {
+  static constexpr bool kAll = true;
+  const Loss &q;
+  int32_t *label;            // [BM], in LDS
+  float bias[8];
+  __device__ __forceinline__ ToStatistics(const Loss &loss, int32_t *lds) : q(loss), label(lds) {}
+  __device__ __forceinline__ void begin(const Product &p, int64_t m0, int t) {
+    if (t >= BM) return;
+    const int64_t l = m0 + t < p.M ? label_at(q.labels, q.label_bytes, m0 + t) : -1;
+    label[t] = counts(q, l) ? (int32_t)l : -1;
+  }
+  template <typename T> __device__ __forceinline__ void columns(int n, int64_t left) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = 0.f;
+    if (q.bias) load8_n(static_cast<const T *>(q.bias) + n, left, bias);
+  }
+  template <typename T, int LANES> __device__ __forceinline__ void row(const Product &p, uint32_t, int64_t m, int local, int n, int64_t left, float (&z)[8]) {
+    float top = -kInf;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      z[e] = e < left ? z[e] + bias[e] : -kInf;
+      top = fmaxf(top, z[e]);
+    }
+    top = lanes_max<LANES>(top);
+    // (a strip of nothing but -inf and NaN: its exponentials are taken against 0, so that only a NaN makes the sum NaN)
+    const float base = top == -kInf ? 0.f : top;
+    float sum = 0.f, distance = 0.f, in = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f((z[e] - base) * kLog2e);
+    sum = lanes_sum<LANES>(sum);
+    if (q.smoothing != 0.f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool is_in = z[e] != -kInf;
+        in += is_in ? 1.f : 0.f;
+        distance += is_in ? z[e] - base : 0.f;
+      }
+      in = lanes_sum<LANES>(in);
+      distance = lanes_sum<LANES>(distance);
+    }
+    if (m >= p.M) return;
+    const int at = label[local] - n;
+    if (at >= 0 && at < 8) {
+      float zl = z[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) zl = at == e ? z[e] : zl;
+      q.z_label[m] = zl;
+    }
+    if ((threadIdx.x & (LANES - 1)) == 0) {
+      const int64_t to = (int64_t)(n / (LANES * 8)) * q.rows + m;
+      if (q.smoothing != 0.f) reinterpret_cast<Stat *>(q.stats)[to] = Stat{top, sum, distance, in};
+      else reinterpret_cast<float2 *>(q.stats)[to] = float2{top, sum};
+    }
+  }
+  template <int LANES> __device__ __forceinline__ void end(int64_t, int, int64_t) const {}
+};
+
+// A tile's logits into softmax - target, times scale / count, and its column sums over a strip of rows.
+template <int BM> struct ToSignal {
+  static constexpr bool kAll = true;
+  const Loss &q;
+  RowInfo *info;             // [BM], in LDS
+  float bias[8], column[8], inverse, f_keep;
+  __device__ __forceinline__ ToSignal(const Loss &loss, RowInfo *lds) : q(loss), info(lds) {}
+  __device__ __forceinline__ void begin(const Product &p, int64_t m0, int t) {
+    inverse = q.head->inverse;
+    f_keep = q.keep * inverse;
+    if (t >= BM) return;
+    RowInfo r = {0.f, 0.f, 0.f, -1};
+    if (m0 + t < p.M) r = q.info[m0 + t];
+    r.f_total *= inverse;
+    r.f_each *= inverse;
+    info[t] = r;
+  }
+  template <typename T> __device__ __forceinline__ void columns(int n, int64_t left) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = column[e] = 0.f;
+    if (q.bias) load8_n(static_cast<const T *>(q.bias) + q.first + n, left, bias);
+  }
+  template <typename T, int LANES> __device__ __forceinline__ void row(const Product &p, uint32_t, int64_t m, int local, int n, int64_t left, float (&z)[8]) {
+    if (m >= p.M || left <= 0) return;
+    const RowInfo r = info[local];
+    const int at = r.label - q.first - n;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      z[e] += bias[e];
+      float g = __builtin_amdgcn_exp2f((z[e] - r.base) * kLog2e) * r.f_total;
+      if (q.smoothing != 0.f) g -= z[e] != -kInf ? r.f_each : 0.f;
+      g -= at == e ? f_keep : 0.f;
+      z[e] = r.label >= 0 && e < left ? g : 0.f;
+      column[e] += z[e];
+    }
+    if (q.signal) store8_n(static_cast<T *>(q.signal) + m * q.ldz + n, 8, z);        // (whole: the rows have room for it)
+  }
+  template <int LANES> __device__ __forceinline__ void end(int64_t strip, int n, int64_t left) {
+    if (!q.db_part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int o = LANES; o < 64; o <<= 1) column[e] += __shfl_xor(column[e], o, 64);
+    if ((threadIdx.x & 63) < LANES) store8_n(q.db_part + strip * columns_of_piece + n, left, column);
+  }
+  int64_t columns_of_piece;
+};
+
+template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
+__global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product p, const Loss q) {
+  __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
+  __shared__ int32_t label[BM];
+  if (blockIdx.x == 0 && threadIdx.x == 0) q.head->done = 0;
+  const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
+  if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<BM>(q, label));
+}
+template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
+__global__ __launch_bounds__(64 * WY * WX * KW) void k_signal(const Product p, const Loss q) {
+  __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
+  __shared__ RowInfo info[BM];
+  const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
+  if (tile == ~0u) return;
+  ToSignal<BM> out(q, info);
+  out.columns_of_piece = p.N;
+  tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, out);
+}
+
+// Joins statistics `b` to `a`: both against the larger of the two largest.
+__device__ __forceinline__ void join(Stat &a, const Stat &b) {
+  if (b.top == -kInf) {        // no class left there, or NaN
+    a.sum += b.sum;
+    a.left += b.left;
+    a.distance += b.distance;
+    return;
+  }
+  if (a.top == -kInf) {
+    a = Stat{b.top, b.sum + a.sum, b.distance + a.distance, b.left + a.left};
+    return;
+  }
+  const float top = fmaxf(a.top, b.top);
+  a.sum = a.sum * __builtin_amdgcn_exp2f((a.top - top) * kLog2e) + b.sum * __builtin_amdgcn_exp2f((b.top - top) * kLog2e);
+  a.distance = fmaf(a.left, a.top - top, a.distance) + fmaf(b.left, b.top - top, b.distance);
+  a.left += b.left;
+  a.top = top;
+}
+
+// 2^lanes rows by the other threads of 1024 over their strips; a row's strips are joined in one order.  The last workgroup adds the losses up, in the workgroups' order.
+__global__ __launch_bounds__(1024) void k_rows(const Loss q) {
+  __shared__ Stat part[1024];
+  __shared__ float losses[64];
+  __shared__ uint8_t used_rows[64];
+  __shared__ bool last;
+  const int here = 1 << q.lanes, t = threadIdx.x, row = t & (here - 1), lane = t >> q.lanes, high = 1024 >> q.lanes;
+  double sum = 0.0;
+  int64_t used_sum = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * here; r0 < q.rows; r0 += (int64_t)gridDim.x * here) {
+    const int64_t r = r0 + row, at = min(r, q.rows - 1);
+    Stat s = {-kInf, 0.f, 0.f, 0.f};
+    if (q.smoothing != 0.f) {
+#pragma unroll 4
+      for (int64_t c = lane; c < q.chunks; c += high) join(s, reinterpret_cast<const Stat *>(q.stats)[c * q.rows + at]);
+    } else {
+#pragma unroll 8
+      for (int64_t c = lane; c < q.chunks; c += high) {
+        const float2 x = reinterpret_cast<const float2 *>(q.stats)[c * q.rows + at];
+        join(s, Stat{x.x, x.y, 0.f, 0.f});
+      }
+    }
+    part[t] = s;
+    for (int h = high / 2; h > 0; h >>= 1) {
+      __syncthreads();
+      if (lane < h) {
+        join(s, part[t + (h << q.lanes)]);
+        part[t] = s;
+      }
+    }
+    if (lane == 0) {
+      losses[row] = 0.f;
+      used_rows[row] = 0;
+    }
+    if (lane == 0 && r < q.rows) {
+      const int64_t label = label_at(q.labels, q.label_bytes, r);
+      const bool used = label != q.ignore, known = counts(q, label), none = s.top == -kInf && s.sum == 0.f;
+      const float base = s.top == -kInf ? 0.f : s.top;
+      float l = logf(s.sum) - q.keep * ((known ? q.z_label[r] : 0.f) - base);
+      if (q.smoothing != 0.f) l -= q.smoothing * (s.distance / s.left);
+      if (none) l = kInf;
+      if (!known) l = __builtin_nanf("");
+      l = used ? l : 0.f;
+      losses[row] = l;
+      used_rows[row] = used;
+      if (q.loss) q.loss[r] = l;
+      q.info[r] = RowInfo{base, 1.f / s.sum, q.smoothing != 0.f ? q.smoothing / s.left : 0.f, known && !none ? (int32_t)label : -1};
+    }
+    __syncthreads();
+    if (t == 0) {
+      for (int i = 0; i < here; ++i) {
+        sum += (double)losses[i];
+        used_sum += used_rows[i];
+      }
+    }
+    __syncthreads();
+  }
+  if (t == 0) {
+    __hip_atomic_store(&q.head->loss[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&q.head->used[blockIdx.x], used_sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (they are where the last workgroup reads them before this one is counted)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = __hip_atomic_fetch_add(&q.head->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last || t >= 64) return;
+  sum = 0.0;
+  used_sum = 0;
+  for (int i = t; i < (int)gridDim.x; i += 64) {
+    sum += __hip_atomic_load(&q.head->loss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    used_sum += __hip_atomic_load(&q.head->used[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  sum = wave_sum_f64(sum);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) used_sum += __shfl_xor(used_sum, o, 64);
+  if (t == 0) {
+    const int64_t count = max(used_sum, (int64_t)1);
+    if (q.mean) *q.mean = (float)(sum / (double)count);
+    q.head->inverse = q.scale / (float)count;
+  }
+}
+
+// x in rows on 16-byte boundaries, zeros for those that do not count.
+template <typename T>
+__global__ __launch_bounds__(256) void k_copy_rows(const Loss q, const Pack p) {
+  constexpr int E = Elem<T>::kPer16;
+  const int64_t per = p.ldd / E;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.rows * per; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per, col = (i - row * per) * E;
+    const bool in = counts(q, label_at(q.labels, q.label_bytes, row));
+    u32x4v x = load16_n(static_cast<const T *>(p.src) + row * p.ld + col, p.cols - col);
+    if (!in) x = u32x4v{0, 0, 0, 0};
+    *reinterpret_cast<u32x4v *>(static_cast<T *>(p.dst) + row * p.ldd + col) = x;
+  }
+}
+__global__ void k_no_rows(float *mean) { *mean = 0.f; }
+
+// ---- host ----
+
+template <typename T, int E, int WY, int WX, int KW>
+void tiles(const Product &p, const Loss &q, bool statistics, bool direct, hipStream_t st) {
+  const unsigned grid = (unsigned)(ceil_div(tiles_of(p), 8) * 8), threads = 64 * WY * WX * KW;
+  auto launch = [&](auto dir, auto stages) {
+    if (statistics) k_statistics<T, E, WY, WX, dir(), stages(), KW><<<grid, threads, 0, st>>>(p, q);
+    else k_signal<T, E, WY, WX, dir(), stages(), KW><<<grid, threads, 0, st>>>(p, q);
+  };
+  if constexpr (E <= 64) {
+    if (!direct) return launch(std::false_type(), std::integral_constant<int, 2>());
+  }
+  if constexpr (E < 256) {
+    if (deep(E, tiles_of(p))) return launch(std::true_type(), std::integral_constant<int, 4>());
+  }
+  launch(std::true_type(), std::integral_constant<int, 2>());
+}
+template <typename T>
+int logits(const Product &p, const Loss &q, int tile, bool statistics, bool direct, hipStream_t st) {
+  if (tile == 32) tiles<T, 32, 1, 1, 4>(p, q, statistics, direct, st);
+  if (tile == 64) tiles<T, 64, 2, 2, 1>(p, q, statistics, direct, st);
+  if constexpr (sizeof(T) == 2) {
+    if (tile == 128) tiles<T, 128, 2, 4, 1>(p, q, statistics, direct, st);
+    if (tile == 256) tiles<T, 256, 2, 4, 1>(p, q, statistics, direct, st);
+  }
+  return ops_launched("linear cross-entropy");
+}
+
+template <typename T>
+int loss(const cada_linear_xent *a, const LossPlan &f) {
+  hipStream_t st = static_cast<hipStream_t>(a->stream);
+  char *ws = static_cast<char *>(a->workspace);
+  Loss q{};
+  q.labels = a->labels; q.bias = a->bias; q.head = reinterpret_cast<LossHead *>(ws);
+  q.stats = reinterpret_cast<float *>(ws + f.off_stats); q.info = reinterpret_cast<RowInfo *>(ws + f.off_info); q.z_label = reinterpret_cast<float *>(ws + f.off_label);
+  q.loss = a->loss ? a->loss : reinterpret_cast<float *>(ws + f.off_loss); q.mean = a->mean;
+  q.rows = a->rows; q.ignore = a->ignore_index; q.chunks = f.chunks; q.classes = (int32_t)a->classes; q.label_bytes = a->label_bytes;
+  q.smoothing = (float)a->smoothing; q.keep = (float)(1.0 - a->smoothing); q.scale = (float)a->scale;
+  const T *x = static_cast<const T *>(a->x), *w = static_cast<const T *>(a->w);
+  int64_t ldx = a->ldx, ldw = a->ldw, x_cols = a->in, w_cols = a->classes;
+  if (f.copy_x) {
+    const Pack k = {a->x, ws + f.off_x, a->ldx, a->rows, a->in, packed_ld(a->in)};
+    k_copy_rows<T><<<many(a->rows * (k.ldd / Elem<T>::kPer16)), 256, 0, st>>>(q, k);
+    if (int rc = ops_launched("linear cross-entropy copy")) return rc;
+    x = static_cast<const T *>(k.dst); ldx = x_cols = k.ldd;
+  }
+  if (f.copy_w) {
+    Packs k{};
+    k.p[0] = Pack{a->w, ws + f.off_w, a->ldw, a->in, a->classes, packed_ld(a->classes)};
+    if (int rc = linear_pack(a->type, k, st)) return rc;
+    w = static_cast<const T *>(k.p[0].dst); ldw = w_cols = k.p[0].ldd;
+  }
+  Product z{};
+  lay(&z, f.logits, x, ldx, w, ldw, a->rows, a->classes, a->in, nullptr);
+  z.b_cols = w_cols;
+  if (int rc = logits<T>(z, q, f.logits.tile, true, f.direct, st)) return rc;
+  while (q.lanes < 6 && ((int64_t)kLossGroups << q.lanes) < a->rows) ++q.lanes;
+  k_rows<<<(unsigned)std::min<int64_t>(ceil_div(a->rows, 1 << q.lanes), kLossGroups), 1024, 0, st>>>(q);
+  if (int rc = ops_launched("linear cross-entropy rows")) return rc;
+  if (!f.signal) return CADA_OK;
+  void *signal = f.grads ? ws + f.off_signal : nullptr;
+  for (int64_t i = 0; i < f.pieces; ++i) {
+    const int64_t first = i * f.piece, here = std::min(f.piece, a->classes - first);
+    q.first = (int32_t)first; q.signal = signal; q.ldz = f.ldz; q.db_part = a->db ? reinterpret_cast<float *>(ws + f.off_db) : nullptr;
+    lay(&z, f.piece_logits, x, ldx, w + first, ldw, a->rows, here, a->in, nullptr);
+    z.b_cols = w_cols - first;
+    if (int rc = logits<T>(z, q, f.piece_logits.tile, false, f.direct, st)) return rc;
+    Product dx{}, dw{};
+    Join j{};
+    if (a->dx) {
+      Cut c = f.dx;
+      c.splits = (int)std::min<int64_t>(c.splits, ceil_div(here, c.k_per_split));        // (the last piece may have less)
+      lay(&dx, c, signal, f.ldz, w + first, ldw, a->rows, a->in, here, nullptr);
+      if (f.pieces > 1 || f.dx.splits > 1) dx.partial = reinterpret_cast<float *>(ws + f.off_dx);
+      dx.add = i > 0;
+      dx.epi.out = a->dx; dx.epi.ldo = a->lddx;
+    }
+    if (a->dw) {
+      lay(&dw, f.dw, x, ldx, signal, f.ldz, a->in, here, a->rows, reinterpret_cast<float *>(ws + f.off_dw));
+      dw.a_cols = x_cols; dw.b_cols = eights(here);
+      dw.epi.out = static_cast<T *>(a->dw) + first; dw.epi.ldo = a->lddw;
+    }
+    if (f.grads) {
+      if (int rc = linear_products(a->type, a->dx ? f.dx.tile : f.dw.tile, f.direct, dx, dw, st)) return rc;
+    }
+    if (i == f.pieces - 1) {
+      j.p[0] = dx;
+      j.p[0].splits = f.dx.splits;
+    }
+    j.p[1] = dw;
+    if (a->db) { j.db_part = q.db_part; j.db = static_cast<T *>(a->db) + first; j.db_parts = (int)f.strips; j.db_n = (int)here; }
+    if (int rc = linear_join(a->type, j, st)) return rc;
+  }
+  return CADA_OK;
+}
+
+bool check(const cada_linear_xent *a) {
+  if (!a) { set_error("the arguments are NULL"); return false; }
+  if (a->rows < 0 || a->rows > (int64_t)1 << 30) { set_error("rows must be in [0, 2^30] (got %lld)", (long long)a->rows); return false; }
+  if (a->in < 1 || a->in > CADA_MAX_WIDTH || a->classes < 1 || a->classes > CADA_MAX_WIDTH) { set_error("in and classes must be in [1, %d] (got %lld, %lld)", CADA_MAX_WIDTH, (long long)a->in, (long long)a->classes); return false; }
+  if (a->type != CADA_F32 && a->type != CADA_BF16) { set_error("type must be CADA_F32 or CADA_BF16 (got %d)", a->type); return false; }
+  if (a->label_bytes != 4 && a->label_bytes != 8) { set_error("label_bytes must be 4 or 8 (got %d)", a->label_bytes); return false; }
+  if (!(a->smoothing >= 0.0 && a->smoothing < 1.0)) { set_error("smoothing must be in [0, 1)"); return false; }
+  const int64_t t = std::max({ceil_div(a->rows, 64) * ceil_div(a->classes, 64), ceil_div(a->rows, 64) * ceil_div(a->in, 64), ceil_div(a->in, 64) * ceil_div(a->classes, 64)});
+  if (t > kMostTiles) { set_error("more than %lld tiles of 64 x 64 outputs", (long long)kMostTiles); return false; }
+  return true;
+}
+
+}  // namespace
+}  // namespace cada
+
+using namespace cada;
+
+extern "C" {
+
+int cada_linear_xent_workspace(cada_linear_xent *a) {
+  if (!check(a)) return CADA_EINVAL;
+  a->workspace_bytes = plan_loss(a).bytes;
+  return CADA_OK;
+}
+
+int cada_linear_cross_entropy(const cada_linear_xent *a) {
+  if (!check(a)) return CADA_EINVAL;
+  const bool any = a->rows > 0;
+  if (any) {
+    if (!ops_check_table("x", a->x, a->ldx, a->in, a->type) || !ops_check_table("w", a->w, a->ldw, a->classes, a->type)) return CADA_EINVAL;
+    if (a->bias && !ops_check_table("bias", a->bias, a->classes, a->classes, a->type)) return CADA_EINVAL;
+    if (!a->labels) { set_error("labels is NULL"); return CADA_EINVAL; }
+    if (reinterpret_cast<uintptr_t>(a->labels) % a->label_bytes != 0) { set_error("labels is not aligned to its elements"); return CADA_EINVAL; }
+    if (a->dx && !ops_check_table("dx", a->dx, a->lddx, a->in, a->type)) return CADA_EINVAL;
+  }
+  if (a->dw && !ops_check_table("dw", a->dw, a->lddw, a->classes, a->type)) return CADA_EINVAL;
+  if (a->db && !ops_check_table("db", a->db, a->classes, a->classes, a->type)) return CADA_EINVAL;
+  if ((a->mean && !ops_check_table("mean", a->mean, 1, 1, CADA_F32)) || (a->loss && !ops_check_table("loss", a->loss, 1, 1, CADA_F32))) return CADA_EINVAL;
+  const LossPlan f = plan_loss(a);
+  if (int rc = ops_check_workspace(a->workspace, a->workspace_bytes, f.bytes)) return rc;
+  const size_t elem = type_bytes(a->type);
+  const Span outs[] = {span("dx", any ? a->dx : nullptr, a->rows, a->lddx, a->in, elem), span("dw", a->dw, a->in, a->lddw, a->classes, elem), span("db", a->db, 1, a->classes, a->classes, elem),
+                       span("loss", a->loss, (size_t)a->rows * 4), span("mean", a->mean, 4), span("workspace", a->workspace, f.bytes)};
+  const Span ins[] = {span("x", any ? a->x : nullptr, a->rows, a->ldx, a->in, elem), span("w", any ? a->w : nullptr, a->in, a->ldw, a->classes, elem), span("bias", any ? a->bias : nullptr, 1, a->classes, a->classes, elem),
+                      span("labels", a->labels, (size_t)a->rows * a->label_bytes)};
+  for (int i = 0; i < 6; ++i) {
+    for (const Span &in : ins)
+      if (!ops_apart(outs[i], in)) return CADA_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (!ops_apart(outs[i], outs[j])) return CADA_EINVAL;
+  }
+  if (!any) {
+    if (a->mean) {
+      k_no_rows<<<1, 1, 0, static_cast<hipStream_t>(a->stream)>>>(a->mean);
+      if (int rc = ops_launched("linear cross-entropy")) return rc;
+    }
+    cada_linear_grad g{};
+    g.in = a->in; g.out = a->classes; g.type = a->type; g.dw = a->dw; g.lddw = a->lddw; g.db = a->db; g.stream = a->stream;
+    return cada_linear_backward(&g);        // (clears both)
+  }
+  return a->type == CADA_BF16 ? loss<bf16>(a, f) : loss<float>(a, f);
+}
+
+}  // extern "C"

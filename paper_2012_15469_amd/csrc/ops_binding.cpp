@@ -328,6 +328,48 @@ PyObject *embedding_backward(PyObject *, PyObject *const *args, Py_ssize_t n_arg
   });
 }
 
+// (x, w, labels, bias, smoothing, ignore_index, scale, need_dx, need_dw, need_db, dx, dw, db, workspace, stream) -> (mean, losses, dx, dw, db)
+PyObject *linear_cross_entropy(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject * {
+    if (n_args != 15) refuse("linear_cross_entropy takes 15 arguments");
+    const at::Tensor &x = needed(args[0], "x"), &w = needed(args[1], "w"), &labels = needed(args[2], "labels");
+    first(x, "x");
+    if (w.dim() != 2) refuse("w must be [in, classes]");
+    cada_linear_xent a{};
+    a.rows = x.size(0); a.in = x.size(1); a.classes = w.size(1); a.type = type_of(x);
+    void *p;
+    table("x", x, a.rows, a.in, x, &p, &a.ldx); a.x = p;
+    table("w", w, a.in, a.classes, x, &p, &a.ldw); a.w = p;
+    whole_numbers("labels", labels, a.rows, x, &a.labels, &a.label_bytes);
+    if (const at::Tensor *t = tensor(args[3], "bias")) { vector("bias", *t, a.classes, x, &p); a.bias = p; }
+    a.smoothing = PyFloat_AsDouble(args[4]); a.ignore_index = PyLong_AsLongLong(args[5]); a.scale = PyFloat_AsDouble(args[6]);
+    if (PyErr_Occurred()) throw Failed{};
+    const at::Tensor loss = at::empty({a.rows}, x.options().dtype(at::kFloat)), mean = at::empty({}, x.options().dtype(at::kFloat));
+    a.loss = loss.data_ptr<float>(); a.mean = mean.data_ptr<float>();
+    at::Tensor dx, dw, db;
+    if (args[7] == Py_True) {
+      const at::Tensor *t = tensor(args[10], "dx");
+      dx = t ? *t : fresh({a.rows, a.in}, x);
+      table("dx", dx, a.rows, a.in, x, &a.dx, &a.lddx);
+    }
+    if (args[8] == Py_True) {
+      const at::Tensor *t = tensor(args[11], "dw");
+      dw = t ? *t : fresh({a.in, a.classes}, x);
+      table("dw", dw, a.in, a.classes, x, &a.dw, &a.lddw);
+    }
+    if (args[9] == Py_True) {
+      const at::Tensor *t = tensor(args[12], "db");
+      db = t ? *t : fresh({a.classes}, x);
+      vector("db", db, a.classes, x, &a.db);
+    }
+    const at::Tensor ws = workspace(&a, args[13], cada_linear_xent_workspace, x);
+    a.stream = stream_of(args[14]);
+    check(cada_linear_cross_entropy(&a));
+    PyObject *m = wrap(mean), *l = wrap(loss), *gx = wrap(dx), *gw = wrap(dw), *gb = wrap(db);
+    return Py_BuildValue("(NNNNN)", m, l, gx, gw, gb);
+  });
+}
+
 PyObject *set_error_class(PyObject *, PyObject *o) {
   Py_INCREF(o);
   Py_XDECREF(g_error);
@@ -343,6 +385,7 @@ PyMethodDef methods[] = {
     {"layer_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(layer_norm_backward)), METH_FASTCALL, nullptr},
     {"embedding_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(embedding_forward)), METH_FASTCALL, nullptr},
     {"embedding_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(embedding_backward)), METH_FASTCALL, nullptr},
+    {"linear_cross_entropy", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(linear_cross_entropy)), METH_FASTCALL, nullptr},
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -4,6 +4,7 @@
 ``layer_norm_forward`` / ``layer_norm_backward``: layer norm of the rows of a table, and its gradients.
 ``embedding_forward`` / ``embedding_backward``: rows of a table by integer tokens, and the table's gradient.
 ``cross_entropy``: the softmax cross-entropy over any number of classes with its gradient.
+``linear_cross_entropy``: the same loss of a last layer's product without its logits in memory, with the layer's gradients.
 ``AdamW``: the step over many tensors at once, moments in 32 or in 8 bits.
 
 Tensors are float32 or bfloat16 on one GPU.  Work goes to ``stream``, by default the device's current stream at the call (AdamW: the one that was current when
@@ -11,7 +12,7 @@ it was made, for its steps too), and nothing synchronises the host; inputs must 
 unless one is, come from torch's caching allocator and belong to that stream.
 
 The calls do not take part in autograd: operands that require gradients are read as they are, outputs have no history, and what is written in place
-(outputs handed in, parameters) counts no version.  The ``..._backward`` functions and the gradient of ``cross_entropy`` are what a backward pass is made of.
+(outputs handed in, parameters) counts no version.  The ``..._backward`` functions and the gradients of the losses are what a backward pass is made of.
 """
 from __future__ import annotations
 
@@ -140,6 +141,18 @@ def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, *, smoothing: floa
     logits [rows, classes]; labels int32 or int64 [rows].  Rows labelled ``ignore_index`` count nowhere; classes at -inf are ruled out.  ``grad`` may be
     the logits themselves.  Losses are float32, the gradient has the logits' type."""
     return _call(_ops.cross_entropy, logits, stream, logits, labels, smoothing, ignore_index, scale, bool(need_grad), grad, workspace)
+
+
+def linear_cross_entropy(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, bias: Optional[torch.Tensor] = None, *, smoothing: float = 0.0, ignore_index: int = -100,
+                         scale: float = 1.0, need_dx: bool = True, need_dw: bool = True, need_db: bool = True, dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
+                         db: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                         ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(mean loss, loss of each row, dx, dw, db): cross_entropy of the logits x w + bias and the gradients of scale * mean loss, without the logits in memory.
+
+    x [rows, in], w [in, classes], bias [classes] or None, all of one type; labels int32 or int64 [rows].  Rows labelled ``ignore_index`` count nowhere, whatever x holds there; classes
+    whose bias is -inf are ruled out.  db is None without a bias unless a ``db`` to write is given.  Outputs handed in are written, not added to."""
+    return _call(_ops.linear_cross_entropy, x, stream, x, w, labels, bias, smoothing, ignore_index, scale, bool(need_dx), bool(need_dw), bool(need_db) and (bias is not None or db is not None),
+                 dx, dw, db, workspace)
 
 
 class AdamW:

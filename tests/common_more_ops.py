@@ -27,7 +27,13 @@ class cada_embedding_grad(C.Structure):
                 ("scale", F64), ("dw", P), ("lddw", I64)] + _END
 
 
-for _name, _type in (("cada_layer_norm_forward", cada_norm), ("cada_layer_norm_backward", cada_norm_grad), ("cada_layer_norm_backward_workspace", cada_norm_grad),
+class cada_linear_xent(C.Structure):
+    _fields_ = [("rows", I64), ("in_", I64), ("classes", I64), ("type", I32), ("label_bytes", I32), ("x", P), ("ldx", I64), ("w", P), ("ldw", I64), ("bias", P), ("labels", P),
+                ("ignore_index", I64), ("smoothing", F64), ("scale", F64), ("mean", P), ("loss", P), ("dx", P), ("lddx", I64), ("dw", P), ("lddw", I64), ("db", P)] + _END
+
+
+for _name, _type in (("cada_linear_xent_workspace", cada_linear_xent), ("cada_linear_cross_entropy", cada_linear_xent),
+                     ("cada_layer_norm_forward", cada_norm), ("cada_layer_norm_backward", cada_norm_grad), ("cada_layer_norm_backward_workspace", cada_norm_grad),
                      ("cada_embedding_forward", cada_embedding), ("cada_embedding_backward", cada_embedding_grad), ("cada_embedding_backward_workspace", cada_embedding_grad)):
     _f = getattr(_lib, _name)
     _f.restype, _f.argtypes = C.c_int, [C.POINTER(_type)]

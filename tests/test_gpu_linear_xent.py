@@ -1,0 +1,259 @@
+"""The loss of a last layer's product and its gradients against the definitions in 64 bits.
+
+Tolerances, with e = 2^-24 and n = in: a logit is a float32 sum of n products, off by (n + 2) e |x| |w| (the row's sum of magnitudes); call its largest over a row dz.  An exponential's argument is off by 2 dz and
+2 e |z - top| log2 e and what the exponential itself is, 4 e, so probabilities are off by p (2 dz + (2 + 2 |z - top|) 2 e + s), s = (classes / 64 + 64) e for the sums; losses by dz (1 + 1) + that of the sum and of the
+logarithm.  A signal g = (p - t) scale / count is off by what p is and 3 e (p + t), and in bf16 by 2^-8 |g|, of which a product's sum of k terms passes on the sum of magnitudes, with (k + 2) e more, and
+its output half a step (2^-8 or e); db is of the signal before that rounding, in float32 sums over the rows."""
+import math
+
+import pytest
+import torch
+
+from paper_2012_15469_amd import ops
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+E = 2.0 ** -24
+
+
+def half_step(dtype):
+    return 2.0 ** -8 if dtype == torch.bfloat16 else E
+
+
+def near(got, want, limit, what):
+    assert got.shape == want.shape
+    worst = float(((got.double() - want).abs() / (limit + half_step(got.dtype) * (want.abs() + limit) + 1e-37)).max()) if got.numel() else 0.0
+    assert worst <= 1.0, "%s: off by %g of its tolerance" % (what, worst)
+
+
+def problem(rows, k, classes, dtype, seed=0, pad=0, shift=0, bias=True, ignored=0.0, masked=0.0, bits=torch.int64):
+    gen = torch.Generator(device="cuda"); gen.manual_seed(seed + rows * 7 + k * 3 + classes)
+    x = torch.randn(rows, k + pad + shift, generator=gen, device="cuda").to(DT[dtype])[:, shift:shift + k]
+    w = (torch.randn(k, classes + pad + shift, generator=gen, device="cuda") * (2.0 / math.sqrt(k))).to(DT[dtype])[:, shift:shift + classes]
+    out = torch.rand(classes, generator=gen, device="cuda") < masked
+    out[0] = False
+    allowed = torch.nonzero(~out)[:, 0]
+    labels = allowed[torch.randint(allowed.numel(), (rows,), generator=gen, device="cuda")]
+    labels = labels.masked_fill(torch.rand(rows, generator=gen, device="cuda") < ignored, -100).to(bits)
+    b = torch.randn(classes, generator=gen, device="cuda").masked_fill(out, -math.inf).to(DT[dtype]) if bias else None
+    return x, w, labels, b
+
+
+def definition(x, w, labels, bias, smoothing, ignore, scale):
+    """Losses, signal and the probabilities' part of its error."""
+    classes = w.shape[1]
+    z = x.double() @ w.double() + (0.0 if bias is None else bias.double())
+    top = z.amax(1, keepdim=True)
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    left = z > -math.inf
+    n_left = left.sum(1, keepdim=True).double()
+    used = labels != ignore
+    known = (labels >= 0) & (labels < classes)
+    at = torch.where(known, labels, 0).long()[:, None]
+    target = torch.zeros_like(z).scatter_(1, at, 1.0 - smoothing) + (smoothing * left.double() / n_left if smoothing else 0.0)
+    loss = lse[:, 0] - (1 - smoothing) * z.gather(1, at)[:, 0] - (smoothing * torch.where(left, z, 0.0).sum(1) / n_left[:, 0] if smoothing else 0.0)
+    loss = torch.where(used, torch.where(known, loss, math.nan), 0.0)
+    count = max(1, int(used.sum()))
+    p = torch.exp(z - lse)
+    in_use = (used & known)[:, None]
+    dz = ((x.shape[1] + 2) * E * (x.double().abs() @ w.double().abs() + (0.0 if bias is None else torch.where(bias == -math.inf, 0.0, bias.double()).abs()))).amax(1, keepdim=True)
+    away = torch.where(left, top - z, 0.0)
+    s = (classes / 64 + 64) * E
+    e_p = p * (2 * dz + (4 + 4 * away) * E + s) + 3 * E * (p + target)
+    e_loss = (2 * dz + s + 8 * E * (1 + lse.abs() + top.abs() + (away.amax(1, keepdim=True) if smoothing else 0.0)))[:, 0]
+    g = torch.where(in_use, p - target, 0.0) * (scale / count)
+    return loss, g, torch.where(in_use, e_p, 0.0) * abs(scale) / count, e_loss, count
+
+
+def check(x, w, labels, bias, smoothing=0.0, ignore=-100, scale=1.0, **kw):
+    rows, k = x.shape
+    mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, labels, bias, smoothing=smoothing, ignore_index=ignore, scale=scale, **kw)
+    l, g, e_g, e_loss, count = definition(x, w, labels, bias, smoothing, ignore, scale)
+    assert torch.equal(torch.isnan(loss), torch.isnan(l))
+    fine = ~torch.isnan(l)
+    near(loss[fine], l[fine], e_loss[fine], "loss")
+    if bool(fine.all()):
+        near(mean, l.sum() / count, e_loss.mean() * rows / count + E * l.abs().sum() / count, "mean")
+    e_s = e_g + (2.0 ** -8 * (g.abs() + e_g) if x.dtype == torch.bfloat16 else 0.0)
+    x64, w64 = torch.where((labels == ignore)[:, None], 0.0, x.double()), w.double()
+    if dx is not None:
+        near(dx, g @ w64.t(), e_s @ w64.abs().t() + (w.shape[1] + 2) * E * (g.abs() @ w64.abs().t()), "dx")
+    if dw is not None:
+        near(dw, x64.t() @ g, x64.abs().t() @ e_s + (rows + 2) * E * (x64.abs().t() @ g.abs()), "dw")
+    if db is not None:
+        near(db, g.sum(0), e_g.sum(0) + (rows + 2) * E * g.abs().sum(0), "db")
+    return mean, loss, dx, dw, db
+
+
+SHAPES = [(1, 1, 1), (1, 1, 2), (1, 8, 1), (2, 3, 5), (3, 7, 3), (1, 64, 1000), (5, 33, 10), (16, 64, 31), (17, 65, 33), (31, 100, 64), (33, 128, 65), (64, 200, 1001), (70, 96, 2048), (127, 301, 129), (129, 64, 4001),
+          (200, 500, 333), (257, 520, 2100), (300, 1000, 640), (600, 72, 8200)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k,classes", SHAPES)
+def test_against_definition(rows, k, classes, dtype):
+    check(*problem(rows, k, classes, dtype))
+    check(*problem(rows, k, classes, dtype, 1, 8, bias=False, ignored=0.3), scale=128.0)
+    check(*problem(rows, k, classes, dtype, 2, 3, 1, ignored=0.3, masked=0.3, bits=torch.int32), smoothing=0.1)
+
+
+# tiles of every size, with and without aligned rows, and more classes than a piece
+@pytest.mark.parametrize("dtype,rows,k,classes,pad", [
+    ("bf16", 1024, 512, 8192, 0), ("bf16", 2048, 256, 16384, 0), ("bf16", 4096, 512, 4096, 0), ("bf16", 4100, 264, 20008, 0), ("bf16", 4100, 261, 20003, 0), ("bf16", 8192, 64, 17001, 8), ("bf16", 70000, 40, 3000, 0),
+    ("f32", 2048, 256, 17001, 0), ("f32", 9000, 100, 5000, 3), ("f32", 40000, 24, 2100, 0), ("bf16", 64, 1024, 50001, 0), ("f32", 64, 512, 50000, 0), ("bf16", 66000, 16, 1025, 0)])
+def test_large(dtype, rows, k, classes, pad):
+    x, w, labels, b = problem(rows, k, classes, dtype, 3, pad, ignored=0.1, masked=0.1)
+    first = check(x, w, labels, b, smoothing=0.1)
+    again = ops.linear_cross_entropy(x, w, labels, b, smoothing=0.1)
+    assert all(torch.equal(a, c) for a, c in zip(first, again))
+
+
+@pytest.mark.parametrize("dtype,rows,k,classes", [("f32", 100, 50, 333), ("bf16", 4096, 128, 17000), ("bf16", 100, 52, 333), ("bf16", 3000, 257, 1001)])
+def test_outputs_one_by_one(dtype, rows, k, classes):
+    x, w, labels, b = problem(rows, k, classes, dtype, 4, ignored=0.2)
+    for flags in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (0, 1, 1), (1, 0, 1), (0, 0, 0)):
+        out = check(x, w, labels, b, need_dx=bool(flags[0]), need_dw=bool(flags[1]), need_db=bool(flags[2]))
+        assert [t is not None for t in out[2:]] == [bool(f) for f in flags]
+    # into tables that are there, rows of wider ones
+    dx, dw, db = (torch.full((r, c + 7), 7.0, dtype=DT[dtype], device="cuda") for r, c in ((rows + 1, k), (k + 1, classes), (1, classes)))
+    want = ops.linear_cross_entropy(x, w, labels, b)
+    got = ops.linear_cross_entropy(x, w, labels, b, dx=dx[:rows, 3:3 + k], dw=dw[:k, 3:3 + classes], db=db[0, 3:3 + classes])
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    dx[:rows, 3:3 + k], dw[:k, 3:3 + classes], db[0, 3:3 + classes] = 7.0, 7.0, 7.0
+    assert all(bool((t == 7.0).all()) for t in (dx, dw, db))
+    assert ops.linear_cross_entropy(x, w, labels)[4] is None
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_as_the_two_operators_apart(dtype):
+    """The loss of this library's own logits."""
+    x, w, labels, b = problem(300, 200, 1500, "f32", 5, ignored=0.1)
+    z, _ = ops.linear_forward(x, w, b)
+    mean, loss, g = ops.cross_entropy(z, labels)
+    m2, l2, dx, dw, db = ops.linear_cross_entropy(x, w, labels, b)
+    assert float((loss - l2).abs().max()) < 2e-5 and abs(float(mean - m2)) < 2e-6
+    dx1, dw1, db1 = ops.linear_backward(g, x, w)
+    for a, c in ((dx, dx1), (dw, dw1), (db, db1)):
+        assert float((a - c).norm() / c.norm()) < 1e-5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [5, 200, 3000])
+def test_rows_where_it_can_go_wrong(classes, dtype):
+    x, w, labels, b = problem(12, 64, classes, dtype, 6)
+    labels = torch.arange(12, device="cuda") % classes
+    clean = ops.linear_cross_entropy(x, w, labels.masked_fill(torch.arange(12, device="cuda") < 4, -100), b)
+    # what rows that do not count hold is not looked at
+    x[0], x[1, 3], x[2], x[3] = math.nan, math.inf, torch.finfo(x.dtype).max, -math.inf
+    got = ops.linear_cross_entropy(x, w, labels.masked_fill(torch.arange(12, device="cuda") < 4, -100), b)
+    assert all(torch.equal(a, c) for a, c in zip(got, clean)) and not got[2][:4].any()
+    # a label that is no class: its loss is NaN, its gradient zero
+    far = labels.clone()
+    far[:4] = -100
+    far[4], far[5] = classes, -7
+    mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, far, b)
+    assert bool(torch.isnan(loss[4:6]).all()) and bool(torch.isnan(mean)) and bool(torch.isfinite(loss[6:]).all()) and not dx[:6].any() and bool(torch.isfinite(dw).all()) and bool(torch.isfinite(db).all())
+    # classes ruled out: all but one, the label's, all of them
+    only = torch.full_like(b, -math.inf)
+    only[1] = 0.5
+    one = torch.full_like(labels, 1)
+    one[:4] = -100
+    mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, one, only, smoothing=0.1)
+    assert float(loss.abs().max()) <= 1e-6 and float(dx.float().abs().max()) <= 1e-6 and float(db.float().abs().max()) <= 1e-6
+    one[4] = 2
+    mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, one, only)
+    assert float(loss[4]) == math.inf and float(mean) == math.inf and bool(torch.isfinite(dx).all()) and abs(float(db[2]) * 8 + 1) < 0.01 and abs(float(db[1]) * 8 - 1) < 0.01
+    none = torch.full_like(b, -math.inf)
+    mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, one, none)
+    assert bool((loss[4:] == math.inf).all()) and not loss[:4].any() and not dx.any() and not dw.any() and not db.any()
+    # a mask of the type's lowest value: finite, and as if ruled out where anything else is left
+    low = torch.full_like(b, torch.finfo(b.dtype).min)
+    mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, one, low)
+    assert bool(torch.isfinite(loss).all()) and bool(torch.isfinite(dx).all()) and bool(torch.isfinite(dw).all())
+    low[1] = 0.0
+    one[4] = 1
+    mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, one, low)
+    assert float(loss.abs().max()) <= 1e-6 and not db[2:].any()
+    # NaN and infinities in rows that count: those rows' losses are NaN
+    x[6, 0], x[7, 1] = math.nan, math.inf
+    loss, dx = ops.linear_cross_entropy(x, w, one, b)[1:3]
+    assert bool(torch.isnan(loss[6:8]).all()) and bool(torch.isfinite(loss[8:]).all()) and bool(torch.isnan(dx[6:8]).all()) and bool(torch.isfinite(dx[8:]).all())
+
+
+def test_large_logits():
+    """Logits of some ten thousand, of either sign: exponentials of differences only."""
+    x, w, labels, b = problem(40, 64, 700, "f32", 8)
+    for shift in (3e4, -3e4):
+        check(x, w, labels, torch.full_like(b, shift), smoothing=0.1)
+        check(300 * x, 30 * w, labels, b)
+
+
+def test_nothing_counts():
+    for rows in (0, 5):
+        x, w, labels, b = problem(max(rows, 1), 24, 40, "bf16")
+        out = ops.linear_cross_entropy(x[:rows], w, torch.full((rows,), 7, device="cuda"), b, ignore_index=7)
+        assert float(out[0]) == 0.0 and out[1].shape == (rows,) and out[2].shape == (rows, 24) and not any(bool(t.any()) for t in out[1:])
+
+
+def test_gradient_against_differences():
+    """Central differences of the definition in 64 bits (step 1e-5: their error is below 1e-8)."""
+    x, w, labels, b = problem(4, 5, 6, "f32", 9)
+    labels[1] = -100
+    b[4] = -math.inf
+    labels[labels == 4] = 0
+    got = ops.linear_cross_entropy(x, w, labels, b, smoothing=0.2, scale=3.0)[2:]
+    leaves = [t.double() for t in (x, w, b)]
+
+    def value():
+        l, _, _, _, count = definition(leaves[0], leaves[1], labels, leaves[2], 0.2, -100, 3.0)
+        return float(l.sum()) / count * 3.0
+
+    for which, leaf in enumerate(leaves):
+        for i in range(leaf.numel()):
+            at = tuple(int(v) for v in torch.unravel_index(torch.tensor(i), leaf.shape))
+            old = float(leaf[at])
+            if math.isinf(old):
+                assert float(got[which][at]) == 0.0
+                continue
+            leaf[at] = old + 1e-5
+            hi = value()
+            leaf[at] = old - 1e-5
+            lo = value()
+            leaf[at] = old
+            assert abs(float(got[which][at]) - (hi - lo) / 2e-5) < 1e-5
+
+
+def test_graph_replays_and_another_stream():
+    x, w, labels, b = problem(300, 130, 1111, "bf16", 10)
+
+    def call(**kw):
+        return ops.linear_cross_entropy(x, w, labels, b, smoothing=0.1, **kw)
+
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for _ in range(3):
+        x.copy_(torch.randn(300, 130, device="cuda"))
+        labels.copy_(torch.randint(1111, (300,), device="cuda"))
+        labels[::9] = -100
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, call()))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    there = call(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(got, there))
+
+
+def test_refusals():
+    x, w, labels, b = problem(4, 8, 16, "f32")
+    for args, kw, text in (((x, w, labels[:3], b), {}, r"labels must be a contiguous int32 or int64 \[4\]"), ((x, w[:7], labels, b), {}, r"w must be \[8, 16\]"), ((x, w, labels, b[:3]), {}, "bias must be a contiguous"),
+                           ((x, w.bfloat16(), labels, b), {}, "w must be Float"), ((x, w, labels.float(), b), {}, "labels must be"), ((x, w, labels, b), dict(dx=x[:, :3]), r"dx must be \[4, 8\]"), ((x.cpu(), w, labels, b), {}, "GPU")):
+        with pytest.raises(ValueError, match=text):
+            ops.linear_cross_entropy(*args, **kw)
+    for kw, text in ((dict(smoothing=1.0), "smoothing"), (dict(dx=x), "dx and x share memory"), (dict(dw=w), "dw and w share memory"), (dict(db=b), "db and bias share memory"),
+                     (dict(workspace=torch.empty(512, dtype=torch.uint8, device="cuda")), "too small")):
+        with pytest.raises(RuntimeError, match=text):
+            ops.linear_cross_entropy(x, w, labels, b, **kw)
