@@ -208,7 +208,7 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
 // workspace while both gradients' products read it.
 constexpr int64_t kSignalBytes = (int64_t)128 << 20, kPieceStep = 256;
 constexpr int kLossGroups = 256;        // workgroups of the rows' statistics, at most: each leaves a part of the losses' sum
-struct LossHead { uint32_t done; float inverse; uint32_t pad[62]; double loss[kLossGroups]; int64_t used[kLossGroups]; };
+struct LossHead { uint32_t done; float factor; uint32_t pad[62]; double loss[kLossGroups]; int64_t used[kLossGroups]; };
 constexpr int strip_columns(int tile) { return tile == 256 ? 64 : 32; }        // of a wavefront's strip of a tile, which has one entry in a row's statistics
 struct LossPlan {
   bool grads, signal, direct, copy_x, copy_w;

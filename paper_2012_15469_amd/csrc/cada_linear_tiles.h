@@ -12,6 +12,7 @@ struct Epilogue {
   void *pre, *out;
   int64_t ldr, ldpre, ldo;
   int act;
+  const float *factor;       // of the sum, in device memory, or null (1)
 };
 
 // One product C[M, N] = sum_k A(m, k) B(k, n).
@@ -264,6 +265,11 @@ template <typename T>
 __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int64_t left, float (&f)[8]) {
   if (left <= 0) return;
   float o[8];
+  if (e.factor) {
+    const float factor = *e.factor;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= factor;
+  }
   if (e.bias) {
     load8_n(static_cast<const T *>(e.bias) + n, left, o);
 #pragma unroll

@@ -2,7 +2,7 @@
 //
 // The logits' tiles (cada_linear_tiles.h) end in statistics: of each row, and of each strip of 32 or 64 columns, the largest logit and the sum of the exponentials of the
 // distances to it.  A row's strips are then joined, as one goes along, to the row's largest and its sum, which is its loss.  For the gradients the logits are formed again in
-// pieces of the classes; their tiles end in softmax - target in the operands' type, from which the products of a layer's gradients are taken while it is in the caches: dw is finished piece by
+// pieces of the classes; their tiles end in softmax - target (but for a factor) in the operands' type, from which the products of a layer's gradients are taken while it is in the caches: dw is finished piece by
 // piece, dx is added up in float32.  That is four products where keeping the logits would take three, and memory for one piece instead of all.
 #include <algorithm>
 
@@ -105,21 +105,19 @@ template <int BM> struct ToStatistics {
   template <int LANES> __device__ __forceinline__ void end(int64_t, int, int64_t) const {}
 };
 
-// A tile's logits into softmax - target, times scale / count, and its column sums over a strip of rows.
+// A tile's logits into the signal (softmax - target) / (1 - smoothing), and its column sums over a strip of rows.  What is left of the gradient's factor, (1 - smoothing) scale / count, is
+// taken to the products' float32 sums: a bf16 signal is rounded, and with that factor in it the label's -(1 - p) of every row would be rounded the same way wherever p is small, up to 2^-8 off
+// (1 / 100 rows), while -1 + p / (1 - smoothing) is next to a value that bf16 has (dx and dw 2.4e-3 from 64 bits, relative in the 2-norm, and 2.9e-3 for an unlucky count; rounding the outputs alone is 1.7e-3).
 template <int BM> struct ToSignal {
   static constexpr bool kAll = true;
   const Loss &q;
   RowInfo *info;             // [BM], in LDS
-  float bias[8], column[8], inverse, f_keep;
+  float bias[8], column[8];
   __device__ __forceinline__ ToSignal(const Loss &loss, RowInfo *lds) : q(loss), info(lds) {}
   __device__ __forceinline__ void begin(const Product &p, int64_t m0, int t) {
-    inverse = q.head->inverse;
-    f_keep = q.keep * inverse;
     if (t >= BM) return;
     RowInfo r = {0.f, 0.f, 0.f, -1};
     if (m0 + t < p.M) r = q.info[m0 + t];
-    r.f_total *= inverse;
-    r.f_each *= inverse;
     info[t] = r;
   }
   template <typename T> __device__ __forceinline__ void columns(int n, int64_t left) {
@@ -136,7 +134,7 @@ template <int BM> struct ToSignal {
       z[e] += bias[e];
       float g = __builtin_amdgcn_exp2f((z[e] - r.base) * kLog2e) * r.f_total;
       if (q.smoothing != 0.f) g -= z[e] != -kInf ? r.f_each : 0.f;
-      g -= at == e ? f_keep : 0.f;
+      g -= at == e ? 1.f : 0.f;
       z[e] = r.label >= 0 && e < left ? g : 0.f;
       column[e] += z[e];
     }
@@ -148,6 +146,9 @@ template <int BM> struct ToSignal {
     for (int e = 0; e < 8; ++e)
 #pragma unroll
       for (int o = LANES; o < 64; o <<= 1) column[e] += __shfl_xor(column[e], o, 64);
+    const float factor = q.head->factor;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) column[e] *= factor;
     if ((threadIdx.x & 63) < LANES) store8_n(q.db_part + strip * columns_of_piece + n, left, column);
   }
   int64_t columns_of_piece;
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
       losses[row] = l;
       used_rows[row] = used;
       if (q.loss) q.loss[r] = l;
-      q.info[r] = RowInfo{base, 1.f / s.sum, q.smoothing != 0.f ? q.smoothing / s.left : 0.f, known && !none ? (int32_t)label : -1};
+      q.info[r] = RowInfo{base, 1.f / (s.sum * q.keep), q.smoothing != 0.f ? q.smoothing / (s.left * q.keep) : 0.f, known && !none ? (int32_t)label : -1};
     }
     __syncthreads();
     if (t == 0) {
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
   if (t == 0) {
     const int64_t count = max(used_sum, (int64_t)1);
     if (q.mean) *q.mean = (float)(sum / (double)count);
-    q.head->inverse = q.scale / (float)count;
+    q.head->factor = q.keep * q.scale / (float)count;
   }
 }
 
@@ -363,12 +364,12 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
       lay(&dx, c, signal, f.ldz, w + first, ldw, a->rows, a->in, here, nullptr);
       if (f.pieces > 1 || f.dx.splits > 1) dx.partial = reinterpret_cast<float *>(ws + f.off_dx);
       dx.add = i > 0;
-      dx.epi.out = a->dx; dx.epi.ldo = a->lddx;
+      dx.epi.out = a->dx; dx.epi.ldo = a->lddx; dx.epi.factor = &q.head->factor;
     }
     if (a->dw) {
       lay(&dw, f.dw, x, ldx, signal, f.ldz, a->in, here, a->rows, reinterpret_cast<float *>(ws + f.off_dw));
       dw.a_cols = x_cols; dw.b_cols = eights(here);
-      dw.epi.out = static_cast<T *>(a->dw) + first; dw.epi.ldo = a->lddw;
+      dw.epi.out = static_cast<T *>(a->dw) + first; dw.epi.ldo = a->lddw; dw.epi.factor = &q.head->factor;
     }
     if (f.grads) {
       if (int rc = linear_products(a->type, a->dx ? f.dx.tile : f.dw.tile, f.direct, dx, dw, st)) return rc;
