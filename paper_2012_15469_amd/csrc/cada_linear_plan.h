@@ -234,8 +234,8 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
       f.pieces = ceil_div(classes, f.piece);
     }
   }
-  // x is read along the contraction for the logits and across it for dw, which takes a copy without the rows that do not count (what they hold is not looked at); w the other way round.
-  const bool x_direct = a->dw || direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, classes, elem);
+  // x is read along the contraction for the logits and across it for dw; for gradients it is copied without the rows that do not count (what they hold is not looked at).
+  const bool x_direct = f.signal || direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, classes, elem);
   const bool tiny = no_tiles(rows, a->ldx, in, elem) || no_tiles(in, a->ldw, classes, elem);
   const Shape whole = {rows, classes, in}, part = {rows, f.piece, in}, grads[2] = {{rows, in, f.piece}, {in, f.piece, rows}};
   const Shape *first = a->dx ? grads : grads + 1;
@@ -249,7 +249,7 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
   }
   if (!x_direct || !w_direct) time[1] += kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, classes, elem));
   f.direct = (x_direct && w_direct) || tiny || time[1] < time[0];
-  f.copy_x = a->dw || (f.direct && !x_direct) || tiny;
+  f.copy_x = f.signal || (f.direct && !x_direct) || tiny;
   f.copy_w = (f.direct && !w_direct) || tiny;
   const Cut *mine = c[f.direct];
   f.logits = mine[0];

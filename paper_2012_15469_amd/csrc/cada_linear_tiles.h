@@ -301,17 +301,15 @@ __device__ __forceinline__ void put_part(const Product &p, uint32_t split, int64
   store8_n(to, 8, f);
 }
 
-// What becomes of a tile's sums: a layer's output, here; a last layer's loss has its own (cada_linear_xent.hip), whose row() all lanes of a row call together, also for rows and columns that
-// do not exist.  A wavefront calls begin() first, then columns() and row() with the eight columns of the lane, then end() with the number of its strip of the table's rows.
+// What becomes of a tile's sums: a layer's output, here; a last layer's loss has its own (cada_linear_xent.hip), which take the sums where the matrix instructions leave them, sums(), and where
+// wavefronts share a tile's contraction and join their sums in LDS, eight columns of a row per lane, row().
 struct ToTable {
-  static constexpr bool kAll = false;
-  __device__ __forceinline__ void begin(const Product &, int64_t, int) const {}
-  template <typename T> __device__ __forceinline__ void columns(int, int64_t) const {}
-  template <typename T, int LANES> __device__ __forceinline__ void row(const Product &p, uint32_t split, int64_t m, int, int n, int64_t left, float (&f)[8]) const {
+  static constexpr bool kOwn = false;
+  __device__ __forceinline__ void begin(const Product &, int64_t, int, int) const {}
+  template <typename T> __device__ __forceinline__ void row(const Product &p, uint32_t split, int64_t m, int n, int64_t left, float (&f)[8]) const {
     if (p.partial) put_part(p, split, m, n, left, f);
     else finish8<T>(p.epi, m, n, left, f);
   }
-  template <int LANES> __device__ __forceinline__ void end(int64_t, int, int64_t) const {}
 };
 
 // WY x WX wavefronts share the tile; with KW = 4 four wavefronts each take the whole (32 x 32) tile and one of the four sub-steps of every step, and their sums are joined
@@ -331,7 +329,7 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   const uint32_t rows_here = min(8u, (uint32_t)p.tiles_m - band * 8), col = in_band / rows_here;
   const int64_t m0 = (int64_t)(band * 8 + in_band - col * rows_here) * BM, m_left = p.M - m0;
   const int n0 = (int)col * BN;
-  out.begin(p, m0, t);
+  out.begin(p, m0, n0, t);
   const int64_t n_left = p.N - n0, k0 = split * p.k_per_split, k1 = min(p.K, k0 + p.k_per_split);
   const T *a = static_cast<const T *>(p.a) + (AKC ? m0 * p.lda + k0 : k0 * p.lda + m0);
   const T *b = static_cast<const T *>(p.b) + (BKC ? n0 * p.ldb + k0 : k0 * p.ldb + n0);
@@ -548,17 +546,20 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
 #pragma unroll
     for (int q = 0; q < 4; ++q) *reinterpret_cast<v4s *>(mine + 8 * q) = v4s{acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
     __syncthreads();
-    if (t < BM * 4 && (OUT::kAll || m0 + t / 4 < p.M)) {
+    if (t < BM * 4 && (OUT::kOwn || m0 + t / 4 < p.M)) {
       const float *src = sums + t / 4 * kLd + (t & 3) * 8;
       float f[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = (src[e] + src[BM * kLd + e]) + (src[2 * BM * kLd + e] + src[3 * BM * kLd + e]);
       const int64_t m = m0 + t / 4, left = (int64_t)p.N - n0 - (t & 3) * 8;
       const int n = n0 + (t & 3) * 8;
-      out.template columns<T>(n, left);
-      out.template row<T, 4>(p, split, m, t / 4, n, left, f);
-      out.template end<4>(m0 / BM * 2 + (t >> 6), n, left);
+      if constexpr (OUT::kOwn) out.template row<T>(p, m0, n0, t, f);
+      else out.template row<T>(p, split, m, n, left, f);
     }
+    return;
+  }
+  if constexpr (OUT::kOwn) {
+    out.template sums<T, FM, FN>(p, acc, m0, n0, wm, wn, lane, lds + wave * (2 * kHalf / (WY * WX)));
     return;
   }
 
@@ -569,7 +570,6 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
   float *strip = reinterpret_cast<float *>(lds) + wave * 32 * kLd;
   const int n = n0 + wn + lane % kLanes * 8;
   const int64_t left = (int64_t)p.N - n;
-  out.template columns<T>(n, left);
 #pragma unroll 1
   for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -590,11 +590,12 @@ __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, un
       const float *src = strip + row * kLd + lane % kLanes * 8;
       const v4s x = *reinterpret_cast<const v4s *>(src), y = *reinterpret_cast<const v4s *>(src + 4);
       float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-      if (OUT::kAll || m < p.M) out.template row<T, kLanes>(p, split, m, wm + 32 * i + row, n, left, f);
+      if constexpr (!OUT::kOwn) {
+        if (m < p.M) out.template row<T>(p, split, m, n, left, f);
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
-  out.template end<kLanes>(m0 / BM * WY + place / WX, n, left);
 }
 
 // Tiles of a launch, dealt to the eight XCDs in consecutive eighths (each has an L2 of its own).  `first`: workgroups of an XCD that have other tiles.

@@ -12,7 +12,7 @@ namespace cada {
 namespace {
 
 struct Stat { float top, sum, distance, left; };      // distance: the sum of z - top over the classes that are left (smoothing), left: their number
-struct RowInfo { float base, f_total, f_each; int32_t label; };      // label: < 0 for a row without gradient
+struct RowInfo { float base, f_total, f_each; int32_t label; };      // base infinite (exponentials are zero), f_total 0, label < 0: a row without gradient
 struct Loss {
   const void *labels, *bias;
   LossHead *head;
@@ -35,142 +35,297 @@ __device__ __forceinline__ int64_t label_at(const void *labels, int bytes, int64
 }
 __device__ __forceinline__ bool counts(const Loss &q, int64_t label) { return label != q.ignore && label >= 0 && label < q.classes; }
 
-// Largest and sum over the LANES lanes (a power of two) that are next to each other.
-template <int LANES> __device__ __forceinline__ float lanes_max(float x) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
-  return x;
-}
-template <int LANES> __device__ __forceinline__ float lanes_sum(float x) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
+// exp(z - base) is the hardware's exp2 of the rounded difference times log2(e): off by |z - base| 2^-23 and an ulp or two, relative.  The difference comes first, so that a mask of the type's lowest value (or a
+// row of nothing else) overflows nowhere.
+__device__ __forceinline__ float power(float z, float base) { return __builtin_amdgcn_exp2f((z - base) * kLog2e); }
+
+// The biases of a tile's columns in LDS: -inf for a column that does not exist, so that it is a class that is ruled out (what the matrix instructions made of it is something of the table's).
+template <typename T> __device__ __forceinline__ void put_bias(const Loss &q, const Product &p, int n0, int t, int columns, float *to) {
+  if (t >= columns) return;
+  const int n = n0 + t;
+  to[t] = n >= p.N ? -kInf : q.bias ? to_f32(static_cast<const T *>(q.bias)[q.first + n]) : 0.f;
 }
 
-// A tile's logits into statistics.
-template <int BM> struct ToStatistics {
-  static constexpr bool kAll = true;
+// A tile's logits into statistics.  A lane has FN x 16 logits of a row, and the lane 32 further the row's others.
+// Bound by the vector unit: an addition, a comparison, two operations and an exponential (four times an operation's time) per logit.
+template <typename T, int BM> struct ToStatistics {
+  static constexpr bool kOwn = true;
   const Loss &q;
   int32_t *label;            // [BM], in LDS
-  float bias[8];
-  __device__ __forceinline__ ToStatistics(const Loss &loss, int32_t *lds) : q(loss), label(lds) {}
-  __device__ __forceinline__ void begin(const Product &p, int64_t m0, int t) {
+  float *bias;               // [BM], in LDS
+  __device__ __forceinline__ ToStatistics(const Loss &loss, int32_t *l, float *b) : q(loss), label(l), bias(b) {}
+  __device__ __forceinline__ void begin(const Product &p, int64_t m0, int n0, int t) {
+    put_bias<T>(q, p, n0, t, BM, bias);
     if (t >= BM) return;
     const int64_t l = m0 + t < p.M ? label_at(q.labels, q.label_bytes, m0 + t) : -1;
     label[t] = counts(q, l) ? (int32_t)l : -1;
   }
-  template <typename T> __device__ __forceinline__ void columns(int n, int64_t left) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = 0.f;
-    if (q.bias) load8_n(static_cast<const T *>(q.bias) + n, left, bias);
+  __device__ __forceinline__ void put(int64_t m, int64_t strip, const Stat &s) const {
+    const int64_t to = strip * q.rows + m;
+    if (q.smoothing != 0.f) reinterpret_cast<Stat *>(q.stats)[to] = s;
+    else reinterpret_cast<float2 *>(q.stats)[to] = float2{s.top, s.sum};
   }
-  template <typename T, int LANES> __device__ __forceinline__ void row(const Product &p, uint32_t, int64_t m, int local, int n, int64_t left, float (&z)[8]) {
-    float top = -kInf;
+  template <typename, int FM, int FN> __device__ __forceinline__ void sums(const Product &p, f32x16 (&z)[FM][FN], int64_t m0, int n0, int wm, int wn, int lane, unsigned char *) {
+    const int half = lane >> 5;
+    Stat s[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) s[i] = Stat{-kInf, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const v4s b = *reinterpret_cast<const v4s *>(bias + wn + 32 * j + 8 * r + 4 * half);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[i][j][4 * r + e] += b[e];
+            s[i].top = fmaxf(s[i].top, z[i][j][4 * r + e]);
+          }
+      }
+    float base[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      s[i].top = fmaxf(s[i].top, __shfl_xor(s[i].top, 32, 64));
+      // (a strip of nothing but -inf and NaN: its exponentials are taken against 0, so that only a NaN makes the sum NaN)
+      base[i] = s[i].top == -kInf ? 0.f : s[i].top;
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[i].sum += power(z[i][j][r], base[i]);
+    if (q.smoothing != 0.f) {
+      float left = 0.f;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const v4s b = *reinterpret_cast<const v4s *>(bias + wn + 32 * j + 8 * r + 4 * half);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool in = b[e] != -kInf;
+            left += in ? 1.f : 0.f;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) s[i].distance += in ? z[i][j][4 * r + e] - base[i] : 0.f;
+          }
+        }
+      left += __shfl_xor(left, 32, 64);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        s[i].distance += __shfl_xor(s[i].distance, 32, 64);
+        s[i].left = left;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      s[i].sum += __shfl_xor(s[i].sum, 32, 64);
+      const int row = wm + 32 * i + (lane & 31);
+      const int64_t m = m0 + row;
+      const int at = label[row] - (n0 + wn);
+      const bool mine = at >= 0 && at < 32 * FN && (at >> 2 & 1) == half;
+      if (__ballot(mine)) {
+        float zl = 0.f;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) zl = at == 32 * j + (r >> 2) * 8 + 4 * half + (r & 3) ? z[i][j][r] : zl;
+        if (mine) q.z_label[m] = zl;
+      }
+      if (half == 0 && m < p.M) put(m, (n0 + wn) / (32 * FN), s[i]);
+    }
+  }
+  // The same of eight columns of a row per lane, four lanes to a row.
+  template <typename> __device__ __forceinline__ void row(const Product &p, int64_t m0, int n0, int t, float (&z)[8]) {
+    const int64_t m = m0 + t / 4;
+    const int c = (t & 3) * 8;
+    Stat s = {-kInf, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      z[e] = e < left ? z[e] + bias[e] : -kInf;
-      top = fmaxf(top, z[e]);
+      z[e] += bias[c + e];
+      s.top = fmaxf(s.top, z[e]);
     }
-    top = lanes_max<LANES>(top);
-    // (a strip of nothing but -inf and NaN: its exponentials are taken against 0, so that only a NaN makes the sum NaN)
-    const float base = top == -kInf ? 0.f : top;
-    float sum = 0.f, distance = 0.f, in = 0.f;
+    s.top = fmaxf(s.top, __shfl_xor(s.top, 1, 64));
+    s.top = fmaxf(s.top, __shfl_xor(s.top, 2, 64));
+    const float base = s.top == -kInf ? 0.f : s.top;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f((z[e] - base) * kLog2e);
-    sum = lanes_sum<LANES>(sum);
-    if (q.smoothing != 0.f) {
+    for (int e = 0; e < 8; ++e) {
+      const bool in = bias[c + e] != -kInf;
+      s.sum += power(z[e], base);
+      s.left += in ? 1.f : 0.f;
+      s.distance += in ? z[e] - base : 0.f;
+    }
+    float *parts[3] = {&s.sum, &s.left, &s.distance};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool is_in = z[e] != -kInf;
-        in += is_in ? 1.f : 0.f;
-        distance += is_in ? z[e] - base : 0.f;
-      }
-      in = lanes_sum<LANES>(in);
-      distance = lanes_sum<LANES>(distance);
+    for (int i = 0; i < 3; ++i) {
+      *parts[i] += __shfl_xor(*parts[i], 1, 64);
+      *parts[i] += __shfl_xor(*parts[i], 2, 64);
     }
     if (m >= p.M) return;
-    const int at = label[local] - n;
+    const int at = label[t / 4] - (n0 + c);
     if (at >= 0 && at < 8) {
       float zl = z[0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) zl = at == e ? z[e] : zl;
       q.z_label[m] = zl;
     }
-    if ((threadIdx.x & (LANES - 1)) == 0) {
-      const int64_t to = (int64_t)(n / (LANES * 8)) * q.rows + m;
-      if (q.smoothing != 0.f) reinterpret_cast<Stat *>(q.stats)[to] = Stat{top, sum, distance, in};
-      else reinterpret_cast<float2 *>(q.stats)[to] = float2{top, sum};
-    }
+    if ((t & 3) == 0) put(m, n0 / 32, s);
   }
-  template <int LANES> __device__ __forceinline__ void end(int64_t, int, int64_t) const {}
 };
 
 // A tile's logits into the signal (softmax - target) / (1 - smoothing), and its column sums over a strip of rows.  What is left of the gradient's factor, (1 - smoothing) scale / count, is
 // taken to the products' float32 sums: a bf16 signal is rounded, and with that factor in it the label's -(1 - p) of every row would be rounded the same way wherever p is small, up to 2^-8 off
 // (1 / 100 rows), while -1 + p / (1 - smoothing) is next to a value that bf16 has (dx and dw 2.4e-3 from 64 bits, relative in the 2-norm, and 2.9e-3 for an unlucky count; rounding the outputs alone is 1.7e-3).
-template <int BM> struct ToSignal {
-  static constexpr bool kAll = true;
+// Rows without gradient have a sum of infinity (and x = 0), classes that are ruled out a logit of -inf.
+template <typename T, int BM> struct ToSignal {
+  static constexpr bool kOwn = true;
   const Loss &q;
   RowInfo *info;             // [BM], in LDS
-  float bias[8], column[8];
-  __device__ __forceinline__ ToSignal(const Loss &loss, RowInfo *lds) : q(loss), info(lds) {}
-  __device__ __forceinline__ void begin(const Product &p, int64_t m0, int t) {
+  float *bias;               // [BM], in LDS
+  __device__ __forceinline__ ToSignal(const Loss &loss, RowInfo *r, float *b) : q(loss), info(r), bias(b) {}
+  __device__ __forceinline__ void begin(const Product &p, int64_t m0, int n0, int t) {
+    put_bias<T>(q, p, n0, t, BM, bias);
     if (t >= BM) return;
-    RowInfo r = {0.f, 0.f, 0.f, -1};
-    if (m0 + t < p.M) r = q.info[m0 + t];
-    info[t] = r;
+    const RowInfo &r = q.info[min(m0 + t, p.M - 1)];
+    const bool in = m0 + t < p.M;
+    info[t].base = in ? r.base : kInf;
+    info[t].f_total = in ? r.f_total : 0.f;
+    info[t].f_each = in ? r.f_each : 0.f;
+    info[t].label = in ? r.label : -1;
   }
-  template <typename T> __device__ __forceinline__ void columns(int n, int64_t left) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = column[e] = 0.f;
-    if (q.bias) load8_n(static_cast<const T *>(q.bias) + q.first + n, left, bias);
+  __device__ __forceinline__ float signal(float z, bool in, const RowInfo &r) const {
+    const float p = power(z, r.base) * r.f_total;
+    return q.smoothing != 0.f ? p - (in ? r.f_each : 0.f) : p;
   }
-  template <typename T, int LANES> __device__ __forceinline__ void row(const Product &p, uint32_t, int64_t m, int local, int n, int64_t left, float (&z)[8]) {
-    if (m >= p.M || left <= 0) return;
-    const RowInfo r = info[local];
-    const int at = r.label - q.first - n;
+  template <typename, int FM, int FN> __device__ __forceinline__ void sums(const Product &p, f32x16 (&z)[FM][FN], int64_t m0, int n0, int wm, int wn, int lane, unsigned char *lds) {
+    constexpr int WN = 32 * FN, kLd = WN + 16 / sizeof(T), kLanes = WN / 8, kRows = 64 / kLanes;
+    const int half = lane >> 5;
+    float column[FN][16];
+    RowInfo info_of[FM];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      z[e] += bias[e];
-      float g = __builtin_amdgcn_exp2f((z[e] - r.base) * kLog2e) * r.f_total;
-      if (q.smoothing != 0.f) g -= z[e] != -kInf ? r.f_each : 0.f;
-      g -= at == e ? 1.f : 0.f;
-      z[e] = r.label >= 0 && e < left ? g : 0.f;
-      column[e] += z[e];
+    for (int i = 0; i < FM; ++i) info_of[i] = info[wm + 32 * i + (lane & 31)];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const v4s b = *reinterpret_cast<const v4s *>(bias + wn + 32 * j + 8 * r + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool in = b[e] != -kInf;
+          column[j][4 * r + e] = 0.f;
+#pragma unroll
+          for (int i = 0; i < FM; ++i) {
+            z[i][j][4 * r + e] = signal(z[i][j][4 * r + e] + b[e], in, info_of[i]);
+            column[j][4 * r + e] += z[i][j][4 * r + e];
+          }
+        }
+      }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int at = info_of[i].label < 0 ? -1 : info_of[i].label - q.first - (n0 + wn);
+      if (__ballot(at >= 0 && at < WN)) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float one = at == 32 * j + (r >> 2) * 8 + 4 * half + (r & 3) ? 1.f : 0.f;
+            z[i][j][r] -= one;
+            column[j][r] -= one;
+          }
+      }
     }
-    if (q.signal) store8_n(static_cast<T *>(q.signal) + m * q.ldz + n, 8, z);        // (whole: the rows have room for it)
+    if (q.signal) {
+      // through LDS, 32 rows at a time, in the table's type, to eight consecutive columns per lane
+      T *strip = reinterpret_cast<T *>(lds);
+      const int n = n0 + wn + lane % kLanes * 8;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            T *to = strip + (lane & 31) * kLd + 32 * j + 8 * r + 4 * half;
+            const f32x16 &f = z[i][j];
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint64_t *>(to) = (uint64_t)f2bf_pk(f[4 * r + 2], f[4 * r + 3]) << 32 | f2bf_pk(f[4 * r], f[4 * r + 1]);
+            else *reinterpret_cast<v4s *>(to) = v4s{f[4 * r], f[4 * r + 1], f[4 * r + 2], f[4 * r + 3]};
+          }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int turn = 0; turn < 32 / kRows; ++turn) {
+          const int row = lane / kLanes + turn * kRows;
+          const int64_t m = m0 + wm + 32 * i + row;
+          const T *from = strip + row * kLd + lane % kLanes * 8;
+          u32x4v x[sizeof(T) / 2];
+#pragma unroll
+          for (int k = 0; k < (int)sizeof(T) / 2; ++k) x[k] = reinterpret_cast<const u32x4v *>(from)[k];
+          if (m < p.M && n < p.N) {        // (eight columns whole: the signal's rows have room for it)
+            T *to = static_cast<T *>(q.signal) + m * q.ldz + n;
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) reinterpret_cast<u32x4v *>(to)[k] = x[k];
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+    }
+    if (!q.db_part) return;
+    // A column's 32 lanes (rows) exchange halves of their sums until each has one column's, of which FN = 1 leaves two lanes with the same.
+    float *all = &column[0][0];
+    int mine = 0;
+#pragma unroll
+    for (int h = 8 * FN; h > 0; h /= 2) {
+      const bool upper = lane & h;
+      mine += upper ? h : 0;
+#pragma unroll
+      for (int e = 0; e < h; ++e) {
+        const float keep = upper ? all[e + h] : all[e], other = upper ? all[e] : all[e + h];
+        all[e] = keep + __shfl_xor(other, h, 64);
+      }
+    }
+    if constexpr (FN == 1) all[0] += __shfl_xor(all[0], 16, 64);
+    const int n = n0 + wn + 32 * (mine >> 4) + 8 * (mine >> 2 & 3) + 4 * half + (mine & 3);
+    if ((FN == 2 || (lane & 16) == 0) && n < p.N) q.db_part[((m0 + wm) / (32 * FM)) * p.N + n] = all[0] * q.head->factor;
   }
-  template <int LANES> __device__ __forceinline__ void end(int64_t strip, int n, int64_t left) {
+  template <typename> __device__ __forceinline__ void row(const Product &p, int64_t m0, int n0, int t, float (&z)[8]) {
+    const int64_t m = m0 + t / 4;
+    const int c = (t & 3) * 8, n = n0 + c;
+    const RowInfo r = info[t / 4];
+    const int at = r.label < 0 ? -1 : r.label - q.first - n;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = signal(z[e] + bias[c + e], bias[c + e] != -kInf, r) - (at == e ? 1.f : 0.f);
+    if (q.signal && m < p.M && n < p.N) store8_n(static_cast<T *>(q.signal) + m * q.ldz + n, 8, z);
     if (!q.db_part) return;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int h = 4; h > 0; h /= 2) {        // lanes 8 h apart: the upper one goes on with the upper half
+      const bool upper = t & 8 * h;
 #pragma unroll
-      for (int o = LANES; o < 64; o <<= 1) column[e] += __shfl_xor(column[e], o, 64);
-    const float factor = q.head->factor;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) column[e] *= factor;
-    if ((threadIdx.x & 63) < LANES) store8_n(q.db_part + strip * columns_of_piece + n, left, column);
+      for (int e = 0; e < h; ++e) {
+        const float keep = upper ? z[e + h] : z[e], other = upper ? z[e] : z[e + h];
+        z[e] = keep + __shfl_xor(other, 8 * h, 64);
+      }
+    }
+    z[0] += __shfl_xor(z[0], 4, 64);
+    const int column = n + (t >> 5 & 1) * 4 + (t >> 4 & 1) * 2 + (t >> 3 & 1);
+    if ((t & 4) == 0 && column < p.N) q.db_part[(m0 / BM * 2 + (t >> 6)) * p.N + column] = z[0] * q.head->factor;
   }
-  int64_t columns_of_piece;
 };
 
 template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product p, const Loss q) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
   __shared__ int32_t label[BM];
+  __shared__ __align__(16) float bias[BM];
   if (blockIdx.x == 0 && threadIdx.x == 0) q.head->done = 0;
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
-  if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<BM>(q, label));
+  if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<T, BM>(q, label, bias));
 }
 template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_signal(const Product p, const Loss q) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
   __shared__ RowInfo info[BM];
+  __shared__ __align__(16) float bias[BM];
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
-  if (tile == ~0u) return;
-  ToSignal<BM> out(q, info);
-  out.columns_of_piece = p.N;
-  tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, out);
+  if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToSignal<T, BM>(q, info, bias));
 }
 
 // Joins statistics `b` to `a`: both against the larger of the two largest.
@@ -238,7 +393,7 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
       losses[row] = l;
       used_rows[row] = used;
       if (q.loss) q.loss[r] = l;
-      q.info[r] = RowInfo{base, 1.f / (s.sum * q.keep), q.smoothing != 0.f ? q.smoothing / (s.left * q.keep) : 0.f, known && !none ? (int32_t)label : -1};
+      q.info[r] = known && used && !none ? RowInfo{base, 1.f / (s.sum * q.keep), q.smoothing != 0.f ? q.smoothing / (s.left * q.keep) : 0.f, (int32_t)label} : RowInfo{kInf, 0.f, 0.f, -1};
     }
     __syncthreads();
     if (t == 0) {
