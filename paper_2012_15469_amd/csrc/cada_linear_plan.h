@@ -32,8 +32,8 @@ constexpr double kJoinLaunch = 4.0, kJoinBytesPerUs = 3.5e6;
 
 struct Shape { int64_t M, N, K; };
 constexpr int64_t kMostTiles = ((int64_t)1 << 23) - 8;        // of a product: 512 threads each, two products, less than 2^32 threads in a launch
-// The cheapest cut of one or two products in one launch (one tile for both) by that estimate, which it returns; tiles up to `widest`.
-inline double cut(const Shape *s, int n, int type, bool direct, int widest, Cut *out, int most_splits = 32) {
+// The cheapest cut of one or two products in one launch (one tile for both) by that estimate, which it returns; tiles up to `widest`.  `more_ends`: what each tile's way out costs besides.
+inline double cut(const Shape *s, int n, int type, bool direct, int widest, Cut *out, int most_splits = 32, const double *more_ends = nullptr) {
   const int64_t step = kStepBytes / (int64_t)type_bytes(type);
   const TileCost *costs = type == CADA_BF16 ? (direct ? kCostBf16 : kCostBf16Registers) : direct ? kCostF32 : kCostF32Registers;
   const int n_costs = type == CADA_BF16 && direct ? 4 : 2;
@@ -60,7 +60,7 @@ inline double cut(const Shape *s, int n, int type, bool direct, int widest, Cut 
         const Option &a = opt[0][i], *b = n > 1 ? &opt[1][j] : nullptr;
         const double tiles = a.tiles + (b ? b->tiles : 0.0), most = b ? std::max(a.steps, b->steps) : a.steps, join = a.join + (b ? b->join : 0.0);
         const double mean = (a.tiles * a.steps + (b ? b->tiles * b->steps : 0.0)) / tiles, per_cu = std::ceil(tiles / kCUs);
-        const double e = std::max(most * (t.alone + t.crowd * std::min(1.0, tiles / kCUs)), per_cu * mean * t.share) + t.ends * std::ceil(per_cu / t.slots) + (join > 0.0 ? join + kJoinLaunch : 0.0);
+        const double e = std::max(most * (t.alone + t.crowd * std::min(1.0, tiles / kCUs)), per_cu * mean * t.share) + t.ends * std::ceil(per_cu / t.slots) + (more_ends ? more_ends[c] * per_cu : 0.0) + (join > 0.0 ? join + kJoinLaunch : 0.0);
         if (e >= best) continue;
         best = e;
         for (int q = 0; q < n; ++q) {
@@ -206,9 +206,12 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
 
 // A last layer's loss: the product [rows, classes] is formed whole once, for each row's statistics, and again in pieces of the classes, whose signal (softmax - target, [rows, piece]) lies in the
 // workspace while both gradients' products read it.
-constexpr int64_t kSignalBytes = (int64_t)128 << 20, kPieceStep = 256;
+constexpr int64_t kSignalBytes = (int64_t)192 << 20, kPieceStep = 256, kLeastPiece = 1024;
 constexpr int kLossGroups = 256;        // workgroups of the rows' statistics, at most: each leaves a part of the losses' sum
 struct LossHead { uint32_t done; float factor; uint32_t pad[62]; double loss[kLossGroups]; int64_t used[kLossGroups]; };
+// What a tile's exponentials cost on its way out, in the microseconds of the table above: 4096 x 1024 x 50001 bf16, all four products, with logits in tiles of 64 2616 us, of 128 2086, of 256 1905; 8192 x 512 x 32000 1923,
+// 1560 and 1372; 1000 x 768 x 30000 344, 288 and 270.
+constexpr double kLossEnds[] = {0.2, 0.7, 3.5, 3.0};
 constexpr int strip_columns(int tile) { return tile == 256 ? 64 : 32; }        // of a wavefront's strip of a tile, which has one entry in a row's statistics
 struct LossPlan {
   bool grads, signal, direct, copy_x, copy_w;
@@ -224,34 +227,40 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
   const size_t elem = type_bytes(a->type);
   f.signal = a->dx || a->dw || a->db;
   f.grads = a->dx || a->dw;
-  f.pieces = 1;
-  f.piece = classes;
-  if (f.signal) {
-    const int64_t most = std::max<int64_t>(kSignalBytes / (rows * (int64_t)elem) / kPieceStep * kPieceStep, 4 * kPieceStep);
-    f.pieces = ceil_div(classes, most);
-    if (f.pieces > 1) {
-      f.piece = ceil_div(ceil_div(classes, f.pieces), kPieceStep) * kPieceStep;
-      f.pieces = ceil_div(classes, f.piece);
-    }
-  }
   // x is read along the contraction for the logits and across it for dw; for gradients it is copied without the rows that do not count (what they hold is not looked at).
   const bool x_direct = f.signal || direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, classes, elem);
   const bool tiny = no_tiles(rows, a->ldx, in, elem) || no_tiles(in, a->ldw, classes, elem);
-  const Shape whole = {rows, classes, in}, part = {rows, f.piece, in}, grads[2] = {{rows, in, f.piece}, {in, f.piece, rows}};
-  const Shape *first = a->dx ? grads : grads + 1;
+  const Shape whole = {rows, classes, in};
   const int n = (a->dx ? 1 : 0) + (a->dw ? 1 : 0);
+  // As few pieces as kSignalBytes allow, or up to three more where their tiles come out more evenly (8192 x 4096 x 65536 bf16 in 6 pieces 15.7 ms, in 8 14.3).
   Cut c[2][4] = {};
-  double time[2];
+  double time[2], best[2] = {1e300, 1e300};
+  int64_t piece[2] = {classes, classes};
   for (int direct = 0; direct < 2; ++direct) {
-    time[direct] = cut(&whole, 1, a->type, direct, widest_tile(in, elem), &c[direct][0], 1);
-    if (f.signal) time[direct] += f.pieces * cut(&part, 1, a->type, direct, widest_tile(in, elem), &c[direct][1], 1);
-    if (n > 0) time[direct] += f.pieces * cut(first, n, a->type, direct, widest_tile(classes, elem), c[direct] + 2);
+    time[direct] = cut(&whole, 1, a->type, direct, widest_tile(in, elem), &c[direct][0], 1, kLossEnds);
+    if (!f.signal) continue;
+    const int64_t least = ceil_div(classes, std::max<int64_t>(kSignalBytes / (rows * (int64_t)elem) / kPieceStep * kPieceStep, kLeastPiece));
+    for (int64_t pieces = least; pieces <= (least == 1 ? 1 : least + 3); ++pieces) {
+      const int64_t p = pieces == 1 ? classes : std::max(kLeastPiece, ceil_div(ceil_div(classes, pieces), kPieceStep) * kPieceStep);
+      const Shape part = {rows, p, in}, grads[2] = {{rows, in, p}, {in, p, rows}};
+      Cut mine[3] = {};
+      double t = cut(&part, 1, a->type, direct, widest_tile(in, elem), &mine[0], 1, kLossEnds);
+      if (n > 0) t += cut(a->dx ? grads : grads + 1, n, a->type, direct, widest_tile(classes, elem), mine + 1);
+      t *= ceil_div(classes, p);
+      if (t >= best[direct]) continue;
+      best[direct] = t;
+      piece[direct] = p;
+      std::copy(mine, mine + 3, c[direct] + 1);
+    }
+    time[direct] += best[direct];
   }
   if (!x_direct || !w_direct) time[1] += kPackLaunch + (x_direct ? 0 : pack_cost(rows, in, elem)) + (w_direct ? 0 : pack_cost(in, classes, elem));
   f.direct = (x_direct && w_direct) || tiny || time[1] < time[0];
   f.copy_x = f.signal || (f.direct && !x_direct) || tiny;
   f.copy_w = (f.direct && !w_direct) || tiny;
   const Cut *mine = c[f.direct];
+  f.piece = piece[f.direct];
+  f.pieces = ceil_div(classes, f.piece);
   f.logits = mine[0];
   f.piece_logits = mine[1];
   if (a->dx) f.dx = mine[2];
