@@ -80,53 +80,93 @@ struct Scatter {
   float *part;                         // [chunks][2][width]: of the run that comes from the chunk before, and of the one that goes on in the next
   int64_t rows, lddy, lddw;
   uint32_t ignore32;                   // the ignored token, or one that is none
-  int32_t vocab, width, token_bytes, lanes, range, chunk;      // range: tokens of a workgroup of k_sort; chunk: sorted positions of one of k_sums
+  int32_t vocab, width, token_bytes, lanes, join_lanes, range, chunk;      // range: tokens of a workgroup of k_sort; chunk: sorted positions of one of k_sums
   uint32_t chunk_blocks;
   float scale;
 };
 
-// A workgroup's tokens are [first, first + range).  Each of its sixteen wavefronts goes over a sixteenth of the positions, twice: it counts its tokens, and, when all have
-// counted, puts their positions down behind those of the smaller tokens and of the wavefronts before it.  Smaller tokens outside the range are only counted.
+// A workgroup's tokens are [first, first + range).  Each of its sixteen wavefronts goes over a sixteenth of the positions and lists those of its tokens; smaller tokens outside the range are only
+// counted.  It counts each of its tokens, and, when all have counted, puts their positions down behind those of the smaller tokens and of the wavefronts before it.  A wavefront whose list is full (tokens
+// that are mostly of one range) goes over its positions again instead.
 // Every workgroup reads all tokens (from L2), so what counts is the operations per token: they are 32-bit numbers, of which those that add nothing are the largest, and 64 of them are skipped together
-// where none is in the range (32768 tokens of a vocabulary of 50001: 37 us with 64-bit comparisons and one batch at a time, 28.7 with eight on their way).
+// where none is in the range.  Equal tokens of a batch are counted together, not by an atomic each (64 additions to one place in LDS are 64 turns).
 constexpr int kSortThreads = 1024, kSortWaves = 16;
 constexpr uint32_t kNoToken = ~0u;
-template <typename W> __device__ __forceinline__ uint32_t token32(const void *tokens, int64_t i, uint32_t ignore) {
+template <typename W> __device__ __forceinline__ uint32_t token32(const W *tokens, uint32_t i, uint32_t ignore) {
   uint32_t k;
   if constexpr (sizeof(W) == 8) {
-    const uint2 x = static_cast<const uint2 *>(tokens)[i];
+    const uint2 x = reinterpret_cast<const uint2 *>(tokens)[i];
     k = x.y ? kNoToken : x.x;
   } else {
-    k = static_cast<const uint32_t *>(tokens)[i];
+    k = reinterpret_cast<const uint32_t *>(tokens)[i];
   }
   return k == ignore ? kNoToken : k;
 }
 template <typename W, int RANGE>
 __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
-  __shared__ int32_t count[kSortWaves][RANGE];
-  __shared__ int32_t wave_sum[2][kSortWaves];
   constexpr int U = 8;        // batches of 64 on their way at once
+  constexpr int kList = RANGE <= 512 ? 1024 : 256, kKeyBits = 11;        // entries: position from the wavefront's first << kKeyBits | token from the range's first
+  __shared__ int32_t count[kSortWaves][RANGE];
+  __shared__ uint32_t list[kSortWaves][kList];
+  __shared__ int32_t wave_sum[2][kSortWaves];
+  static_assert(RANGE <= 1 << kKeyBits, "");
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const uint64_t lower = (1ull << lane) - 1;
   const uint32_t first = blockIdx.x * (uint32_t)a.range, range = min((uint32_t)a.range, (uint32_t)a.vocab - first);
-  const int64_t per = (a.rows + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64, from = wave * per, to = min(a.rows, from + per);
+  // (a wavefront's positions, from its first on: at most 2^26)
+  const int64_t per = (a.rows + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64, from = wave * per;
+  const int mine = (int)max((int64_t)0, min(a.rows - from, per));
+  const W *tokens = static_cast<const W *>(a.tokens) + from;
   for (int i = t; i < kSortWaves * RANGE; i += kSortThreads) (&count[0][0])[i] = 0;
-  __syncthreads();
   auto batches = [&](auto each) __attribute__((always_inline)) {        // each(position, token)
-    for (int64_t i0 = from; i0 < to; i0 += 64 * U) {
+    int i0 = 0;
+    for (; i0 + 64 * U <= mine; i0 += 64 * U) {
       uint32_t k[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) k[u] = token32<W>(a.tokens, min(i0 + 64 * u + lane, to - 1), a.ignore32);
+      for (int u = 0; u < U; ++u) k[u] = token32(tokens, (uint32_t)(i0 + 64 * u + lane), a.ignore32);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i0 + 64 * u >= to) break;
-        each(i0 + 64 * u + lane, i0 + 64 * u + lane < to ? k[u] : kNoToken);
-      }
+      for (int u = 0; u < U; ++u) each(i0 + 64 * u + lane, k[u]);
+    }
+    for (; i0 < mine; i0 += 64) {
+      const uint32_t k = token32(tokens, (uint32_t)min(i0 + lane, mine - 1), a.ignore32);
+      each(i0 + lane, i0 + lane < mine ? k : kNoToken);
     }
   };
-  int32_t below = 0;
-  batches([&](int64_t, uint32_t k) __attribute__((always_inline)) {
+  int32_t below = 0, listed = 0;
+  batches([&](int i, uint32_t k) __attribute__((always_inline)) {
     below += __popcll(__ballot(k < first));
-    if (k - first < range) atomicAdd(&count[wave][k - first], 1);
+    const uint64_t in = __ballot(k - first < range);
+    if (in) {
+      const int n = __popcll(in);
+      if (listed + n <= kList && k - first < range) list[wave][listed + __popcll(in & lower)] = (uint32_t)i << kKeyBits | (k - first);
+      listed += n;
+    }
+  });
+  const bool all_listed = listed <= kList && per <= 1 << (32 - kKeyBits);
+  // Calls each(first lane of those with a token, which lanes, position, token from the range's first) for the tokens of each batch.
+  auto tokens_of_mine = [&](auto each) __attribute__((always_inline)) {
+    auto batch = [&](int i, int32_t k) __attribute__((always_inline)) {
+      uint64_t left = __ballot(k >= 0);
+      while (left) {
+        const int32_t one = __builtin_amdgcn_readlane(k, __builtin_ctzll(left));
+        const uint64_t same = __ballot(k == one);
+        each(same, i, one, k == one);
+        left &= ~same;
+      }
+    };
+    if (all_listed) {
+      for (int e = 0; e < listed; e += 64) {
+        const uint32_t x = list[wave][min(e + lane, kList - 1)];
+        batch((int)(x >> kKeyBits), e + lane < listed ? (int32_t)(x & ((1u << kKeyBits) - 1)) : -1);
+      }
+    } else {
+      batches([&](int i, uint32_t k) __attribute__((always_inline)) { batch(i, k - first < range ? (int32_t)(k - first) : -1); });
+    }
+  };
+  volatile int32_t *places = count[wave];
+  __syncthreads();
+  tokens_of_mine([&](uint64_t same, int, int32_t k, bool) __attribute__((always_inline)) {
+    if (lane == __builtin_ctzll(same)) places[k] = places[k] + (int32_t)__popcll(same);
   });
   if (lane == 0) wave_sum[0][wave] = below;
   __syncthreads();
@@ -137,12 +177,12 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
   int32_t base = below;
   for (int k0 = 0; k0 < RANGE; k0 += kSortThreads) {
     const int k = k0 + t;
-    int32_t mine = 0;
+    int32_t total = 0;
     if (k < RANGE) {
 #pragma unroll
-      for (int w = 0; w < kSortWaves; ++w) mine += count[w][k];
+      for (int w = 0; w < kSortWaves; ++w) total += count[w][k];
     }
-    int32_t sum = mine;
+    int32_t sum = total;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int32_t other = __shfl_up(sum, o, 64);
@@ -157,7 +197,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
       before += w < wave ? wave_sum[1][w] : 0;
       all += wave_sum[1][w];
     }
-    int32_t at = before + sum - mine;
+    int32_t at = before + sum - total;
     if ((uint32_t)k < range) a.start[first + k] = at;
     if (k < RANGE) {
 #pragma unroll
@@ -171,24 +211,15 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
   }
   if (t == 0 && first + range == (uint32_t)a.vocab) a.start[a.vocab] = base;
   __syncthreads();
-  volatile int32_t *mine = count[wave];
-  batches([&](int64_t i, uint32_t token) __attribute__((always_inline)) {
-    const bool in = token - first < range;
-    const int32_t k = in ? (int32_t)(token - first) : -1;
-    uint64_t left = __ballot(in);
-    while (left) {
-      const int32_t one = __builtin_amdgcn_readlane(k, __builtin_ctzll(left));
-      const uint64_t same = __ballot(k == one);
-      if (k == one) {
-        const int32_t at = mine[one] + __popcll(same & ((1ull << lane) - 1));
-        a.order[at] = (int32_t)i;
-        a.key[at] = (int32_t)token;
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (lane == __builtin_ctzll(same)) mine[one] = mine[one] + (int32_t)__popcll(same);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      left &= ~same;
+  tokens_of_mine([&](uint64_t same, int i, int32_t k, bool here) __attribute__((always_inline)) {
+    if (here) {
+      const int32_t at = places[k] + __popcll(same & lower);
+      a.order[at] = (int32_t)(from + i);
+      a.key[at] = (int32_t)first + k;
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (lane == __builtin_ctzll(same)) places[k] = places[k] + (int32_t)__popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   });
 }
 
@@ -255,33 +286,36 @@ __global__ __launch_bounds__(256) void k_sums(const Scatter a) {
   flush(hi < n && a.key[hi] == now);
 }
 
-// A run that crosses borders: a workgroup at each border, which has something to do if it is the run's first.  256 columns at a time, four per lane, the parts dealt to four wavefronts.
+// A run that crosses borders: a workgroup at each border, which has something to do if it is the run's first.  Four columns per lane, 2^join_lanes lanes (up to 64) along a part; the
+// parts are dealt to the others of the workgroup, whose sums are added in their order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_join(const Scatter a) {
-  __shared__ float sums[4][256];
+  __shared__ v4s sums[256];
   const int64_t b = (int64_t)blockIdx.x + 1, at = b * a.chunk;
   const int32_t n = a.start[a.vocab], v = a.key[at], before = a.key[at - 1];        // (asked for together; behind the last position they are what was there)
   if (at >= n || before != v) return;
   const int32_t start = a.start[v], end = a.start[v + 1];
   if (start < at - a.chunk) return;
   const int64_t last = (end - 1) / a.chunk, parts = last - b + 2;        // of chunk b - 1 what goes on, of the others what comes from before
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  for (int64_t c0 = (int64_t)blockIdx.y * 256; c0 < a.width; c0 += (int64_t)gridDim.y * 256) {
+  const int along = 1 << a.join_lanes, deep = 256 >> a.join_lanes, lane = threadIdx.x & (along - 1), turn = threadIdx.x >> a.join_lanes;
+  for (int64_t c0 = (int64_t)blockIdx.y * along * 4; c0 < a.width; c0 += (int64_t)gridDim.y * along * 4) {
     const int64_t c = c0 + lane * 4;
-    float s[4] = {};
+    v4s s = {0.f, 0.f, 0.f, 0.f};
     if (c < a.width) {
 #pragma unroll 8
-      for (int64_t i = wave; i < parts; i += 4) {
+      for (int64_t i = turn; i < parts; i += deep) {
         const u32x4v x = load16_n(a.part + (2 * (b - 1 + i) + (i == 0 ? 1 : 0)) * a.width + c, a.width - c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += __uint_as_float(x[e]);
+        s += __builtin_bit_cast(v4s, x);
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sums[wave][lane * 4 + e] = s[e];
+    sums[threadIdx.x] = s;
     __syncthreads();
-    if (c0 + t < a.width) static_cast<T *>(a.dw)[(int64_t)v * a.lddw + c0 + t] = from_f32<T>(((sums[0][t] + sums[1][t]) + (sums[2][t] + sums[3][t])) * a.scale);
+    if (threadIdx.x < along * 4 && c0 + threadIdx.x < a.width) {
+      float x = sums[threadIdx.x >> 2][threadIdx.x & 3];
+      for (int i = 1; i < deep; ++i) x += sums[i * along + (threadIdx.x >> 2)][threadIdx.x & 3];
+      static_cast<T *>(a.dw)[(int64_t)v * a.lddw + c0 + threadIdx.x] = from_f32<T>(x * a.scale);
+    }
   }
 }
 
@@ -324,9 +358,11 @@ ScatterPlan plan_scatter(const cada_embedding_grad *a) {
   if (a->rows == 0) return p;
   // a workgroup's range of tokens: one for each CU, and no more than its counts have room for
   p.range = (int32_t)std::min<int64_t>(2048, ceil_div(a->vocab, 256));
-  // chunks for every CU a few times over, where that leaves some rows to each
-  p.chunk = 16;
-  while (p.chunk < 128 && (int64_t)p.chunk * 1024 < a->rows) p.chunk *= 2;
+  // chunks for a million lanes, where that leaves some rows to each and no run in too many parts
+  const int64_t lanes = std::min<int64_t>(ceil_div(a->width, 16 / (int)type_bytes(a->type)), 1024);
+  p.chunk = 8;
+  while (p.chunk < 128 && (int64_t)p.chunk << 18 < a->rows * lanes) p.chunk *= 2;
+  while (p.chunk < 128 && (int64_t)p.chunk << 13 < a->rows) p.chunk *= 2;
   p.chunks = ceil_div(a->rows, p.chunk);
   p.off_order = ops_align((size_t)(a->vocab + 1) * 4);
   p.off_key = p.off_order + ops_align((size_t)a->rows * 4);
@@ -359,7 +395,7 @@ int scatter(const cada_embedding_grad *a, const ScatterPlan &p) {
   Scatter s{};
   s.tokens = a->tokens; s.dy = a->dy; s.dw = a->dw; s.rows = a->rows; s.ignore32 = a->ignore_index >= 0 && a->ignore_index < a->vocab ? (uint32_t)a->ignore_index : kNoToken; s.lddy = a->lddy; s.lddw = a->lddw;
   s.start = reinterpret_cast<int32_t *>(ws); s.order = reinterpret_cast<int32_t *>(ws + p.off_order); s.key = reinterpret_cast<int32_t *>(ws + p.off_key); s.part = reinterpret_cast<float *>(ws + p.off_part);
-  s.vocab = (int32_t)a->vocab; s.width = (int32_t)a->width; s.token_bytes = a->token_bytes; s.lanes = lanes_for(a->width, E); s.range = p.range; s.chunk = p.chunk;
+  s.vocab = (int32_t)a->vocab; s.width = (int32_t)a->width; s.token_bytes = a->token_bytes; s.lanes = lanes_for(a->width, E); s.join_lanes = std::min(6, lanes_for(a->width, 4)); s.range = p.range; s.chunk = p.chunk;
   s.scale = (float)a->scale;
   const unsigned groups = (unsigned)ceil_div(a->vocab, p.range);
   auto sort = [&](auto token) {
@@ -377,7 +413,7 @@ int scatter(const cada_embedding_grad *a, const ScatterPlan &p) {
   k_sums<T><<<dim3(s.chunk_blocks + fill, across), 256, 0, st>>>(s);
   if (int rc = ops_launched("embedding gradient")) return rc;
   if (p.chunks == 1) return CADA_OK;
-  k_join<T><<<dim3((unsigned)p.chunks - 1, (unsigned)std::min<int64_t>(ceil_div(a->width, 256), 1024)), 256, 0, st>>>(s);
+  k_join<T><<<dim3((unsigned)p.chunks - 1, (unsigned)std::min<int64_t>(ceil_div(a->width, (int64_t)4 << s.join_lanes), 1024)), 256, 0, st>>>(s);
   return ops_launched("embedding join");
 }
 

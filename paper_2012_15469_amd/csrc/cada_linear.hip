@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
   if (lane == 0 && c < j.db_n) {
 #pragma unroll
     for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x];
-    static_cast<T *>(j.db)[c] = from_f32<T>(s);
+    static_cast<T *>(j.db)[c] = from_f32<T>(j.db_factor ? s * *j.db_factor : s);
   }
 }
 
@@ -304,6 +304,16 @@ void forward_tiles(const Product &p, bool dir, hipStream_t st) {
 }
 
 template <typename T>
+void forward_tiles_of(int tile, bool direct, const Product &p, hipStream_t st) {
+  if (tile == 32) forward_tiles<T, 32, 1, 1, 4>(p, direct, st);
+  if (tile == 64) forward_tiles<T, 64, 2, 2, 1>(p, direct, st);
+  if constexpr (sizeof(T) == 2) {
+    if (tile == 128) forward_tiles<T, 128, 2, 4, 1>(p, direct, st);
+    if (tile == 256) forward_tiles<T, 256, 2, 4, 1>(p, direct, st);
+  }
+}
+
+template <typename T>
 int launch_join(Join &j, hipStream_t st) {
   int64_t total = 0;
   for (int i = 0; i < 2; ++i) {
@@ -343,13 +353,8 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
     else if constexpr (sizeof(T) == 4) k_few_rows<T, 32><<<grid, kFewThreads, 0, st>>>(p);
   } else if (f.by_element) {
     k_by_element<T, true, false, NO_SIGNAL><<<many(a->rows * a->out), 256, 0, st>>>(p);
-  } else if (f.cut.tile == 32) {
-    forward_tiles<T, 32, 1, 1, 4>(p, f.direct, st);
-  } else if (f.cut.tile == 64) {
-    forward_tiles<T, 64, 2, 2, 1>(p, f.direct, st);
-  } else if constexpr (sizeof(T) == 2) {
-    if (f.cut.tile == 128) forward_tiles<T, 128, 2, 4, 1>(p, f.direct, st);
-    if (f.cut.tile == 256) forward_tiles<T, 256, 2, 4, 1>(p, f.direct, st);
+  } else {
+    forward_tiles_of<T>(f.cut.tile, f.direct, p, st);
   }
   if (int rc = ops_launched("linear")) return rc;
   if (p.splits == 1) return CADA_OK;
@@ -458,6 +463,11 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
 
 }  // namespace
 
+int linear_sums(int type, int tile, bool direct, const Product &p, hipStream_t st) {
+  if (type == CADA_BF16) forward_tiles_of<bf16>(tile, direct, p, st);
+  else forward_tiles_of<float>(tile, direct, p, st);
+  return ops_launched("linear");
+}
 int linear_products(int type, int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st) { return type == CADA_BF16 ? products<bf16>(tile, direct, dx, dw, st) : products<float>(tile, direct, dx, dw, st); }
 int linear_join(int type, Join &j, hipStream_t st) { return type == CADA_BF16 ? launch_join<bf16>(j, st) : launch_join<float>(j, st); }
 int linear_pack(int type, Packs &a, hipStream_t st) { return type == CADA_BF16 ? launch_pack<bf16>(a, st) : launch_pack<float>(a, st); }

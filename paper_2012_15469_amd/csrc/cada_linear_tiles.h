@@ -39,6 +39,7 @@ struct Join {
   int64_t groups[2];         // M * ceil(N / 8), 0 where there is nothing to join
   const float *db_part;      // [db_parts][N of the second product] or null
   void *db;
+  const float *db_factor;    // of the column sums, in device memory, or null (1)
   int db_parts, db_n;
   unsigned db_block;         // the first workgroup of the column sums
 };
@@ -47,6 +48,7 @@ struct Pack { const void *src; void *dst; int64_t ld, rows, cols, ldd; };
 struct Packs { Pack p[2]; int64_t pieces[2]; };
 
 // Products, joins and copies of a type (CADA_F32 or CADA_BF16), for other files than cada_linear.hip.
+int linear_sums(int type, int tile, bool direct, const Product &p, hipStream_t st);        // a forward product whose sums go to p.partial
 int linear_products(int type, int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st);
 int linear_join(int type, Join &j, hipStream_t st);
 int linear_pack(int type, Packs &a, hipStream_t st);

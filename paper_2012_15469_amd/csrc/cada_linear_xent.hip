@@ -3,7 +3,8 @@
 // The logits' tiles (cada_linear_tiles.h) end in statistics: of each row, and of each strip of 32 or 64 columns, the largest logit and the sum of the exponentials of the
 // distances to it.  A row's strips are then joined, as one goes along, to the row's largest and its sum, which is its loss.  For the gradients the logits are formed again in
 // pieces of the classes; their tiles end in softmax - target (but for a factor) in the operands' type, from which the products of a layer's gradients are taken while it is in the caches: dw is finished piece by
-// piece, dx is added up in float32.  That is four products where keeping the logits would take three, and memory for one piece instead of all.
+// piece, dx is added up in float32.  That is four products where keeping the logits would take three, and memory for one piece instead of all.  Logits that are not
+// more than a piece are kept in float32 (k_kept_rows).
 #include <algorithm>
 
 #include "cada_linear_tiles.h"
@@ -23,6 +24,8 @@ struct Loss {
   float *db_part;            // [strips][piece] or null
   int64_t rows, ignore, ldz, chunks;
   int32_t classes, label_bytes, first;      // first: the piece's first class
+  const float *kept, *kept_bias;            // kept logits without their bias, in `splits` parts; the biases in float32, -inf behind the last class
+  int32_t splits;
   int32_t lanes;             // rows of a workgroup of k_rows, as a power of two
   float smoothing, keep, scale;      // keep = 1 - smoothing, rounded once
 };
@@ -284,7 +287,7 @@ template <typename T, int BM> struct ToSignal {
     }
     if constexpr (FN == 1) all[0] += __shfl_xor(all[0], 16, 64);
     const int n = n0 + wn + 32 * (mine >> 4) + 8 * (mine >> 2 & 3) + 4 * half + (mine & 3);
-    if ((FN == 2 || (lane & 16) == 0) && n < p.N) q.db_part[((m0 + wm) / (32 * FM)) * p.N + n] = all[0] * q.head->factor;
+    if ((FN == 2 || (lane & 16) == 0) && n < p.N) q.db_part[((m0 + wm) / (32 * FM)) * p.N + n] = all[0];
   }
   template <typename> __device__ __forceinline__ void row(const Product &p, int64_t m0, int n0, int t, float (&z)[8]) {
     const int64_t m = m0 + t / 4;
@@ -306,16 +309,62 @@ template <typename T, int BM> struct ToSignal {
     }
     z[0] += __shfl_xor(z[0], 4, 64);
     const int column = n + (t >> 5 & 1) * 4 + (t >> 4 & 1) * 2 + (t >> 3 & 1);
-    if ((t & 4) == 0 && column < p.N) q.db_part[(m0 / BM * 2 + (t >> 6)) * p.N + column] = z[0] * q.head->factor;
+    if ((t & 4) == 0 && column < p.N) q.db_part[(m0 / BM * 2 + (t >> 6)) * p.N + column] = z[0];
   }
 };
+
+__device__ __forceinline__ void clear_counters(LossHead *head) {        // (by a launch before the one that counts)
+  if (threadIdx.x < kCounters) head->done[threadIdx.x * kLineWords] = 0;
+  if (threadIdx.x == 0) head->full[0] = 0;
+}
+// The workgroups' losses and numbers of rows that count, whose last one to come adds them up in the workgroups' order: `sum` and `used` are thread 0's.
+__device__ __forceinline__ void add_up(const Loss &q, double sum, int64_t used) {
+  __shared__ bool last;
+  const int t = threadIdx.x;
+  if (t == 0) {
+    // (few workgroups count themselves in the one place, 12 ns each and one trip less)
+    const bool few = gridDim.x <= 256;
+    const uint32_t c = blockIdx.x % kCounters, of_mine = (gridDim.x - c + kCounters - 1) / kCounters, counters = few ? gridDim.x : kCounters;
+    __hip_atomic_store(&q.head->loss[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&q.head->used[blockIdx.x], used, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (they are where the last workgroup reads them before this one is counted)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = (few || __hip_atomic_fetch_add(&q.head->done[c * kLineWords], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of_mine - 1) &&
+           __hip_atomic_fetch_add(&q.head->full[0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == counters - 1;
+  }
+  __syncthreads();
+  if (!last || t >= 64) return;
+  sum = 0.0;
+  used = 0;
+#pragma unroll 4
+  for (int i = t; i < (int)gridDim.x; i += 64) {
+    sum += __hip_atomic_load(&q.head->loss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    used += __hip_atomic_load(&q.head->used[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  sum = wave_sum_f64(sum);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) used += __shfl_xor(used, o, 64);
+  if (t == 0) {
+    const int64_t count = max(used, (int64_t)1);
+    if (q.mean) *q.mean = (float)(sum / (double)count);
+    q.head->factor = q.keep * q.scale / (float)count;
+  }
+}
+// A row's loss from its statistics and its label's logit (log(sum exp z) - keep z_y - smoothing mean_left z, with the largest taken out of all three).
+__device__ __forceinline__ float loss_of(const Loss &q, const Stat &s, float base, float z_label, bool used, bool known) {
+  float l = logf(s.sum) - q.keep * (z_label - base);
+  if (q.smoothing != 0.f) l -= q.smoothing * (s.distance / s.left);
+  if (s.top == -kInf && s.sum == 0.f) l = kInf;
+  if (!known) l = __builtin_nanf("");
+  return used ? l : 0.f;
+}
 
 template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product p, const Loss q) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
   __shared__ int32_t label[BM];
   __shared__ __align__(16) float bias[BM];
-  if (blockIdx.x == 0 && threadIdx.x == 0) q.head->done = 0;
+  if (blockIdx.x == 0) clear_counters(q.head);
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
   if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<T, BM>(q, label, bias));
 }
@@ -352,7 +401,6 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
   __shared__ Stat part[1024];
   __shared__ float losses[64];
   __shared__ uint8_t used_rows[64];
-  __shared__ bool last;
   const int here = 1 << q.lanes, t = threadIdx.x, row = t & (here - 1), lane = t >> q.lanes, high = 1024 >> q.lanes;
   double sum = 0.0;
   int64_t used_sum = 0;
@@ -385,11 +433,7 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
       const int64_t label = label_at(q.labels, q.label_bytes, r);
       const bool used = label != q.ignore, known = counts(q, label), none = s.top == -kInf && s.sum == 0.f;
       const float base = s.top == -kInf ? 0.f : s.top;
-      float l = logf(s.sum) - q.keep * ((known ? q.z_label[r] : 0.f) - base);
-      if (q.smoothing != 0.f) l -= q.smoothing * (s.distance / s.left);
-      if (none) l = kInf;
-      if (!known) l = __builtin_nanf("");
-      l = used ? l : 0.f;
+      const float l = loss_of(q, s, base, known ? q.z_label[r] : 0.f, used, known);
       losses[row] = l;
       used_rows[row] = used;
       if (q.loss) q.loss[r] = l;
@@ -404,41 +448,189 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
     }
     __syncthreads();
   }
-  if (t == 0) {
-    __hip_atomic_store(&q.head->loss[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&q.head->used[blockIdx.x], used_sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // (they are where the last workgroup reads them before this one is counted)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    last = __hip_atomic_fetch_add(&q.head->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-  }
-  __syncthreads();
-  if (!last || t >= 64) return;
-  sum = 0.0;
-  used_sum = 0;
-  for (int i = t; i < (int)gridDim.x; i += 64) {
-    sum += __hip_atomic_load(&q.head->loss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    used_sum += __hip_atomic_load(&q.head->used[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  sum = wave_sum_f64(sum);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) used_sum += __shfl_xor(used_sum, o, 64);
-  if (t == 0) {
-    const int64_t count = max(used_sum, (int64_t)1);
-    if (q.mean) *q.mean = (float)(sum / (double)count);
-    q.head->factor = q.keep * q.scale / (float)count;
-  }
+  add_up(q, sum, used_sum);
 }
 
-// x in rows on 16-byte boundaries, zeros for those that do not count.
+// Kept logits: a group of LANES lanes takes a row, V pieces of four classes per lane, which stay in registers from the statistics to the signal.  A workgroup goes on to further rows and adds up, in
+// registers too, its part of the signal's column sums.  Bound by memory: the logits are read once (in all their parts), the signal is written once.
+template <int LANES, int N> __device__ __forceinline__ void group_join(float (&x)[N], float (*part)[N], bool largest) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float y = __shfl_xor(x[i], o, 64);
+      x[i] = largest ? fmaxf(x[i], y) : x[i] + y;
+    }
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) part[threadIdx.x >> 6][i] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = part[0][i];
+#pragma unroll
+      for (int w = 1; w < LANES / 64; ++w) x[i] = largest ? fmaxf(x[i], part[w][i]) : x[i] + part[w][i];
+    }
+  }
+}
+template <typename T, int LANES, int V>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const Loss q) {
+  constexpr int kGroups = LANES < 256 ? 256 / LANES : 1;
+  __shared__ float part_top[LANES / 64][1], part_sum[LANES / 64][3];
+  __shared__ double group_loss[kGroups];
+  __shared__ int64_t group_used[kGroups];
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, columns = (q.classes + 7) / 8 * 8;
+  v4s z[V], column[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) column[v] = v4s{0.f, 0.f, 0.f, 0.f};
+  double losses = 0.0;
+  int64_t used_rows = 0;
+  const int64_t stride = (int64_t)gridDim.x * kGroups;
+  v4s next[V];        // the next row's first part, on its way while this row is worked on
+  int64_t next_label;
+  auto ask = [&](int64_t at) __attribute__((always_inline)) {
+    at = min(at, q.rows - 1);
+    next_label = label_at(q.labels, q.label_bytes, at);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * LANES + lane) * 4;
+      next[v] = v4s{-kInf, -kInf, -kInf, -kInf};
+      if (c < columns) next[v] = *reinterpret_cast<const v4s *>(q.kept + at * columns + c);
+    }
+  };
+  ask((int64_t)blockIdx.x * kGroups + group);
+  for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < q.rows; r0 += stride) {
+    const int64_t r = min(r0 + group, q.rows - 1);
+    const bool here = r0 + group < q.rows;
+    const float *from = q.kept + r * columns;
+    const int64_t label = next_label;
+#pragma unroll
+    for (int v = 0; v < V; ++v) z[v] = next[v];
+    if (r0 + stride < q.rows) ask(r0 + stride + group);
+    const bool used = label != q.ignore, known = counts(q, label);
+    float top[1] = {-kInf}, z_label = 0.f;
+    if (known) {
+      for (int i = 0; i < q.splits; ++i) z_label += from[i * q.rows * columns + label];
+      z_label += q.kept_bias[label];
+    }
+    for (int i = 1; i < q.splits; ++i) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (v * LANES + lane) * 4;
+        if (c < columns) z[v] += *reinterpret_cast<const v4s *>(from + i * q.rows * columns + c);
+      }
+    }
+    float s[3] = {0.f, 0.f, 0.f};        // sum, left, distance
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * LANES + lane) * 4;
+      if (c < columns) z[v] += *reinterpret_cast<const v4s *>(q.kept_bias + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (c + e >= q.classes) z[v][e] = -kInf;        // (what lies behind the last class is no sum of anything)
+        top[0] = fmaxf(top[0], z[v][e]);
+      }
+    }
+    group_join<LANES>(top, part_top, true);
+    const float base = top[0] == -kInf ? 0.f : top[0];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[0] += power(z[v][e], base);
+        if (q.smoothing != 0.f) {
+          const bool in = z[v][e] != -kInf;
+          s[1] += in ? 1.f : 0.f;
+          s[2] += in ? z[v][e] - base : 0.f;
+        }
+      }
+    group_join<LANES>(s, part_sum, false);
+    const Stat stat = {top[0], s[0], s[2], s[1]};
+    if (lane == 0 && here) {
+      const float l = loss_of(q, stat, base, z_label, used, known);
+      if (q.loss) q.loss[r] = l;
+      losses += (double)l;
+      used_rows += used;
+    }
+    if (!here) continue;        // (no barrier until the next row's: a workgroup's groups go on together)
+    const bool flat = !used || !known || (top[0] == -kInf && s[0] == 0.f);
+    const float f_total = flat ? 0.f : 1.f / (s[0] * q.keep), f_each = flat || q.smoothing == 0.f ? 0.f : q.smoothing / (s[1] * q.keep), from_top = flat ? kInf : base;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * LANES + lane) * 4;
+      if (c >= columns) continue;
+      v4s g;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        g[e] = power(z[v][e], from_top) * f_total - (z[v][e] != -kInf ? f_each : 0.f);
+        if (flat) g[e] = 0.f;        // (whatever the logits are)
+        else if (label == c + e) g[e] -= 1.f;
+      }
+      column[v] += g;
+      if (q.signal) {
+        T *to = static_cast<T *>(q.signal) + r * q.ldz + c;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint64_t *>(to) = (uint64_t)f2bf_pk(g[2], g[3]) << 32 | f2bf_pk(g[0], g[1]);
+        else *reinterpret_cast<v4s *>(to) = g;
+      }
+    }
+  }
+  if (q.db_part) {
+    float *to = q.db_part + (int64_t)blockIdx.x * q.classes;
+    if constexpr (kGroups > 1) {        // (the groups' sums in their order)
+      __shared__ v4s sums[kGroups][V * LANES];
+#pragma unroll
+      for (int v = 0; v < V; ++v) sums[group][v * LANES + lane] = column[v];
+      __syncthreads();
+      for (int c = threadIdx.x; c < q.classes; c += 256) {
+        float x = 0.f;
+        for (int i = 0; i < kGroups; ++i) x += sums[i][c >> 2][c & 3];
+        to[c] = x;
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = (v * LANES + lane) * 4 + e;
+          if (c < q.classes) to[c] = column[v][e];
+        }
+    }
+  }
+  if (lane == 0) {
+    group_loss[group] = losses;
+    group_used[group] = used_rows;
+  }
+  __syncthreads();
+  losses = 0.0;
+  used_rows = 0;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kGroups; ++i) {
+      losses += group_loss[i];
+      used_rows += group_used[i];
+    }
+  }
+  add_up(q, losses, used_rows);
+}
+
+// Copies in rows on 16-byte boundaries: of x, with zeros for rows that do not count, and of w, each where there is one to make; and of the biases in float32 for kept logits.
 template <typename T>
-__global__ __launch_bounds__(256) void k_copy_rows(const Loss q, const Pack p) {
+__global__ __launch_bounds__(256) void k_copy(const Loss q, const Packs a, float *bias) {
   constexpr int E = Elem<T>::kPer16;
-  const int64_t per = p.ldd / E;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.rows * per; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / per, col = (i - row * per) * E;
-    const bool in = counts(q, label_at(q.labels, q.label_bytes, row));
+  if (blockIdx.x == 0) clear_counters(q.head);
+  const int64_t biases = bias ? (q.classes + 7) / 8 * 8 : 0;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < a.pieces[0] + a.pieces[1] + biases; at += (int64_t)gridDim.x * 256) {
+    if (at >= a.pieces[0] + a.pieces[1]) {
+      const int64_t n = at - a.pieces[0] - a.pieces[1];
+      bias[n] = n >= q.classes ? -kInf : q.bias ? to_f32(static_cast<const T *>(q.bias)[n]) : 0.f;
+      continue;
+    }
+    const int which = at < a.pieces[0] ? 0 : 1;
+    const Pack &p = a.p[which];
+    const int64_t i = at - (which ? a.pieces[0] : 0), per = p.ldd / E, row = i / per, col = (i - row * per) * E;
     u32x4v x = load16_n(static_cast<const T *>(p.src) + row * p.ld + col, p.cols - col);
-    if (!in) x = u32x4v{0, 0, 0, 0};
+    if (which == 0 && !counts(q, label_at(q.labels, q.label_bytes, row))) x = u32x4v{0, 0, 0, 0};
     *reinterpret_cast<u32x4v *>(static_cast<T *>(p.dst) + row * p.ldd + col) = x;
   }
 }
@@ -473,6 +665,18 @@ int logits(const Product &p, const Loss &q, int tile, bool statistics, bool dire
 }
 
 template <typename T>
+int kept_rows(const Loss &q, hipStream_t st) {
+  const KeptShape s = kept_shape(q.rows, q.classes);
+  const unsigned grid = (unsigned)std::min(ceil_div(q.rows, std::max(1, 256 / s.lanes)), s.groups), threads = (unsigned)std::max(256, s.lanes);
+  if (s.lanes == 64 && s.pieces == 1) k_kept_rows<T, 64, 1><<<grid, threads, 0, st>>>(q);
+  if (s.lanes == 64 && s.pieces == 4) k_kept_rows<T, 64, 4><<<grid, threads, 0, st>>>(q);
+  if (s.lanes == 256 && s.pieces == 1) k_kept_rows<T, 256, 1><<<grid, threads, 0, st>>>(q);
+  if (s.lanes == 256 && s.pieces == 4) k_kept_rows<T, 256, 4><<<grid, threads, 0, st>>>(q);
+  if (s.lanes == 512 && s.pieces == 8) k_kept_rows<T, 512, 8><<<grid, threads, 0, st>>>(q);
+  return ops_launched("linear cross-entropy rows");
+}
+
+template <typename T>
 int loss(const cada_linear_xent *a, const LossPlan &f) {
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   char *ws = static_cast<char *>(a->workspace);
@@ -484,33 +688,47 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
   q.smoothing = (float)a->smoothing; q.keep = (float)(1.0 - a->smoothing); q.scale = (float)a->scale;
   const T *x = static_cast<const T *>(a->x), *w = static_cast<const T *>(a->w);
   int64_t ldx = a->ldx, ldw = a->ldw, x_cols = a->in, w_cols = a->classes;
+  Packs k{};
   if (f.copy_x) {
-    const Pack k = {a->x, ws + f.off_x, a->ldx, a->rows, a->in, packed_ld(a->in)};
-    k_copy_rows<T><<<many(a->rows * (k.ldd / Elem<T>::kPer16)), 256, 0, st>>>(q, k);
-    if (int rc = ops_launched("linear cross-entropy copy")) return rc;
-    x = static_cast<const T *>(k.dst); ldx = x_cols = k.ldd;
+    k.p[0] = Pack{a->x, ws + f.off_x, a->ldx, a->rows, a->in, packed_ld(a->in)};
+    k.pieces[0] = a->rows * (k.p[0].ldd / Elem<T>::kPer16);
+    x = static_cast<const T *>(k.p[0].dst); ldx = x_cols = k.p[0].ldd;
   }
   if (f.copy_w) {
-    Packs k{};
-    k.p[0] = Pack{a->w, ws + f.off_w, a->ldw, a->in, a->classes, packed_ld(a->classes)};
-    if (int rc = linear_pack(a->type, k, st)) return rc;
-    w = static_cast<const T *>(k.p[0].dst); ldw = w_cols = k.p[0].ldd;
+    k.p[1] = Pack{a->w, ws + f.off_w, a->ldw, a->in, a->classes, packed_ld(a->classes)};
+    k.pieces[1] = a->in * (k.p[1].ldd / Elem<T>::kPer16);
+    w = static_cast<const T *>(k.p[1].dst); ldw = w_cols = k.p[1].ldd;
+  }
+  float *bias = f.kept ? reinterpret_cast<float *>(ws + f.off_bias) : nullptr;
+  if (f.copy_x || f.copy_w) {
+    k_copy<T><<<many(k.pieces[0] + k.pieces[1] + (bias ? eights(a->classes) : 0)), 256, 0, st>>>(q, k, bias);
+    if (int rc = ops_launched("linear cross-entropy copy")) return rc;
   }
   Product z{};
   lay(&z, f.logits, x, ldx, w, ldw, a->rows, a->classes, a->in, nullptr);
   z.b_cols = w_cols;
-  if (int rc = logits<T>(z, q, f.logits.tile, true, f.direct, st)) return rc;
-  while (q.lanes < 6 && ((int64_t)kLossGroups << q.lanes) < a->rows) ++q.lanes;
-  k_rows<<<(unsigned)std::min<int64_t>(ceil_div(a->rows, 1 << q.lanes), kLossGroups), 1024, 0, st>>>(q);
-  if (int rc = ops_launched("linear cross-entropy rows")) return rc;
+  if (f.kept) {
+    z.partial = reinterpret_cast<float *>(ws + f.off_stats);
+    q.kept = z.partial; q.kept_bias = bias; q.splits = f.logits.splits; q.signal = f.grads ? ws + f.off_signal : nullptr; q.ldz = f.ldz;
+    q.db_part = a->db ? reinterpret_cast<float *>(ws + f.off_db) : nullptr;
+    if (int rc = linear_sums(a->type, f.logits.tile, f.direct, z, st)) return rc;
+    if (int rc = kept_rows<T>(q, st)) return rc;
+  } else {
+    if (int rc = logits<T>(z, q, f.logits.tile, true, f.direct, st)) return rc;
+    while (q.lanes < 6 && ((int64_t)kLossGroups << q.lanes) < a->rows) ++q.lanes;
+    k_rows<<<(unsigned)std::min<int64_t>(ceil_div(a->rows, 1 << q.lanes), kLossGroups), 1024, 0, st>>>(q);
+    if (int rc = ops_launched("linear cross-entropy rows")) return rc;
+  }
   if (!f.signal) return CADA_OK;
   void *signal = f.grads ? ws + f.off_signal : nullptr;
   for (int64_t i = 0; i < f.pieces; ++i) {
     const int64_t first = i * f.piece, here = std::min(f.piece, a->classes - first);
     q.first = (int32_t)first; q.signal = signal; q.ldz = f.ldz; q.db_part = a->db ? reinterpret_cast<float *>(ws + f.off_db) : nullptr;
-    lay(&z, f.piece_logits, x, ldx, w + first, ldw, a->rows, here, a->in, nullptr);
-    z.b_cols = w_cols - first;
-    if (int rc = logits<T>(z, q, f.piece_logits.tile, false, f.direct, st)) return rc;
+    if (!f.kept) {
+      lay(&z, f.piece_logits, x, ldx, w + first, ldw, a->rows, here, a->in, nullptr);
+      z.b_cols = w_cols - first;
+      if (int rc = logits<T>(z, q, f.piece_logits.tile, false, f.direct, st)) return rc;
+    }
     Product dx{}, dw{};
     Join j{};
     if (a->dx) {
@@ -534,7 +752,7 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
       j.p[0].splits = f.dx.splits;
     }
     j.p[1] = dw;
-    if (a->db) { j.db_part = q.db_part; j.db = static_cast<T *>(a->db) + first; j.db_parts = (int)f.strips; j.db_n = (int)here; }
+    if (a->db) { j.db_part = q.db_part; j.db_factor = &q.head->factor; j.db = static_cast<T *>(a->db) + first; j.db_parts = (int)f.strips; j.db_n = (int)here; }
     if (int rc = linear_join(a->type, j, st)) return rc;
   }
   return CADA_OK;

@@ -477,7 +477,9 @@ NormGradPlan plan_grad(const cada_norm_grad *a) {
     p.rows_per_part = std::max<int64_t>(16, ceil_div(a->rows, ceil_div(4 * kCUs, columns)));
     p.parts = ceil_div(a->rows, p.rows_per_part);
   } else {
-    p.parts = std::min(ceil_div(a->rows, rows_at_once(p.shape)), (p.shape.lanes <= 256 ? 2 : 1) * kCUs);
+    // (as many turns of rows for each, and no more parts than that takes)
+    const int64_t turns = ceil_div(a->rows, rows_at_once(p.shape));
+    p.parts = ceil_div(turns, ceil_div(turns, (p.shape.lanes <= 256 ? 2 : 1) * kCUs));
   }
   if ((a->dw || a->db) && (p.parts > 1 || p.shape.pieces == 0)) p.bytes = ops_align((size_t)2 * p.parts * a->width * 4);
   return p;
