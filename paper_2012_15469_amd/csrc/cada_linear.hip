@@ -109,13 +109,13 @@ __device__ __forceinline__ Turn backward_tile(const Product &dx, const Product &
   const bool in_first = (blockIdx.x >> 3) < first;
   return Turn{in_first ? tile_of_block(n_first) : tile_of_block(n_second, first), in_first == dw_first};
 }
-template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW, bool PIECES>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_backward(const Product dx, const Product dw) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BN, STAGES, KW)];
   const Turn turn = backward_tile(dx, dw);
   if (turn.tile == ~0u) return;
-  if (turn.dw) tile_product<T, BM, BN, WY, WX, false, false, DIRECT, STAGES, KW>(dw, turn.tile, lds);
-  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT, STAGES, KW>(dx, turn.tile, lds);
+  if (turn.dw) tile_product<T, BM, BN, WY, WX, false, false, DIRECT, STAGES, KW, NO_SIGNAL>(dw, turn.tile, lds, ToTable<PIECES>());
+  else tile_product<T, BM, BN, WY, WX, true, true, DIRECT, STAGES, KW, NO_SIGNAL>(dx, turn.tile, lds, ToTable<PIECES>());
 }
 
 // The same for small gradients: any alignment, and dz formed on the way (dy's and pre's rows in the place of dz's).
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void k_by_element(const Product p) {
   }
 }
 
-template <typename T>
+template <typename T, bool PIECES>
 __global__ __launch_bounds__(256) void k_join(const Join j) {
   int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;
 #pragma unroll
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
         }
       }
       float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      finish8<T>(p.epi, m, n, left, f);
+      finish8<T, PIECES>(p.epi, m, n, left, f);
       return;
     }
     g -= j.groups[i];
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
   if (lane == 0 && c < j.db_n) {
 #pragma unroll
     for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x];
-    static_cast<T *>(j.db)[c] = from_f32<T>(j.db_factor ? s * *j.db_factor : s);
+    static_cast<T *>(j.db)[c] = from_f32<T>(PIECES ? s * *j.db_factor : s);
   }
 }
 
@@ -313,7 +313,7 @@ void forward_tiles_of(int tile, bool direct, const Product &p, hipStream_t st) {
   }
 }
 
-template <typename T>
+template <typename T, bool PIECES>
 int launch_join(Join &j, hipStream_t st) {
   int64_t total = 0;
   for (int i = 0; i < 2; ++i) {
@@ -323,7 +323,7 @@ int launch_join(Join &j, hipStream_t st) {
   j.db_block = (unsigned)ceil_div(total, 256);
   const unsigned grid = j.db_block + (j.db_part ? (unsigned)ceil_div(j.db_n, 32) : 0);
   if (grid == 0) return CADA_OK;
-  k_join<T><<<grid, 256, 0, st>>>(j);
+  k_join<T, PIECES><<<grid, 256, 0, st>>>(j);
   return ops_launched("linear join");
 }
 
@@ -360,7 +360,7 @@ int forward(const cada_linear *a, const ForwardPlan &f) {
   if (p.splits == 1) return CADA_OK;
   Join j{};
   j.p[0] = p;
-  return launch_join<T>(j, st);
+  return launch_join<T, false>(j, st);
 }
 
 // ---- backward ----
@@ -371,25 +371,25 @@ int zero_table(void *p, int64_t ld, int64_t rows, int64_t n, hipStream_t st) {
   return ops_launched("linear clear");
 }
 
-template <typename T, int E, int WY, int WX, int KW>
+template <typename T, int E, int WY, int WX, int KW, bool PIECES>
 void backward_tiles(const Product &dx, const Product &dw, bool dir, hipStream_t st) {
   const unsigned grid = (unsigned)((ceil_div(tiles_of(dx), 8) + ceil_div(tiles_of(dw), 8)) * 8);
   if constexpr (E <= 64) {
-    if (!dir) { k_backward<T, E, E, WY, WX, false, 2, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw); return; }
+    if (!dir) { k_backward<T, E, E, WY, WX, false, 2, KW, PIECES><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw); return; }
   }
   if constexpr (E < 256) {
-    if (deep(E, tiles_of(dx) + tiles_of(dw))) { k_backward<T, E, E, WY, WX, true, 4, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw); return; }
+    if (deep(E, tiles_of(dx) + tiles_of(dw))) { k_backward<T, E, E, WY, WX, true, 4, KW, PIECES><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw); return; }
   }
-  k_backward<T, E, E, WY, WX, true, 2, KW><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw);
+  k_backward<T, E, E, WY, WX, true, 2, KW, PIECES><<<grid, 64 * WY * WX * KW, 0, st>>>(dx, dw);
 }
 
-template <typename T>
+template <typename T, bool PIECES>
 int products(int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st) {
-  if (tile == 32) backward_tiles<T, 32, 1, 1, 4>(dx, dw, direct, st);
-  if (tile == 64) backward_tiles<T, 64, 2, 2, 1>(dx, dw, direct, st);
+  if (tile == 32) backward_tiles<T, 32, 1, 1, 4, PIECES>(dx, dw, direct, st);
+  if (tile == 64) backward_tiles<T, 64, 2, 2, 1, PIECES>(dx, dw, direct, st);
   if constexpr (sizeof(T) == 2) {
-    if (tile == 128) backward_tiles<T, 128, 2, 4, 1>(dx, dw, direct, st);
-    if (tile == 256) backward_tiles<T, 256, 2, 4, 1>(dx, dw, direct, st);
+    if (tile == 128) backward_tiles<T, 128, 2, 4, 1, PIECES>(dx, dw, direct, st);
+    if (tile == 256) backward_tiles<T, 256, 2, 4, 1, PIECES>(dx, dw, direct, st);
   }
   return ops_launched("linear gradients");
 }
@@ -450,7 +450,7 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
       k_backward_small<T, 32, 1, 4><<<grid, 256, 0, st>>>(dx, dw);
     } else if (b.small) {
       k_backward_small<T, 64, 2, 1><<<grid, 256, 0, st>>>(dx, dw);
-    } else if (int rc = linear_products(a->type, tile, b.direct, dx, dw, st)) {
+    } else if (int rc = products<T, false>(tile, b.direct, dx, dw, st)) {
       return rc;
     }
     if (int rc = ops_launched("linear gradients")) return rc;
@@ -458,7 +458,7 @@ int backward(const cada_linear_grad *a, const BackwardPlan &b) {
   Join j{};
   j.p[0] = dx; j.p[1] = dw;
   if (a->db && (!db_by_products || b.dw.splits > 1)) { j.db_part = db_part; j.db = a->db; j.db_parts = (int)b.row_blocks; j.db_n = (int)a->out; }
-  return launch_join<T>(j, st);
+  return launch_join<T, false>(j, st);
 }
 
 }  // namespace
@@ -468,8 +468,8 @@ int linear_sums(int type, int tile, bool direct, const Product &p, hipStream_t s
   else forward_tiles_of<float>(tile, direct, p, st);
   return ops_launched("linear");
 }
-int linear_products(int type, int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st) { return type == CADA_BF16 ? products<bf16>(tile, direct, dx, dw, st) : products<float>(tile, direct, dx, dw, st); }
-int linear_join(int type, Join &j, hipStream_t st) { return type == CADA_BF16 ? launch_join<bf16>(j, st) : launch_join<float>(j, st); }
+int linear_products(int type, int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st) { return type == CADA_BF16 ? products<bf16, true>(tile, direct, dx, dw, st) : products<float, true>(tile, direct, dx, dw, st); }
+int linear_join(int type, Join &j, hipStream_t st) { return type == CADA_BF16 ? launch_join<bf16, true>(j, st) : launch_join<float, true>(j, st); }
 int linear_pack(int type, Packs &a, hipStream_t st) { return type == CADA_BF16 ? launch_pack<bf16>(a, st) : launch_pack<float>(a, st); }
 
 bool ops_check_table(const char *name, const void *p, int64_t ld, int64_t cols, int type) {

@@ -12,7 +12,7 @@ struct Epilogue {
   void *pre, *out;
   int64_t ldr, ldpre, ldo;
   int act;
-  const float *factor;       // of the sum, in device memory, or null (1)
+  const float *factor;       // PIECES: of the sum, in device memory
 };
 
 // One product C[M, N] = sum_k A(m, k) B(k, n).
@@ -23,7 +23,7 @@ struct Product {
   int64_t k_per_split;       // a multiple of the step
   int32_t N, tiles_m, tiles_n, splits;
   float *partial;            // [splits][M][N up to whole groups of eight], or null: sums that k_join joins and finishes (splits > 1, or a contraction that goes on in another launch)
-  int32_t add;               // to what is in `partial` already
+  int32_t add;               // PIECES: to what is in `partial` already
   Epilogue epi;
   // small gradients: the operand that is the signal is read as dy, and dz = dy * act'(pre) is formed on its way into LDS
   const void *pre;
@@ -39,7 +39,7 @@ struct Join {
   int64_t groups[2];         // M * ceil(N / 8), 0 where there is nothing to join
   const float *db_part;      // [db_parts][N of the second product] or null
   void *db;
-  const float *db_factor;    // of the column sums, in device memory, or null (1)
+  const float *db_factor;    // PIECES: of the column sums, in device memory
   int db_parts, db_n;
   unsigned db_block;         // the first workgroup of the column sums
 };
@@ -47,7 +47,7 @@ struct Join {
 struct Pack { const void *src; void *dst; int64_t ld, rows, cols, ldd; };
 struct Packs { Pack p[2]; int64_t pieces[2]; };
 
-// Products, joins and copies of a type (CADA_F32 or CADA_BF16), for other files than cada_linear.hip.
+// Products, joins and copies of a type (CADA_F32 or CADA_BF16), for other files than cada_linear.hip; products and joins with PIECES.
 int linear_sums(int type, int tile, bool direct, const Product &p, hipStream_t st);        // a forward product whose sums go to p.partial
 int linear_products(int type, int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st);
 int linear_join(int type, Join &j, hipStream_t st);
@@ -263,11 +263,11 @@ __device__ __forceinline__ f32x16 multiply(v4s a, v4s b, f32x16 c) {
 }
 
 // Eight consecutive columns n .. of row m of a finished sum; `left` of them exist.
-template <typename T>
+template <typename T, bool PIECES = false>
 __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int64_t left, float (&f)[8]) {
   if (left <= 0) return;
   float o[8];
-  if (e.factor) {
+  if constexpr (PIECES) {
     const float factor = *e.factor;
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= factor;
@@ -291,10 +291,10 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int
 }
 
 // Eight columns of an unfinished sum.
-__device__ __forceinline__ void put_part(const Product &p, uint32_t split, int64_t m, int n, int64_t left, float (&f)[8]) {
+template <bool PIECES> __device__ __forceinline__ void put_part(const Product &p, uint32_t split, int64_t m, int n, int64_t left, float (&f)[8]) {
   if (left <= 0) return;
   float *to = p.partial + ((int64_t)split * p.M + m) * eights(p.N) + n;
-  if (p.add) {
+  if (PIECES && p.add) {
     float o[8];
     load8_n(to, 8, o);
 #pragma unroll
@@ -303,21 +303,21 @@ __device__ __forceinline__ void put_part(const Product &p, uint32_t split, int64
   store8_n(to, 8, f);
 }
 
-// What becomes of a tile's sums: a layer's output, here; a last layer's loss has its own (cada_linear_xent.hip), which take the sums where the matrix instructions leave them, sums(), and where
+// What becomes of a tile's sums: a layer's output, here (PIECES: of a contraction that comes in several launches, with a factor that is in device memory); a last layer's loss has its own (cada_linear_xent.hip), which take the sums where the matrix instructions leave them, sums(), and where
 // wavefronts share a tile's contraction and join their sums in LDS, eight columns of a row per lane, row().
-struct ToTable {
+template <bool PIECES = false> struct ToTable {
   static constexpr bool kOwn = false;
   __device__ __forceinline__ void begin(const Product &, int64_t, int, int) const {}
   template <typename T> __device__ __forceinline__ void row(const Product &p, uint32_t split, int64_t m, int n, int64_t left, float (&f)[8]) const {
-    if (p.partial) put_part(p, split, m, n, left, f);
-    else finish8<T>(p.epi, m, n, left, f);
+    if (p.partial) put_part<PIECES>(p, split, m, n, left, f);
+    else finish8<T, PIECES>(p.epi, m, n, left, f);
   }
 };
 
 // WY x WX wavefronts share the tile; with KW = 4 four wavefronts each take the whole (32 x 32) tile and one of the four sub-steps of every step, and their sums are joined
 // on the way out: short steps for few outputs.
 enum { NO_SIGNAL = 0, A_SIGNAL = 1, B_SIGNAL = 2 };
-template <typename T, int BM, int BN, int WY, int WX, bool AKC, bool BKC, bool DIRECT, int STAGES, int KW = 1, int SIGNAL = NO_SIGNAL, typename OUT = ToTable>
+template <typename T, int BM, int BN, int WY, int WX, bool AKC, bool BKC, bool DIRECT, int STAGES, int KW = 1, int SIGNAL = NO_SIGNAL, typename OUT = ToTable<>>
 __device__ __forceinline__ void tile_product(const Product &p, uint32_t tile, unsigned char *lds, OUT out = OUT()) {
   constexpr int TH = 64 * WY * WX * KW, NK = 4 / KW;
   typedef Side<T, AKC, BM, TH> SA;
