@@ -209,7 +209,8 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
 constexpr int64_t kSignalBytes = (int64_t)192 << 20, kPieceStep = 256, kLeastPiece = 1024;
 // Where all classes are one piece anyway and a float32 copy of the logits is no larger than a piece may be, the logits are kept between the two, which saves the second product: they go to a pass over the rows
 // as the product's float32 sums (in parts, where its contraction is split).
-constexpr int64_t kKeptClasses = 16384;        // a workgroup's registers hold a row
+constexpr int64_t kKeptClasses = 16384;        // a workgroup's registers hold a row; the logits of longer ones are left behind by the statistics' tiles, and a pass over them makes the signal
+constexpr int64_t kLeftColumns = 2048;         // of a workgroup of that pass
 // (bf16 8192 x 4096 x 4000 975 -> 820 us, 1000 x 4096 x 16000 570 -> 490, 8192 x 512 x 1000 88 -> 84; float32 4096 x 256 x 4000 336 -> 272, 120 x 500 x 1001 41 -> 32.5; bf16 2048 x 128 x 10000 110 -> 113)
 constexpr double kKeptBytesPerUs = 3.2e6, kKeptLaunch = 3.0;
 struct KeptShape { int lanes, pieces; int64_t groups; };        // of a row, pieces of four classes per lane, and workgroups at most
@@ -229,16 +230,19 @@ struct LossHead {
   double loss[kMostGroups];
   int64_t used[kMostGroups];
 };
+// Up to so many rows, dw is an outer product each lane forms of its columns, and not tiles whose way in and out is all that they are (6 x 3104 x 35488 float32: both gradients by tiles 306 us, where
+// reading and writing the two tables takes 184).
+constexpr int64_t kOuterRows = 16;
 // What a tile's exponentials cost on its way out, in the microseconds of the table above: 4096 x 1024 x 50001 bf16, all four products, with logits in tiles of 64 2616 us, of 128 2086, of 256 1905; 8192 x 512 x 32000 1923,
 // 1560 and 1372; 1000 x 768 x 30000 344, 288 and 270.
 constexpr double kLossEnds[] = {0.2, 0.7, 3.5, 3.0};
 constexpr int strip_columns(int tile) { return tile == 256 ? 64 : 32; }        // of a wavefront's strip of a tile, which has one entry in a row's statistics
 struct LossPlan {
-  bool grads, signal, kept, direct, copy_x, copy_w;
+  bool grads, signal, kept, left, outer, direct, copy_x, copy_w;
   Cut logits, piece_logits, dx, dw;
-  int64_t piece, pieces, chunks, ldz, strips;      // strips: of the signal's rows, each with a part of db
+  int64_t piece, pieces, chunks, ldz, strips, left_rows;      // strips: of the signal's rows, each with a part of db; left_rows: of a workgroup of the pass over logits that were left behind
   int stat_floats;
-  size_t off_bias, off_stats, off_info, off_label, off_loss, off_signal, off_dx, off_dw, off_db, off_x, off_w, bytes;
+  size_t off_bias, off_stats, off_left, off_info, off_label, off_loss, off_signal, off_dx, off_dw, off_db, off_x, off_w, bytes;
 };
 inline LossPlan plan_loss(const cada_linear_xent *a) {
   LossPlan f{};
@@ -251,12 +255,13 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
   const bool x_direct = f.signal || direct_kc(a->x, a->ldx, elem), w_direct = direct_oc(a->w, a->ldw, classes, elem);
   const bool tiny = no_tiles(rows, a->ldx, in, elem) || no_tiles(in, a->ldw, classes, elem);
   const Shape whole = {rows, classes, in};
-  const int n = (a->dx ? 1 : 0) + (a->dw ? 1 : 0);
+  f.outer = a->dw && rows <= kOuterRows;
+  const int n = (a->dx ? 1 : 0) + (a->dw && !f.outer ? 1 : 0);
   // As few pieces as kSignalBytes allow, or up to three more where their tiles come out more evenly (8192 x 4096 x 65536 bf16 in 6 pieces 15.7 ms, in 8 14.3).
   const int64_t logits_bytes = rows * eights(classes) * 4;
-  const bool may_keep = f.signal && classes <= kKeptClasses && logits_bytes <= kSignalBytes;
+  const bool may_keep = f.signal && logits_bytes <= kSignalBytes;
   Cut c[2][4] = {};
-  bool kept[2] = {};
+  bool kept[2] = {}, left[2] = {};
   double time[2], best[2] = {1e300, 1e300};
   int64_t piece[2] = {classes, classes};
   for (int direct = 0; direct < 2; ++direct) {
@@ -273,12 +278,18 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
       if (pieces == 1 && may_keep) {
         // (the part of the estimate that is the gradients' products is the same)
         Cut k;
-        const double again = cut(&part, 1, a->type, direct, widest_tile(in, elem), &mine[0], 1, kLossEnds), formed_twice = time[direct] + again;
-        const double once = cut(&whole, 1, a->type, direct, widest_tile(in, elem), &k, (int)std::min<int64_t>(32, kSignalBytes / logits_bytes)) + kKeptLaunch + (double)logits_bytes * (1.5 + 0.25 * elem / 2) / kKeptBytesPerUs;
-        if (once < formed_twice) {
-          kept[direct] = true;
-          c[direct][0] = k;
-          t += once - formed_twice;
+        const double again = cut(&part, 1, a->type, direct, widest_tile(in, elem), &mine[0], 1, kLossEnds), pass = kKeptLaunch + (double)logits_bytes * (1.5 + 0.25 * elem / 2) / kKeptBytesPerUs;
+        if (classes > kKeptClasses) {
+          left[direct] = pass < again;
+          if (left[direct]) t += pass - again;
+        } else {
+          const double formed_twice = time[direct] + again;
+          const double once = cut(&whole, 1, a->type, direct, widest_tile(in, elem), &k, (int)std::min<int64_t>(32, kSignalBytes / logits_bytes)) + pass;
+          kept[direct] = once < formed_twice;
+          if (kept[direct]) {
+            c[direct][0] = k;
+            t += once - formed_twice;
+          }
         }
       }
       if (t >= best[direct]) continue;
@@ -296,18 +307,22 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
   f.piece = piece[f.direct];
   f.pieces = ceil_div(classes, f.piece);
   f.kept = kept[f.direct];
+  f.left = left[f.direct];
   f.logits = mine[0];
   f.piece_logits = mine[1];
   if (a->dx) f.dx = mine[2];
-  if (a->dw) f.dw = mine[2 + n - 1];
+  if (a->dw && !f.outer) f.dw = mine[2 + n - 1];
   f.chunks = ceil_div(classes, f.logits.tile) * (f.logits.tile / strip_columns(f.logits.tile));
   f.stat_floats = a->smoothing != 0.0 ? 4 : 2;
   f.ldz = eights(f.piece);
   const KeptShape shape = kept_shape(rows, classes);
-  if (f.signal) f.strips = f.kept ? std::min(ceil_div(rows, std::max(1, 256 / shape.lanes)), shape.groups) : 2 * ceil_div(rows, f.piece_logits.tile);
+  // (workgroups of the pass for every CU several times over, and no more parts of db than that takes)
+  f.left_rows = std::max<int64_t>(1, ceil_div(rows * ceil_div(classes, kLeftColumns), 8 * kCUs));
+  if (f.signal) f.strips = f.kept ? std::min(ceil_div(rows, std::max(1, 256 / shape.lanes)), shape.groups) : f.left ? ceil_div(rows, f.left_rows) : 2 * ceil_div(rows, f.piece_logits.tile);
   size_t off = ops_align(sizeof(LossHead));
   f.off_bias = off; off += f.kept ? ops_align((size_t)eights(classes) * 4) : 0;
   f.off_stats = off; off += f.kept ? ops_align((size_t)f.logits.splits * logits_bytes) : ops_align((size_t)f.chunks * rows * f.stat_floats * 4);
+  f.off_left = off; off += f.left ? ops_align((size_t)logits_bytes) : 0;
   f.off_info = off; off += ops_align((size_t)rows * 16);
   f.off_label = off; off += ops_align((size_t)rows * 4);
   f.off_loss = off; off += a->loss ? 0 : ops_align((size_t)rows * 4);

@@ -4,7 +4,7 @@
 // distances to it.  A row's strips are then joined, as one goes along, to the row's largest and its sum, which is its loss.  For the gradients the logits are formed again in
 // pieces of the classes; their tiles end in softmax - target (but for a factor) in the operands' type, from which the products of a layer's gradients are taken while it is in the caches: dw is finished piece by
 // piece, dx is added up in float32.  That is four products where keeping the logits would take three, and memory for one piece instead of all.  Logits that are not
-// more than a piece are kept in float32 (k_kept_rows).
+// more than a piece are kept in float32: for a pass over whole rows (k_kept_rows), or, of long rows, left behind by the statistics (k_left_signal).
 #include <algorithm>
 
 #include "cada_linear_tiles.h"
@@ -26,6 +26,8 @@ struct Loss {
   int32_t classes, label_bytes, first;      // first: the piece's first class
   const float *kept, *kept_bias;            // kept logits without their bias, in `splits` parts; the biases in float32, -inf behind the last class
   int32_t splits;
+  float *left;               // [rows][classes up to whole groups of eight]: where statistics leave the logits, with their bias, or null
+  int64_t left_rows;
   int32_t lanes;             // rows of a workgroup of k_rows, as a power of two
   float smoothing, keep, scale;      // keep = 1 - smoothing, rounded once
 };
@@ -51,7 +53,7 @@ template <typename T> __device__ __forceinline__ void put_bias(const Loss &q, co
 
 // A tile's logits into statistics.  A lane has FN x 16 logits of a row, and the lane 32 further the row's others.
 // Bound by the vector unit: an addition, a comparison, two operations and an exponential (four times an operation's time) per logit.
-template <typename T, int BM> struct ToStatistics {
+template <typename T, int BM, bool LEFT> struct ToStatistics {
   static constexpr bool kOwn = true;
   const Loss &q;
   int32_t *label;            // [BM], in LDS
@@ -85,6 +87,15 @@ template <typename T, int BM> struct ToStatistics {
             z[i][j][4 * r + e] += b[e];
             s[i].top = fmaxf(s[i].top, z[i][j][4 * r + e]);
           }
+        if (FM >= 4) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (LEFT) {
+          const int n = n0 + wn + 32 * j + 8 * r + 4 * half, columns = (q.classes + 7) / 8 * 8;
+#pragma unroll
+          for (int i = 0; i < FM; ++i) {
+            const int64_t m = m0 + wm + 32 * i + (lane & 31);
+            if (m < p.M && n < columns) *reinterpret_cast<v4s *>(q.left + m * columns + n) = v4s{z[i][j][4 * r], z[i][j][4 * r + 1], z[i][j][4 * r + 2], z[i][j][4 * r + 3]};
+          }
+        }
       }
     float base[FM];
 #pragma unroll
@@ -98,7 +109,10 @@ template <typename T, int BM> struct ToStatistics {
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[i].sum += power(z[i][j][r], base[i]);
+        for (int r = 0; r < 16; ++r) {
+          s[i].sum += power(z[i][j][r], base[i]);
+          if (FM >= 4 && r % 8 == 7) __builtin_amdgcn_sched_barrier(0);        // (few at a time: interleaved, they spill)
+        }
     if (q.smoothing != 0.f) {
       float left = 0.f;
 #pragma unroll
@@ -113,6 +127,7 @@ template <typename T, int BM> struct ToStatistics {
 #pragma unroll
             for (int i = 0; i < FM; ++i) s[i].distance += in ? z[i][j][4 * r + e] - base[i] : 0.f;
           }
+          if (FM >= 4) __builtin_amdgcn_sched_barrier(0);
         }
       left += __shfl_xor(left, 32, 64);
 #pragma unroll
@@ -166,6 +181,13 @@ template <typename T, int BM> struct ToStatistics {
       *parts[i] += __shfl_xor(*parts[i], 2, 64);
     }
     if (m >= p.M) return;
+    if constexpr (LEFT) {
+      if (n0 + c < p.N) {
+        v4s *to = reinterpret_cast<v4s *>(q.left + m * ((q.classes + 7) / 8 * 8) + n0 + c);
+        to[0] = v4s{z[0], z[1], z[2], z[3]};
+        to[1] = v4s{z[4], z[5], z[6], z[7]};
+      }
+    }
     const int at = label[t / 4] - (n0 + c);
     if (at >= 0 && at < 8) {
       float zl = z[0];
@@ -359,14 +381,14 @@ __device__ __forceinline__ float loss_of(const Loss &q, const Stat &s, float bas
   return used ? l : 0.f;
 }
 
-template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
+template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW, bool LEFT>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product p, const Loss q) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
   __shared__ int32_t label[BM];
   __shared__ __align__(16) float bias[BM];
   if (blockIdx.x == 0) clear_counters(q.head);
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
-  if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<T, BM>(q, label, bias));
+  if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<T, BM, LEFT>(q, label, bias));
 }
 template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_signal(const Product p, const Loss q) {
@@ -614,6 +636,87 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const L
   add_up(q, losses, used_rows);
 }
 
+// Logits that the statistics left behind into the signal, eight classes of a row per lane, and its column sums over a workgroup's rows.
+template <typename T>
+__global__ __launch_bounds__(256) void k_left_signal(const Loss q) {
+  const int c = ((int)blockIdx.x * 256 + threadIdx.x) * 8, columns = (q.classes + 7) / 8 * 8;
+  static_assert(kLeftColumns == 256 * 8, "");
+  if (c >= columns) return;
+  const int64_t r0 = (int64_t)blockIdx.y * q.left_rows, r1 = min(q.rows, r0 + q.left_rows);
+  float bias[8], column[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = column[e] = 0.f;
+  if (q.bias) load8_n(static_cast<const T *>(q.bias) + c, q.classes - c, bias);
+#pragma unroll 4
+  for (int64_t r = r0; r < r1; ++r) {
+    const RowInfo &row = q.info[r];
+    const float base = row.base, f_total = row.f_total, f_each = row.f_each;
+    const int at = row.label < 0 ? -1 : row.label - c;
+    float z[8];
+    load8_n(q.left + r * columns + c, 8, z);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float g = power(z[e], base) * f_total;
+      if (q.smoothing != 0.f) g -= bias[e] != -kInf ? f_each : 0.f;
+      g -= at == e ? 1.f : 0.f;
+      z[e] = row.label < 0 || c + e >= q.classes ? 0.f : g;
+      column[e] += z[e];
+    }
+    if (q.signal) store8_n(static_cast<T *>(q.signal) + r * q.ldz + c, 8, z);
+  }
+  if (q.db_part) store8_n(q.db_part + (int64_t)blockIdx.y * q.classes + c, q.classes - c, column);
+}
+
+// dw of up to R rows: a lane keeps a piece of 16 bytes of the signal's rows, times the factor, and goes down dw's rows, x's values for which wait in LDS.  Bound by the writes of dw.
+struct Outer {
+  const void *x, *signal;
+  void *dw;
+  const float *factor;
+  int64_t ldx, ldz, lddw;
+  int32_t rows, in, columns, per;      // per: rows of dw of a workgroup
+  uint32_t across;                     // workgroups along a row
+};
+constexpr int kOuterPer = 64;
+template <typename T, int R>
+__global__ __launch_bounds__(256) void k_outer(const Outer a) {
+  constexpr int E = Elem<T>::kPer16;
+  __shared__ __align__(16) float xs[kOuterPer][R];
+  const uint32_t down = blockIdx.x / a.across;
+  const int c = (int)(blockIdx.x - down * a.across) * 256 * E + threadIdx.x * E, k0 = (int)down * a.per, here = min(a.per, a.in - k0);
+  for (int i = threadIdx.x; i < here * R; i += 256) {
+    const int r = i / here, k = i - r * here;
+    xs[k][r] = r < a.rows ? to_f32(static_cast<const T *>(a.x)[r * a.ldx + k0 + k]) : 0.f;
+  }
+  const float factor = *a.factor;
+  float g[R][E];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    u32x4v raw = {0, 0, 0, 0};
+    if (r < a.rows && c < a.columns) raw = *reinterpret_cast<const u32x4v *>(static_cast<const T *>(a.signal) + r * a.ldz + c);      // (whole: the signal's rows have room for it)
+    unpack<T>(raw, g[r]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) g[r][e] *= factor;
+  }
+  __syncthreads();
+  if (c >= a.columns) return;
+  T *to = static_cast<T *>(a.dw) + (int64_t)k0 * a.lddw + c;
+  const int left = a.columns - c;
+#pragma unroll 2
+  for (int k = 0; k < here; ++k, to += a.lddw) {
+    float f[E] = {};
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[e] = fmaf(xs[k][r], g[r][e], f[e]);
+    if (left >= E) {
+      store16(to, pack<T>(f));
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) if (e < left) to[e] = from_f32<T>(f[e]);
+    }
+  }
+}
+
 // Copies in rows on 16-byte boundaries: of x, with zeros for rows that do not count, and of w, each where there is one to make; and of the biases in float32 for kept logits.
 template <typename T>
 __global__ __launch_bounds__(256) void k_copy(const Loss q, const Packs a, float *bias) {
@@ -642,7 +745,8 @@ template <typename T, int E, int WY, int WX, int KW>
 void tiles(const Product &p, const Loss &q, bool statistics, bool direct, hipStream_t st) {
   const unsigned grid = (unsigned)(ceil_div(tiles_of(p), 8) * 8), threads = 64 * WY * WX * KW;
   auto launch = [&](auto dir, auto stages) {
-    if (statistics) k_statistics<T, E, WY, WX, dir(), stages(), KW><<<grid, threads, 0, st>>>(p, q);
+    if (statistics && q.left) k_statistics<T, E, WY, WX, dir(), stages(), KW, true><<<grid, threads, 0, st>>>(p, q);
+    else if (statistics) k_statistics<T, E, WY, WX, dir(), stages(), KW, false><<<grid, threads, 0, st>>>(p, q);
     else k_signal<T, E, WY, WX, dir(), stages(), KW><<<grid, threads, 0, st>>>(p, q);
   };
   if constexpr (E <= 64) {
@@ -714,6 +818,8 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
     if (int rc = linear_sums(a->type, f.logits.tile, f.direct, z, st)) return rc;
     if (int rc = kept_rows<T>(q, st)) return rc;
   } else {
+    q.left = f.left ? reinterpret_cast<float *>(ws + f.off_left) : nullptr;
+    q.left_rows = f.left_rows;
     if (int rc = logits<T>(z, q, f.logits.tile, true, f.direct, st)) return rc;
     while (q.lanes < 6 && ((int64_t)kLossGroups << q.lanes) < a->rows) ++q.lanes;
     k_rows<<<(unsigned)std::min<int64_t>(ceil_div(a->rows, 1 << q.lanes), kLossGroups), 1024, 0, st>>>(q);
@@ -724,7 +830,10 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
   for (int64_t i = 0; i < f.pieces; ++i) {
     const int64_t first = i * f.piece, here = std::min(f.piece, a->classes - first);
     q.first = (int32_t)first; q.signal = signal; q.ldz = f.ldz; q.db_part = a->db ? reinterpret_cast<float *>(ws + f.off_db) : nullptr;
-    if (!f.kept) {
+    if (f.left) {
+      k_left_signal<T><<<dim3((unsigned)ceil_div(a->classes, kLeftColumns), (unsigned)f.strips), 256, 0, st>>>(q);
+      if (int rc = ops_launched("linear cross-entropy signal")) return rc;
+    } else if (!f.kept) {
       lay(&z, f.piece_logits, x, ldx, w + first, ldw, a->rows, here, a->in, nullptr);
       z.b_cols = w_cols - first;
       if (int rc = logits<T>(z, q, f.piece_logits.tile, false, f.direct, st)) return rc;
@@ -739,12 +848,23 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
       dx.add = i > 0;
       dx.epi.out = a->dx; dx.epi.ldo = a->lddx; dx.epi.factor = &q.head->factor;
     }
-    if (a->dw) {
+    if (f.outer) {
+      Outer o{};
+      o.x = x; o.signal = signal; o.dw = static_cast<T *>(a->dw) + first; o.factor = &q.head->factor; o.ldx = ldx; o.ldz = f.ldz; o.lddw = a->lddw;
+      o.rows = (int32_t)a->rows; o.in = (int32_t)a->in; o.columns = (int32_t)here;
+      o.across = (uint32_t)ceil_div(here, 256 * Elem<T>::kPer16);
+      o.per = (int32_t)std::clamp<int64_t>(ceil_div(a->in * o.across, 16 * kCUs), 4, kOuterPer);
+      const unsigned grid = o.across * (unsigned)ceil_div(a->in, o.per);
+      if (a->rows <= 4) k_outer<T, 4><<<grid, 256, 0, st>>>(o);
+      else if (a->rows <= 8) k_outer<T, 8><<<grid, 256, 0, st>>>(o);
+      else k_outer<T, 16><<<grid, 256, 0, st>>>(o);
+      if (int rc = ops_launched("linear cross-entropy outer product")) return rc;
+    } else if (a->dw) {
       lay(&dw, f.dw, x, ldx, signal, f.ldz, a->in, here, a->rows, reinterpret_cast<float *>(ws + f.off_dw));
       dw.a_cols = x_cols; dw.b_cols = eights(here);
       dw.epi.out = static_cast<T *>(a->dw) + first; dw.epi.ldo = a->lddw; dw.epi.factor = &q.head->factor;
     }
-    if (f.grads) {
+    if (a->dx || (a->dw && !f.outer)) {
       if (int rc = linear_products(a->type, a->dx ? f.dx.tile : f.dw.tile, f.direct, dx, dw, st)) return rc;
     }
     if (i == f.pieces - 1) {

@@ -108,6 +108,21 @@ def test_large(dtype, rows, k, classes, pad):
     assert all(torch.equal(a, c) for a, c in zip(first, again))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k,classes,pad", [(1, 300, 20011, 0), (4, 17, 40000, 3), (5, 700, 17000, 8), (8, 129, 33333, 1), (9, 64, 16392, 0), (16, 1000, 20480, 0), (16, 333, 50001, 0), (17, 100, 30000, 0), (255, 70, 18000, 5),
+                                                (256, 64, 16385, 0), (257, 64, 16385, 0), (3, 5000, 16, 0), (2, 40000, 9, 0)])
+def test_few_rows_and_many_classes(rows, k, classes, pad, dtype):
+    """Logits that are kept and read again, and dw as an outer product, around the borders of both."""
+    check(*problem(rows, k, classes, dtype, 11, pad, ignored=0.2 if rows > 1 else 0.0, masked=0.1), smoothing=0.1)
+    x, w, labels, b = problem(rows, k, classes, dtype, 12, pad, bias=False)
+    first = check(x, w, labels, b, scale=64.0)
+    for i, names in enumerate(("dx", "dw")):
+        only = ops.linear_cross_entropy(x, w, labels, b, scale=64.0, need_dx=i == 0, need_dw=i == 1)
+        assert torch.equal(only[1], first[1]) or float((only[1] - first[1]).abs().max()) < 1e-4
+        want = first[2 + i].double()
+        assert float((only[2 + i].double() - want).norm()) <= (2.0 ** -7 if dtype == "bf16" else 1e-5) * float(want.norm())
+
+
 @pytest.mark.parametrize("dtype,rows,k,classes", [("f32", 100, 50, 333), ("bf16", 4096, 128, 17000), ("bf16", 100, 52, 333), ("bf16", 3000, 257, 1001)])
 def test_outputs_one_by_one(dtype, rows, k, classes):
     x, w, labels, b = problem(rows, k, classes, dtype, 4, ignored=0.2)

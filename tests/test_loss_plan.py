@@ -11,16 +11,16 @@ from common_more_ops import cada_linear_xent, filled
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 1 << 20          # an aligned address that nobody reads
 ELEM = {0: 4, 1: 2}
-NAMES = ("grads", "signal", "kept", "direct", "copy_x", "copy_w", "tile", "splits", "piece_tile", "dx_tile", "dx_splits", "dx_per", "dw_tile", "dw_splits", "dw_per", "piece", "pieces", "chunks", "ldz", "strips", "floats",
-         "bias", "stats", "info", "label", "loss", "signal_at", "dx", "dw", "db", "x", "w", "bytes")
+NAMES = ("grads", "signal", "kept", "left", "direct", "copy_x", "copy_w", "outer", "tile", "splits", "piece_tile", "dx_tile", "dx_splits", "dx_per", "dw_tile", "dw_splits", "dw_per", "piece", "pieces", "chunks", "ldz", "strips", "left_rows", "floats",
+         "bias", "stats", "left_at", "info", "label", "loss", "signal_at", "dx", "dw", "db", "x", "w", "bytes")
 _SRC = """
 #include "cada_linear_plan.h"
 using namespace cada;
 extern "C" {
 void plan(const cada_linear_xent *a, long *out) {
   const LossPlan f = plan_loss(a);
-  const long v[] = {f.grads, f.signal, f.kept, f.direct, f.copy_x, f.copy_w, f.logits.tile, f.logits.splits, f.piece_logits.tile, f.dx.tile, f.dx.splits, (long)f.dx.k_per_split, f.dw.tile, f.dw.splits, (long)f.dw.k_per_split,
-                    (long)f.piece, (long)f.pieces, (long)f.chunks, (long)f.ldz, (long)f.strips, f.stat_floats, (long)f.off_bias, (long)f.off_stats, (long)f.off_info, (long)f.off_label, (long)f.off_loss, (long)f.off_signal,
+  const long v[] = {f.grads, f.signal, f.kept, f.left, f.direct, f.copy_x, f.copy_w, f.outer, f.logits.tile, f.logits.splits, f.piece_logits.tile, f.dx.tile, f.dx.splits, (long)f.dx.k_per_split, f.dw.tile, f.dw.splits, (long)f.dw.k_per_split,
+                    (long)f.piece, (long)f.pieces, (long)f.chunks, (long)f.ldz, (long)f.strips, (long)f.left_rows, f.stat_floats, (long)f.off_bias, (long)f.off_stats, (long)f.off_left, (long)f.off_info, (long)f.off_label, (long)f.off_loss, (long)f.off_signal,
                     (long)f.off_dx, (long)f.off_dw, (long)f.off_db, (long)f.off_x, (long)f.off_w, (long)f.bytes};
   std::copy(v, v + sizeof(v) / sizeof(v[0]), out);
 }
@@ -56,15 +56,17 @@ def check(f, a, dll):
     assert f["pieces"] >= 1 and (f["pieces"] - 1) * f["piece"] < classes <= f["pieces"] * f["piece"] and (f["pieces"] == 1 or f["piece"] % 256 == 0) and f["ldz"] >= f["piece"]
     assert f["tile"] in (32, 64, 128, 256) and (f["direct"] or f["tile"] <= 64) and (a.type == 1 or f["tile"] <= 64)
     if f["kept"]:
-        assert f["signal"] and f["pieces"] == 1 and classes <= 16384 and f["splits"] * rows * e8(classes) * 4 <= 192 << 20 and f["strips"] <= dll.most_groups()
+        assert f["signal"] and f["pieces"] == 1 and classes <= 16384 and not f["left"] and f["splits"] * rows * e8(classes) * 4 <= 192 << 20 and f["strips"] <= dll.most_groups()
     else:
         assert f["splits"] == 1 and f["chunks"] * {256: 64}.get(f["tile"], 32) >= classes
-        if f["signal"]:
+        if f["left"]:
+            assert f["signal"] and f["pieces"] == 1 and classes > 16384 and rows * e8(classes) * 4 <= 192 << 20 and f["strips"] * f["left_rows"] >= rows and f["strips"] < 65536
+        elif f["signal"]:
             assert f["strips"] * f["piece_tile"] // 2 >= rows
     # the workspace
-    sizes = [("bias", e8(classes) * 4 if f["kept"] else 0), ("stats", f["splits"] * rows * e8(classes) * 4 if f["kept"] else f["chunks"] * rows * f["floats"] * 4), ("info", rows * 16), ("label", rows * 4), ("loss", 0 if a.loss else rows * 4),
+    sizes = [("bias", e8(classes) * 4 if f["kept"] else 0), ("stats", f["splits"] * rows * e8(classes) * 4 if f["kept"] else f["chunks"] * rows * f["floats"] * 4), ("left_at", rows * e8(classes) * 4 if f["left"] else 0), ("info", rows * 16), ("label", rows * 4), ("loss", 0 if a.loss else rows * 4),
              ("signal_at", rows * f["ldz"] * elem if f["grads"] else 0), ("dx", f["dx_splits"] * rows * e8(k) * 4 if a.dx and (f["pieces"] > 1 or f["dx_splits"] > 1) else 0),
-             ("dw", f["dw_splits"] * k * e8(f["piece"]) * 4 if a.dw and f["dw_splits"] > 1 else 0), ("db", f["strips"] * f["piece"] * 4 if a.db else 0), ("x", rows * dll.packed(k) * elem if f["copy_x"] else 0),
+             ("dw", f["dw_splits"] * k * e8(f["piece"]) * 4 if a.dw and not f["outer"] and f["dw_splits"] > 1 else 0), ("db", f["strips"] * f["piece"] * 4 if a.db else 0), ("x", rows * dll.packed(k) * elem if f["copy_x"] else 0),
              ("w", k * dll.packed(classes) * elem if f["copy_w"] else 0)]
     ends = [f[name] for name, _ in sizes[1:]] + [f["bytes"]]
     assert f["bias"] >= 1024
@@ -79,10 +81,11 @@ def check(f, a, dll):
     if a.dx:
         assert f["dx_tile"] * f["ldz"] * elem <= 1 << 32 and f["dx_tile"] * ldw * elem <= 1 << 32
         assert f["dx_splits"] * f["dx_per"] >= f["piece"] > (f["dx_splits"] - 1) * f["dx_per"]
-    if a.dw:
+    assert f["outer"] == (bool(a.dw) and rows <= 16)
+    if a.dw and not f["outer"]:
         assert step * ldx * elem <= 1 << 32 and step * f["ldz"] * elem <= 1 << 32
         assert f["dw_splits"] * f["dw_per"] >= rows > (f["dw_splits"] - 1) * f["dw_per"]
-    if a.dx and a.dw:
+    if a.dx and a.dw and not f["outer"]:
         assert f["dx_tile"] == f["dw_tile"]
     # tables that are read directly: rows on 16-byte boundaries, whole pieces
     if f["direct"]:
