@@ -190,9 +190,10 @@ __global__ __launch_bounds__(1024) void k_norm_wide(const Norm a) {
 
 // dx of the rows, and the sums of dw and db over a workgroup's rows.
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kThreads<LANES>, LANES == 1024 ? 4 : 2) void k_norm_grad(const NormGrad a) {
+__global__ __launch_bounds__(kThreads<LANES>, 2) void k_norm_grad(const NormGrad a) {
   constexpr int E = Elem<T>::kPer16, kAtOnce = kRowsAtOnce<LANES>, kCols = LANES * V * E;
-  constexpr bool kAhead = LANES < 1024;        // (registers for a second row)
+  constexpr bool kAhead = V * E <= 16;        // (registers for a second row)
+  constexpr bool kHeld = V < 8;              // (and for the weights and what is added, which are read where they are used otherwise: 8000 x 16000 float32 920 us with both held, 640 without)
   __shared__ float part[2][LANES > 64 ? LANES / 64 : 1][2];
   __shared__ float sums[LANES <= 64 ? kAtOnce * kCols : 1];
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, whole = a.width / E * E;
@@ -207,12 +208,21 @@ __global__ __launch_bounds__(kThreads<LANES>, LANES == 1024 ? 4 : 2) void k_norm
     at = min(at, last);
     to.x.load(x + at * a.ldx, a.width, lane);
     to.dy.load(dy + at * a.lddy, a.width, lane);
-    if (res) to.res.load(res + at * a.ldr, a.width, lane);
+    if (kHeld && res) to.res.load(res + at * a.ldr, a.width, lane);
     to.mean = a.mean[at];
     to.rstd = a.rstd[at];
   };
   load(row, r);
-  if (a.weight) weight.load(static_cast<const T *>(a.weight), a.width, lane);
+  const T *w = static_cast<const T *>(a.weight);
+  weight.behind = 1.f;
+  if (kHeld && w) weight.load(w, a.width, lane);
+  else if (w && lane < a.width - whole) weight.behind = to_f32(w[whole + lane]);
+  // a piece of the weights
+  auto weights = [&](int v, float (&f)[E]) __attribute__((always_inline)) {
+    if constexpr (kHeld) return weight.get(v, f);
+    const int c = (v * LANES + lane) * E;
+    unpack<T>(c < whole ? load16(w + c) : u32x4v{0, 0, 0, 0}, f);
+  };
   float dw[V][E] = {}, db[V][E] = {}, dw_behind = 0.f, db_behind = 0.f;
   int turn = 0;
   for (int64_t r0 = (int64_t)blockIdx.x * kAtOnce; r0 < a.rows; r0 += stride, r += stride, turn ^= 1) {
@@ -225,7 +235,7 @@ __global__ __launch_bounds__(kThreads<LANES>, LANES == 1024 ? 4 : 2) void k_norm
     for (int v = 0; v < V; ++v) {
       row.dy.get(v, f);
       row.x.get(v, u);
-      if (a.weight) weight.get(v, g);
+      if (w) weights(v, g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         u[e] = (u[e] - mean) * rstd;
@@ -233,13 +243,13 @@ __global__ __launch_bounds__(kThreads<LANES>, LANES == 1024 ? 4 : 2) void k_norm
           dw[v][e] = fmaf(f[e], u[e], dw[v][e]);
           db[v][e] += f[e];
         }
-        if (a.weight) f[e] *= g[e];
+        if (w) f[e] *= g[e];
         s[0] += f[e];
         s[1] = fmaf(f[e], u[e], s[1]);
       }
       if constexpr (!kAhead) __builtin_amdgcn_sched_barrier(0);        // (piece by piece: interleaved, they spill)
     }
-    const float u_behind = (row.x.behind - mean) * rstd, g_behind = row.dy.behind * (a.weight ? weight.behind : 1.f);
+    const float u_behind = (row.x.behind - mean) * rstd, g_behind = row.dy.behind * (w ? weight.behind : 1.f);
     if (here) {
       dw_behind = fmaf(row.dy.behind, u_behind, dw_behind);
       db_behind += row.dy.behind;
@@ -255,22 +265,23 @@ __global__ __launch_bounds__(kThreads<LANES>, LANES == 1024 ? 4 : 2) void k_norm
           const int c = (v * LANES + lane) * E;
           row.dy.get(v, f);
           row.x.get(v, u);
-          if (a.weight) {
-            weight.get(v, g);
+          if (w) {
+            weights(v, g);
 #pragma unroll
             for (int e = 0; e < E; ++e) f[e] *= g[e];
           }
 #pragma unroll
           for (int e = 0; e < E; ++e) f[e] = rstd * (f[e] - mean_g - (u[e] - mean) * rstd * mean_gu);
           if (res) {
-            row.res.get(v, g);
+            if constexpr (kHeld) row.res.get(v, g);
+            else unpack<T>(c < whole ? load16(res + r * a.ldr + c) : u32x4v{0, 0, 0, 0}, g);
 #pragma unroll
             for (int e = 0; e < E; ++e) f[e] += g[e];
           }
           if (c < whole) store16(dx + r * a.lddx + c, pack<T>(f));
           if constexpr (!kAhead) __builtin_amdgcn_sched_barrier(0);
         }
-        if (lane < a.width - whole) dx[r * a.lddx + whole + lane] = from_f32<T>(rstd * (g_behind - mean_g - u_behind * mean_gu) + (res ? row.res.behind : 0.f));
+        if (lane < a.width - whole) dx[r * a.lddx + whole + lane] = from_f32<T>(rstd * (g_behind - mean_g - u_behind * mean_gu) + (!res ? 0.f : kHeld ? row.res.behind : to_f32(res[r * a.ldr + whole + lane])));
       }
     }
     if (more) {
@@ -391,26 +402,28 @@ __global__ __launch_bounds__(1024) void k_norm_grad_wide(const NormGrad a) {
   }
 }
 
-// The parts of the column sums, in their order: a workgroup takes 32 columns, eight lanes of each every eighth part.
-template <typename T>
-__global__ __launch_bounds__(256) void k_norm_join(const NormGrad a) {
-  __shared__ float part[8][32];
+// The parts of the column sums, in their order: a workgroup takes 32 columns, LANES lanes of each every LANES-th part (32 where there are few columns: 617 columns of 300 parts 4.9 -> 4.0 us; 16000 of 256
+// with 8 lanes 6.8 us, with 32 11).
+template <typename T, int LANES>
+__global__ __launch_bounds__(32 * LANES) void k_norm_join(const NormGrad a) {
+  __shared__ float part[LANES][33];
   T *out = static_cast<T *>(blockIdx.y == 0 ? a.dw : a.db);
   if (!out) return;
-  const int c = (int)blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
+  const int column = threadIdx.x & 31, lane = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + column;
   const float *src = a.part + (int64_t)blockIdx.y * a.parts * a.width + c;
   float s = 0.f;
   if (c < a.width) {
 #pragma unroll 8
-    for (int i = lane; i < a.parts; i += 8) s += src[(int64_t)i * a.width];
+    for (int i = lane; i < a.parts; i += LANES) s += src[(int64_t)i * a.width];
   }
-  part[lane][threadIdx.x & 31] = s;
+  part[lane][column] = s;
   __syncthreads();
-  if (lane == 0 && c < a.width) {
+  // (a column's sums to LANES neighbouring lanes)
+  const int mine = threadIdx.x / LANES;
+  s = part[threadIdx.x % LANES][mine];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x];
-    out[c] = from_f32<T>(s);
-  }
+  for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (threadIdx.x % LANES == 0 && (int)blockIdx.x * 32 + mine < a.width) out[blockIdx.x * 32 + mine] = from_f32<T>(s);
 }
 template <typename T>
 __global__ __launch_bounds__(256) void k_norm_clear(T *dw, T *db, int width) {
@@ -426,6 +439,7 @@ NormShape norm_shape(int64_t width, int per16) {
   const int64_t n = ceil_div(width, per16);
   if (n <= per16) return {per16, 1};
   if (n <= 16) return {16, 1};
+  if (n <= 32) return {32, 1};
   if (n <= 64) return {64, 1};
   if (n <= 128) return {64, 2};
   if (n <= 256) return {64, 4};
@@ -435,16 +449,18 @@ NormShape norm_shape(int64_t width, int per16) {
   if (n <= 4096) return {512, 8};
   return {1024, 0};
 }
-// The gradient's lanes hold the sums of their columns besides the rows: sixteen columns each, and rows beyond 16384 are wide.
+// The gradient's lanes hold the sums of their columns besides the rows: sixteen columns each, or 32 for rows that take a workgroup of 512; rows beyond 16384 are wide.  (Workgroups of 1024, whose lanes have
+// half the registers, spill: 8000 x 16000 bf16 514 us.)
 NormShape norm_grad_shape(int64_t width, int per16) {
   const int64_t n = ceil_div(width, per16);
   const int most = 16 / per16;
   if (n <= per16) return {per16, 1};
   if (n <= 16) return {16, 1};
-  for (int lanes = 64; lanes <= 1024; lanes *= 2)
+  if (n <= 32) return {32, 1};
+  for (int lanes = 64; lanes <= 512; lanes *= 2)
     for (int pieces = 1; pieces <= most; pieces *= 2)
       if (n <= lanes * pieces && (lanes == 64 || pieces == most)) return {lanes, pieces};
-  return {1024, 0};
+  return n <= 1024 * most ? NormShape{512, 2 * most} : NormShape{1024, 0};
 }
 int64_t rows_at_once(const NormShape &s) { return s.lanes <= 64 ? 256 / s.lanes : 1; }
 
@@ -460,7 +476,7 @@ int forward(const Norm &n, hipStream_t st) {
     k_norm_wide<T><<<(unsigned)std::min(n.rows, 2 * kCUs), 1024, 0, st>>>(n);
   } else {
     const unsigned grid = (unsigned)std::min(ceil_div(n.rows, rows_at_once(s)), (s.lanes <= 256 ? 8 : 4) * kCUs);
-    by_shape(s, [&](auto shape) { k_norm<T, shape.lanes, shape.pieces><<<grid, kThreads<shape.lanes>, 0, st>>>(n); }, ShapeOf<E, 1>(), ShapeOf<16, 1>(), ShapeOf<64, 1>(), ShapeOf<64, 2>(),
+    by_shape(s, [&](auto shape) { k_norm<T, shape.lanes, shape.pieces><<<grid, kThreads<shape.lanes>, 0, st>>>(n); }, ShapeOf<E, 1>(), ShapeOf<16, 1>(), ShapeOf<32, 1>(), ShapeOf<64, 1>(), ShapeOf<64, 2>(),
              ShapeOf<64, 4>(), ShapeOf<256, 2>(), ShapeOf<256, 4>(), ShapeOf<512, 4>(), ShapeOf<512, 8>());
   }
   return ops_launched("layer norm");
@@ -504,13 +520,14 @@ int backward(const cada_norm_grad *a, const NormGradPlan &p) {
   } else if (sums || a->dx) {
     constexpr int E = Elem<T>::kPer16, most = 16 / E;
     by_shape(p.shape, [&](auto shape) {
-      if constexpr (shape.pieces <= most) k_norm_grad<T, shape.lanes, shape.pieces><<<(unsigned)p.parts, kThreads<shape.lanes>, 0, st>>>(n);
-    }, ShapeOf<E, 1>(), ShapeOf<16, 1>(), ShapeOf<64, 1>(),
-             ShapeOf<64, 2>(), ShapeOf<64, 4>(), ShapeOf<128, most>(), ShapeOf<256, most>(), ShapeOf<512, most>(), ShapeOf<1024, most>());
+      if constexpr (shape.pieces <= most || shape.lanes == 512) k_norm_grad<T, shape.lanes, shape.pieces><<<(unsigned)p.parts, kThreads<shape.lanes>, 0, st>>>(n);
+    }, ShapeOf<E, 1>(), ShapeOf<16, 1>(), ShapeOf<32, 1>(), ShapeOf<64, 1>(), ShapeOf<64, 2>(), ShapeOf<64, 4>(), ShapeOf<128, most>(), ShapeOf<256, most>(), ShapeOf<512, most>(), ShapeOf<512, 2 * most>());
   }
   if (int rc = ops_launched("layer norm gradients")) return rc;
   if (p.bytes == 0) return CADA_OK;
-  k_norm_join<T><<<dim3((unsigned)ceil_div(a->width, 32), 2), 256, 0, st>>>(n);
+  const dim3 grid((unsigned)ceil_div(a->width, 32), 2);
+  if (a->width <= 4096) k_norm_join<T, 32><<<grid, 1024, 0, st>>>(n);
+  else k_norm_join<T, 8><<<grid, 256, 0, st>>>(n);
   return ops_launched("layer norm join");
 }
 
