@@ -90,7 +90,7 @@ struct Scatter {
 // that are mostly of one range) goes over its positions again instead.
 // Every workgroup reads all tokens (from L2), so what counts is the operations per token: they are 32-bit numbers, of which those that add nothing are the largest, and 64 of them are skipped together
 // where none is in the range.  Equal tokens of a batch are counted together, not by an atomic each (64 additions to one place in LDS are 64 turns).
-constexpr int kSortThreads = 1024, kSortWaves = 16;
+constexpr int kSortThreads = 1024, kSortWaves = 16, kFewRange = 2048;
 constexpr uint32_t kNoToken = ~0u;
 template <typename W> __device__ __forceinline__ uint32_t token32(const W *tokens, uint32_t i, uint32_t ignore) {
   uint32_t k;
@@ -319,6 +319,116 @@ __global__ __launch_bounds__(256) void k_join(const Scatter a) {
   }
 }
 
+// Few positions, one per thread: a workgroup finds those of its range of tokens and sorts them in LDS (by counting, for each, the smaller ones).  2^lanes threads go along a row; the others of 1024 take
+// other tokens' rows, or, of a token that occurs more than sixteen times, every so many sixteen of them, whose sums are joined in their order.  One launch for three (us, that of
+// the three in brackets: 400 tokens of 1001 x 301 float32 6.5 (12.0), with a token's frequency as in text 7.4 (12.4), all one token 25 (19); of 50001 x 1024 bf16 16.3 (22.8); 400 of 2 x 2048 bf16 21 (15)).
+constexpr int kFewPositions = 512, kFewThreads = 1024;
+template <typename T, typename W>
+__global__ __launch_bounds__(kFewThreads) void k_few(const Scatter a) {
+  constexpr int E = Elem<T>::kPer16, U = 16, kPosBits = 9, kWaves = kFewThreads / 64;
+  __shared__ uint32_t listed[kFewPositions];
+  __shared__ uint16_t position[kFewPositions], token[kFewPositions], long_at[kFewPositions / U], long_size[kFewPositions / U];
+  __shared__ uint8_t size[kFewPositions], any[kFewRange];        // size: of the run that begins there, 0: none, or a long one
+  __shared__ float sums[kFewThreads * E];
+  __shared__ int waves[kWaves], n_long;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, rows = (int)a.rows;
+  const uint32_t first = blockIdx.x * (uint32_t)a.range, range = min((uint32_t)a.range, (uint32_t)a.vocab - first);
+  const uint32_t k = t < rows ? token32(static_cast<const W *>(a.tokens), (uint32_t)t, a.ignore32) : kNoToken;
+  const bool in = k - first < range;
+  const uint64_t mask = __ballot(in);
+  if (lane == 0) waves[wave] = __popcll(mask);
+  if (t < kFewPositions) size[t] = 0;
+  if (t == 0) n_long = 0;
+  for (int i = t; i < (int)range; i += kFewThreads) any[i] = 0;
+  __syncthreads();
+  int before = 0, n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    before += w < wave ? waves[w] : 0;
+    n += waves[w];
+  }
+  const uint32_t mine = (k - first) << kPosBits | t;
+  if (in) {
+    listed[before + __popcll(mask & ((1ull << lane) - 1))] = mine;
+    any[k - first] = 1;
+  }
+  __syncthreads();
+  if (in) {
+    int at = 0, smaller_tokens = 0, equal = 0;
+    for (int i = 0; i < n; ++i) {
+      const uint32_t x = listed[i];
+      at += x < mine;
+      smaller_tokens += x >> kPosBits < k - first;
+      equal += x >> kPosBits == k - first;
+    }
+    position[at] = (uint16_t)t;
+    token[at] = (uint16_t)(k - first);
+    if (at == smaller_tokens) {        // (its first)
+      if (equal > U) {
+        const int r = atomicAdd(&n_long, 1);        // (in which order they are worked on changes no sum)
+        long_at[r] = (uint16_t)at;
+        long_size[r] = (uint16_t)equal;
+      } else {
+        size[at] = (uint8_t)equal;
+      }
+    }
+  }
+  __syncthreads();
+  const int high = kFewThreads >> a.lanes, group = t >> a.lanes, piece = ((int)blockIdx.y << a.lanes) + (t & ((1 << a.lanes) - 1));
+  const bool here = piece * E < a.width;
+  const int col = first_column<T>(piece, a.width);
+  T *dw = static_cast<T *>(a.dw) + (int64_t)first * a.lddw + col;
+  const T *dy = static_cast<const T *>(a.dy) + col;
+  // up to sixteen rows from sorted position i on
+  auto add = [&](float (&acc)[E], int i, int rows_here) __attribute__((always_inline)) {
+    u32x4v raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      raw[u] = u32x4v{0, 0, 0, 0};
+      if (u < rows_here) raw[u] = load_piece(dy + position[i + u] * a.lddy, a.width);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[E];
+      unpack<T>(raw[u], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += f[e];
+    }
+  };
+  if (here) {
+    const float zero[E] = {};
+    for (uint32_t v = group; v < range; v += high)
+      if (!any[v]) store_piece(dw + v * a.lddw, a.width, zero);
+    for (int i = group; i < n; i += high) {
+      if (size[i] == 0) continue;
+      float acc[E] = {};
+      add(acc, i, size[i]);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] *= a.scale;
+      store_piece(dw + token[i] * a.lddw, a.width, acc);
+    }
+  }
+  for (int r = 0; r < n_long; ++r) {
+    const int at = long_at[r], count = long_size[r];
+    float acc[E] = {};
+    if (here)
+      for (int i = group * U; i < count; i += high * U) add(acc, at + i, min(U, count - i));
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[e * kFewThreads + t] = acc[e];
+    __syncthreads();
+    if (here && group == 0) {
+      for (int g = 1; g < high; ++g) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += sums[e * kFewThreads + (g << a.lanes) + t];
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] *= a.scale;
+      store_piece(dw + token[at] * a.lddw, a.width, acc);
+    }
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void k_clear(T *p, int64_t ld, int64_t rows, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * n; i += (int64_t)gridDim.x * 256) {
@@ -352,10 +462,15 @@ int lanes_for(int64_t width, int per16) {
 }
 unsigned slices(int64_t width, int per16, int lanes) { return (unsigned)ceil_div(width, (int64_t)per16 << lanes); }
 
-struct ScatterPlan { int32_t range, chunk; int64_t chunks; size_t off_order, off_key, off_part, bytes; };
+struct ScatterPlan { bool few; int32_t range, chunk; int64_t chunks; size_t off_order, off_key, off_part, bytes; };
 ScatterPlan plan_scatter(const cada_embedding_grad *a) {
   ScatterPlan p{};
   if (a->rows == 0) return p;
+  p.few = a->rows <= std::min<int64_t>(kFewPositions, 128 * a->vocab);        // (long runs go through one workgroup)
+  if (p.few) {        // (no more workgroups than find their tokens and clear their rows at once)
+    p.range = (int32_t)std::min<int64_t>(kFewRange, ceil_div(a->vocab, 1024));
+    return p;
+  }
   // a workgroup's range of tokens: one for each CU, and no more than its counts have room for
   p.range = (int32_t)std::min<int64_t>(2048, ceil_div(a->vocab, 256));
   // chunks for a million lanes, where that leaves some rows to each and no run in too many parts
@@ -398,6 +513,12 @@ int scatter(const cada_embedding_grad *a, const ScatterPlan &p) {
   s.vocab = (int32_t)a->vocab; s.width = (int32_t)a->width; s.token_bytes = a->token_bytes; s.lanes = lanes_for(a->width, E); s.join_lanes = std::min(6, lanes_for(a->width, 4)); s.range = p.range; s.chunk = p.chunk;
   s.scale = (float)a->scale;
   const unsigned groups = (unsigned)ceil_div(a->vocab, p.range);
+  if (p.few) {
+    const dim3 grid(groups, slices(a->width, E, s.lanes));
+    if (a->token_bytes == 8) k_few<T, int64_t><<<grid, kFewThreads, 0, st>>>(s);
+    else k_few<T, int32_t><<<grid, kFewThreads, 0, st>>>(s);
+    return ops_launched("embedding gradient");
+  }
   auto sort = [&](auto token) {
     typedef decltype(token) W;
     if (p.range <= 256) k_sort<W, 256><<<groups, kSortThreads, 0, st>>>(s);

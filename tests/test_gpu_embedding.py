@@ -94,7 +94,7 @@ def test_gradient(width, dtype):
 
 @pytest.mark.parametrize("rows,vocab,kind", [
     (20000, 50001, "all"), (20000, 50001, "one"), (20000, 50001, "near"), (20000, 65536, "few"), (40000, 65537, "all"), (40000, 131073, "near"), (16384, 600001, "all"), (150000, 4, "all"), (150000, 3000, "one"), (200000, 1, "one"),
-    (130000, 2, "few"), (1023, 70000, "all"), (1025, 70000, "near"), (5, 3000000, "all")])
+    (130000, 2, "few"), (1023, 70000, "all"), (1025, 70000, "near"), (5, 3000000, "all"), (512, 3000000, "near"), (511, 50001, "one"), (512, 1000, "few"), (513, 1000, "few"), (512, 256, "all"), (64, 2, "all"), (256, 2, "all"), (257, 2, "all"), (128, 1, "one"), (129, 1, "one"), (200, 1025, "near"), (300, 20, "all"), (500, 40, "few")])
 def test_gradient_exactly(rows, vocab, kind):
     """Small integers: every count of tokens in a range and every length of a run, each sum exactly."""
     gen = torch.Generator(device="cuda"); gen.manual_seed(rows)
@@ -104,6 +104,17 @@ def test_gradient_exactly(rows, vocab, kind):
         tokens[::13] = -100
         check_backward(dy, tokens, vocab, exactly=True)
         check_backward(dy, tokens.int(), vocab, exactly=True)
+
+
+@pytest.mark.parametrize("each", [1, 15, 16, 17, 31, 33, 64, 65, 100])
+def test_runs_of_few_positions(each):
+    """One launch: runs of up to sixteen rows and longer ones, next to each other."""
+    for width, dtype in ((40, torch.float32), (2100, torch.bfloat16), (7, torch.bfloat16)):
+        tokens = torch.cat([torch.arange(3, device="cuda").repeat_interleave(each), torch.arange(3, 10, device="cuda")])
+        dy = torch.randint(-8, 9, (tokens.numel(), width), device="cuda").to(dtype)
+        for vocab in (10, 3000):
+            order = torch.randperm(tokens.numel(), device="cuda")
+            check_backward(dy[order], tokens[order], vocab, exactly=True)
 
 
 @pytest.mark.parametrize("chunk_rows", [15, 16, 17, 31, 32, 33, 47, 48, 49])
