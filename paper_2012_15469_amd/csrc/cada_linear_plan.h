@@ -233,12 +233,13 @@ struct LossHead {
 // Up to so many rows, dw is an outer product each lane forms of its columns, and not tiles whose way in and out is all that they are (6 x 3104 x 35488 float32: both gradients by tiles 306 us, where
 // reading and writing the two tables takes 184).
 constexpr int64_t kOuterRows = 16;
+constexpr int kWideColumns = 128;
 // What a tile's exponentials cost on its way out, in the microseconds of the table above: 4096 x 1024 x 50001 bf16, all four products, with logits in tiles of 64 2616 us, of 128 2086, of 256 1905; 8192 x 512 x 32000 1923,
 // 1560 and 1372; 1000 x 768 x 30000 344, 288 and 270.
 constexpr double kLossEnds[] = {0.2, 0.7, 3.5, 3.0};
 constexpr int strip_columns(int tile) { return tile == 256 ? 64 : 32; }        // of a wavefront's strip of a tile, which has one entry in a row's statistics
 struct LossPlan {
-  bool grads, signal, kept, left, outer, direct, copy_x, copy_w;
+  bool grads, signal, kept, left, wide, outer, direct, copy_x, copy_w;
   Cut logits, piece_logits, dx, dw;
   int64_t piece, pieces, chunks, ldz, strips, left_rows;      // strips: of the signal's rows, each with a part of db; left_rows: of a workgroup of the pass over logits that were left behind
   int stat_floats;
@@ -312,7 +313,11 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
   f.piece_logits = mine[1];
   if (a->dx) f.dx = mine[2];
   if (a->dw && !f.outer) f.dw = mine[2 + n - 1];
-  f.chunks = ceil_div(classes, f.logits.tile) * (f.logits.tile / strip_columns(f.logits.tile));
+  // Up to 64 rows of bf16 read the weights in tiles of 128 columns where these fill the CUs and leave no round of them mostly empty (64 x 1024 x 50001 48 -> 39 us, 1 x 4096 x 65536 113 -> 98; 64 x 1024 x 10000
+  // 15.4 and 21, 40 x 4096 x 65537 148 and 164; float32 50 x 1000 x 30000 47 and 48).
+  const int64_t wide_tiles = ceil_div(classes, kWideColumns), slots = (f.direct ? 3 : 2) * kCUs;
+  f.wide = a->type == CADA_BF16 && rows <= 64 && f.logits.tile == 64 && !f.kept && !f.left && wide_tiles >= kCUs && (wide_tiles <= slots || 4 * wide_tiles >= 3 * ceil_div(wide_tiles, slots) * slots);
+  f.chunks = f.wide ? wide_tiles * (kWideColumns / 32) : ceil_div(classes, f.logits.tile) * (f.logits.tile / strip_columns(f.logits.tile));
   f.stat_floats = a->smoothing != 0.0 ? 4 : 2;
   f.ldz = eights(f.piece);
   const KeptShape shape = kept_shape(rows, classes);

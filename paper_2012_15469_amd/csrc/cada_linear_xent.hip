@@ -53,14 +53,14 @@ template <typename T> __device__ __forceinline__ void put_bias(const Loss &q, co
 
 // A tile's logits into statistics.  A lane has FN x 16 logits of a row, and the lane 32 further the row's others.
 // Bound by the vector unit: an addition, a comparison, two operations and an exponential (four times an operation's time) per logit.
-template <typename T, int BM, bool LEFT> struct ToStatistics {
+template <typename T, int BM, int BN, bool LEFT> struct ToStatistics {
   static constexpr bool kOwn = true;
   const Loss &q;
   int32_t *label;            // [BM], in LDS
-  float *bias;               // [BM], in LDS
+  float *bias;               // [BN], in LDS
   __device__ __forceinline__ ToStatistics(const Loss &loss, int32_t *l, float *b) : q(loss), label(l), bias(b) {}
   __device__ __forceinline__ void begin(const Product &p, int64_t m0, int n0, int t) {
-    put_bias<T>(q, p, n0, t, BM, bias);
+    put_bias<T>(q, p, n0, t, BN, bias);
     if (t >= BM) return;
     const int64_t l = m0 + t < p.M ? label_at(q.labels, q.label_bytes, m0 + t) : -1;
     label[t] = counts(q, l) ? (int32_t)l : -1;
@@ -381,14 +381,14 @@ __device__ __forceinline__ float loss_of(const Loss &q, const Stat &s, float bas
   return used ? l : 0.f;
 }
 
-template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW, bool LEFT>
+template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW, bool LEFT>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product p, const Loss q) {
-  __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
+  __shared__ __align__(16) unsigned char lds[tile_lds(BM, BN, STAGES, KW)];
   __shared__ int32_t label[BM];
-  __shared__ __align__(16) float bias[BM];
+  __shared__ __align__(16) float bias[BN];
   if (blockIdx.x == 0) clear_counters(q.head);
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
-  if (tile != ~0u) tile_product<T, BM, BM, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<T, BM, LEFT>(q, label, bias));
+  if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<T, BM, BN, LEFT>(q, label, bias));
 }
 template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_signal(const Product p, const Loss q) {
@@ -420,7 +420,7 @@ __device__ __forceinline__ void join(Stat &a, const Stat &b) {
 
 // 2^lanes rows by the other threads of 1024 over their strips; a row's strips are joined in one order.  The last workgroup adds the losses up, in the workgroups' order.
 __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
-  __shared__ Stat part[1024];
+  __shared__ Stat part[16][64];
   __shared__ float losses[64];
   __shared__ uint8_t used_rows[64];
   const int here = 1 << q.lanes, t = threadIdx.x, row = t & (here - 1), lane = t >> q.lanes, high = 1024 >> q.lanes;
@@ -439,12 +439,27 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
         join(s, Stat{x.x, x.y, 0.f, 0.f});
       }
     }
-    part[t] = s;
-    for (int h = high / 2; h > 0; h >>= 1) {
+    // a row's lanes of a wavefront, then its wavefronts, in their order
+    for (int o = here; o < 64; o <<= 1) {
+      Stat other = {__shfl_xor(s.top, o, 64), __shfl_xor(s.sum, o, 64), 0.f, 0.f};
+      if (q.smoothing != 0.f) {
+        other.distance = __shfl_xor(s.distance, o, 64);
+        other.left = __shfl_xor(s.left, o, 64);
+      }
+      if (t & o) {        // (in one order for both)
+        join(other, s);
+        s = other;
+      } else {
+        join(s, other);
+      }
+    }
+    if ((t & 63) < here) part[t >> 6][row] = s;
+    for (int h = 8; h > 0; h >>= 1) {
       __syncthreads();
       if (lane < h) {
-        join(s, part[t + (h << q.lanes)]);
-        part[t] = s;
+        s = part[lane][row];
+        join(s, part[lane + h][row]);
+        part[lane][row] = s;
       }
     }
     if (lane == 0) {
@@ -745,8 +760,8 @@ template <typename T, int E, int WY, int WX, int KW>
 void tiles(const Product &p, const Loss &q, bool statistics, bool direct, hipStream_t st) {
   const unsigned grid = (unsigned)(ceil_div(tiles_of(p), 8) * 8), threads = 64 * WY * WX * KW;
   auto launch = [&](auto dir, auto stages) {
-    if (statistics && q.left) k_statistics<T, E, WY, WX, dir(), stages(), KW, true><<<grid, threads, 0, st>>>(p, q);
-    else if (statistics) k_statistics<T, E, WY, WX, dir(), stages(), KW, false><<<grid, threads, 0, st>>>(p, q);
+    if (statistics && q.left) k_statistics<T, E, E, WY, WX, dir(), stages(), KW, true><<<grid, threads, 0, st>>>(p, q);
+    else if (statistics) k_statistics<T, E, E, WY, WX, dir(), stages(), KW, false><<<grid, threads, 0, st>>>(p, q);
     else k_signal<T, E, WY, WX, dir(), stages(), KW><<<grid, threads, 0, st>>>(p, q);
   };
   if constexpr (E <= 64) {
@@ -756,6 +771,14 @@ void tiles(const Product &p, const Loss &q, bool statistics, bool direct, hipStr
     if (deep(E, tiles_of(p))) return launch(std::true_type(), std::integral_constant<int, 4>());
   }
   launch(std::true_type(), std::integral_constant<int, 2>());
+}
+// Statistics of up to 64 rows of bf16: tiles twice as wide (LossPlan::wide says when).
+int wide_statistics(Product p, const Loss &q, bool direct, hipStream_t st) {
+  p.tiles_n = (int32_t)ceil_div(p.N, kWideColumns);
+  const unsigned grid = (unsigned)(ceil_div(tiles_of(p), 8) * 8);
+  if (direct) k_statistics<bf16, 64, kWideColumns, 1, 4, true, 2, 1, false><<<grid, 256, 0, st>>>(p, q);
+  else k_statistics<bf16, 64, kWideColumns, 1, 4, false, 2, 1, false><<<grid, 256, 0, st>>>(p, q);
+  return ops_launched("linear cross-entropy");
 }
 template <typename T>
 int logits(const Product &p, const Loss &q, int tile, bool statistics, bool direct, hipStream_t st) {
@@ -820,7 +843,7 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
   } else {
     q.left = f.left ? reinterpret_cast<float *>(ws + f.off_left) : nullptr;
     q.left_rows = f.left_rows;
-    if (int rc = logits<T>(z, q, f.logits.tile, true, f.direct, st)) return rc;
+    if (int rc = f.wide ? wide_statistics(z, q, f.direct, st) : logits<T>(z, q, f.logits.tile, true, f.direct, st)) return rc;
     while (q.lanes < 6 && ((int64_t)kLossGroups << q.lanes) < a->rows) ++q.lanes;
     k_rows<<<(unsigned)std::min<int64_t>(ceil_div(a->rows, 1 << q.lanes), kLossGroups), 1024, 0, st>>>(q);
     if (int rc = ops_launched("linear cross-entropy rows")) return rc;

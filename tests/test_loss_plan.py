@@ -11,7 +11,7 @@ from common_more_ops import cada_linear_xent, filled
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 1 << 20          # an aligned address that nobody reads
 ELEM = {0: 4, 1: 2}
-NAMES = ("grads", "signal", "kept", "left", "direct", "copy_x", "copy_w", "outer", "tile", "splits", "piece_tile", "dx_tile", "dx_splits", "dx_per", "dw_tile", "dw_splits", "dw_per", "piece", "pieces", "chunks", "ldz", "strips", "left_rows", "floats",
+NAMES = ("grads", "signal", "kept", "left", "wide", "direct", "copy_x", "copy_w", "outer", "tile", "splits", "piece_tile", "dx_tile", "dx_splits", "dx_per", "dw_tile", "dw_splits", "dw_per", "piece", "pieces", "chunks", "ldz", "strips", "left_rows", "floats",
          "bias", "stats", "left_at", "info", "label", "loss", "signal_at", "dx", "dw", "db", "x", "w", "bytes")
 _SRC = """
 #include "cada_linear_plan.h"
@@ -19,7 +19,7 @@ using namespace cada;
 extern "C" {
 void plan(const cada_linear_xent *a, long *out) {
   const LossPlan f = plan_loss(a);
-  const long v[] = {f.grads, f.signal, f.kept, f.left, f.direct, f.copy_x, f.copy_w, f.outer, f.logits.tile, f.logits.splits, f.piece_logits.tile, f.dx.tile, f.dx.splits, (long)f.dx.k_per_split, f.dw.tile, f.dw.splits, (long)f.dw.k_per_split,
+  const long v[] = {f.grads, f.signal, f.kept, f.left, f.wide, f.direct, f.copy_x, f.copy_w, f.outer, f.logits.tile, f.logits.splits, f.piece_logits.tile, f.dx.tile, f.dx.splits, (long)f.dx.k_per_split, f.dw.tile, f.dw.splits, (long)f.dw.k_per_split,
                     (long)f.piece, (long)f.pieces, (long)f.chunks, (long)f.ldz, (long)f.strips, (long)f.left_rows, f.stat_floats, (long)f.off_bias, (long)f.off_stats, (long)f.off_left, (long)f.off_info, (long)f.off_label, (long)f.off_loss, (long)f.off_signal,
                     (long)f.off_dx, (long)f.off_dw, (long)f.off_db, (long)f.off_x, (long)f.off_w, (long)f.bytes};
   std::copy(v, v + sizeof(v) / sizeof(v[0]), out);
@@ -58,6 +58,7 @@ def check(f, a, dll):
     if f["kept"]:
         assert f["signal"] and f["pieces"] == 1 and classes <= 16384 and not f["left"] and f["splits"] * rows * e8(classes) * 4 <= 192 << 20 and f["strips"] <= dll.most_groups()
     else:
+        assert not f["wide"] or (rows <= 64 and a.type == 1 and f["tile"] == 64 and f["chunks"] == -(-classes // 128) * 4)
         assert f["splits"] == 1 and f["chunks"] * {256: 64}.get(f["tile"], 32) >= classes
         if f["left"]:
             assert f["signal"] and f["pieces"] == 1 and classes > 16384 and rows * e8(classes) * 4 <= 192 << 20 and f["strips"] * f["left_rows"] >= rows and f["strips"] < 65536
