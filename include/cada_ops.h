@@ -221,7 +221,8 @@ int cada_cross_entropy(const cada_xent *a);
 /* The same loss of the logits z = x w + bias of a last layer, and its gradients, without the logits in memory: z is formed in float32 and goes into each row's statistics, and, for the
  * gradients, again in pieces of the classes, whose (softmax - target) lies in the workspace in the operands' type while
  *   dx = (softmax - target) w^T,  dw = x^T (softmax - target),  db = column sums of it (before it is rounded to that type)
- * are formed, all times scale / max(1, number of rows that are not ignored).  (Logits of less than a piece are kept in the workspace in between.)  A class is ruled out by a bias of -inf.  Rows that are ignored, or whose label is no class, get dx = 0
+ * are formed, all times scale / max(1, number of rows that are not ignored).  (Logits of less than a piece are kept in the workspace in between.)  A class is ruled out by a bias of -inf; w is
+ * read there all the same.  Rows that are ignored, or whose label is no class, get dx = 0
  * and count nowhere, whatever x holds there.  Outputs that are NULL are not formed. */
 typedef struct cada_linear_xent {
   int64_t rows;          /* 0 .. 2^30 */

@@ -560,13 +560,17 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const L
       }
     }
     float s[3] = {0.f, 0.f, 0.f};        // sum, left, distance
+    uint32_t in = 0;        // which of the lane's classes are not ruled out
+    static_assert(4 * V <= 32, "");
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (v * LANES + lane) * 4;
-      if (c < columns) z[v] += *reinterpret_cast<const v4s *>(q.kept_bias + c);
+      const v4s b = *reinterpret_cast<const v4s *>(q.kept_bias + min(c, columns - 4));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (c + e >= q.classes) z[v][e] = -kInf;        // (what lies behind the last class is no sum of anything)
+        const bool left = c + e < q.classes && b[e] != -kInf;
+        in |= left ? 1u << (4 * v + e) : 0u;
+        z[v][e] = c + e < q.classes ? z[v][e] + b[e] : -kInf;        // (what lies behind the last class is no sum of anything)
         top[0] = fmaxf(top[0], z[v][e]);
       }
     }
@@ -578,9 +582,9 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const L
       for (int e = 0; e < 4; ++e) {
         s[0] += power(z[v][e], base);
         if (q.smoothing != 0.f) {
-          const bool in = z[v][e] != -kInf;
-          s[1] += in ? 1.f : 0.f;
-          s[2] += in ? z[v][e] - base : 0.f;
+          const bool left = in >> (4 * v + e) & 1;
+          s[1] += left ? 1.f : 0.f;
+          s[2] += left ? z[v][e] - base : 0.f;
         }
       }
     group_join<LANES>(s, part_sum, false);
@@ -601,7 +605,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const L
       v4s g;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        g[e] = power(z[v][e], from_top) * f_total - (z[v][e] != -kInf ? f_each : 0.f);
+        g[e] = power(z[v][e], from_top) * f_total - (in >> (4 * v + e) & 1 ? f_each : 0.f);
         if (flat) g[e] = 0.f;        // (whatever the logits are)
         else if (label == c + e) g[e] -= 1.f;
       }

@@ -504,7 +504,7 @@ template <typename T>
 int backward(const cada_norm_grad *a, const NormGradPlan &p) {
   hipStream_t st = static_cast<hipStream_t>(a->stream);
   NormGrad n{};
-  n.dy = a->dy; n.x = a->x; n.weight = a->weight; n.residual = a->residual; n.mean = a->mean; n.rstd = a->rstd;
+  n.dy = a->dy; n.x = a->x; n.weight = a->weight; n.residual = a->dx ? a->residual : nullptr; n.mean = a->mean; n.rstd = a->rstd;
   n.dx = a->dx; n.dw = a->dw; n.db = a->db; n.part = static_cast<float *>(a->workspace);
   n.rows = a->rows; n.lddy = a->lddy; n.ldx = a->ldx; n.ldr = a->ldr; n.lddx = a->lddx;
   n.width = (int32_t)a->width; n.parts = (int32_t)p.parts; n.rows_per_part = p.rows_per_part;
@@ -583,7 +583,7 @@ int cada_layer_norm_backward(const cada_norm_grad *a) {
     if (!ops_check_table("dy", a->dy, a->lddy, a->width, a->type) || !ops_check_table("x", a->x, a->ldx, a->width, a->type)) return CADA_EINVAL;
     if (!ops_check_table("mean", a->mean, 1, 1, CADA_F32) || !ops_check_table("rstd", a->rstd, 1, 1, CADA_F32)) return CADA_EINVAL;
     if (a->weight && !ops_check_table("weight", a->weight, a->width, a->width, a->type)) return CADA_EINVAL;
-    if (a->residual && !ops_check_table("residual", a->residual, a->ldr, a->width, a->type)) return CADA_EINVAL;
+    if (a->dx && a->residual && !ops_check_table("residual", a->residual, a->ldr, a->width, a->type)) return CADA_EINVAL;
     if (a->dx && !ops_check_table("dx", a->dx, a->lddx, a->width, a->type)) return CADA_EINVAL;
   }
   if (a->dw && !ops_check_table("dw", a->dw, a->width, a->width, a->type)) return CADA_EINVAL;

@@ -205,6 +205,21 @@ def test_large_logits():
         check(300 * x, 30 * w, labels, b)
 
 
+@pytest.mark.parametrize("rows,classes", [(6, 700), (6, 20000), (70, 5000)])
+def test_a_logit_that_overflows(rows, classes):
+    """A product past float32 makes a logit -inf: a class of probability zero that is not ruled out, whichever way the statistics are formed."""
+    x, w, labels, b = problem(rows, 16, classes, "f32", 13)
+    w[0], x[:, 0] = 0.0, 0.0
+    w[0, 3], x[2, 0] = -10.0, 3e38
+    labels.fill_(1)
+    for smoothing in (0.0, 0.1):
+        for grads in (False, True):
+            mean, loss, dx, dw, db = ops.linear_cross_entropy(x, w, labels, b, smoothing=smoothing, need_dx=grads, need_dw=grads, need_db=grads)
+            assert bool(torch.isfinite(loss[:2]).all()) and bool(torch.isfinite(loss[3:]).all()) and float(loss[2]) == (math.inf if smoothing else float(loss[2])) and not math.isnan(float(loss[2]))
+            if grads:
+                assert bool(torch.isfinite(db).all()) and bool(torch.isfinite(dx).all())
+
+
 def test_nothing_counts():
     for rows in (0, 5):
         x, w, labels, b = problem(max(rows, 1), 24, 40, "bf16")

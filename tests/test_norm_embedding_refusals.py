@@ -97,3 +97,8 @@ def test_tensors_that_are_not_on_a_gpu(call):
 def test_what_is_no_tensor(call, text):
     with pytest.raises(ValueError, match=text):
         call()
+
+
+def test_a_residual_that_is_not_needed_is_not_looked_at():
+    """Without dx: neither its row length nor where it lies."""
+    refused("cada_layer_norm_backward", cada_norm_grad, NORM_GRAD, dict(dx=None, residual=8 * MB, ldr=1, db=8 * MB), -1, "db and dw" + SHARE)
