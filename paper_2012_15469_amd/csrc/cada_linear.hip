@@ -470,7 +470,6 @@ int linear_sums(int type, int tile, bool direct, const Product &p, hipStream_t s
 }
 int linear_products(int type, int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st) { return type == CADA_BF16 ? products<bf16, true>(tile, direct, dx, dw, st) : products<float, true>(tile, direct, dx, dw, st); }
 int linear_join(int type, Join &j, hipStream_t st) { return type == CADA_BF16 ? launch_join<bf16, true>(j, st) : launch_join<float, true>(j, st); }
-int linear_pack(int type, Packs &a, hipStream_t st) { return type == CADA_BF16 ? launch_pack<bf16>(a, st) : launch_pack<float>(a, st); }
 
 bool ops_check_table(const char *name, const void *p, int64_t ld, int64_t cols, int type) {
   if (!p) { set_error("%s is NULL", name); return false; }

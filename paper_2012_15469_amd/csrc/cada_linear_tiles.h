@@ -51,7 +51,6 @@ struct Packs { Pack p[2]; int64_t pieces[2]; };
 int linear_sums(int type, int tile, bool direct, const Product &p, hipStream_t st);        // a forward product whose sums go to p.partial
 int linear_products(int type, int tile, bool direct, const Product &dx, const Product &dw, hipStream_t st);
 int linear_join(int type, Join &j, hipStream_t st);
-int linear_pack(int type, Packs &a, hipStream_t st);
 
 // Workgroups of 256 threads for so many items, which the kernel's loop takes on from there.
 inline unsigned many(int64_t items) { return (unsigned)std::min<int64_t>(ceil_div(items, 256), 1 << 20); }

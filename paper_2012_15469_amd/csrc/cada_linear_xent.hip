@@ -201,7 +201,8 @@ template <typename T, int BM, int BN, bool LEFT> struct ToStatistics {
 
 // A tile's logits into the signal (softmax - target) / (1 - smoothing), and its column sums over a strip of rows.  What is left of the gradient's factor, (1 - smoothing) scale / count, is
 // taken to the products' float32 sums: a bf16 signal is rounded, and with that factor in it the label's -(1 - p) of every row would be rounded the same way wherever p is small, up to 2^-8 off
-// (1 / 100 rows), while -1 + p / (1 - smoothing) is next to a value that bf16 has (dx and dw 2.4e-3 from 64 bits, relative in the 2-norm, and 2.9e-3 for an unlucky count; rounding the outputs alone is 1.7e-3).
+// (1 / 100 rows), while -1 + p / (1 - smoothing) is next to a value that bf16 has (100, 96 and 300 rows:
+// dx and dw 1.75e-3, 1.77e-3 and 1.70e-3 from 64 bits, relative in the 2-norm; with the factor in the signal 2.2e-3, 2.9e-3 and 2.5e-3; rounding the outputs alone is 1.66e-3).
 // Rows without gradient have a sum of infinity (and x = 0), classes that are ruled out a logit of -inf.
 template <typename T, int BM> struct ToSignal {
   static constexpr bool kOwn = true;
@@ -381,6 +382,8 @@ __device__ __forceinline__ float loss_of(const Loss &q, const Stat &s, float bas
   return used ? l : 0.f;
 }
 
+// The logits, formed a first time for the rows' statistics: bound by the matrix instructions where there are many rows (8192 x 4096 x 65536 bf16 3360 us, 1.31 PFLOP/s; 4096 x 1024 x 50001 424 us, 0.99: 12.25
+// rounds of tiles of 256 x 256, one to a CU, take 13), by the weights where there are few (64 x 1024 x 50001, whose odd rows go through registers: 25 us, 4.1 TB/s).
 template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW, bool LEFT>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product p, const Loss q) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BN, STAGES, KW)];
@@ -390,6 +393,7 @@ __global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product 
   const uint32_t tile = tile_of_block((uint32_t)p.tiles_m * p.tiles_n);
   if (tile != ~0u) tile_product<T, BM, BN, WY, WX, true, false, DIRECT, STAGES, KW, NO_SIGNAL>(p, tile, lds, ToStatistics<T, BM, BN, LEFT>(q, label, bias));
 }
+// The logits of a piece, formed again for its signal (the largest case above: eight pieces of 442 us, 1.24 PFLOP/s; the other: three of 169, whose 4.1 rounds take 5).
 template <typename T, int BM, int WY, int WX, bool DIRECT, int STAGES, int KW = 1>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_signal(const Product p, const Loss q) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BM, STAGES, KW)];
@@ -418,7 +422,8 @@ __device__ __forceinline__ void join(Stat &a, const Stat &b) {
   a.top = top;
 }
 
-// 2^lanes rows by the other threads of 1024 over their strips; a row's strips are joined in one order.  The last workgroup adds the losses up, in the workgroups' order.
+// 2^lanes rows by the other threads of 1024 over their strips; a row's strips are joined in one order.  The last workgroup adds the losses up, in the workgroups' order.  (64 rows
+// of 1563 strips 9 us, 8192 of 1024 28: the launch, a workgroup's strips, and the wait for the last one's sum.)
 __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
   __shared__ Stat part[16][64];
   __shared__ float losses[64];
@@ -489,7 +494,7 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
 }
 
 // Kept logits: a group of LANES lanes takes a row, V pieces of four classes per lane, which stay in registers from the statistics to the signal.  A workgroup goes on to further rows and adds up, in
-// registers too, its part of the signal's column sums.  Bound by memory: the logits are read once (in all their parts), the signal is written once.
+// registers too, its part of the signal's column sums.  The logits are read once (in all their parts), the signal is written once.
 template <int LANES, int N> __device__ __forceinline__ void group_join(float (&x)[N], float (*part)[N], bool largest) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
@@ -512,6 +517,7 @@ template <int LANES, int N> __device__ __forceinline__ void group_join(float (&x
     }
   }
 }
+// (8192 x 1000 to bf16 22 us, 2.2 TB/s; 1000 x 16000 47 us, 2.0; 120 x 1001 to float32 8: the wait between a row's read, its sums and its signal.)
 template <typename T, int LANES, int V>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const Loss q) {
   constexpr int kGroups = LANES < 256 ? 256 / LANES : 1;
@@ -655,7 +661,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const L
   add_up(q, losses, used_rows);
 }
 
-// Logits that the statistics left behind into the signal, eight classes of a row per lane, and its column sums over a workgroup's rows.
+// Logits that the statistics left behind into the signal, eight classes of a row per lane, and its column sums over a workgroup's rows (300 x 32000 float32 13.6 us, 5.6 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void k_left_signal(const Loss q) {
   const int c = ((int)blockIdx.x * 256 + threadIdx.x) * 8, columns = (q.classes + 7) / 8 * 8;
@@ -686,7 +692,8 @@ __global__ __launch_bounds__(256) void k_left_signal(const Loss q) {
   if (q.db_part) store8_n(q.db_part + (int64_t)blockIdx.y * q.classes + c, q.classes - c, column);
 }
 
-// dw of up to R rows: a lane keeps a piece of 16 bytes of the signal's rows, times the factor, and goes down dw's rows, x's values for which wait in LDS.  Bound by the writes of dw.
+// dw of up to R rows: a lane keeps a piece of 16 bytes of the signal's rows, times the factor, and goes down dw's rows, x's values for which wait in LDS.  Bound by the writes of dw where
+// rows are few (6 rows, 3104 x 35488 float32: 441 MB in 63 us, 7.0 TB/s; 16 rows, 1024 x 35488 bf16: 73 MB in 29 us, 2.5).
 struct Outer {
   const void *x, *signal;
   void *dw;
@@ -736,7 +743,8 @@ __global__ __launch_bounds__(256) void k_outer(const Outer a) {
   }
 }
 
-// Copies in rows on 16-byte boundaries: of x, with zeros for rows that do not count, and of w, each where there is one to make; and of the biases in float32 for kept logits.
+// Copies in rows on 16-byte boundaries: of x, with zeros for rows that do not count, and of w, each where there is one to make; and of the biases in float32 for kept logits.  Bound by memory (x of
+// 4096 x 1024 and w of 1024 x 50001 bf16: 222 MB in 50 us, 4.4 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void k_copy(const Loss q, const Packs a, float *bias) {
   constexpr int E = Elem<T>::kPer16;
