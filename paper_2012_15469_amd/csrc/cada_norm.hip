@@ -563,7 +563,7 @@ int cada_layer_norm_forward(const cada_norm *a) {
   const Span ins[] = {x, span("weight", a->weight, 1, a->width, a->width, elem), span("bias", a->bias, 1, a->width, a->width, elem)};
   const bool in_place = a->x == a->y && (a->ldx == a->ldy || a->rows == 1);
   for (const Span &in : ins)
-    if ((!(in.at == a->x && in_place) && !ops_apart(y, in)) || !ops_apart(mean, in) || !ops_apart(rstd, in)) return CADA_EINVAL;
+    if ((!(&in == ins && in_place) && !ops_apart(y, in)) || !ops_apart(mean, in) || !ops_apart(rstd, in)) return CADA_EINVAL;
   if (!ops_apart(y, mean) || !ops_apart(y, rstd) || !ops_apart(mean, rstd)) return CADA_EINVAL;
   Norm n{};
   n.x = a->x; n.weight = a->weight; n.bias = a->bias; n.y = a->y; n.mean = a->mean; n.rstd = a->rstd;

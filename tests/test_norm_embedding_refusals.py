@@ -52,6 +52,12 @@ def test_y_in_place_is_not_what_is_refused():
     refused("cada_layer_norm_forward", cada_norm, NORM, dict(y=1 * MB, rstd=5 * MB), -1, "mean and rstd" + SHARE)
 
 
+@pytest.mark.parametrize("name", ["weight", "bias"])
+def test_y_in_the_place_of_x_is_not_in_that_of_weights_there(name):
+    # (mean and rstd share memory too, so that a call that got past the weights would still be refused before it reached a device)
+    refused("cada_layer_norm_forward", cada_norm, NORM, {"y": 1 * MB, name: 1 * MB, "rstd": 5 * MB}, -1, f"y and {name}" + SHARE)
+
+
 @pytest.mark.parametrize("kw,text", [
     (dict(rows=-1), "rows"), (dict(rows=(1 << 30) + 1), "rows"), (dict(vocab=0), "vocab"), (dict(vocab=(1 << 24) + 1), "vocab"), (dict(width=0), "width"), (dict(type=7), "type"), (dict(token_bytes=2), "token_bytes"),
     (dict(scale=float("nan")), "scale"), (dict(scale=1e39), "scale"), (dict(tokens=None), "tokens is NULL"), (dict(tokens=MB + 4), "tokens is not aligned"), (dict(w=None), "w is NULL"), (dict(y=None), "y is NULL"),
