@@ -129,9 +129,17 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) each(i0 + 64 * u + lane, k[u]);
     }
-    for (; i0 < mine; i0 += 64) {
-      const uint32_t k = token32(tokens, (uint32_t)min(i0 + lane, mine - 1), a.ignore32);
-      each(i0 + lane, i0 + lane < mine ? k : kNoToken);
+    if (i0 < mine) {
+      uint32_t k[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + 64 * u + lane;
+        k[u] = token32(tokens, (uint32_t)min(i, mine - 1), a.ignore32);
+        k[u] = i < mine ? k[u] : kNoToken;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i0 + 64 * u < mine) each(i0 + 64 * u + lane, k[u]);
     }
   };
   int32_t below = 0, listed = 0;
@@ -145,16 +153,19 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
     }
   });
   const bool all_listed = listed <= kList && per <= 1 << (32 - kKeyBits);
-  // Calls each(first lane of those with a token, which lanes, position, token from the range's first) for the tokens of each batch.
+  // Calls each(position, token from the range's first or -1, the lanes that have the same one) for batches of mine.  Equal tokens are found by a ballot for each of their bits, and a batch makes one trip to
+  // LDS, however many tokens it has.
+  const int bits = 32 - __builtin_clz(max(range, 2u) - 1);
   auto tokens_of_mine = [&](auto each) __attribute__((always_inline)) {
     auto batch = [&](int i, int32_t k) __attribute__((always_inline)) {
-      uint64_t left = __ballot(k >= 0);
-      while (left) {
-        const int32_t one = __builtin_amdgcn_readlane(k, __builtin_ctzll(left));
-        const uint64_t same = __ballot(k == one);
-        each(same, i, one, k == one);
-        left &= ~same;
+      uint64_t same = __ballot(k >= 0);
+      if (!same) return;
+      for (int b = 0; b < bits; ++b) {
+        const bool one = k >> b & 1;
+        const uint64_t ones = __ballot(one);
+        same &= one ? ones : ~ones;
       }
+      each(i, k, same);
     };
     if (all_listed) {
       for (int e = 0; e < listed; e += 64) {
@@ -167,8 +178,8 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
   };
   volatile int32_t *places = count[wave];
   __syncthreads();
-  tokens_of_mine([&](uint64_t same, int, int32_t k, bool) __attribute__((always_inline)) {
-    if (lane == __builtin_ctzll(same)) places[k] = places[k] + (int32_t)__popcll(same);
+  tokens_of_mine([&](int, int32_t k, uint64_t same) __attribute__((always_inline)) {
+    if (k >= 0 && (same & lower) == 0) __hip_atomic_fetch_add(&count[wave][k], (int32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   });
   if (lane == 0) wave_sum[0][wave] = below;
   __syncthreads();
@@ -213,15 +224,15 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
   }
   if (t == 0 && first + range == (uint32_t)a.vocab) a.start[a.vocab] = base;
   __syncthreads();
-  tokens_of_mine([&](uint64_t same, int i, int32_t k, bool here) __attribute__((always_inline)) {
-    if (here) {
-      const int32_t at = places[k] + __popcll(same & lower);
+  tokens_of_mine([&](int i, int32_t k, uint64_t same) __attribute__((always_inline)) {
+    if (k >= 0) {
+      const int32_t base = places[k], at = base + __popcll(same & lower);
       a.order[at] = (int32_t)(from + i);
       a.key[at] = (int32_t)first + k;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if ((same & lower) == 0) places[k] = base + (int32_t)__popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (lane == __builtin_ctzll(same)) places[k] = places[k] + (int32_t)__popcll(same);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   });
 }
 
@@ -288,36 +299,71 @@ __global__ __launch_bounds__(256) void k_sums(const Scatter a) {
   flush(hi < n && a.key[hi] == now);
 }
 
-// A run that crosses borders: a workgroup at each border, which has something to do if it is the run's first.  Four columns per lane, 2^join_lanes lanes (up to 64) along a part; the
-// parts are dealt to the others of the workgroup, whose sums are added in their order.  Bound by the trips to memory of a run's search and its parts (13 us in the case above).
+// Runs that cross borders: a wavefront at each border, which has something to do if it is its run's first.  It adds the run's parts up by itself, four columns per lane and 2^join_lanes lanes along a part,
+// or leaves a run of many parts to its whole workgroup: a workgroup's sixteen borders are at most one such run's first.  No sum's order goes by time.
+constexpr int kJoinWaves = 16, kLongRun = kJoinWaves + 1;        // a run of more parts crosses more borders than a workgroup has
 template <typename T>
-__global__ __launch_bounds__(256) void k_join(const Scatter a) {
-  __shared__ v4s sums[256];
-  const int64_t b = (int64_t)blockIdx.x + 1, at = b * a.chunk;
-  const int32_t n = a.start[a.vocab], v = a.key[at], before = a.key[at - 1];        // (asked for together; behind the last position they are what was there)
-  if (at >= n || before != v) return;
-  const int32_t start = a.start[v], end = a.start[v + 1];
-  if (start < at - a.chunk) return;
-  const int64_t last = (end - 1) / a.chunk, parts = last - b + 2;        // of chunk b - 1 what goes on, of the others what comes from before
-  const int along = 1 << a.join_lanes, deep = 256 >> a.join_lanes, lane = threadIdx.x & (along - 1), turn = threadIdx.x >> a.join_lanes;
-  for (int64_t c0 = (int64_t)blockIdx.y * along * 4; c0 < a.width; c0 += (int64_t)gridDim.y * along * 4) {
-    const int64_t c = c0 + lane * 4;
+__global__ __launch_bounds__(64 * kJoinWaves) void k_join(const Scatter a) {
+  __shared__ v4s sums[kJoinWaves][64];
+  __shared__ int32_t long_token, long_parts;
+  __shared__ int64_t long_border;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int along = 1 << a.join_lanes, turns = 64 >> a.join_lanes, turn = lane >> a.join_lanes, in_row = lane & (along - 1);
+  const int64_t columns = (int64_t)gridDim.y * along * 4;
+  // the sum of parts first, first + step, ...; then of the wavefront's turns
+  auto sum_parts = [&](int64_t border, int32_t parts, int first, int step, int64_t c) __attribute__((always_inline)) {
     v4s s = {0.f, 0.f, 0.f, 0.f};
     if (c < a.width) {
 #pragma unroll 8
-      for (int64_t i = turn; i < parts; i += deep) {
-        const u32x4v x = load16_n(a.part + (2 * (b - 1 + i) + (i == 0 ? 1 : 0)) * a.width + c, a.width - c);
+      for (int i = first; i < parts; i += step) {        // of chunk border - 1 what goes on, of the others what comes from before
+        const u32x4v x = load16_n(a.part + (2 * (border - 1 + i) + (i == 0 ? 1 : 0)) * a.width + c, a.width - c);
         s += __builtin_bit_cast(v4s, x);
       }
     }
-    __syncthreads();
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < along * 4 && c0 + threadIdx.x < a.width) {
-      float x = sums[threadIdx.x >> 2][threadIdx.x & 3];
-      for (int i = 1; i < deep; ++i) x += sums[i * along + (threadIdx.x >> 2)][threadIdx.x & 3];
-      static_cast<T *>(a.dw)[(int64_t)v * a.lddw + c0 + threadIdx.x] = from_f32<T>(x * a.scale);
+    for (int o = along; o < 64; o <<= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += __shfl_xor(s[e], o, 64);
+    return s;
+  };
+  if (t == 0) long_parts = 0;
+  const int64_t b = (int64_t)blockIdx.x * kJoinWaves + wave + 1, at = b * a.chunk, i = min(at, a.rows - 1);
+  const int32_t n = a.start[a.vocab], v = a.key[i], before = a.key[i - 1];        // (asked for together; behind the last position they are what was there)
+  int32_t parts = 0;
+  if (at < n && before == v) {
+    const int32_t start = a.start[v], end = a.start[v + 1];
+    if (start >= at - a.chunk) parts = (int32_t)((end - 1) / a.chunk - b + 2);
+  }
+  __syncthreads();
+  if (parts > kLongRun) {
+    if (lane == 0) {
+      long_token = v;
+      long_border = b;
+      long_parts = parts;
     }
+  } else if (parts > 0) {
+    for (int64_t c0 = (int64_t)blockIdx.y * along * 4; c0 < a.width; c0 += columns) {
+      const int64_t c = c0 + in_row * 4;
+      const v4s s = sum_parts(b, parts, turn, turns, c);
+      if (turn == 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < a.width) static_cast<T *>(a.dw)[(int64_t)v * a.lddw + c + e] = from_f32<T>(s[e] * a.scale);
+      }
+    }
+  }
+  __syncthreads();
+  if (long_parts == 0) return;
+  for (int64_t c0 = (int64_t)blockIdx.y * along * 4; c0 < a.width; c0 += columns) {
+    const v4s s = sum_parts(long_border, long_parts, wave * turns + turn, kJoinWaves * turns, c0 + in_row * 4);
+    if (turn == 0) sums[wave][in_row] = s;
+    __syncthreads();
+    if (t < along * 4 && c0 + t < a.width) {
+      float x = sums[0][t >> 2][t & 3];
+#pragma unroll
+      for (int w = 1; w < kJoinWaves; ++w) x += sums[w][t >> 2][t & 3];
+      static_cast<T *>(a.dw)[(int64_t)long_token * a.lddw + c0 + t] = from_f32<T>(x * a.scale);
+    }
+    __syncthreads();
   }
 }
 
@@ -536,7 +582,7 @@ int scatter(const cada_embedding_grad *a, const ScatterPlan &p) {
   k_sums<T><<<dim3(s.chunk_blocks + fill, across), 256, 0, st>>>(s);
   if (int rc = ops_launched("embedding gradient")) return rc;
   if (p.chunks == 1) return CADA_OK;
-  k_join<T><<<dim3((unsigned)p.chunks - 1, (unsigned)std::min<int64_t>(ceil_div(a->width, (int64_t)4 << s.join_lanes), 1024)), 256, 0, st>>>(s);
+  k_join<T><<<dim3((unsigned)ceil_div(p.chunks - 1, kJoinWaves), (unsigned)std::min<int64_t>(ceil_div(a->width, (int64_t)4 << s.join_lanes), 1024)), 64 * kJoinWaves, 0, st>>>(s);
   return ops_launched("embedding join");
 }
 

@@ -423,7 +423,7 @@ __device__ __forceinline__ void join(Stat &a, const Stat &b) {
 }
 
 // 2^lanes rows by the other threads of 1024 over their strips; a row's strips are joined in one order.  The last workgroup adds the losses up, in the workgroups' order.  (64 rows
-// of 1563 strips 9 us, 8192 of 1024 28: the launch, a workgroup's strips, and the wait for the last one's sum.)
+// of 1564 strips 9 us, 8192 of 1024 28: the launch, a workgroup's strips, and the wait for the last one's sum.  Labels and their logits asked for before the strips: the same.)
 __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
   __shared__ Stat part[16][64];
   __shared__ float losses[64];

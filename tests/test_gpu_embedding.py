@@ -126,6 +126,21 @@ def test_runs_around_the_ends_of_chunks(chunk_rows):
         check_backward(dy[order], tokens[order], 41, exactly=True)
 
 
+@pytest.mark.parametrize("width", [3, 8, 100, 260, 1001])
+def test_runs_over_many_chunks(width):
+    """Runs over 15 to 18, 33 and 200 chunks of eight sorted positions, each beginning and ending at every place of a chunk, with runs of one to nine positions between them; sums exactly."""
+    lengths = []
+    for n in (15, 16, 17, 18, 33, 200):
+        for off in (-1, 0, 1, 3):
+            lengths += [8 * n + off, 1 + len(lengths) % 9]
+    tokens = torch.arange(len(lengths), device="cuda").repeat_interleave(torch.tensor(lengths, device="cuda"))
+    for dtype in (torch.float32, torch.bfloat16):
+        dy = torch.randint(-8, 9, (tokens.numel(), width), device="cuda").to(dtype)
+        for order in (torch.arange(tokens.numel(), device="cuda"), torch.randperm(tokens.numel(), device="cuda")):
+            check_backward(dy[order], tokens[order], len(lengths), exactly=True)
+            check_backward(dy[order], tokens[order].int() + 100, 1000, exactly=True)
+
+
 def test_the_order_of_a_sum():
     """Equal tokens' rows are added in their order, chunk by chunk: a row of 2^24, ones that it swallows, and its negative."""
     dy = torch.ones(6, 8, device="cuda")
