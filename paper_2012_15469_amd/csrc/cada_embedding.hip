@@ -88,7 +88,7 @@ struct Scatter {
 
 // A workgroup's tokens are [first, first + range).  Each of its sixteen wavefronts goes over a sixteenth of the positions and lists those of its tokens; smaller tokens outside the range are only
 // counted.  It counts each of its tokens, and, when all have counted, puts their positions down behind those of the smaller tokens and of the wavefronts before it.  A wavefront whose list is full (tokens
-// that are mostly of one range) goes over its positions again instead.
+// that are mostly of one range) goes over the positions behind those of its list again.
 // Every workgroup reads all tokens (from L2), so what counts is the operations per token: they are 32-bit numbers, of which those that add nothing are the largest, and 64 of them are skipped together
 // where none is in the range.  Equal tokens of a batch are counted together, not by an atomic each (64 additions to one place in LDS are 64 turns).
 // 32768 tokens of 50001: 14 us (37 with 64-bit comparisons and no lists); 80000 tokens of 27 values, with the sums, 34 us; all of them one value, which is one workgroup's list, 189.
@@ -107,7 +107,7 @@ template <typename W> __device__ __forceinline__ uint32_t token32(const W *token
 template <typename W, int RANGE>
 __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
   constexpr int U = 8;        // batches of 64 on their way at once
-  constexpr int kList = RANGE <= 512 ? 1024 : 256, kKeyBits = 11;        // entries: position from the wavefront's first << kKeyBits | token from the range's first
+  constexpr int kList = RANGE <= 256 ? 2048 : RANGE <= 512 ? 1024 : 256, kKeyBits = 11;        // entries: position from the wavefront's first << kKeyBits | token from the range's first
   __shared__ int32_t count[kSortWaves][RANGE];
   __shared__ uint32_t list[kSortWaves][kList];
   __shared__ int32_t wave_sum[2][kSortWaves];
@@ -120,14 +120,13 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
   const int mine = (int)max((int64_t)0, min(a.rows - from, per));
   const W *tokens = static_cast<const W *>(a.tokens) + from;
   for (int i = t; i < kSortWaves * RANGE; i += kSortThreads) (&count[0][0])[i] = 0;
-  auto batches = [&](auto each) __attribute__((always_inline)) {        // each(position, token)
-    int i0 = 0;
+  auto batches = [&](int i0, auto each) __attribute__((always_inline)) {        // each(position of the batch's first token, a lane's token), from the batch at i0 on
     for (; i0 + 64 * U <= mine; i0 += 64 * U) {
       uint32_t k[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) k[u] = token32(tokens, (uint32_t)(i0 + 64 * u + lane), a.ignore32);
 #pragma unroll
-      for (int u = 0; u < U; ++u) each(i0 + 64 * u + lane, k[u]);
+      for (int u = 0; u < U; ++u) each(i0 + 64 * u, k[u]);
     }
     if (i0 < mine) {
       uint32_t k[U];
@@ -139,20 +138,25 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (i0 + 64 * u < mine) each(i0 + 64 * u + lane, k[u]);
+        if (i0 + 64 * u < mine) each(i0 + 64 * u, k[u]);
     }
   };
-  int32_t below = 0, listed = 0;
-  batches([&](int i, uint32_t k) __attribute__((always_inline)) {
+  // (how many are of the range, of which so many are listed, all of those before position `rest`)
+  int32_t below = 0, found = per <= 1 << (32 - kKeyBits) ? 0 : kList + 1, listed = 0, rest = 0;
+  batches(0, [&](int i, uint32_t k) __attribute__((always_inline)) {
     below += __popcll(__ballot(k < first));
     const uint64_t in = __ballot(k - first < range);
     if (in) {
-      const int n = __popcll(in);
-      if (listed + n <= kList && k - first < range) list[wave][listed + __popcll(in & lower)] = (uint32_t)i << kKeyBits | (k - first);
-      listed += n;
+      const int32_t at = found;
+      found += __popcll(in);
+      if (found <= kList) {
+        if (k - first < range) list[wave][at + __popcll(in & lower)] = (uint32_t)(i + lane) << kKeyBits | (k - first);
+        listed = found;
+        rest = i + 64;
+      }
     }
   });
-  const bool all_listed = listed <= kList && per <= 1 << (32 - kKeyBits);
+  if (found <= kList) rest = mine;
   // Calls each(position, token from the range's first or -1, the lanes that have the same one) for batches of mine.  Equal tokens are found by a ballot for each of their bits, and a batch makes one trip to
   // LDS, however many tokens it has.
   const int bits = 32 - __builtin_clz(max(range, 2u) - 1);
@@ -167,14 +171,11 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
       }
       each(i, k, same);
     };
-    if (all_listed) {
-      for (int e = 0; e < listed; e += 64) {
-        const uint32_t x = list[wave][min(e + lane, kList - 1)];
-        batch((int)(x >> kKeyBits), e + lane < listed ? (int32_t)(x & ((1u << kKeyBits) - 1)) : -1);
-      }
-    } else {
-      batches([&](int i, uint32_t k) __attribute__((always_inline)) { batch(i, k - first < range ? (int32_t)(k - first) : -1); });
+    for (int e = 0; e < listed; e += 64) {
+      const uint32_t x = list[wave][min(e + lane, kList - 1)];
+      batch((int)(x >> kKeyBits), e + lane < listed ? (int32_t)(x & ((1u << kKeyBits) - 1)) : -1);
     }
+    if (rest < mine) batches(rest, [&](int i, uint32_t k) __attribute__((always_inline)) { batch(i + lane, k - first < range ? (int32_t)(k - first) : -1); });
   };
   volatile int32_t *places = count[wave];
   __syncthreads();
