@@ -452,8 +452,9 @@ NormShape norm_shape(int64_t width, int per16) {
   if (n <= 4096) return {512, 8};
   return {1024, 0};
 }
-// The gradient's lanes hold the sums of their columns besides the rows: sixteen columns each, or 32 for rows that take a workgroup of 512; rows beyond 16384 are wide.  (Workgroups of 1024, whose lanes have
-// half the registers, spill: 8000 x 16000 bf16 514 us.)
+// The gradient's lanes hold the sums of their columns besides the rows: sixteen columns each, or 24 or 32 for rows that take a workgroup of 512; rows beyond 16384 are wide.  (Workgroups of 1024, whose lanes
+// have half the registers, spill: 8000 x 16000 bf16 514 us.  24 columns do not, 28 and 32 of float32 do: 12206 x 8864 float32 248 us with 24, 434 with 32; 8000 x 12000 with a residual 293 and 510, bf16 156
+// and 169.  24 with the next row asked for ahead, and for that the weights where they are used, 319, 388, 214.)
 NormShape norm_grad_shape(int64_t width, int per16) {
   const int64_t n = ceil_div(width, per16);
   const int most = 16 / per16;
@@ -463,6 +464,7 @@ NormShape norm_grad_shape(int64_t width, int per16) {
   for (int lanes = 64; lanes <= 512; lanes *= 2)
     for (int pieces = 1; pieces <= most; pieces *= 2)
       if (n <= lanes * pieces && (lanes == 64 || pieces == most)) return {lanes, pieces};
+  if (n <= 768 * most) return {512, most + most / 2};
   return n <= 1024 * most ? NormShape{512, 2 * most} : NormShape{1024, 0};
 }
 int64_t rows_at_once(const NormShape &s) { return s.lanes <= 64 ? 256 / s.lanes : 1; }
@@ -524,7 +526,7 @@ int backward(const cada_norm_grad *a, const NormGradPlan &p) {
     constexpr int E = Elem<T>::kPer16, most = 16 / E;
     by_shape(p.shape, [&](auto shape) {
       if constexpr (shape.pieces <= most || shape.lanes == 512) k_norm_grad<T, shape.lanes, shape.pieces><<<(unsigned)p.parts, kThreads<shape.lanes>, 0, st>>>(n);
-    }, ShapeOf<E, 1>(), ShapeOf<16, 1>(), ShapeOf<32, 1>(), ShapeOf<64, 1>(), ShapeOf<64, 2>(), ShapeOf<64, 4>(), ShapeOf<128, most>(), ShapeOf<256, most>(), ShapeOf<512, most>(), ShapeOf<512, 2 * most>());
+    }, ShapeOf<E, 1>(), ShapeOf<16, 1>(), ShapeOf<32, 1>(), ShapeOf<64, 1>(), ShapeOf<64, 2>(), ShapeOf<64, 4>(), ShapeOf<128, most>(), ShapeOf<256, most>(), ShapeOf<512, most>(), ShapeOf<512, most + most / 2>(), ShapeOf<512, 2 * most>());
   }
   if (int rc = ops_launched("layer norm gradients")) return rc;
   if (p.bytes == 0) return CADA_OK;

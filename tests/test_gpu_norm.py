@@ -66,7 +66,7 @@ def check_backward(dy, x, m, r, w, res, **kw):
     return dx, dw, db
 
 
-WIDTHS = [1, 2, 3, 7, 8, 9, 15, 16, 17, 31, 63, 64, 65, 127, 129, 255, 257, 500, 513, 617, 1000, 1025, 2047, 2049, 3001, 4096, 4100, 8191, 8193, 12000, 16384, 16385, 32768, 32771, 70001]
+WIDTHS = [1, 2, 3, 7, 8, 9, 15, 16, 17, 31, 63, 64, 65, 127, 129, 255, 257, 500, 513, 617, 1000, 1025, 2047, 2049, 3001, 4096, 4100, 8191, 8193, 12000, 12288, 12291, 16384, 16385, 32768, 32771, 70001]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -82,7 +82,7 @@ def test_against_definition(width, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,width", [(2, 4096), (511, 1000), (513, 4096), (1030, 617), (2060, 40), (3000, 9), (5000, 3), (520, 17000), (600, 8192)])
+@pytest.mark.parametrize("rows,width", [(2, 4096), (511, 1000), (513, 4096), (1030, 617), (2060, 40), (3000, 9), (5000, 3), (520, 17000), (600, 8192), (600, 9001)])
 def test_many_rows(rows, width, dtype):
     """More rows than a launch has groups, so that a group takes several and the sums come in parts."""
     gen = torch.Generator(device="cuda"); gen.manual_seed(rows)
