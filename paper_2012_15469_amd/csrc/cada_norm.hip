@@ -238,9 +238,11 @@ __global__ __launch_bounds__(kThreads<LANES>, 2) void k_norm_grad(const NormGrad
       row.dy.get(v, f);
       row.x.get(v, u);
       if (w) weights(v, g);
+      // (a column that does not exist holds zero: its u, which may pass float32 where no column's of the row does, is nothing)
+      const float rstd_here = (v * LANES + lane) * E < whole ? rstd : 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        u[e] = (u[e] - mean) * rstd;
+        u[e] = (u[e] - mean) * rstd_here;
         if (here) {
           dw[v][e] = fmaf(f[e], u[e], dw[v][e]);
           db[v][e] += f[e];
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(kThreads<LANES>, 2) void k_norm_grad(const NormGrad
       }
       if constexpr (!kAhead) __builtin_amdgcn_sched_barrier(0);        // (piece by piece: interleaved, they spill)
     }
-    const float u_behind = (row.x.behind - mean) * rstd, g_behind = row.dy.behind * (w ? weight.behind : 1.f);
+    const float u_behind = (row.x.behind - mean) * (lane < a.width - whole ? rstd : 0.f), g_behind = row.dy.behind * (w ? weight.behind : 1.f);
     if (here) {
       dw_behind = fmaf(row.dy.behind, u_behind, dw_behind);
       db_behind += row.dy.behind;
