@@ -12,7 +12,9 @@
 namespace cada {
 namespace {
 
-struct Stat { float top, sum, distance, left; };      // distance: the sum of z - top over the classes that are left (smoothing), left: their number
+// distance: the sum of (z - top) share over the classes that are left (smoothing), left: their number.  With share = 1 / classes such sums, and joins of
+// them, overflow nowhere that z - top does not: a mask of the type's lowest value at any number of classes leaves a loss of some 1e37.
+struct Stat { float top, sum, distance, left; };
 struct RowInfo { float base, f_total, f_each; int32_t label; };      // base infinite (exponentials are zero), f_total 0, label < 0: a row without gradient
 struct Loss {
   const void *labels, *bias;
@@ -29,7 +31,7 @@ struct Loss {
   float *left;               // [rows][classes up to whole groups of eight]: where statistics leave the logits, with their bias, or null
   int64_t left_rows;
   int32_t lanes;             // rows of a workgroup of k_rows, as a power of two
-  float smoothing, keep, scale;      // keep = 1 - smoothing, rounded once
+  float smoothing, keep, scale, share;      // keep = 1 - smoothing, rounded once
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -125,7 +127,7 @@ template <typename T, int BM, int BN, bool LEFT> struct ToStatistics {
             const bool in = b[e] != -kInf;
             left += in ? 1.f : 0.f;
 #pragma unroll
-            for (int i = 0; i < FM; ++i) s[i].distance += in ? z[i][j][4 * r + e] - base[i] : 0.f;
+            for (int i = 0; i < FM; ++i) s[i].distance = fmaf(in ? z[i][j][4 * r + e] - base[i] : 0.f, q.share, s[i].distance);
           }
           if (FM >= 4) __builtin_amdgcn_sched_barrier(0);
         }
@@ -172,7 +174,7 @@ template <typename T, int BM, int BN, bool LEFT> struct ToStatistics {
       const bool in = bias[c + e] != -kInf;
       s.sum += power(z[e], base);
       s.left += in ? 1.f : 0.f;
-      s.distance += in ? z[e] - base : 0.f;
+      s.distance = fmaf(in ? z[e] - base : 0.f, q.share, s.distance);
     }
     float *parts[3] = {&s.sum, &s.left, &s.distance};
 #pragma unroll
@@ -376,7 +378,7 @@ __device__ __forceinline__ void add_up(const Loss &q, double sum, int64_t used) 
 // A row's loss from its statistics and its label's logit (log(sum exp z) - keep z_y - smoothing mean_left z, with the largest taken out of all three).
 __device__ __forceinline__ float loss_of(const Loss &q, const Stat &s, float base, float z_label, bool used, bool known) {
   float l = logf(s.sum) - q.keep * (z_label - base);
-  if (q.smoothing != 0.f) l -= q.smoothing * (s.distance / s.left);
+  if (q.smoothing != 0.f) l -= q.smoothing * s.distance * ((float)q.classes / s.left);
   if (s.top == -kInf && s.sum == 0.f) l = kInf;
   if (!known) l = __builtin_nanf("");
   return used ? l : 0.f;
@@ -404,7 +406,7 @@ __global__ __launch_bounds__(64 * WY * WX * KW) void k_signal(const Product p, c
 }
 
 // Joins statistics `b` to `a`: both against the larger of the two largest.
-__device__ __forceinline__ void join(Stat &a, const Stat &b) {
+template <bool SMOOTH> __device__ __forceinline__ void join(Stat &a, const Stat &b, float share) {
   if (b.top == -kInf) {        // no class left there, or NaN
     a.sum += b.sum;
     a.left += b.left;
@@ -417,13 +419,16 @@ __device__ __forceinline__ void join(Stat &a, const Stat &b) {
   }
   const float top = fmaxf(a.top, b.top);
   a.sum = a.sum * __builtin_amdgcn_exp2f((a.top - top) * kLog2e) + b.sum * __builtin_amdgcn_exp2f((b.top - top) * kLog2e);
-  a.distance = fmaf(a.left, a.top - top, a.distance) + fmaf(b.left, b.top - top, b.distance);
-  a.left += b.left;
+  if constexpr (SMOOTH) {
+    a.distance = fmaf(a.left * share, a.top - top, a.distance) + fmaf(b.left * share, b.top - top, b.distance);
+    a.left += b.left;
+  }
   a.top = top;
 }
 
 // 2^lanes rows by the other threads of 1024 over their strips; a row's strips are joined in one order.  The last workgroup adds the losses up, in the workgroups' order.  (64 rows
 // of 1564 strips 9 us, 8192 of 1024 28: the launch, a workgroup's strips, and the wait for the last one's sum.  Labels and their logits asked for before the strips: the same.)
+template <bool SMOOTH>
 __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
   __shared__ Stat part[16][64];
   __shared__ float losses[64];
@@ -434,28 +439,28 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
   for (int64_t r0 = (int64_t)blockIdx.x * here; r0 < q.rows; r0 += (int64_t)gridDim.x * here) {
     const int64_t r = r0 + row, at = min(r, q.rows - 1);
     Stat s = {-kInf, 0.f, 0.f, 0.f};
-    if (q.smoothing != 0.f) {
+    if constexpr (SMOOTH) {
 #pragma unroll 4
-      for (int64_t c = lane; c < q.chunks; c += high) join(s, reinterpret_cast<const Stat *>(q.stats)[c * q.rows + at]);
+      for (int64_t c = lane; c < q.chunks; c += high) join<true>(s, reinterpret_cast<const Stat *>(q.stats)[c * q.rows + at], q.share);
     } else {
 #pragma unroll 8
       for (int64_t c = lane; c < q.chunks; c += high) {
         const float2 x = reinterpret_cast<const float2 *>(q.stats)[c * q.rows + at];
-        join(s, Stat{x.x, x.y, 0.f, 0.f});
+        join<false>(s, Stat{x.x, x.y, 0.f, 0.f}, q.share);
       }
     }
     // a row's lanes of a wavefront, then its wavefronts, in their order
     for (int o = here; o < 64; o <<= 1) {
       Stat other = {__shfl_xor(s.top, o, 64), __shfl_xor(s.sum, o, 64), 0.f, 0.f};
-      if (q.smoothing != 0.f) {
+      if constexpr (SMOOTH) {
         other.distance = __shfl_xor(s.distance, o, 64);
         other.left = __shfl_xor(s.left, o, 64);
       }
       if (t & o) {        // (in one order for both)
-        join(other, s);
+        join<SMOOTH>(other, s, q.share);
         s = other;
       } else {
-        join(s, other);
+        join<SMOOTH>(s, other, q.share);
       }
     }
     if ((t & 63) < here) part[t >> 6][row] = s;
@@ -463,7 +468,7 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
       __syncthreads();
       if (lane < h) {
         s = part[lane][row];
-        join(s, part[lane + h][row]);
+        join<SMOOTH>(s, part[lane + h][row], q.share);
         part[lane][row] = s;
       }
     }
@@ -479,7 +484,7 @@ __global__ __launch_bounds__(1024) void k_rows(const Loss q) {
       losses[row] = l;
       used_rows[row] = used;
       if (q.loss) q.loss[r] = l;
-      q.info[r] = known && used && !none ? RowInfo{base, 1.f / (s.sum * q.keep), q.smoothing != 0.f ? q.smoothing / (s.left * q.keep) : 0.f, (int32_t)label} : RowInfo{kInf, 0.f, 0.f, -1};
+      q.info[r] = known && used && !none ? RowInfo{base, 1.f / (s.sum * q.keep), SMOOTH ? q.smoothing / (s.left * q.keep) : 0.f, (int32_t)label} : RowInfo{kInf, 0.f, 0.f, -1};
     }
     __syncthreads();
     if (t == 0) {
@@ -590,7 +595,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_kept_rows(const L
         if (q.smoothing != 0.f) {
           const bool left = in >> (4 * v + e) & 1;
           s[1] += left ? 1.f : 0.f;
-          s[2] += left ? z[v][e] - base : 0.f;
+          s[2] = fmaf(left ? z[v][e] - base : 0.f, q.share, s[2]);
         }
       }
     group_join<LANES>(s, part_sum, false);
@@ -824,7 +829,7 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
   q.stats = reinterpret_cast<float *>(ws + f.off_stats); q.info = reinterpret_cast<RowInfo *>(ws + f.off_info); q.z_label = reinterpret_cast<float *>(ws + f.off_label);
   q.loss = a->loss ? a->loss : reinterpret_cast<float *>(ws + f.off_loss); q.mean = a->mean;
   q.rows = a->rows; q.ignore = a->ignore_index; q.chunks = f.chunks; q.classes = (int32_t)a->classes; q.label_bytes = a->label_bytes;
-  q.smoothing = (float)a->smoothing; q.keep = (float)(1.0 - a->smoothing); q.scale = (float)a->scale;
+  q.smoothing = (float)a->smoothing; q.keep = (float)(1.0 - a->smoothing); q.scale = (float)a->scale; q.share = (float)(1.0 / (double)a->classes);
   const T *x = static_cast<const T *>(a->x), *w = static_cast<const T *>(a->w);
   int64_t ldx = a->ldx, ldw = a->ldw, x_cols = a->in, w_cols = a->classes;
   Packs k{};
@@ -857,7 +862,9 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
     q.left_rows = f.left_rows;
     if (int rc = f.wide ? wide_statistics(z, q, f.direct, st) : logits<T>(z, q, f.logits.tile, true, f.direct, st)) return rc;
     while (q.lanes < 6 && ((int64_t)kLossGroups << q.lanes) < a->rows) ++q.lanes;
-    k_rows<<<(unsigned)std::min<int64_t>(ceil_div(a->rows, 1 << q.lanes), kLossGroups), 1024, 0, st>>>(q);
+    const unsigned groups = (unsigned)std::min<int64_t>(ceil_div(a->rows, 1 << q.lanes), kLossGroups);
+    if (q.smoothing != 0.f) k_rows<true><<<groups, 1024, 0, st>>>(q);
+    else k_rows<false><<<groups, 1024, 0, st>>>(q);
     if (int rc = ops_launched("linear cross-entropy rows")) return rc;
   }
   if (!f.signal) return CADA_OK;
