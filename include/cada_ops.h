@@ -218,12 +218,14 @@ typedef struct cada_xent {
 int cada_xent_workspace(cada_xent *a); /* rows, classes, type, mean and loss are read */
 int cada_cross_entropy(const cada_xent *a);
 
-/* The same loss of the logits z = x w + bias of a last layer, and its gradients, without the logits in memory: z is formed in float32 and goes into each row's statistics, and, for the
- * gradients, again in pieces of the classes, whose (softmax - target) lies in the workspace in the operands' type while
- *   dx = (softmax - target) w^T,  dw = x^T (softmax - target),  db = column sums of it (before it is rounded to that type)
- * are formed, all times scale / max(1, number of rows that are not ignored).  (Logits of less than a piece are kept in the workspace in between.)  A class is ruled out by a bias of -inf; w is
- * read there all the same.  Rows that are ignored, or whose label is no class, get dx = 0
- * and count nowhere, whatever x holds there.  Outputs that are NULL are not formed. */
+/* The same loss of the logits z = x w + bias of a last layer, and its gradients, without the logits in memory:
+ *   dx = g w^T,  dw = x^T g,  db = column sums of g,  g = (softmax(z) - target) * scale / max(1, number of rows that are not ignored)
+ * z is formed in float32 for each row's statistics and, for the gradients, again in pieces of the classes, whose softmax - target
+ * lies in the workspace in the operands' type (db is summed before that rounding).  Logits of less than a piece are kept in
+ * the workspace in between.  Outputs that are NULL are not formed.
+ * A class is ruled out by a bias of -inf; w is read there all the same.  An ignored row counts nowhere.  One whose label is neither
+ * ignore_index nor in [0, classes) has loss NaN, and so has the mean; it is one of the rows that are not ignored.  Either has
+ * dx = 0 and no part in dw and db, whatever x holds there. */
 typedef struct cada_linear_xent {
   int64_t rows;          /* 0 .. 2^30 */
   int64_t in, classes;   /* 1 .. CADA_MAX_WIDTH; of the tables' products, at most 2^23 - 8 tiles of 64 x 64 */

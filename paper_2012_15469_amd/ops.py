@@ -149,8 +149,10 @@ def linear_cross_entropy(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor,
                          ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
     """(mean loss, loss of each row, dx, dw, db): cross_entropy of the logits x w + bias and the gradients of scale * mean loss, without the logits in memory.
 
-    x [rows, in], w [in, classes], bias [classes] or None, all of one type; labels int32 or int64 [rows].  Rows labelled ``ignore_index`` count nowhere, whatever x holds there; classes
-    whose bias is -inf are ruled out.  db is None without a bias unless a ``db`` to write is given.  Outputs handed in are written, not added to."""
+    x [rows, in], w [in, classes], bias [classes] or None, all of one type; labels int32 or int64 [rows].  Rows labelled ``ignore_index`` count nowhere, whatever x holds there; a row
+    whose label is no class has loss NaN (and so has the mean), no gradient, and is among the rows that the gradients are divided by.  Classes whose bias is -inf are ruled out.
+    db is None without a bias unless a ``db`` to write is given.  Outputs handed in are written, not added to.  w has contiguous rows: an embedding's table [vocab, width] that is the last
+    layer too is copied transposed for this call, and dw back."""
     return _call(_ops.linear_cross_entropy, x, stream, x, w, labels, bias, smoothing, ignore_index, scale, bool(need_dx), bool(need_dw), bool(need_db) and (bias is not None or db is not None),
                  dx, dw, db, workspace)
 
