@@ -145,8 +145,8 @@ typedef struct cada_norm_grad {
 int cada_layer_norm_backward_workspace(cada_norm_grad *a); /* rows, width, type, and whether dw and db are wanted */
 int cada_layer_norm_backward(const cada_norm_grad *a);
 
-/* Rows of a table by integer tokens: y[i] = scale w[token i], in float32, rounded once.  The row of a token that is ignore_index is zero (also where
- * ignore_index is in [0, vocab)); that of any other token outside [0, vocab) is NaN. */
+/* Rows of a table by integer tokens: y[i] = scale w[token i], in float32, rounded once.  The row of a token that is ignore_index is zero
+ * (also where ignore_index is in [0, vocab)); that of any other token outside [0, vocab) is NaN. */
 typedef struct cada_embedding {
   int64_t rows;         /* 0 .. 2^30 */
   int64_t vocab;        /* 1 .. 2^24 */
@@ -165,8 +165,9 @@ typedef struct cada_embedding {
 
 int cada_embedding_forward(const cada_embedding *a); /* needs no workspace */
 
-/* Its gradient: dw[v] = scale times the sum of dy[i] over the tokens i that are v, in their order, in float32, rounded once.  All of dw is written: a row whose
- * token does not occur is zero.  Tokens that are ignore_index or outside [0, vocab) add nothing. */
+/* Its gradient: dw[v] = scale times the sum of dy[i] over the tokens i that are v, in float32, rounded once.  The additions have one order, which
+ * depends on the sizes, the type and the tokens only: that of the tokens within a few of them, whose sums are then joined.  All of dw is written:
+ * a row whose token does not occur is zero.  Tokens that are ignore_index or outside [0, vocab) add nothing. */
 typedef struct cada_embedding_grad {
   int64_t rows, vocab, width; /* as above */
   int32_t type;

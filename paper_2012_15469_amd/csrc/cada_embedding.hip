@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_join(const Scatter a) {
 }
 
 // Few positions, one per thread: a workgroup finds those of its range of tokens and sorts them in LDS (by counting, for each, the smaller ones).  2^lanes threads go along a row; the others of 1024 take
-// other tokens' rows, or, of a token that occurs more than sixteen times, every so many sixteen of them, whose sums are joined in their order.  One launch for three (us, that of
+// other tokens' rows, or, of a token that occurs more than sixteen times, every so many sixteen of them, whose sums are joined in the groups' order.  One launch for three (us, that of
 // the three in brackets: 400 tokens of 1001 x 301 float32 6.7 (12.2), with a token's frequency as in text 7.1 (14.1), all one token 25 (13); of 50001 x 1024 bf16 16.6 (23.2); 400 of 2 x 2048 bf16 21 (12)).
 constexpr int kFewPositions = 512, kFewThreads = 1024;
 template <typename T, typename W>

@@ -129,7 +129,8 @@ def embedding_forward(tokens: torch.Tensor, w: torch.Tensor, *, scale: float = 1
 
 def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, *, scale: float = 1.0, ignore_index: int = -100, dw: Optional[torch.Tensor] = None,
                        workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """dw [vocab, width] of embedding_forward from the gradient of its output: zero where a token does not occur.  Equal tokens' rows are added in their order."""
+    """dw [vocab, width] of embedding_forward from the gradient of its output: zero where a token does not occur.  Equal tokens' rows are added in one order,
+    which depends on the sizes, the type and the tokens only."""
     return _call(_ops.embedding_backward, dy, stream, dy, tokens, vocab, scale, ignore_index, dw, workspace)
 
 
