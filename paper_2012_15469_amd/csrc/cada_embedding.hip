@@ -86,13 +86,14 @@ struct Scatter {
   float scale;
 };
 
-// A workgroup's tokens are [first, first + range).  Each of its sixteen wavefronts goes over a sixteenth of the positions and lists those of its tokens; smaller tokens outside the range are only
-// counted.  It counts each of its tokens, and, when all have counted, puts their positions down behind those of the smaller tokens and of the wavefronts before it.  A wavefront whose list is full (tokens
-// that are mostly of one range) goes over the positions behind those of its list again.
-// Every workgroup reads all tokens (from L2), so what counts is the operations per token: they are 32-bit numbers, of which those that add nothing are the largest, and 64 of them are skipped together
-// where none is in the range.  Equal tokens of a batch are counted together, not by an atomic each (64 additions to one place in LDS are 64 turns).
-// 32768 tokens of 50001: 13 us (37 with 64-bit comparisons and no lists); 100000 tokens of 27 values, with frequencies as in text, 30 (74 with lists of 1024, all of whose tokens were read again);
-// 131072 of 30000 35.  The whole gradient of 80000 tokens of 27, evenly, in rows of 64 bf16 30 us; all of them one, which is one workgroup's list, 83.
+// A workgroup's tokens are [first, first + range).  Each of its sixteen wavefronts goes over a sixteenth of the positions and lists those of its tokens;
+// smaller tokens outside the range are only counted.  It counts each of its tokens, and, when all have counted, puts their positions down behind those of the
+// smaller tokens and of the wavefronts before it.  A wavefront whose list is full (tokens that are mostly of one range) goes over the positions behind those of
+// its list again.  Every workgroup reads all tokens (from L2), so what counts is the operations per token: they are 32-bit numbers, of which those that add
+// nothing are the largest, and 64 of them are skipped together where none is in the range.  Equal tokens of a batch are counted together, not by an atomic each
+// (64 additions to one place in LDS are 64 turns).  32768 tokens of 50001: 13 us (37 with 64-bit comparisons and no lists); 100000 tokens of 27 values, with
+// frequencies as in text, 30 (74 with lists of 1024, all of whose tokens were read again); 131072 of 30000 35.  The whole gradient of 80000 tokens of 27,
+// evenly, in rows of 64 bf16 30 us; all of them one, which is one workgroup's list, 83.
 constexpr int kSortThreads = 1024, kSortWaves = 16, kFewRange = 2048;
 constexpr uint32_t kNoToken = ~0u;
 template <typename W> __device__ __forceinline__ uint32_t token32(const W *tokens, uint32_t i, uint32_t ignore) {
@@ -158,8 +159,8 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const Scatter a) {
     }
   });
   if (found <= kList) rest = mine;
-  // Calls each(position, token from the range's first or -1, the lanes that have the same one) for batches of mine.  Equal tokens are found by a ballot for each of their bits, and a batch makes one trip to
-  // LDS, however many tokens it has.
+  // Calls each(position, token from the range's first or -1, the lanes that have the same one) for batches of mine.  Equal tokens are found by a ballot for
+  // each of their bits, and a batch makes one trip to LDS, however many tokens it has.
   const int bits = 32 - __builtin_clz(max(range, 2u) - 1);
   auto tokens_of_mine = [&](auto each) __attribute__((always_inline)) {
     auto batch = [&](int i, int32_t k) __attribute__((always_inline)) {
@@ -301,9 +302,10 @@ __global__ __launch_bounds__(256) void k_sums(const Scatter a) {
   flush(hi < n && a.key[hi] == now);
 }
 
-// Runs that cross borders: a wavefront at each border, which has something to do if it is its run's first.  It adds the run's parts up by itself, four columns per lane and 2^join_lanes lanes along a part,
-// or leaves a run of many parts to its whole workgroup: a workgroup's sixteen borders are at most one such run's first (40735 tokens of 3527 with frequencies as in text, rows of 400 bf16, the longest run in
-// hundreds of parts: 9.9 us, and 41 with a workgroup of four wavefronts at each border; 32768 of 50001 x 2048 7.0 and 13).  Bound by the trips to memory of a run's search and its parts.  No sum's order goes by time.
+// Runs that cross borders: a wavefront at each border, which has something to do if it is its run's first.  It adds the run's parts up by itself, four columns
+// per lane and 2^join_lanes lanes along a part, or leaves a run of many parts to its whole workgroup: a workgroup's sixteen borders are at most one such run's
+// first (40735 tokens of 3527 with frequencies as in text, rows of 400 bf16, the longest run in hundreds of parts: 9.9 us, and 41 with a workgroup of four
+// wavefronts at each border; 32768 of 50001 x 2048 7.0 and 13).  Bound by the trips to memory of a run's search and its parts.  No sum's order goes by time.
 constexpr int kJoinWaves = 16, kLongRun = kJoinWaves + 1;        // a run of more parts crosses more borders than a workgroup has
 template <typename T>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_join(const Scatter a) {
@@ -370,9 +372,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_join(const Scatter a) {
   }
 }
 
-// Few positions, one per thread: a workgroup finds those of its range of tokens and sorts them in LDS (by counting, for each, the smaller ones).  2^lanes threads go along a row; the others of 1024 take
-// other tokens' rows, or, of a token that occurs more than sixteen times, every so many sixteen of them, whose sums are joined in the groups' order.  One launch for three (us, that of
-// the three in brackets: 400 tokens of 1001 x 301 float32 6.7 (12.2), with a token's frequency as in text 7.1 (14.1), all one token 25 (13); of 50001 x 1024 bf16 16.6 (23.2); 400 of 2 x 2048 bf16 21 (12)).
+// Few positions, one per thread: a workgroup finds those of its range of tokens and sorts them in LDS (by counting, for each, the smaller ones).  2^lanes
+// threads go along a row; the others of 1024 take other tokens' rows, or, of a token that occurs more than sixteen times, every so many sixteen of them, whose
+// sums are joined in the groups' order.  One launch for three (us, that of the three in brackets: 400 tokens of 1001 x 301 float32 6.7 (12.2), with a token's
+// frequency as in text 7.1 (14.1), all one token 25 (13); of 50001 x 1024 bf16 16.6 (23.2); 400 of 2 x 2048 bf16 21 (12)).
 constexpr int kFewPositions = 512, kFewThreads = 1024;
 template <typename T, typename W>
 __global__ __launch_bounds__(kFewThreads) void k_few(const Scatter a) {

@@ -89,8 +89,9 @@ inline bool direct_oc(const void *p, int64_t ld, int64_t cols, size_t elem) { re
 // Whether a table is too small for a read of 16 bytes, or a tile of it too large for offsets in 32 bits.
 inline bool no_tiles(int64_t rows, int64_t ld, int64_t cols, size_t elem) { return ((rows - 1) * ld + cols) * (int64_t)elem < 16 || 64 * ld * (int64_t)elem >= (int64_t)1 << 32; }
 
-// Rows and outputs that are a read of the weights; more rows cost little or no more as 32 x 32 tiles (4 x 1024 x 4096 bf16 7.4 us as rows, 6.0 as tiles, from memory 9.8 and 7.9; float32 8.5 and 10.8, 13.4 and 13.3), and
-// more outputs would make a second workgroup for some CUs (1 x 4096 x 50000 bf16 118 us as rows, 91 as tiles; float32 186 and 157).
+// Rows and outputs that are a read of the weights; more rows cost little or no more as 32 x 32 tiles (4 x 1024 x 4096 bf16 7.4 us as rows, 6.0 as tiles, from
+// memory 9.8 and 7.9; float32 8.5 and 10.8, 13.4 and 13.3), and more outputs would make a second workgroup for some CUs (1 x 4096 x 50000 bf16 118 us as rows,
+// 91 as tiles; float32 186 and 157).
 inline bool few_rows(int64_t rows, int64_t out) { return rows <= kFewRows && out <= 64 * kCUs; }
 // Columns of a workgroup there: a line of memory of bf16 weights (half a line each from two: 4096 x 4096 17 us, not 11); of float32 ones a line, for twice the workgroups, or
 // two lines where that fills the CUs (single row from memory, contraction not split: 4096 x 1024 28 us with 32 columns and 36 with 64, 8192 x 16384 127 and 104).
@@ -207,11 +208,12 @@ inline BackwardPlan plan_backward(const cada_linear_grad *a) {
 // A last layer's loss: the product [rows, classes] is formed whole once, for each row's statistics, and again in pieces of the classes, whose signal (softmax - target, [rows, piece]) lies in the
 // workspace while both gradients' products read it.
 constexpr int64_t kSignalBytes = (int64_t)192 << 20, kPieceStep = 256, kLeastPiece = 1024;
-// Where all classes are one piece anyway and a float32 copy of the logits is no larger than a piece may be, the logits are kept between the two, which saves the second product: they go to a pass over the rows
-// as the product's float32 sums (in parts, where its contraction is split).
+// Where all classes are one piece anyway and a float32 copy of the logits is no larger than a piece may be, the logits are kept between the two, which saves
+// the second product: they go to a pass over the rows as the product's float32 sums (in parts, where its contraction is split).
 constexpr int64_t kKeptClasses = 16384;        // a workgroup's registers hold a row; the logits of longer ones are left behind by the statistics' tiles, and a pass over them makes the signal
 constexpr int64_t kLeftColumns = 2048;         // of a workgroup of that pass
-// (bf16 8192 x 4096 x 4000 975 -> 820 us, 1000 x 4096 x 16000 570 -> 490, 8192 x 512 x 1000 88 -> 84; float32 4096 x 256 x 4000 336 -> 272, 120 x 500 x 1001 41 -> 32.5; bf16 2048 x 128 x 10000 110 -> 113)
+// (bf16 8192 x 4096 x 4000 975 -> 820 us, 1000 x 4096 x 16000 570 -> 490, 8192 x 512 x 1000 88 -> 84; float32 4096 x 256 x 4000 336 -> 272, 120 x 500 x 1001
+// 41 -> 32.5; bf16 2048 x 128 x 10000 110 -> 113)
 constexpr double kKeptBytesPerUs = 3.2e6, kKeptLaunch = 3.0;
 struct KeptShape { int lanes, pieces; int64_t groups; };        // of a row, pieces of four classes per lane, and workgroups at most
 inline KeptShape kept_shape(int64_t rows, int64_t classes) {
@@ -234,8 +236,8 @@ struct LossHead {
 // reading and writing the two tables takes 184).
 constexpr int64_t kOuterRows = 16;
 constexpr int kWideColumns = 128;
-// What a tile's exponentials cost on its way out, in the microseconds of the table above: 4096 x 1024 x 50001 bf16, all four products, with logits in tiles of 64 2616 us, of 128 2086, of 256 1905; 8192 x 512 x 32000 1923,
-// 1560 and 1372; 1000 x 768 x 30000 344, 288 and 270.
+// What a tile's exponentials cost on its way out, in the microseconds of the table above: 4096 x 1024 x 50001 bf16, all four products, with logits in tiles of
+// 64 2616 us, of 128 2086, of 256 1905; 8192 x 512 x 32000 1923, 1560 and 1372; 1000 x 768 x 30000 344, 288 and 270.
 constexpr double kLossEnds[] = {0.2, 0.7, 3.5, 3.0};
 constexpr int strip_columns(int tile) { return tile == 256 ? 64 : 32; }        // of a wavefront's strip of a tile, which has one entry in a row's statistics
 struct LossPlan {
@@ -313,8 +315,8 @@ inline LossPlan plan_loss(const cada_linear_xent *a) {
   f.piece_logits = mine[1];
   if (a->dx) f.dx = mine[2];
   if (a->dw && !f.outer) f.dw = mine[2 + n - 1];
-  // Up to 64 rows of bf16 read the weights in tiles of 128 columns where these fill the CUs and leave no round of them mostly empty (64 x 1024 x 50001 48 -> 39 us, 1 x 4096 x 65536 113 -> 98; 64 x 1024 x 10000
-  // 15.4 and 21, 40 x 4096 x 65537 148 and 164; float32 50 x 1000 x 30000 47 and 48).
+  // Up to 64 rows of bf16 read the weights in tiles of 128 columns where these fill the CUs and leave no round of them mostly empty (64 x 1024 x 50001
+  // 48 -> 39 us, 1 x 4096 x 65536 113 -> 98; 64 x 1024 x 10000 15.4 and 21, 40 x 4096 x 65537 148 and 164; float32 50 x 1000 x 30000 47 and 48).
   const int64_t wide_tiles = ceil_div(classes, kWideColumns), slots = (f.direct ? 3 : 2) * kCUs;
   f.wide = a->type == CADA_BF16 && rows <= 64 && f.logits.tile == 64 && !f.kept && !f.left && wide_tiles >= kCUs && (wide_tiles <= slots || 4 * wide_tiles >= 3 * ceil_div(wide_tiles, slots) * slots);
   f.chunks = f.wide ? wide_tiles * (kWideColumns / 32) : ceil_div(classes, f.logits.tile) * (f.logits.tile / strip_columns(f.logits.tile));

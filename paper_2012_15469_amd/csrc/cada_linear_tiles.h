@@ -302,8 +302,9 @@ template <bool PIECES> __device__ __forceinline__ void put_part(const Product &p
   store8_n(to, 8, f);
 }
 
-// What becomes of a tile's sums: a layer's output, here (PIECES: of a contraction that comes in several launches, with a factor that is in device memory); a last layer's loss has its own (cada_linear_xent.hip), which take the sums where the matrix instructions leave them, sums(), and where
-// wavefronts share a tile's contraction and join their sums in LDS, eight columns of a row per lane, row().
+// What becomes of a tile's sums: a layer's output, here (PIECES: of a contraction that comes in several launches, with a factor that is in device memory); a
+// last layer's loss has its own (cada_linear_xent.hip), which take the sums where the matrix instructions leave them, sums(), and where wavefronts share a
+// tile's contraction and join their sums in LDS, eight columns of a row per lane, row().
 template <bool PIECES = false> struct ToTable {
   static constexpr bool kOwn = false;
   __device__ __forceinline__ void begin(const Product &, int64_t, int, int) const {}

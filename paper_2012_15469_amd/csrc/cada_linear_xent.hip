@@ -1,10 +1,11 @@
 // The softmax cross-entropy of a last layer's product, with its gradients, without the logits in memory (cada_ops.h).
 //
-// The logits' tiles (cada_linear_tiles.h) end in statistics: of each row, and of each strip of 32 or 64 columns, the largest logit and the sum of the exponentials of the
-// distances to it.  A row's strips are then joined, as one goes along, to the row's largest and its sum, which is its loss.  For the gradients the logits are formed again in
-// pieces of the classes; their tiles end in softmax - target (but for a factor) in the operands' type, from which the products of a layer's gradients are taken while it is in the caches: dw is finished piece by
-// piece, dx is added up in float32.  That is four products where keeping the logits would take three, and memory for one piece instead of all.  Logits that are not
-// more than a piece are kept in float32: for a pass over whole rows (k_kept_rows), or, of long rows, left behind by the statistics (k_left_signal).
+// The logits' tiles (cada_linear_tiles.h) end in statistics: of each row, and of each strip of 32 or 64 columns, the largest logit and the sum of the
+// exponentials of the distances to it.  A row's strips are then joined, as one goes along, to the row's largest and its sum, which is its loss.  For the
+// gradients the logits are formed again in pieces of the classes; their tiles end in softmax - target (but for a factor) in the operands' type, from which the
+// products of a layer's gradients are taken while it is in the caches: dw is finished piece by piece, dx is added up in float32.  That is four products where
+// keeping the logits would take three, and memory for one piece instead of all.  Logits that are not more than a piece are kept in float32: for a pass over
+// whole rows (k_kept_rows), or, of long rows, left behind by the statistics (k_left_signal).
 #include <algorithm>
 
 #include "cada_linear_tiles.h"
@@ -42,8 +43,8 @@ __device__ __forceinline__ int64_t label_at(const void *labels, int bytes, int64
 }
 __device__ __forceinline__ bool counts(const Loss &q, int64_t label) { return label != q.ignore && label >= 0 && label < q.classes; }
 
-// exp(z - base) is the hardware's exp2 of the rounded difference times log2(e): off by |z - base| 2^-23 and an ulp or two, relative.  The difference comes first, so that a mask of the type's lowest value (or a
-// row of nothing else) overflows nowhere.
+// exp(z - base) is the hardware's exp2 of the rounded difference times log2(e): off by |z - base| 2^-23 and an ulp or two, relative.  The difference comes
+// first, so that a mask of the type's lowest value (or a row of nothing else) overflows nowhere.
 __device__ __forceinline__ float power(float z, float base) { return __builtin_amdgcn_exp2f((z - base) * kLog2e); }
 
 // The biases of a tile's columns in LDS: -inf for a column that does not exist, so that it is a class that is ruled out (what the matrix instructions made of it is something of the table's).
@@ -384,8 +385,9 @@ __device__ __forceinline__ float loss_of(const Loss &q, const Stat &s, float bas
   return used ? l : 0.f;
 }
 
-// The logits, formed a first time for the rows' statistics: bound by the matrix instructions where there are many rows (8192 x 4096 x 65536 bf16 3360 us, 1.31 PFLOP/s; 4096 x 1024 x 50001 424 us, 0.99: 12.25
-// rounds of tiles of 256 x 256, one to a CU, take 13), by the weights where there are few (64 x 1024 x 50001, whose odd rows go through registers: 25 us, 4.1 TB/s).
+// The logits, formed a first time for the rows' statistics: bound by the matrix instructions where there are many rows (8192 x 4096 x 65536 bf16 3360 us,
+// 1.31 PFLOP/s; 4096 x 1024 x 50001 424 us, 0.99: 12.25 rounds of tiles of 256 x 256, one to a CU, take 13), by the weights where there are few
+// (64 x 1024 x 50001, whose odd rows go through registers: 25 us, 4.1 TB/s).
 template <typename T, int BM, int BN, int WY, int WX, bool DIRECT, int STAGES, int KW, bool LEFT>
 __global__ __launch_bounds__(64 * WY * WX * KW) void k_statistics(const Product p, const Loss q) {
   __shared__ __align__(16) unsigned char lds[tile_lds(BM, BN, STAGES, KW)];

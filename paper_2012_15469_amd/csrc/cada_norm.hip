@@ -189,8 +189,8 @@ __global__ __launch_bounds__(1024) void k_norm_wide(const Norm a) {
   }
 }
 
-// dx of the rows, and the sums of dw and db over a workgroup's rows: these cross no lanes until a workgroup ends, only the two sums of dx do, for each row (2400 x 617 float32: 9.2 us, where the columns
-// fill 60 % of a group's registers).
+// dx of the rows, and the sums of dw and db over a workgroup's rows: these cross no lanes until a workgroup ends, only the two sums of dx do, for each row
+// (2400 x 617 float32: 8.8 us in two turns of 300 workgroups; 2048 rows in one turn of 512 6.6, a single row 3.7).
 template <typename T, int LANES, int V>
 __global__ __launch_bounds__(kThreads<LANES>, 2) void k_norm_grad(const NormGrad a) {
   constexpr int E = Elem<T>::kPer16, kAtOnce = kRowsAtOnce<LANES>, kCols = LANES * V * E;
@@ -407,8 +407,8 @@ __global__ __launch_bounds__(1024) void k_norm_grad_wide(const NormGrad a) {
   }
 }
 
-// The parts of the column sums, in their order: a workgroup takes 32 columns, LANES lanes of each every LANES-th part (32 where there are few columns: 617 columns of 300 parts 4.9 -> 4.0 us; 16000 of 256
-// with 8 lanes 6.8 us, with 32 11).
+// The parts of the column sums, in their order: a workgroup takes 32 columns, LANES lanes of each every LANES-th part (32 where there are few columns: 617
+// columns of 300 parts 4.9 -> 4.0 us; 16000 of 256 with 8 lanes 6.8 us, with 32 11).
 template <typename T, int LANES>
 __global__ __launch_bounds__(32 * LANES) void k_norm_join(const NormGrad a) {
   __shared__ float part[LANES][33];
@@ -454,9 +454,10 @@ NormShape norm_shape(int64_t width, int per16) {
   if (n <= 4096) return {512, 8};
   return {1024, 0};
 }
-// The gradient's lanes hold the sums of their columns besides the rows: sixteen columns each, or 24 or 32 for rows that take a workgroup of 512; rows beyond 16384 are wide.  (Workgroups of 1024, whose lanes
-// have half the registers, spill: 8000 x 16000 bf16 514 us.  24 columns do not, 28 and 32 of float32 do: 12206 x 8864 float32 248 us with 24, 434 with 32; 8000 x 12000 with a residual 293 and 510, bf16 156
-// and 169.  24 with the next row asked for ahead, and for that the weights where they are used, 319, 388, 214.)
+// The gradient's lanes hold the sums of their columns besides the rows: sixteen columns each, or 24 or 32 for rows that take a workgroup of 512; rows beyond
+// 16384 are wide.  (Workgroups of 1024, whose lanes have half the registers, spill: 8000 x 16000 bf16 514 us.  24 columns do not, 28 and 32 of float32 do:
+// 12206 x 8864 float32 248 us with 24, 434 with 32; 8000 x 12000 with a residual 293 and 510, bf16 156 and 169.  24 with the next row asked for ahead, and for
+// that the weights where they are used, 319, 388, 214.)
 NormShape norm_grad_shape(int64_t width, int per16) {
   const int64_t n = ceil_div(width, per16);
   const int most = 16 / per16;

@@ -1,4 +1,5 @@
-"""The embedding's gradient: runs of equal tokens around the ends of chunks of eight sorted positions, and the order of a sum, which is one for given shapes and tokens."""
+"""The embedding's gradient: runs of equal tokens around the ends of chunks of eight sorted positions, and the order of a sum, which is one for given shapes
+and tokens."""
 import pytest
 import torch
 

@@ -1,9 +1,11 @@
-"""The loss of a last layer with smoothed labels and a bias of the type's lowest value at most of its classes: such a class is not ruled out, so the loss is smoothing times the mean distance of the
-logits from the label's, some 3e37, which float32 has, although two of its terms together are more than float32 has.
+"""The loss of a last layer with smoothed labels and a bias of the type's lowest value at most of its classes: such a class is not ruled out, so the loss is
+smoothing times the mean distance of the logits from the label's, some 3e37, which float32 has, although two of its terms together are more than float32
+has.
 
-Tolerances, with e = 2^-24: the loss is a sum of one sign, but for the ordinary logits, which are less than a step of it; each of its terms is off by 4 e relative (the logit, the difference, the factor, the sum it enters), an addition by e, of which
-there are 64 one after the other in a strip of columns, up to classes / 32 strips, and 32 in the joins, and the last operations take 8: (classes / 32 + 108) e in all.  Probabilities and gradients are those of a mask at -120,
-whose exponential, 8e-53, is as good as zero: their tolerances are the ones of the formulas there."""
+Tolerances, with e = 2^-24: the loss is a sum of one sign, but for the ordinary logits, which are less than a step of it; each of its terms is off by 4 e
+relative (the logit, the difference, the factor, the sum it enters), an addition by e, of which there are 64 one after the other in a strip of columns, up
+to classes / 32 strips, and 32 in the joins, and the last operations take 8: (classes / 32 + 108) e in all.  Probabilities and gradients are those of a mask
+at -120, whose exponential, 8e-53, is as good as zero: their tolerances are the ones of the formulas there."""
 import pytest
 import torch
 
@@ -13,7 +15,8 @@ from test_gpu_linear_xent import DT, E, definition, near, problem
 pytestmark = pytest.mark.gpu
 
 # rows, in, classes: logits that are kept (of one and of several lanes' pieces), that the statistics leave behind, that are formed again, in tiles of every size, one piece and several
-SHAPES = [(12, 64, 5), (12, 64, 200), (12, 64, 3000), (300, 40, 1001), (2500, 24, 900), (40, 33, 16001), (6, 64, 20000), (300, 50, 30001), (4100, 64, 20008), (20000, 16, 3000), (64, 72, 65536), (1, 40, 40000)]
+SHAPES = [(12, 64, 5), (12, 64, 200), (12, 64, 3000), (300, 40, 1001), (2500, 24, 900), (40, 33, 16001), (6, 64, 20000), (300, 50, 30001), (4100, 64, 20008),
+          (20000, 16, 3000), (64, 72, 65536), (1, 40, 40000)]
 
 
 def lowest(rows, k, classes, dtype, share):
@@ -60,7 +63,8 @@ def test_lowest_values(rows, k, classes, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,classes", [(12, 200), (12, 3000), (6, 20000), (2500, 900), (1, 1)])
 def test_nothing_but_lowest_values(rows, classes, dtype):
-    """Every class at the lowest value: logits as far from each other as the products are, none of which the type's lowest value shows; the loss is that of even classes."""
+    """Every class at the lowest value: logits as far from each other as the products are, none of which the type's lowest value shows; the loss is that of
+    even classes."""
     x, w, labels, _ = problem(rows, 30, classes, dtype, 22)
     b = torch.full((classes,), torch.finfo(DT[dtype]).min, dtype=DT[dtype], device="cuda")
     for grads in (False, True):

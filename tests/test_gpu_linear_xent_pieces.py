@@ -1,5 +1,5 @@
-"""The loss of a last layer in several pieces of the classes; next to the two operators that it is made of; rows far apart; a logit past float32; what its means and gradients are divided by.  Tolerances as in
-test_gpu_linear_xent.py, which checks against the definitions in 64 bits."""
+"""The loss of a last layer in several pieces of the classes; next to the two operators that it is made of; rows far apart; a logit past float32; what its
+means and gradients are divided by.  Tolerances as in test_gpu_linear_xent.py, which checks against the definitions in 64 bits."""
 import math
 
 import pytest
@@ -28,8 +28,9 @@ def test_pieces(dtype, rows, k, classes, pad):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,k,classes", [(300, 200, 1500), (7, 64, 20000), (2000, 80, 30000)])
 def test_next_to_the_two_operators_apart(rows, k, classes, dtype):
-    """linear_forward rounds logits to their type, h |z| each (h half a step), so losses differ by at most 2 h max |z| besides both sides' own errors, and p by p (2 h max |z|); cross_entropy rounds its gradient to that type, as this operator rounds its
-    signal: h |g| on either side.  The products pass these on as sums of magnitudes."""
+    """linear_forward rounds logits to their type, h |z| each (h half a step), so losses differ by at most 2 h max |z| besides both sides' own errors, and p by
+    p (2 h max |z|); cross_entropy rounds its gradient to that type, as this operator rounds its signal: h |g| on either side.  The products pass these on
+    as sums of magnitudes."""
     x, w, labels, b = problem(rows, k, classes, dtype, 5, ignored=0.1)
     h = half_step(DT[dtype])
     z, _ = ops.linear_forward(x, w, b)
@@ -51,7 +52,8 @@ def test_next_to_the_two_operators_apart(rows, k, classes, dtype):
 
 @pytest.mark.parametrize("rows,classes", [(6, 700), (6, 20000), (70, 5000), (4100, 17000)])
 def test_a_logit_that_overflows(rows, classes):
-    """A product past float32 makes a logit -inf: without smoothing its row's loss is that of the other classes, in whichever way the statistics are formed, and the class's part of the gradients is zero."""
+    """A product past float32 makes a logit -inf: without smoothing its row's loss is that of the other classes, in whichever way the statistics are formed,
+    and the class's part of the gradients is zero."""
     x, w, labels, b = problem(rows, 16, classes, "f32", 13)
     w[0], x[:, 0] = 0.0, 0.0
     labels.fill_(1)
@@ -71,7 +73,8 @@ def test_a_logit_that_overflows(rows, classes):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,classes", [(40, 300), (6, 20000), (3000, 17001)])
 def test_what_it_is_divided_by(rows, classes, dtype):
-    """Ignored rows count nowhere.  A row whose label is no class has loss NaN, and so has the mean, no gradient, and is one of those that the other rows' gradients are divided by, as for cross_entropy."""
+    """Ignored rows count nowhere.  A row whose label is no class has loss NaN, and so has the mean, no gradient, and is one of those that the other rows'
+    gradients are divided by, as for cross_entropy."""
     x, w, labels, b = problem(rows, 32, classes, dtype, 14)
     labels[0] = -100
     for bad in (classes, -1, classes + 5):

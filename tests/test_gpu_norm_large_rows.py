@@ -1,5 +1,5 @@
-"""Layer norm's gradients of rows whose mean times rstd passes float32, where (x - mean) rstd is nothing of the sort: lanes without a column hold zeros, whose distance from such a mean is infinite, and
-must add nothing to their row's sums.
+"""Layer norm's gradients of rows whose mean times rstd passes float32, where (x - mean) rstd is nothing of the sort: lanes without a column hold zeros, whose
+distance from such a mean is infinite, and must add nothing to their row's sums.
 
 A constant row has u = (x - mean) rstd = 0 in every column, so dx = rstd (g - mean of g) + residual, and the row's dy enters db but not dw."""
 import pytest

@@ -1,5 +1,6 @@
-"""Layer norm of more rows than a launch has groups of lanes (2048 workgroups forward, 1024 of 512 lanes; 512 and 256 backward; up to 64 rows of a workgroup at once): a group takes several rows, the next of which is asked for
-before a row is written, also where it is written in the place of what was read, and the last turn is partly filled."""
+"""Layer norm of more rows than a launch has groups of lanes (2048 workgroups forward, 1024 of 512 lanes; 512 and 256 backward; up to 64 rows of a workgroup at
+once): a group takes several rows, the next of which is asked for before a row is written, also where it is written in the place of what was read, and the
+last turn is partly filled."""
 import pytest
 import torch
 
@@ -41,7 +42,8 @@ def test_turns(rows, width, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,width", [(8199, 617), (2051, 4096), (1030, 9001)])
 def test_no_turn_sees_another(rows, width, dtype):
-    """A row of NaN, infinities or the largest values changes its own results only, whichever turn it comes in (but for the sums over the rows, which are not asked for)."""
+    """A row of NaN, infinities or the largest values changes its own results only, whichever turn it comes in (but for the sums over the rows, which are not
+    asked for)."""
     gen = torch.Generator(device="cuda"); gen.manual_seed(width)
     x, dy, w = table(gen, rows, width, dtype), table(gen, rows, width, dtype), table(gen, 1, width, dtype)[0]
     y, m, r = ops.layer_norm_forward(x, w, keep_stats=True)

@@ -1,4 +1,5 @@
-"""What the shapes of common_loss_shapes.py are cut into, on the host: several pieces with products in tiles of every size, with and without parts of the contraction, and a last piece with fewer parts than the others."""
+"""What the shapes of common_loss_shapes.py are cut into, on the host: several pieces with products in tiles of every size, with and without parts of the
+contraction, and a last piece with fewer parts than the others."""
 from common_loss_shapes import PIECES
 from test_loss_plan import check, plan  # noqa: F401
 
