@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few_rows(const Product p) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = part[0][m][cg * 8 + e];
   if (p.splits > 1) store8_n(p.partial + ((int64_t)blockIdx.y * p.M + m) * eights(p.N) + n, left > 0 ? 8 : 0, f);
-  else finish8<T>(p.epi, m, n, left, f);
+  else finish8<T>(p, m, n, left, f);
 }
 
 // dx and dw in one launch (either may have no tiles), the one with the longer contraction first: its tiles would be the launch's tail.
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void k_by_element(const Product p) {
       sum = fmaf(a, b, sum);
     }
     float f[8] = {sum};
-    finish8<T>(p.epi, m, (int)n, 1, f);
+    finish8<T>(p, m, (int)n, 1, f);
     if (SIGNAL == B_SIGNAL && p.db && m == 0) static_cast<T *>(p.db)[n] = from_f32<T>(column);
   }
 }
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(256) void k_join(const Join j) {
         }
       }
       float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      finish8<T, PIECES>(p.epi, m, n, left, f);
+      finish8<T, PIECES>(p, m, n, left, f);
       return;
     }
     g -= j.groups[i];

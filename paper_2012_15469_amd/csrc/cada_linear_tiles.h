@@ -12,7 +12,6 @@ struct Epilogue {
   void *pre, *out;
   int64_t ldr, ldpre, ldo;
   int act;
-  const float *factor;       // PIECES: of the sum, in device memory
 };
 
 // One product C[M, N] = sum_k A(m, k) B(k, n).
@@ -23,7 +22,6 @@ struct Product {
   int64_t k_per_split;       // a multiple of the step
   int32_t N, tiles_m, tiles_n, splits;
   float *partial;            // [splits][M][N up to whole groups of eight], or null: sums that k_join joins and finishes (splits > 1, or a contraction that goes on in another launch)
-  int32_t add;               // PIECES: to what is in `partial` already
   Epilogue epi;
   // small gradients: the operand that is the signal is read as dy, and dz = dy * act'(pre) is formed on its way into LDS
   const void *pre;
@@ -31,6 +29,10 @@ struct Product {
   int32_t act;
   void *db;                  // column sums of dz (or null), by the tiles of the first rows; their parts where the contraction is split
   float *db_part;            // [splits][N]
+  // PIECES: a factor of finished sums, in device memory, and whether unfinished ones are added to what is in `partial` already.  (Behind all that a layer's
+  // products read: with the two before the epilogue and in it, 1 x 1024 x 4096 bf16 6.14 us instead of 6.00, 15499 x 2097 x 16 23.15 instead of 22.96.)
+  const float *factor;
+  int32_t add;
 };
 
 // Joins the sums of a split contraction, in the order of the splits, and finishes them; eight columns per thread.
@@ -263,11 +265,12 @@ __device__ __forceinline__ f32x16 multiply(v4s a, v4s b, f32x16 c) {
 
 // Eight consecutive columns n .. of row m of a finished sum; `left` of them exist.
 template <typename T, bool PIECES = false>
-__device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int n, int64_t left, float (&f)[8]) {
+__device__ __forceinline__ void finish8(const Product &p, int64_t m, int n, int64_t left, float (&f)[8]) {
   if (left <= 0) return;
+  const Epilogue &e = p.epi;
   float o[8];
   if constexpr (PIECES) {
-    const float factor = *e.factor;
+    const float factor = *p.factor;
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= factor;
   }
@@ -310,7 +313,7 @@ template <bool PIECES = false> struct ToTable {
   __device__ __forceinline__ void begin(const Product &, int64_t, int, int) const {}
   template <typename T> __device__ __forceinline__ void row(const Product &p, uint32_t split, int64_t m, int n, int64_t left, float (&f)[8]) const {
     if (p.partial) put_part<PIECES>(p, split, m, n, left, f);
-    else finish8<T, PIECES>(p.epi, m, n, left, f);
+    else finish8<T, PIECES>(p, m, n, left, f);
   }
 };
 

@@ -890,7 +890,7 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
       lay(&dx, c, signal, f.ldz, w + first, ldw, a->rows, a->in, here, nullptr);
       if (f.pieces > 1 || f.dx.splits > 1) dx.partial = reinterpret_cast<float *>(ws + f.off_dx);
       dx.add = i > 0;
-      dx.epi.out = a->dx; dx.epi.ldo = a->lddx; dx.epi.factor = &q.head->factor;
+      dx.epi.out = a->dx; dx.epi.ldo = a->lddx; dx.factor = &q.head->factor;
     }
     if (f.outer) {
       Outer o{};
@@ -906,7 +906,7 @@ int loss(const cada_linear_xent *a, const LossPlan &f) {
     } else if (a->dw) {
       lay(&dw, f.dw, x, ldx, signal, f.ldz, a->in, here, a->rows, reinterpret_cast<float *>(ws + f.off_dw));
       dw.a_cols = x_cols; dw.b_cols = eights(here);
-      dw.epi.out = static_cast<T *>(a->dw) + first; dw.epi.ldo = a->lddw; dw.epi.factor = &q.head->factor;
+      dw.epi.out = static_cast<T *>(a->dw) + first; dw.epi.ldo = a->lddw; dw.factor = &q.head->factor;
     }
     if (a->dx || (a->dw && !f.outer)) {
       if (int rc = linear_products(a->type, a->dx ? f.dx.tile : f.dw.tile, f.direct, dx, dw, st)) return rc;
